@@ -68,7 +68,13 @@ typedef enum {
  * consumes them). An INT4 row is 9d/16 bytes and needs d to be a multiple of
  * 256; its activations x are bf16.
  */
-typedef enum { TS_F32 = 0, TS_BF16 = 1, TS_INT4 = 2 } ts_dtype;
+typedef enum {
+    TS_F32 = 0,
+    TS_BF16 = 1,
+    TS_INT4 = 2,
+    TS_E4M3 = 3  /* only where named below: 8-bit floating point (4 exponent and 3 fraction bits, largest value
+                    448, no infinity) with fp32 scales for blocks of 128: the products over many tokens */
+} ts_dtype;
 
 typedef struct ts_ffn ts_ffn;     /* one dReLU FFN (one layer or one expert) */
 typedef struct ts_moe ts_moe;     /* one top-k MoE layer over ts_ffn experts */
@@ -361,6 +367,126 @@ ts_status ts_graph_capture_stack_fused(ts_graph** out, ts_ffn* const* layers, in
                                        int batch, const int32_t* const* active_idx, const int* n_active);
 ts_status ts_graph_launch(ts_graph* g, cudaStream_t stream);
 void ts_graph_destroy(ts_graph* g);
+
+/*
+ * Layers of routed experts over many tokens at once (a prompt, a large batch).
+ *
+ * The forwards above read single weight rows, which pays while few tokens leave
+ * most neurons inactive. Over a prompt every neuron is active for some token, so
+ * the same layer (Sec. 4: top_k of n_experts, each expert Eq. 1 + Eq. 2) is a few
+ * large matrix products. The steps are entry points of their own:
+ *     ts_route         experts of every token, tokens of every expert
+ *     ts_gather_rows   rows in the experts' order, copied
+ *     ts_quant_rows    the same, rounded to TS_E4M3
+ *     ts_grouped_*     each expert's rows times its weights
+ *     ts_combine_rows  each token's rows summed by their routing weights
+ * and ts_prompt_forward runs them in a row. All are asynchronous on `stream`, do
+ * not allocate and may be captured in a CUDA graph. The paper has no counterpart to
+ * how tokens are grouped or rounded to 8 bits: these are readings.
+ */
+
+/*
+ * Routing of `tokens` tokens from the router's logits.
+ *   logits     device [tokens][n_experts] fp32
+ *   n_experts  1..256, top_k 1..min(8, n_experts)
+ *   sel, w     device [tokens][top_k]: the picked experts, largest logit first (the
+ *              lower index wins a tie), and the softmax over the picked logits
+ *   offsets    device [n_experts + 1]: expert e has rows offsets[e] .. offsets[e + 1] - 1
+ *   rows       device [tokens * top_k]: the token of each row, ascending within an
+ *              expert; entries from offsets[n_experts] on are left as they were
+ *   slots      device [tokens][top_k]: the row of each pick
+ * An expert whose logit is -infinity or NaN is never picked. A token with fewer
+ * experts left than top_k (padding: none) gets sel = -1, w = 0, slot = -1 for the
+ * rest. Picks of logit +infinity share the weight equally. tokens == 0 writes
+ * offsets only. No atomics: the same logits give the same rows.
+ */
+ts_status ts_route(const float* logits, int tokens, int n_experts, int top_k, int32_t* sel, float* w,
+                   int32_t* offsets, int32_t* rows, int32_t* slots, cudaStream_t stream);
+
+/*
+ * out[r] = x[rows[r]] for r < min(*n, max_rows); the rows of `out` behind are left as they were.
+ *   x         device, n_src rows of k elements (TS_BF16 or TS_F32), ldx elements apart
+ *   rows      device [max_rows] int32, NULL: row r itself. An entry outside
+ *             0..n_src-1 leaves its row of `out` as it was.
+ *   n         device int32 (as &offsets[n_experts] of ts_route), NULL: max_rows
+ *   out       device [max_rows][k], same type
+ * Rows of x and out start on 16-byte boundaries.
+ */
+ts_status ts_gather_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, const int32_t* rows,
+                         const int32_t* n, int max_rows, void* out, cudaStream_t stream);
+
+/*
+ * Rows rounded to TS_E4M3 with an fp32 scale for each block of 128 elements:
+ *     scale[b][r] = max |x[rows[r]][128 b .. 128 b + 127]| / 448
+ * (at least 2^-100; 1 where the block is all zero) and q[r][i] = x / scale, rounded to the nearest, ties
+ * to even. Arguments as ts_gather_rows (TS_BF16 or TS_F32; k a multiple of 16).
+ *   q         device [max_rows][k] e4m3
+ *   scale     device [ceil(k / 128)][max_rows] fp32: a block's scales lie together
+ * NaN stays NaN in its place; a block that holds an infinity has an infinite scale and
+ * stands for NaN throughout.
+ */
+ts_status ts_quant_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, const int32_t* rows,
+                        const int32_t* n, int max_rows, void* q, float* scale, cudaStream_t stream);
+
+/*
+ * y[t][:] = sum over j < top_k of w[t][j] * src[slots[t][j]][:], in order of j, in fp32.
+ *   src       device [n_rows][n] TS_F32 or TS_BF16
+ *   slots, w  device [tokens][top_k]; a slot outside 0..n_rows-1 adds nothing
+ *   top_k     1..8; n >= 1
+ *   y         device [tokens][n] fp32, overwritten
+ */
+ts_status ts_combine_rows(const void* src, ts_dtype dtype, int n_rows, int n, const int32_t* slots, const float* w,
+                          int tokens, int top_k, float* y, cudaStream_t stream);
+
+typedef struct ts_grouped ts_grouped; /* matrix products of groups of rows, each with its own weights */
+
+typedef enum {
+    TS_NK = 0,  /* a weight matrix is [n][k]: y = x W^T (as w_gate, w_up) */
+    TS_KN = 1   /* [k][n]: y = x W (as w_down, stored by neuron)          */
+} ts_layout;
+
+/*
+ * Products of ragged groups of rows: for each group e,
+ *     y[r] = x[r] . W_e                                      (plain)
+ *     y[r] = max(0, x[r] . W_e) * max(0, x[r] . U_e)         (gated: Eq. 1 with the dReLU of Eq. 2)
+ * for offsets[e] <= r < offsets[e + 1]. One group is an ordinary matrix product.
+ *   n_groups   1..256
+ *   n, k       outputs and inputs of a weight matrix
+ *   wdtype     TS_BF16 (x bf16) or TS_E4M3 (x e4m3)
+ *   layout     TS_NK, or TS_KN for plain TS_BF16 products
+ *   w          host array of n_groups device pointers (borrowed, 16-byte aligned), each
+ *              [n][k] or [k][n]; rows of weights start on 16-byte boundaries
+ *   w_up       NULL, or the same for U (gated)
+ *   scale, scale_up  TS_E4M3: host arrays of device pointers, each [ceil(n / 128)][ceil(k / 128)]
+ *              fp32: a scale for each 128 x 128 block of weights. NULL for TS_BF16.
+ *   max_rows   largest number of rows of a forward
+ * k must be a multiple of 8 (TS_BF16) or 16 (TS_E4M3), n of 8 for TS_KN.
+ * Products are exact, sums are held in fp32. Returns TS_ERR_INVALID_ARG,
+ * TS_ERR_UNSUPPORTED (wdtype or layout without a kernel), TS_ERR_OOM or TS_ERR_CUDA.
+ */
+ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dtype wdtype, ts_layout layout,
+                            const void* const* w, const void* const* w_up, const float* const* scale,
+                            const float* const* scale_up, int max_rows);
+void ts_grouped_destroy(ts_grouped* h);
+
+/*
+ * One forward over `rows` rows (0..max_rows; 0 is a no-op).
+ *   x, ldx     device, rows of k elements ldx apart, each starting on a 16-byte boundary
+ *   x_scale, ld_scale  TS_E4M3: device [ceil(k / 128)][ld_scale] fp32, ld_scale >= rows (as
+ *              ts_quant_rows writes them). NULL for TS_BF16.
+ *   offsets    device [n_groups + 1] int32, ascending, within 0..rows; NULL with one
+ *              group: all rows. A group whose bounds are descending or out of range is
+ *              skipped and recorded (ts_grouped_get_error: TS_ERR_BAD_INDEX).
+ *   y, ldy     device, rows of n elements ldy apart (ydtype TS_BF16, rounded once, or TS_F32); rows
+ *              that no group has are left as they were
+ * One forward may be in flight per handle.
+ */
+ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const float* x_scale, int64_t ld_scale,
+                             const int32_t* offsets, int rows, void* y, int64_t ldy, ts_dtype ydtype,
+                             cudaStream_t stream);
+/* As ts_ffn_get_error and ts_ffn_check_scratch. */
+ts_status ts_grouped_get_error(ts_grouped* h, cudaStream_t stream);
+ts_status ts_grouped_check_scratch(ts_grouped* h, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

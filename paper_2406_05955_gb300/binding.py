@@ -23,13 +23,15 @@ LIB_PATH = os.path.join(_HERE, "_build", "debug", "libtsffn_debug.so") if _DEBUG
 
 TS_OK, TS_ERR_INVALID_ARG, TS_ERR_CUDA, TS_ERR_OOM, TS_ERR_BAD_INDEX, TS_ERR_TIMEOUT, \
     TS_ERR_UNSUPPORTED, TS_ERR_SCRATCH = range(8)
-TS_F32, TS_BF16, TS_INT4 = 0, 1, 2
+TS_F32, TS_BF16, TS_INT4, TS_E4M3 = 0, 1, 2, 3
+TS_NK, TS_KN = 0, 1
 
 _lock = threading.Lock()
 _lib = None
 
 P = ctypes.c_void_p
 I = ctypes.c_int
+L64 = ctypes.c_int64
 PP = ctypes.POINTER(ctypes.c_void_p)
 IP = ctypes.POINTER(ctypes.c_int)
 
@@ -69,6 +71,15 @@ SIGNATURES = {
     "ts_graph_capture_stack_predicted": (I, [PP, P, P, I, P, I, P, P]),
     "ts_graph_launch": (I, [P, P]),
     "ts_graph_destroy": (None, [P]),
+    "ts_route": (I, [P, I, I, I, P, P, P, P, P, P]),
+    "ts_gather_rows": (I, [P, L64, I, I, I, P, P, I, P, P]),
+    "ts_quant_rows": (I, [P, L64, I, I, I, P, P, I, P, P, P]),
+    "ts_combine_rows": (I, [P, I, I, I, P, P, I, I, P, P]),
+    "ts_grouped_create": (I, [PP, I, I, I, I, I, P, P, P, P, I]),
+    "ts_grouped_destroy": (None, [P]),
+    "ts_grouped_forward": (I, [P, P, L64, P, L64, P, I, P, L64, I, P]),
+    "ts_grouped_get_error": (I, [P, P]),
+    "ts_grouped_check_scratch": (I, [P, P]),
 }
 
 

@@ -24,7 +24,7 @@ LIB = os.path.join(OUT_DIR, "libtsffn.so")
 DEBUG_DIR = os.path.join(OUT_DIR, "debug")
 DEBUG_LIB = os.path.join(DEBUG_DIR, "libtsffn_debug.so")
 SOURCES = ["ts_api.cu", "ts_gate_up.cu", "ts_down.cu", "ts_router.cu", "ts_noalloc.cu", "ts_wide.cu", "ts_mid.cu",
-           "ts_topk.cu", "ts_predict.cu"]
+           "ts_topk.cu", "ts_predict.cu", "ts_route.cu", "ts_rows.cu", "ts_grouped.cu", "ts_prompt_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
               "-I", INCLUDE, "-I", CSRC]

@@ -10,6 +10,7 @@
 #include <new>
 #include <vector>
 
+#include "ts_arena.h"
 #include "ts_ffn.h"
 #include "ts_kernels.cuh"
 #include "ts_predict.h"
@@ -19,13 +20,11 @@ using namespace tsffn;
 
 namespace {
 
-constexpr size_t kAlign = 256;
 // rows of the next layer's W_gate each gate+up CTA prefetches into L2 (stack
 // mode, fp32 passes of 3-8 tokens and bf16 passes of 3-4 over few rows: the
 // gathered down kernel k_down issues them)
 constexpr int kPrefetchRows = 32;
 
-size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 int elem_size(ts_dtype dt) { return dt == TS_BF16 ? 2 : 4; }  // fp32 / bf16 weights
 // activations: bf16 for bf16 and INT4 weights, fp32 for fp32 weights
@@ -57,7 +56,6 @@ ts_status device_info(DeviceInfo* di) {
     return TS_OK;
 }
 
-// Carves sub-buffers out of one device allocation.
 // One NVTX range per layer of the stack calls, so that a profiler's timeline
 // shows the layers (header-only NVTX: with no tool attached the calls return
 // at once). The ranges are host-side: inside a stream capture they mark the
@@ -72,59 +70,6 @@ struct LayerRange {
     LayerRange(const LayerRange&) = delete;
     LayerRange& operator=(const LayerRange&) = delete;
 };
-
-// A handle's device scratch: blocks carved out of one allocation. Every block
-// is followed by a guard zone of kGuardBytes filled with kGuardByte when the
-// arena is allocated; check_arena reads the zones back, so a kernel that
-// writes past the end of a scratch block is caught by the tests instead of
-// silently corrupting the next block.
-constexpr size_t kGuardBytes = kAlign;
-constexpr unsigned char kGuardByte = 0xA5;
-
-struct Arena {
-    size_t bytes = 0;
-    char* base = nullptr;
-    std::vector<size_t> guards;  // offsets of the guard zones
-    size_t take(size_t n) {
-        const size_t off = bytes;
-        bytes += align_up(n);
-        guards.push_back(bytes);
-        bytes += kGuardBytes;
-        return off;
-    }
-    template <typename P>
-    P* at(size_t off) const { return reinterpret_cast<P*>(base + off); }
-};
-
-ts_status alloc_arena(Arena* ar) {
-    if (cudaMalloc(&ar->base, ar->bytes) != cudaSuccess) {
-        cudaGetLastError();
-        ar->base = nullptr;
-        return TS_ERR_OOM;
-    }
-    bool ok = cudaMemset(ar->base, 0, ar->bytes) == cudaSuccess;
-    for (size_t g : ar->guards) ok = ok && cudaMemset(ar->base + g, kGuardByte, kGuardBytes) == cudaSuccess;
-    if (!ok) {
-        cudaFree(ar->base);
-        ar->base = nullptr;
-        return TS_ERR_CUDA;
-    }
-    return TS_OK;
-}
-
-// Synchronise `stream` and compare every guard zone with its fill.
-ts_status check_arena(const Arena& ar, cudaStream_t stream) {
-    if (!ar.base) return TS_ERR_INVALID_ARG;
-    if (cudaStreamSynchronize(stream) != cudaSuccess) return TS_ERR_CUDA;
-    std::vector<unsigned char> buf(kGuardBytes);
-    for (size_t g : ar.guards) {
-        if (cudaMemcpy(buf.data(), ar.base + g, kGuardBytes, cudaMemcpyDeviceToHost) != cudaSuccess)
-            return TS_ERR_CUDA;
-        for (unsigned char b : buf)
-            if (b != kGuardByte) return TS_ERR_SCRATCH;
-    }
-    return TS_OK;
-}
 
 // Scratch of the grouped kernels: per-expert c values and bitmaps, and the
 // device status word.

@@ -1,0 +1,252 @@
+"""ctypes binding of libtsffn's operators over many tokens (routed experts, grouped products): marshalling only.
+
+Tensors are CUDA tensors of the current device; others are refused. Outputs that are not given are allocated on
+the stream of the call. A call on another stream than the current one is ordered after nothing by itself: the
+caller makes that stream wait for the tensors, and keeps them alive until it is done.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+import torch
+
+from .binding import (TS_BF16, TS_E4M3, TS_F32, TS_KN, TS_NK, _check, lib)
+
+_CODES = {torch.float32: TS_F32, torch.bfloat16: TS_BF16, torch.float8_e4m3fn: TS_E4M3}
+_LAYOUTS = {"nk": TS_NK, "kn": TS_KN}
+BLOCK = 128  # elements of one scale
+
+
+def _tensor(t, what: str, dtypes, dim: int, rows_apart: bool = False) -> torch.Tensor:
+    """``t``, checked: on the current device, its type and dimensions, contiguous (or only each row of it)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, not on the current device")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if t.dim() != dim:
+        raise ValueError(f"{what} must have {dim} dimensions")
+    if rows_apart:
+        if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+            raise ValueError(f"{what} must have contiguous rows")
+    elif not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t
+
+
+def _shaped(t, what: str, dtype, shape) -> torch.Tensor:
+    _tensor(t, what, (dtype,), len(shape))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Elements from a row to the next one."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class _On:
+    """The stream of a call: its handle, and allocation on it."""
+
+    def __init__(self, stream):
+        if stream is None:
+            self.stream, self.handle = None, torch.cuda.current_stream().cuda_stream
+        else:
+            self.stream = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+            self.handle = self.stream.cuda_stream
+
+    def empty(self, *shape, dtype):
+        if self.stream is None:
+            return torch.empty(*shape, dtype=dtype, device="cuda")
+        with torch.cuda.stream(self.stream):
+            return torch.empty(*shape, dtype=dtype, device="cuda")
+
+
+class Routing(NamedTuple):
+    sel: torch.Tensor      # int32 [tokens][top_k] picked experts, -1: none
+    w: torch.Tensor        # fp32 [tokens][top_k] their weights
+    offsets: torch.Tensor  # int32 [experts + 1] first row of each expert
+    rows: torch.Tensor     # int32 [tokens * top_k] token of each row
+    slots: torch.Tensor    # int32 [tokens][top_k] row of each pick, -1: none
+
+
+def route(logits: torch.Tensor, top_k: int, sel=None, w=None, offsets=None, rows=None, slots=None,
+          stream=None) -> Routing:
+    """``ts_route``: each token's ``top_k`` experts by fp32 ``logits [tokens][experts]``, and each expert's tokens."""
+    _tensor(logits, "logits", (torch.float32,), 2)
+    t, e = logits.shape
+    k, on, i32 = int(top_k), _On(stream), torch.int32
+    sel = on.empty(t, k, dtype=i32) if sel is None else _shaped(sel, "sel", i32, (t, k))
+    w = on.empty(t, k, dtype=torch.float32) if w is None else _shaped(w, "w", torch.float32, (t, k))
+    offsets = on.empty(e + 1, dtype=i32) if offsets is None else _shaped(offsets, "offsets", i32, (e + 1,))
+    rows = on.empty(t * k, dtype=i32) if rows is None else _shaped(rows, "rows", i32, (t * k,))
+    slots = on.empty(t, k, dtype=i32) if slots is None else _shaped(slots, "slots", i32, (t, k))
+    _check(lib().ts_route(logits.data_ptr(), t, e, k, sel.data_ptr(), w.data_ptr(), offsets.data_ptr(),
+                          rows.data_ptr(), slots.data_ptr(), on.handle), "ts_route")
+    return Routing(sel, w, offsets, rows, slots)
+
+
+def _row_list(x, rows, n, max_rows):
+    """(pointer of the list, pointer of the count, rows of the output)."""
+    rp = np_ = None
+    if rows is not None:
+        _tensor(rows, "rows", (torch.int32,), 1)
+        rp, m = rows.data_ptr(), rows.shape[0]
+    else:
+        m = x.shape[0]
+    if max_rows is not None and max_rows != m:
+        raise ValueError(f"the output must have {m} rows")
+    if n is not None:
+        _tensor(n, "n", (torch.int32,), 1)
+        if n.shape[0] != 1:
+            raise ValueError("n must have one element")
+        np_ = n.data_ptr()
+    return rp, np_, m
+
+
+def gather_rows(x: torch.Tensor, rows: torch.Tensor, n=None, out=None, stream=None) -> torch.Tensor:
+    """``ts_gather_rows``: ``out[r] = x[rows[r]]`` for ``r < n`` (a device int32, as ``offsets[-1:]``; all rows
+    without); the other rows of ``out`` are left as they were."""
+    _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
+    rp, np_, m = _row_list(x, rows, n, None if out is None else out.shape[0])
+    on = _On(stream)
+    out = on.empty(m, x.shape[1], dtype=x.dtype) if out is None else _shaped(out, "out", x.dtype, (m, x.shape[1]))
+    _check(lib().ts_gather_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], x.shape[1], rp, np_, m,
+                                out.data_ptr(), on.handle), "ts_gather_rows")
+    return out
+
+
+def quant_rows(x: torch.Tensor, rows=None, n=None, q=None, scale=None, stream=None):
+    """``ts_quant_rows``: (q e4m3 [rows][k], scale fp32 [ceil(k / 128)][rows]) of the rows of ``x`` that are listed
+    (all of them without a list)."""
+    _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
+    k = x.shape[1]
+    rp, np_, m = _row_list(x, rows, n, None if q is None else q.shape[0])
+    on, kb = _On(stream), -(-k // BLOCK)
+    q = on.empty(m, k, dtype=torch.float8_e4m3fn) if q is None else _shaped(q, "q", torch.float8_e4m3fn, (m, k))
+    scale = on.empty(kb, m, dtype=torch.float32) if scale is None else _shaped(scale, "scale", torch.float32, (kb, m))
+    _check(lib().ts_quant_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], k, rp, np_, m, q.data_ptr(),
+                               scale.data_ptr(), on.handle), "ts_quant_rows")
+    return q, scale
+
+
+def combine_rows(src: torch.Tensor, slots: torch.Tensor, w: torch.Tensor, out=None, stream=None) -> torch.Tensor:
+    """``ts_combine_rows``: fp32 ``out[t] = sum_j w[t][j] src[slots[t][j]]``; a slot outside ``src`` adds nothing."""
+    _tensor(src, "src", (torch.bfloat16, torch.float32), 2)
+    _tensor(slots, "slots", (torch.int32,), 2)
+    t, k = slots.shape
+    _shaped(w, "w", torch.float32, (t, k))
+    on = _On(stream)
+    out = on.empty(t, src.shape[1], dtype=torch.float32) if out is None else \
+        _shaped(out, "out", torch.float32, (t, src.shape[1]))
+    _check(lib().ts_combine_rows(src.data_ptr(), _CODES[src.dtype], src.shape[0], src.shape[1], slots.data_ptr(),
+                                 w.data_ptr(), t, k, out.data_ptr(), on.handle), "ts_combine_rows")
+    return out
+
+
+def _pointers(ts):
+    return None if ts is None else ctypes.cast((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]), ctypes.c_void_p)
+
+
+class Grouped:
+    """Products of ragged groups of rows, each group with its own weights (``ts_grouped_*``): ``y[r] = x[r] W_e^T``
+    over borrowed ``w[e] [n][k]`` (``layout="kn"``: ``x[r] W_e`` over ``[k][n]``), bf16, or e4m3 with fp32
+    ``scale[e] [ceil(n / 128)][ceil(k / 128)]``. ``w`` is a tensor (one group), a list of them, or a stacked one."""
+
+    def __init__(self, w, layout: str = "nk", scale=None, max_rows: int = 1, _up=None, _scale_up=None):
+        w, up, scale, scale_up = (None if t is None else self._matrices(t) for t in (w, _up, scale, _scale_up))
+        if layout not in _LAYOUTS:
+            raise ValueError('layout must be "nk" or "kn"')
+        for t in w + (up or []):
+            _tensor(t, "w", (torch.bfloat16, torch.float8_e4m3fn), 2)
+            if t.shape != w[0].shape or t.dtype != w[0].dtype:
+                raise ValueError("the groups' weights must share one shape and type")
+        if up is not None and len(up) != len(w):
+            raise ValueError("as many w_up as w_gate are needed")
+        self.groups, self.dtype, self.max_rows = len(w), w[0].dtype, int(max_rows)
+        self.n, self.k = (int(v) for v in (w[0].shape if layout == "nk" else w[0].shape[::-1]))
+        e8 = self.dtype == torch.float8_e4m3fn
+        for s, of in ((scale, w), (scale_up, up)):
+            if (s is not None) != (e8 and of is not None):
+                raise ValueError("e4m3 weights need scales, and only they have any")
+            if s is not None and len(s) != len(of):
+                raise ValueError("as many scales as weights are needed")
+            for t in s or []:
+                _shaped(t, "scale", torch.float32, (-(-self.n // BLOCK), -(-self.k // BLOCK)))
+        self._keep = (w, up, scale, scale_up)
+        h = ctypes.c_void_p()
+        self._h = None
+        _check(lib().ts_grouped_create(ctypes.byref(h), self.groups, self.n, self.k, _CODES[self.dtype],
+                                       _LAYOUTS[layout], _pointers(w), _pointers(up), _pointers(scale),
+                                       _pointers(scale_up), self.max_rows), "ts_grouped_create")
+        self._h = h
+
+    @classmethod
+    def gated(cls, w_gate, w_up, scale_gate=None, scale_up=None, max_rows: int = 1) -> "Grouped":
+        """``y[r] = max(0, x[r] G_e^T) * max(0, x[r] U_e^T)``: the dReLU products of Eq. 2."""
+        return cls(w_gate, scale=scale_gate, max_rows=max_rows, _up=w_up, _scale_up=scale_up)
+
+    @staticmethod
+    def _matrices(t):
+        if isinstance(t, torch.Tensor):
+            t = [t] if t.dim() == 2 else list(t.unbind(0)) if t.dim() == 3 else []
+        t = list(t)
+        if not t:
+            raise ValueError("weights are a matrix, a list of them, or a stacked tensor")
+        return t
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if self._h is None:
+            raise RuntimeError("handle is closed")
+        return self._h
+
+    def forward(self, x: torch.Tensor, offsets=None, x_scale=None, y=None, stream=None) -> torch.Tensor:
+        """``y`` (bf16 or fp32, bf16 without one) of the groups of rows ``offsets[e] .. offsets[e + 1] - 1`` of ``x``; rows
+        that no group has are left as they were. e4m3 rows come with ``x_scale``, as ``quant_rows`` gives it."""
+        _tensor(x, "x", (self.dtype,), 2, rows_apart=True)
+        rows = x.shape[0]
+        if x.shape[1] != self.k:
+            raise ValueError(f"x must be [rows][{self.k}]")
+        op = sp = None
+        if offsets is not None:
+            op = _shaped(offsets, "offsets", torch.int32, (self.groups + 1,)).data_ptr()
+        ld = 0
+        if x_scale is not None:
+            _tensor(x_scale, "x_scale", (torch.float32,), 2, rows_apart=True)
+            if x_scale.shape[0] != -(-self.k // BLOCK) or x_scale.shape[1] < rows:
+                raise ValueError(f"x_scale must be [{-(-self.k // BLOCK)}][rows]")
+            sp, ld = x_scale.data_ptr(), _ld(x_scale)
+        on = _On(stream)
+        if y is None:
+            y = on.empty(rows, self.n, dtype=torch.bfloat16)
+        else:
+            _tensor(y, "y", (torch.bfloat16, torch.float32), 2, rows_apart=True)
+            if tuple(y.shape) != (rows, self.n):
+                raise ValueError(f"y must be [{rows}][{self.n}]")
+        _check(lib().ts_grouped_forward(self.handle, x.data_ptr(), _ld(x), sp, ld, op, rows, y.data_ptr(), _ld(y),
+                                        _CODES[y.dtype], on.handle), "ts_grouped_forward")
+        return y
+
+    __call__ = forward
+
+    def get_error(self, stream=None) -> int:
+        return int(lib().ts_grouped_get_error(self.handle, _On(stream).handle))
+
+    def check_scratch(self, stream=None) -> int:
+        """Status of the scratch guard zones (as Ffn.check_scratch)."""
+        return int(lib().ts_grouped_check_scratch(self.handle, _On(stream).handle))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None:
+            lib().ts_grouped_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
