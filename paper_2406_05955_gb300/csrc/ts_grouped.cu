@@ -1,6 +1,19 @@
 // ts_grouped.cu -- products of ragged groups of rows with each group's own weights: y = x W_e, or
 // max(0, x W_e) max(0, x U_e) (Eq. 1 with the dReLU of Eq. 2), over bf16 weights or e4m3 ones with a scale for
-// each 128 x 128 block (and one for each 128 elements of a row of x).
+// each 128 x 128 block (and one for each 128 elements of a row of x), on the 5th-generation tensor cores.
+//
+// A tile is D[i][t] = W[i] . x_t for 256 weight rows i (gated: 128 neurons, gate and up rows) and up to 256 rows t of
+// one group. The weights are the MMA's M and the rows of x its N, which may be any multiple of 16: a group's rows are
+// cut into equal tiles, so ragged groups waste at most 15 rows a tile, and one kernel serves one row and thousands.
+//
+// A tile belongs to a pair of CTAs (tcgen05 cta_group::2): each loads its 128 weight rows and half of the rows of x, and
+// the MMA reads both halves of x, so that a pair moves 64 KB for 2 x 256 x 256 x 64 flop and not 96 (one CTA
+// alone would have to fetch 96 bytes a clock from L2 to keep its tensor core busy, a pair 64 a CTA).
+//
+// Roles of a CTA's warps: 0 loads stages of 128 bytes of k by TMA, 1 (of the first CTA) issues the MMAs, 4-11 take the
+// sums out of tensor memory, where two accumulators take turns. They keep running sums in fp32 registers and add an
+// accumulator to them every kChunk stages: the tensor cores truncate when they accumulate, which 64 steps do not show,
+// and each 128 of k of e4m3 products has scales of its own, which enter there.
 #include <cuda_fp8.h>
 
 #include "ts_grouped.h"
@@ -9,98 +22,639 @@
 namespace tsffn {
 namespace {
 
-constexpr int kT = 64;   // rows and columns of a block's tile
-constexpr int kKT = 16;  // of k per step
+constexpr int kCtaThreads = 384;
+constexpr int kEpiWarp0 = 4;
+constexpr int kStageW = 16384;                  // weights of a stage: 128 rows of 128 bytes
+constexpr int kMaxStages = 12;
+constexpr int kStageMem = 216 * 1024 - 4096;    // bytes of all stages
+constexpr int kBand = 8;                        // tiles of x that one sweep over the weights serves
+constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
-__device__ __forceinline__ float elem(const void* p, size_t i, bool e4m3) {
-    if (e4m3) return float(static_cast<const __nv_fp8_e4m3*>(p)[i]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+
+struct Shared {
+    uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
+    uint32_t tmem;
+    int fail;
+    int max_cols;                               // widest tile
+    int first[kMaxGroups + 1];                  // tiles before each group
+    int row0[kMaxGroups], rows[kMaxGroups];
+    float scale[kEpiWarps][2][128];             // e4m3: scales of a warp's rows of x, this stage's and the next one's
+};
+
+// ---- cluster and tcgen05 helpers (pairs of CTAs) ---------------------------
+__device__ __forceinline__ uint32_t cta_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// address of this CTA's `p` in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// 2-D box into this CTA's shared memory, its bytes counted by the barrier at `bar` (a CTA of the pair)
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+template <bool E8>
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (E8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+// arrive on `bar` of both CTAs when the MMAs issued so far have completed
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+}
+// 16 lanes x 64 columns: of each 8 columns, thread t gets columns 2 (t % 4) and + 1 of lanes t / 4 (v[4 j], v[4 j + 1])
+// and t / 4 + 8 (v[4 j + 2], v[4 j + 3])
+__device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// shared-memory descriptors with the 128-byte swizzle: k along the 128-byte rows (atoms of 8 rows, 1024 bytes apart) ...
+__device__ __forceinline__ uint64_t desc_k(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// ... or 64 weight rows along them (8 of k an atom, `lbo` bytes between blocks of 64 weight rows)
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t lbo) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-// One 64 x 64 tile of y per block, 4 x 4 outputs a thread; tiles of rows are numbered group by group.
-template <bool E4M3, bool GATED, bool KN>
-__global__ void __launch_bounds__(256) k_grouped(const GroupedLaunch L) {
-    __shared__ float xs[kKT][kT + 4], wt[GATED ? 2 : 1][kKT][kT + 4];
-    int tile = blockIdx.y, g = -1, r0 = 0, r1 = 0;
-    for (int e = 0; e < L.n_groups; ++e) {
-        const int a = L.offsets ? L.offsets[e] : 0, b = L.offsets ? L.offsets[e + 1] : L.rows;
-        if (a < 0 || b < a || b > L.rows) {
-            if (threadIdx.x == 0) atomicOr(L.status, kStatusBadIndex);
-            continue;
-        }
-        const int t = (b - a + kT - 1) / kT;
-        if (tile < t) {
-            g = e;
-            r0 = a + tile * kT;
-            r1 = min(b, r0 + kT);
-            break;
-        }
-        tile -= t;
+// pairs of fp32 in one instruction
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pack2(uint32_t a, uint32_t b) { return (f32x2)b << 32 | a; }
+__device__ __forceinline__ float lo2(f32x2 v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi2(f32x2 v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// Registers: the warps that keep the sums get those that the others do not need. Of the block's 384 x 168 = 64512,
+// 128 x 80 + 256 x 208 = 63488 are dealt out.
+__device__ __forceinline__ void regs_shrink() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
+__device__ __forceinline__ void regs_grow() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+
+// ---- tiles and their parts --------------------------------------------------
+// The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
+// are dealt out evenly, in order, so that all pairs end together: a pair's share begins and ends anywhere in a tile.
+struct Parts {
+    int pairs, steps;      // CTA pairs, stages of a tile
+    int whole;             // rounds of whole tiles
+    long long total;       // steps of the rest
+    int sharers;           // pairs that get some of them
+    __device__ Parts(int tiles, int pairs_, int steps_) : pairs(pairs_), steps(steps_) {
+        whole = tiles % pairs == 0 ? tiles / pairs : max(0, tiles / pairs - 1);
+        total = (long long)(tiles - whole * pairs) * steps;
+        sharers = (int)max(1ll, min((long long)pairs, total / kMinSteps));
     }
-    if (g < 0) return;
-    const GroupWeights gw = L.weights[g];
-    const int c0 = blockIdx.x * kT, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const int kb_n = (L.k + kScaleBlock - 1) / kScaleBlock;
-    float acc[GATED ? 2 : 1][4][4] = {};
-    for (int k0 = 0; k0 < L.k; k0 += kKT) {
-        for (int i = tid; i < kT * kKT; i += 256) {
-            const int r = i / kKT, kk = k0 + i % kKT;
-            float v = 0.0f;
-            if (r0 + r < r1 && kk < L.k) {
-                v = elem(L.x, (size_t)(r0 + r) * L.ldx + kk, E4M3);
-                if (E4M3) v *= L.x_scale[(size_t)(kk / kScaleBlock) * L.ld_scale + r0 + r];
+    __device__ long long begin(int q) const { return total * q / sharers; }
+    // the pair that has step s
+    __device__ int owner(long long s) const {
+        int q = (int)(s * sharers / total);
+        while (begin(q) > s) --q;
+        while (begin(q + 1) <= s) ++q;
+        return q;
+    }
+};
+
+struct Seg {
+    int tile, k0, k1;       // stages [k0, k1) of a tile
+    int rest;               // its number among the tiles that are shared, -1: a whole one
+    int g, wt, row0, rows, cols;  // group, tile of weights, first row of x, rows, and their number rounded up to 16
+};
+
+struct Walk {
+    const Shared& sh;
+    const Parts parts;
+    const int pair, n_groups, w_tiles;
+    int round = 0;
+    long long at, end;
+    __device__ Walk(const Shared& s, const GroupedLaunch& L, int pair_, int w_tiles_, int steps)
+        : sh(s), parts(s.first[L.n_groups], L.pairs, steps), pair(pair_), n_groups(L.n_groups), w_tiles(w_tiles_) {
+        at = pair < parts.sharers ? parts.begin(pair) : 0;
+        end = pair < parts.sharers ? parts.begin(pair + 1) : 0;
+    }
+    __device__ bool next(Seg& s) {
+        if (round < parts.whole) {
+            s.tile = round * parts.pairs + pair;
+            s.rest = -1;
+            s.k0 = 0;
+            s.k1 = parts.steps;
+            ++round;
+        } else {
+            if (at >= end) return false;
+            s.rest = (int)(at / parts.steps);
+            s.tile = parts.whole * parts.pairs + s.rest;
+            s.k0 = (int)(at - (long long)s.rest * parts.steps);
+            s.k1 = (int)min((long long)parts.steps, s.k0 + (end - at));
+            at += s.k1 - s.k0;
+        }
+        int lo = 0, hi = n_groups;  // the last group whose first tile is not behind
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (sh.first[mid] <= s.tile) lo = mid;
+            else hi = mid;
+        }
+        s.g = lo;
+        int t = s.tile - sh.first[lo];
+        const int n = sh.rows[lo], tiles = (n + kMaxTileRows - 1) / kMaxTileRows;
+        const int band = t / (kBand * w_tiles), width = min(kBand, tiles - band * kBand);
+        t -= band * kBand * w_tiles;
+        s.wt = t / width;
+        const int j = band * kBand + t % width;
+        const int high = tile_rows(n, tiles);
+        s.row0 = sh.row0[lo] + j * high;
+        s.rows = max(0, min(high, n - j * high));
+        s.cols = high;
+        return true;
+    }
+    // rows of each of the tiles that n rows are cut into
+    __device__ static int tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 15) / 16 * 16; }
+};
+
+template <bool E8, bool GATED, bool KN>
+struct Kind {
+    static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
+    static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
+    static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
+    static constexpr int kBoxes = GATED ? 8 : KN ? 2 : 1;  // boxes of weights of a CTA's stage
+    static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
+};
+
+__device__ __forceinline__ bool wait_for(uint64_t* bar, unsigned parity, Shared& sh) {
+    if (mbar_wait(bar, parity)) return true;
+    sh.fail = 1;
+    return false;
+}
+
+template <bool E8, bool GATED, bool KN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_grouped(const __grid_constant__ GroupedLaunch L) {
+    using K = Kind<E8, GATED, KN>;
+    extern __shared__ __align__(1024) unsigned char sm_raw[];
+    __shared__ Shared sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = cta_rank();
+    const int pair = blockIdx.x >> 1;
+    const int steps = (L.k + K::kStep - 1) / K::kStep, w_tiles = (L.n + K::kTileN - 1) / K::kTileN;
+
+    // ---- set-up: barriers, tensor memory, the groups' tiles ----
+    if (warp == 0) {
+        int tiles_before = 0, widest = 16;
+        for (int e0 = 0; e0 < L.n_groups; e0 += kWarp) {
+            const int e = e0 + lane;
+            int a = 0, n = 0;
+            if (e < L.n_groups) {
+                a = L.offsets != nullptr ? L.offsets[e] : 0;
+                const int b = L.offsets != nullptr ? L.offsets[e + 1] : L.rows;
+                const bool ok = a >= 0 && b >= a && b <= L.rows;
+                if (!ok && blockIdx.x == 0) atomicOr(L.status, kStatusBadIndex);
+                n = ok ? b - a : 0;
+                sh.row0[e] = a;
+                sh.rows[e] = n;
             }
-            xs[i % kKT][r] = v;
-            const int c = KN ? i % kT : i / kKT, kw = KN ? i / kT : i % kKT;
+            const int tiles = (n + kMaxTileRows - 1) / kMaxTileRows;
+            if (n > 0) widest = max(widest, Walk::tile_rows(n, tiles));
+            int sum = tiles * w_tiles;
 #pragma unroll
-            for (int p = 0; p < (GATED ? 2 : 1); ++p) {
-                float u = 0.0f;
-                if (c0 + c < L.n && k0 + kw < L.k) {
-                    const size_t at = KN ? (size_t)(k0 + kw) * L.n + c0 + c : (size_t)(c0 + c) * L.k + k0 + kw;
-                    u = elem(p ? gw.u : gw.w, at, E4M3);
-                    if (E4M3) u *= (p ? gw.us : gw.ws)[(size_t)((c0 + c) / kScaleBlock) * kb_n + (k0 + kw) / kScaleBlock];
+            for (int o = 1; o < kWarp; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            if (e < L.n_groups) sh.first[e + 1] = tiles_before + sum;
+            tiles_before += __shfl_sync(0xffffffffu, sum, kWarp - 1);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) widest = max(widest, __shfl_xor_sync(0xffffffffu, widest, o));
+        if (lane == 0) {
+            sh.first[0] = 0;
+            sh.max_cols = widest;
+        }
+    } else if (warp == 1 && lane == 0) {
+        for (int s = 0; s < kMaxStages; ++s) {
+            mbar_init(&sh.full[s], 1);
+            mbar_init(&sh.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sh.tfull[b], 1);
+            mbar_init(&sh.tempty[b], 2 * kEpiWarps);
+        }
+        sh.fail = 0;
+        mbar_fence_init();
+    } else if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    cluster_sync();
+    tc_after();
+
+    const uint32_t sm0 = (smem_u32(sm_raw) + 1023u) & ~1023u;
+    // the smallest box of x that holds a CTA's half of the widest tile sets the size of a stage
+    const int x_rows_max = max(8, 1 << (32 - __clz(sh.max_cols / 2 - 1)));
+    const uint32_t stage_bytes = kStageW + x_rows_max * 128;
+    const int stages = min(kMaxStages, kStageMem / (int)stage_bytes);
+    Walk walk(sh, L, pair, w_tiles, steps);
+    Seg sg;
+
+    if (warp < kEpiWarp0) {
+        regs_shrink();
+        if (warp == 0) {
+            // ---- loads: lane i < kBoxes a box of weights, the next one the rows of x ----
+            int st = 0, n_loaded = 0;
+            unsigned ph = 0;
+            bool ok = true;
+            while (ok && walk.next(sg)) {
+                const GroupWeights* gw = L.weights + sg.g;
+                const int x_rows = max(8, 1 << (32 - __clz(sg.cols / 2 - 1))), xi = __ffs(x_rows) - 4;
+                const uint32_t bytes = 2u * (kStageW + x_rows * 128);
+                const CUtensorMap* map = &L.x[xi];
+                uint32_t off = kStageW;
+                int cy = sg.row0 + (int)rank * (sg.cols / 2), cx = 0;  // coordinate of the box besides k's
+                if (lane < K::kBoxes) {
+                    if constexpr (GATED) {  // 16 gate rows and 16 up rows in turn
+                        map = lane & 1 ? &gw->u : &gw->w;
+                        off = lane * 2048;
+                        cy = sg.wt * 128 + (int)rank * 64 + (lane >> 1) * 16;
+                    } else if constexpr (KN) {
+                        map = &gw->w;
+                        off = lane * 8192;
+                        cx = sg.wt * 256 + (int)rank * 128 + lane * 64;
+                    } else {
+                        map = &gw->w;
+                        off = 0;
+                        cy = sg.wt * 256 + (int)rank * 128;
+                    }
                 }
-                wt[p][kw][c] = u;
+                for (int k = sg.k0; k < sg.k1; ++k) {
+                    if (n_loaded >= stages) ok = wait_for(&sh.empty[st], ph ^ 1u, sh);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (rank == 0 && lane == 0) mbar_arrive_expect_tx(&sh.full[st], bytes);
+                    __syncwarp();
+                    const uint32_t dst = sm0 + st * stage_bytes + off, bar = in_cta(&sh.full[st], 0);
+                    if (lane <= K::kBoxes) {
+                        if (KN && lane < K::kBoxes) tma_box(dst, map, cx, k * K::kStep, bar);
+                        else tma_box(dst, map, k * K::kStep, cy, bar);
+                    }
+                    ++n_loaded;
+                    if (++st == stages) {
+                        st = 0;
+                        ph ^= 1u;
+                    }
+                }
+            }
+            // the last stages' releases come from the other CTA: wait for them before leaving
+            if (n_loaded < stages) {
+                st = 0;
+                ph = 1;
+            }
+            for (int i = min(n_loaded, stages); ok && i > 0; --i) {
+                ok = __all_sync(0xffffffffu, wait_for(&sh.empty[st], ph ^ 1u, sh));
+                if (++st == stages) {
+                    st = 0;
+                    ph ^= 1u;
+                }
+            }
+        } else if (warp == 1) {
+            // ---- MMAs, by one thread of the first CTA ----
+            if (rank == 0 && lane == 0) {
+                int st = 0, chunk = 0;
+                unsigned ph = 0;
+                bool ok = true;
+                while (ok && walk.next(sg)) {
+                    const uint32_t idesc = K::kIdesc | (uint32_t)(sg.cols >> 3) << 17;
+                    for (int k = sg.k0; ok && k < sg.k1;) {
+                        const int kc = min(sg.k1, k + K::kChunk);
+                        const int buf = chunk & 1;
+                        if (chunk >= 2) ok = wait_for(&sh.tempty[buf], ((chunk >> 1) & 1) ^ 1u, sh);
+                        tc_after();
+                        const uint32_t d = sh.tmem + buf * 256;
+                        for (int first = k; ok && k < kc; ++k) {
+                            ok = wait_for(&sh.full[st], ph, sh);
+                            if (!ok) break;
+                            tc_after();
+                            const uint32_t a0 = sm0 + st * stage_bytes;
+                            const uint64_t bd = desc_k(a0 + kStageW);
+                            const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
+                            pair_commit(&sh.empty[st]);
+                            if (++st == stages) {
+                                st = 0;
+                                ph ^= 1u;
+                            }
+                        }
+                        if (ok) pair_commit(&sh.tfull[buf]);
+                        ++chunk;
+                    }
+                }
+            }
+            __syncwarp();
+        }
+    } else {
+        regs_grow();
+        // ---- sums: warp ew holds lanes 32 (ew % 4) .. + 31 of the columns of half ew / 4 of a tile ----
+        const int ew = warp - kEpiWarp0, q = ew & 3, half = ew >> 2;
+        const uint32_t lane_addr = sh.tmem + ((uint32_t)(32 * q) << 16);
+        int chunk = 0;
+        bool ok = true;
+        while (ok && walk.next(sg)) {
+            const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8
+            f32x2 acc[2][2][16];  // [16 lanes][64 columns][of 8 columns: lanes t / 4, lanes t / 4 + 8]
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i >> 5][(i >> 4) & 1][i & 15] = 0ull;
+            const GroupWeights* gw = L.weights + sg.g;
+            const float* xs = nullptr;
+            const float* ws[2] = {nullptr, nullptr};
+            float next_x[4], next_w[2];
+            auto fetch = [&](int k) {  // e4m3: the scales of a stage
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = lane + 32 * i;
+                    next_x[i] = c < cols && c0 + c < sg.rows ? __ldg(xs + (size_t)k * L.ld_scale + c) : 0.0f;
+                }
+                next_w[0] = __ldg(ws[0] + k);
+                if (GATED) next_w[1] = __ldg(ws[1] + k);
+            };
+            if constexpr (E8) {
+                const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
+                xs = L.x_scale + sg.row0 + c0;
+                ws[0] = gw->ws + (size_t)block * steps;
+                if (GATED) ws[1] = gw->us + (size_t)block * steps;
+                fetch(sg.k0);
+            }
+            for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
+                const int buf = chunk & 1;
+                float* mine = sh.scale[ew][buf];
+                f32x2 w2[2];
+                if constexpr (E8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mine[lane + 32 * i] = next_x[i];
+                    w2[0] = pack2(__float_as_uint(next_w[0]), __float_as_uint(next_w[0]));
+                    w2[1] = GATED ? pack2(__float_as_uint(next_w[1]), __float_as_uint(next_w[1])) : w2[0];
+                    __syncwarp();
+                    if (k + 1 < sg.k1) fetch(k + 1);
+                }
+                ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> 1) & 1, sh));
+                if (!ok) break;
+                tc_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (64 * c >= cols) break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t r[32];
+                        tc_ld64(lane_addr + ((uint32_t)(16 * h) << 16) + buf * 256 + c0 + 64 * c, r);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            if constexpr (E8) {
+                                const float2 s = *reinterpret_cast<const float2*>(&mine[64 * c + 8 * j + 2 * (lane & 3)]);
+                                const f32x2 s2 = mul2(pack2(__float_as_uint(s.x), __float_as_uint(s.y)), w2[h]);
+                                acc[h][c][2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), s2, acc[h][c][2 * j]);
+                                acc[h][c][2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), s2, acc[h][c][2 * j + 1]);
+                            } else {
+                                acc[h][c][2 * j] = add2(acc[h][c][2 * j], pack2(r[4 * j], r[4 * j + 1]));
+                                acc[h][c][2 * j + 1] = add2(acc[h][c][2 * j + 1], pack2(r[4 * j + 2], r[4 * j + 3]));
+                            }
+                        }
+                    }
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) arrive_at(in_cta(&sh.tempty[buf], 0));
+            }
+            if (!ok) break;
+            if (sg.k1 - sg.k0 < steps) {
+                // A part of a tile: left in global memory; the warp that comes last adds the parts in the order of k.
+                const Parts& P = walk.parts;
+                const long long s0 = (long long)sg.rest * steps;
+                const int p0 = P.owner(s0), p1 = P.owner(s0 + steps - 1);
+                auto part_of = [&](int p) {  // a pair's first tile is in its slot 0, its last one in slot 1
+                    const int slot = P.begin(p) >= s0 ? 0 : 1;
+                    return reinterpret_cast<f32x2*>(L.partial) +
+                           ((size_t)((p * 2 + slot) * 2 + (int)rank) * kEpiWarps + ew) * (L.part_chunks * 1024) + lane;
+                };
+                f32x2* to = part_of(pair);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (64 * c < cols)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) __stcg(to + (c * 32 + i) * kWarp, acc[i >> 4][c][i & 15]);
+                __threadfence();
+                __syncwarp();
+                unsigned* count = L.arrived + ((size_t)sg.rest * 2 + rank) * kEpiWarps + ew;
+                unsigned before = 0;
+                if (lane == 0) before = atomicAdd(count, 1u);
+                before = __shfl_sync(0xffffffffu, before, 0);
+                if ((int)before != p1 - p0) continue;
+                __threadfence();
+                if (lane == 0) *count = 0u;
+                for (int p = p0; p <= p1; ++p) {
+                    const f32x2* from = part_of(p);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        if (64 * c < cols)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const f32x2 v = __ldcg(from + (c * 32 + i) * kWarp);
+                                acc[i >> 4][c][i & 15] = p == p0 ? v : add2(acc[i >> 4][c][i & 15], v);
+                            }
+                }
+            }
+            // outputs: [16 lanes h][8 lanes r] of each 8 columns
+            const int mlane = lane >> 2, n0 = GATED ? sg.wt * 128 + (int)rank * 64 + q * 16 : sg.wt * 256 + (int)rank * 128 + q * 32;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (64 * c >= cols) break;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+#pragma unroll
+                    for (int h = 0; h < (GATED ? 1 : 2); ++h) {
+                        float v0 = lo2(acc[h][c][i]), v1 = hi2(acc[h][c][i]);
+                        if constexpr (GATED) {
+                            const float u0 = lo2(acc[1][c][i]), u1 = hi2(acc[1][c][i]);
+                            v0 = v0 > 0.0f && u0 > 0.0f ? v0 * u0 : 0.0f;
+                            v1 = v1 > 0.0f && u1 > 0.0f ? v1 * u1 : 0.0f;
+                        }
+                        const int n = n0 + 16 * h + 8 * (i & 1) + mlane;
+                        if (8 * (8 * c + (i >> 1)) >= cols) continue;
+                        if (L.y_f32) {
+                            float* y = static_cast<float*>(L.y) + (size_t)(sg.row0 + col) * L.ldy + n;
+                            if (n < L.n && col < sg.rows) y[0] = v0;
+                            if (n < L.n && col + 1 < sg.rows) y[L.ldy] = v1;
+                        } else {
+                            // lanes l and l ^ 4 hold neighbouring outputs: each takes both of one row
+                            const bool odd = mlane & 1;
+                            const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 4);
+                            const float a = odd ? other : v0, b = odd ? v1 : other;
+                            const int row = col + (odd ? 1 : 0), m = n - (odd ? 1 : 0);
+                            __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + row) * L.ldy + m;
+                            if (row < sg.rows) {
+                                if (L.y_pairs && m + 1 < L.n) {
+                                    *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(a, b);
+                                } else {
+                                    if (m < L.n) y[0] = __float2bfloat16_rn(a);
+                                    if (m + 1 < L.n) y[1] = __float2bfloat16_rn(b);
+                                }
+                            }
+                        }
+                    }
+                }
             }
         }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < kKT; ++kk)
-#pragma unroll
-            for (int p = 0; p < (GATED ? 2 : 1); ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc[p][i][j] = fmaf(xs[kk][ty * 4 + i], wt[p][kk][tx + 16 * j], acc[p][i][j]);
-        __syncthreads();
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int r = r0 + ty * 4 + i, c = c0 + tx + 16 * j;
-            if (r >= r1 || c >= L.n) continue;
-            float v = acc[0][i][j];
-            if (GATED) v = v > 0.0f && acc[GATED ? 1 : 0][i][j] > 0.0f ? v * acc[GATED ? 1 : 0][i][j] : 0.0f;
-            const size_t at = (size_t)r * L.ldy + c;
-            if (L.y_f32) static_cast<float*>(L.y)[at] = v;
-            else static_cast<__nv_bfloat16*>(L.y)[at] = __float2bfloat16_rn(v);
-        }
+
+    // ---- the end: no CTA leaves while the other may still signal or read it ----
+    if (*reinterpret_cast<volatile int*>(&sh.fail)) {  // copies may be in flight: give them time to land
+        if (tid == 0) atomicOr(L.status, kStatusTimeout);
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    __syncthreads();
+    tc_before();
+    __syncwarp();
+    cluster_sync();
+    if (warp == 2) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(512) : "memory");
+    }
+}
+
+constexpr int kDynSmem = kStageMem + 1024;
+
+template <typename F>
+cudaError_t each_kernel(F&& f) {
+    cudaError_t e = f(k_grouped<false, false, false>);
+    if (e == cudaSuccess) e = f(k_grouped<false, false, true>);
+    if (e == cudaSuccess) e = f(k_grouped<false, true, false>);
+    if (e == cudaSuccess) e = f(k_grouped<true, false, false>);
+    if (e == cudaSuccess) e = f(k_grouped<true, true, false>);
+    return e;
+}
+
+using Kernel = void (*)(GroupedLaunch);
+Kernel pick(bool e4m3, bool gated, bool kn) {
+    if (e4m3) return gated ? k_grouped<true, true, false> : k_grouped<true, false, false>;
+    if (gated) return k_grouped<false, true, false>;
+    return kn ? k_grouped<false, false, true> : k_grouped<false, false, false>;
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static const EncodeFn fn = []() -> EncodeFn {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
 }
 
 }  // namespace
 
+bool grouped_map(CUtensorMap* m, const void* p, bool e4m3, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const int size = e4m3 ? 1 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(ld * size)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows}, one[2] = {1, 1};
+    return fn(m, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims,
+              strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t prepare_grouped() {
+    return each_kernel(
+        [](Kernel k) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmem); });
+}
+
+namespace {
+void configure(cudaLaunchConfig_t* cfg, int pairs, cudaStream_t stream) {
+    cfg->gridDim = dim3(2 * pairs);
+    cfg->blockDim = dim3(kCtaThreads);
+    cfg->dynamicSmemBytes = kDynSmem;
+    cfg->stream = stream;
+}
+}  // namespace
+
+int grouped_pairs(bool e4m3, bool gated, bool kn) {
+    cudaLaunchConfig_t cfg{};
+    configure(&cfg, 1, nullptr);
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {2, 1, 1};
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, pick(e4m3, gated, kn), &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    return n;
+}
+
 cudaError_t launch_grouped(const GroupedLaunch& a, bool e4m3, bool gated, bool kn, cudaStream_t stream) {
-    const int groups = a.offsets ? a.n_groups : 1;
-    const dim3 grid((unsigned)((a.n + kT - 1) / kT), (unsigned)((a.rows + kT - 1) / kT + groups));
-    if (e4m3)
-        gated ? k_grouped<true, true, false><<<grid, 256, 0, stream>>>(a)
-              : k_grouped<true, false, false><<<grid, 256, 0, stream>>>(a);
-    else if (gated)
-        k_grouped<false, true, false><<<grid, 256, 0, stream>>>(a);
-    else
-        kn ? k_grouped<false, false, true><<<grid, 256, 0, stream>>>(a)
-           : k_grouped<false, false, false><<<grid, 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    configure(&cfg, a.pairs, stream);
+    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn), a);
 }
 
 }  // namespace tsffn

@@ -1,6 +1,7 @@
 // ts_grouped.h -- launch parameters and launchers of the operators over many tokens (ts_route.cu, ts_rows.cu, ts_grouped.cu).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -41,19 +42,23 @@ struct CombineLaunch {
     float* y;
 };
 
-// Weights of one group.
+// Weights of one group: where TMA finds them, and TS_E4M3 scales. Device memory.
 struct GroupWeights {
-    const void* w;
-    const void* u;   // gated
-    const float* ws; // TS_E4M3 scales
+    CUtensorMap w;
+    CUtensorMap u;   // gated
+    const float* ws;
     const float* us;
 };
 
+constexpr int kXMaps = 5;         // maps of x: boxes of 8, 16, 32, 64 and 128 rows
+constexpr int kMaxTileRows = 256; // rows of x of a tile
+constexpr int kEpiWarps = 8;
+
+// A CTA pair's tiles of the products, and the parts of tiles that several pairs share.
 struct GroupedLaunch {
+    CUtensorMap x[kXMaps];
     int n_groups, n, k;
     const GroupWeights* weights;  // device [n_groups]
-    const void* x;
-    int64_t ldx;
     const float* x_scale;         // [k / 128][ld_scale]
     int64_t ld_scale;
     const int32_t* offsets;       // [n_groups + 1] or nullptr (one group)
@@ -61,8 +66,26 @@ struct GroupedLaunch {
     void* y;
     int64_t ldy;
     int y_f32;
+    int y_pairs;                  // bf16 rows of y start on 4-byte boundaries
+    int pairs;                    // CTA pairs of the grid
+    int part_chunks;              // 64-column chunks of a warp's part in `partial`: 1 or 2
+    float* partial;               // [pairs][2][2 CTAs][kEpiWarps][part_chunks * 2048]
+    unsigned* arrived;            // [2 * pairs][2 CTAs][kEpiWarps], zero between calls
     unsigned* status;
 };
+
+// Bytes of GroupedLaunch::partial for tiles of up to `rows` rows, and entries of `arrived`.
+inline int grouped_part_chunks(int rows) { return rows > 128 ? 2 : 1; }
+inline size_t grouped_partial_bytes(int pairs, int chunks) { return (size_t)pairs * 2 * 2 * kEpiWarps * chunks * 2048 * 4; }
+inline size_t grouped_arrived(int pairs) { return (size_t)pairs * 2 * 2 * kEpiWarps; }
+
+// Tensor map of a [rows][cols] matrix (ld elements apart) whose boxes are 128 bytes wide and box_rows high, with the
+// 128-byte swizzle; false where it cannot be made.
+bool grouped_map(CUtensorMap* m, const void* p, bool e4m3, int64_t cols, int64_t rows, int64_t ld, int box_rows);
+constexpr int grouped_w_box(bool gated, bool kn) { return gated ? 16 : kn ? 64 : 128; }
+cudaError_t prepare_grouped();
+// CTA pairs that can be resident at once.
+int grouped_pairs(bool e4m3, bool gated, bool kn);
 
 cudaError_t launch_route(const RouteLaunch& a, cudaStream_t stream);
 cudaError_t launch_gather_rows(const RowsLaunch& a, int elem_bytes, cudaStream_t stream);

@@ -1,6 +1,7 @@
 // ts_prompt_api.cu -- the C ABI of the operators over many tokens (include/ts_ffn.h): argument checks, handles, launches.
 #include <stdint.h>
 
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -38,7 +39,55 @@ struct ts_grouped {
     Arena arena;
     GroupWeights* weights = nullptr;  // device [n_groups]
     unsigned* status = nullptr;
+    int pairs = 0, part_chunks = 1;
+    float* partial = nullptr;
+    unsigned* arrived = nullptr;
 };
+
+namespace {
+
+// Tensor maps of the weights, scratch and its contents.
+ts_status grouped_init(ts_grouped* h, std::vector<GroupWeights>& table, int n_groups, int n, int k, ts_dtype wdtype,
+                       ts_layout layout, const void* const* w, const void* const* w_up, const float* const* scale,
+                       const float* const* scale_up, int max_rows) {
+    const bool e8 = wdtype == TS_E4M3, gated = w_up != nullptr, kn = layout == TS_KN;
+    h->n_groups = n_groups;
+    h->n = n;
+    h->k = k;
+    h->max_rows = max_rows;
+    h->dt = wdtype;
+    h->layout = layout;
+    h->gated = gated;
+    if (prepare_grouped() != cudaSuccess) return TS_ERR_CUDA;
+    h->pairs = grouped_pairs(e8, gated, kn);
+    if (h->pairs < 1) return TS_ERR_CUDA;
+    h->part_chunks = grouped_part_chunks(max_rows);
+    const int box = grouped_w_box(gated, kn);
+    const int64_t cols = kn ? n : k, rows = kn ? k : n;
+    for (int e = 0; e < n_groups; ++e) {
+        GroupWeights& g = table[(size_t)e];
+        g.ws = e8 ? scale[e] : nullptr;
+        g.us = e8 && gated ? scale_up[e] : nullptr;
+        if (!grouped_map(&g.w, w[e], e8, cols, rows, cols, box)) return TS_ERR_CUDA;
+        if (gated && !grouped_map(&g.u, w_up[e], e8, cols, rows, cols, box)) return TS_ERR_CUDA;
+    }
+    const size_t bytes = sizeof(GroupWeights) * (size_t)n_groups;
+    const size_t o_w = h->arena.take(bytes), o_status = h->arena.take(sizeof(unsigned));
+    const size_t o_arrived = h->arena.take(grouped_arrived(h->pairs) * sizeof(unsigned));
+    const size_t o_partial = h->arena.take(grouped_partial_bytes(h->pairs, h->part_chunks));
+    const ts_status s = alloc_arena(&h->arena);
+    if (s != TS_OK) return s;
+    h->weights = h->arena.at<GroupWeights>(o_w);
+    h->status = h->arena.at<unsigned>(o_status);
+    h->arrived = h->arena.at<unsigned>(o_arrived);
+    h->partial = h->arena.at<float>(o_partial);
+    if (cudaMemcpy(h->weights, table.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess ||
+        cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess)
+        return TS_ERR_CUDA;
+    return TS_OK;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -88,45 +137,23 @@ ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dty
     if (k % (e8 ? 16 : 8) != 0 || (layout == TS_KN && n % 8 != 0)) return TS_ERR_INVALID_ARG;
     if (layout == TS_KN && (e8 || gated)) return TS_ERR_UNSUPPORTED;
     if (e8 != (scale != nullptr) || (e8 && gated) != (scale_up != nullptr)) return TS_ERR_INVALID_ARG;
+    for (int e = 0; e < n_groups; ++e)
+        if (!w[e] || !aligned16(w[e]) || (gated && (!w_up[e] || !aligned16(w_up[e]))) || (e8 && !scale[e]) ||
+            (e8 && gated && !scale_up[e]))
+            return TS_ERR_INVALID_ARG;
     std::vector<GroupWeights> table;
     ts_grouped* h = nullptr;
     try {
         table.resize((size_t)n_groups);
         h = new ts_grouped;
+        h->arena.guards.reserve(8);
     } catch (const std::bad_alloc&) {
+        delete h;
         return TS_ERR_OOM;
     }
-    for (int e = 0; e < n_groups; ++e) {
-        GroupWeights& g = table[(size_t)e];
-        g.w = w[e];
-        g.u = gated ? w_up[e] : nullptr;
-        g.ws = e8 ? scale[e] : nullptr;
-        g.us = e8 && gated ? scale_up[e] : nullptr;
-        if (!g.w || !aligned16(g.w) || (gated && (!g.u || !aligned16(g.u))) || (e8 && !g.ws) || (e8 && gated && !g.us)) {
-            delete h;
-            return TS_ERR_INVALID_ARG;
-        }
-    }
-    h->n_groups = n_groups;
-    h->n = n;
-    h->k = k;
-    h->max_rows = max_rows;
-    h->dt = wdtype;
-    h->layout = layout;
-    h->gated = gated;
-    const size_t o_w = h->arena.take(sizeof(GroupWeights) * (size_t)n_groups), o_status = h->arena.take(sizeof(unsigned));
-    ts_status s = alloc_arena(&h->arena);
-    if (s == TS_OK) {
-        h->weights = h->arena.at<GroupWeights>(o_w);
-        h->status = h->arena.at<unsigned>(o_status);
-        if (cudaMemcpy(h->weights, table.data(), sizeof(GroupWeights) * (size_t)n_groups, cudaMemcpyHostToDevice) !=
-                cudaSuccess ||
-            cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess)
-            s = TS_ERR_CUDA;
-    }
+    const ts_status s = grouped_init(h, table, n_groups, n, k, wdtype, layout, w, w_up, scale, scale_up, max_rows);
     if (s != TS_OK) {
-        if (h->arena.base) cudaFree(h->arena.base);
-        delete h;
+        ts_grouped_destroy(h);
         return s;
     }
     *out = h;
@@ -135,7 +162,7 @@ ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dty
 
 void ts_grouped_destroy(ts_grouped* h) {
     if (!h) return;
-    cudaFree(h->arena.base);
+    if (h->arena.base) cudaFree(h->arena.base);
     delete h;
 }
 
@@ -149,13 +176,17 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     if (!x || !y || !aligned16(x) || ldx < h->k || ldx * elem_size(h->dt) % 16 != 0 || ldy < h->n)
         return TS_ERR_INVALID_ARG;
     if (e8 ? (!x_scale || ld_scale < rows) : x_scale != nullptr) return TS_ERR_INVALID_ARG;
-    GroupedLaunch a{};
+    GroupedLaunch a;
+    // boxes of up to half of the widest tile that so many rows can give
+    const int widest = std::min(kMaxTileRows, (rows + 15) / 16 * 16);
+    for (int i = 0; i < kXMaps; ++i) {
+        if (!grouped_map(&a.x[i], x, e8, h->k, rows, ldx, 8 << i)) return TS_ERR_CUDA;
+        if ((8 << i) >= widest / 2) break;
+    }
     a.n_groups = h->n_groups;
     a.n = h->n;
     a.k = h->k;
     a.weights = h->weights;
-    a.x = x;
-    a.ldx = ldx;
     a.x_scale = x_scale;
     a.ld_scale = ld_scale;
     a.offsets = offsets;
@@ -163,6 +194,11 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     a.y = y;
     a.ldy = ldy;
     a.y_f32 = ydtype == TS_F32;
+    a.y_pairs = ldy % 2 == 0 && ((uintptr_t)y & 3u) == 0;
+    a.pairs = h->pairs;
+    a.part_chunks = h->part_chunks;
+    a.partial = h->partial;
+    a.arrived = h->arrived;
     a.status = h->status;
     return launched(launch_grouped(a, e8, h->gated, h->layout == TS_KN, stream));
 }
