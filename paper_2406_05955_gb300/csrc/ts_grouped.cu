@@ -22,12 +22,13 @@
 namespace tsffn {
 namespace {
 
-constexpr int kCtaThreads = 384;
 constexpr int kEpiWarp0 = 4;
+constexpr int kCtaThreads = (kEpiWarp0 + kEpiWarps) * kWarp;
 constexpr int kStageW = 16384;                  // weights of a stage: 128 rows of 128 bytes
 constexpr int kMaxStages = 12;
-constexpr int kStageMem = 216 * 1024 - 4096;    // bytes of all stages
+constexpr int kStageMem = 204 * 1024;           // bytes of all stages
 constexpr int kBand = 8;                        // tiles of x that one sweep over the weights serves
+constexpr int kScaleSlots = 4;
 constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
 
@@ -38,7 +39,9 @@ struct Shared {
     int max_cols;                               // widest tile
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
-    float scale[kEpiWarps][2][128];             // e4m3: scales of a warp's rows of x, this stage's and the next one's
+    // e4m3: scales of a warp's rows of x and of its weights (gate and up), for this stage and the next ones
+    alignas(16) float scale[kEpiWarps][kScaleSlots][128];
+    float wscale[kEpiWarps][kScaleSlots][2];
 };
 
 // ---- cluster and tcgen05 helpers (pairs of CTAs) ---------------------------
@@ -56,8 +59,9 @@ __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
     return a;
 }
+// (It passes on nothing that was written to memory, so the release needs no wider scope than the CTA.)
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // 2-D box into this CTA's shared memory, its bytes counted by the barrier at `bar` (a CTA of the pair)
 __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -67,6 +71,21 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// 4-byte copy global -> shared, 0 where not `take`
+__device__ __forceinline__ void cp4(float* dst, const float* src, bool take) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(take ? 4u : 0u) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 template <bool E8>
@@ -139,9 +158,20 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
 }
 
 // Registers: the warps that keep the sums get those that the others do not need. Of the block's 384 x 168 = 64512,
-// 128 x 80 + 256 x 208 = 63488 are dealt out.
-__device__ __forceinline__ void regs_shrink() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
-__device__ __forceinline__ void regs_grow() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+// 128 x 56 + 256 x 224 = 64512 are dealt out.
+__device__ __forceinline__ void regs_shrink() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
+__device__ __forceinline__ void regs_grow() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+
+__device__ __forceinline__ uint32_t bf16x2(f32x2 v) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo2(v), hi2(v));
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+// four 8 x 8 matrices, each turned round: lane i gives the place of row i % 8 of matrix i / 8
+__device__ __forceinline__ void stmatrix(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c),
+                 "r"(d)
+                 : "memory");
+}
 
 // ---- tiles and their parts --------------------------------------------------
 // The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
@@ -230,10 +260,19 @@ struct Kind {
     static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
 };
 
+// Bounded wait; the clock is read only now and then.
 __device__ __forceinline__ bool wait_for(uint64_t* bar, unsigned parity, Shared& sh) {
-    if (mbar_wait(bar, parity)) return true;
-    sh.fail = 1;
-    return false;
+    unsigned long long t0 = 0;
+    for (int i = 1; !mbar_try_wait_sleep(bar, parity, 10000u); ++i) {
+        if ((i & 255) != 0) continue;
+        const unsigned long long t = global_ns();
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > kWaitLimitNs) {
+            sh.fail = 1;
+            return false;
+        }
+    }
+    return true;
 }
 
 template <bool E8, bool GATED, bool KN>
@@ -367,36 +406,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 }
             }
         } else if (warp == 1) {
-            // ---- MMAs, by one thread of the first CTA ----
-            if (rank == 0 && lane == 0) {
+            // ---- MMAs, by the first CTA. The whole warp runs the loop and one lane issues, so that what the MMAs take
+            // is known to be the same for all lanes and stays in uniform registers. ----
+            if (rank == 0) {
+                const uint32_t tmem = uniform(sh.tmem), base = uniform(sm0), size = uniform(stage_bytes);
+                const int n_st = (int)uniform((uint32_t)stages);
                 int st = 0, chunk = 0;
                 unsigned ph = 0;
                 bool ok = true;
                 while (ok && walk.next(sg)) {
-                    const uint32_t idesc = K::kIdesc | (uint32_t)(sg.cols >> 3) << 17;
-                    for (int k = sg.k0; ok && k < sg.k1;) {
-                        const int kc = min(sg.k1, k + K::kChunk);
+                    const uint32_t idesc = K::kIdesc | (uniform((uint32_t)sg.cols) >> 3) << 17;
+                    const int k_end = (int)uniform((uint32_t)sg.k1);
+                    for (int k = (int)uniform((uint32_t)sg.k0); ok && k < k_end;) {
+                        const int kc = min(k_end, k + K::kChunk);
                         const int buf = chunk & 1;
                         if (chunk >= 2) ok = wait_for(&sh.tempty[buf], ((chunk >> 1) & 1) ^ 1u, sh);
                         tc_after();
-                        const uint32_t d = sh.tmem + buf * 256;
+                        const uint32_t d = tmem + buf * 256;
                         for (int first = k; ok && k < kc; ++k) {
                             ok = wait_for(&sh.full[st], ph, sh);
                             if (!ok) break;
                             tc_after();
-                            const uint32_t a0 = sm0 + st * stage_bytes;
+                            const uint32_t a0 = base + st * size;
                             const uint64_t bd = desc_k(a0 + kStageW);
                             const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
+                            if (elect_one()) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
-                            pair_commit(&sh.empty[st]);
-                            if (++st == stages) {
+                                for (int i = 0; i < 4; ++i)
+                                    pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
+                                pair_commit(&sh.empty[st]);
+                                if (k + 1 == kc) pair_commit(&sh.tfull[buf]);
+                            }
+                            __syncwarp();
+                            if (++st == n_st) {
                                 st = 0;
                                 ph ^= 1u;
                             }
                         }
-                        if (ok) pair_commit(&sh.tfull[buf]);
                         ++chunk;
                     }
                 }
@@ -405,8 +451,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         }
     } else {
         regs_grow();
-        // ---- sums: warp ew holds lanes 32 (ew % 4) .. + 31 of the columns of half ew / 4 of a tile ----
-        const int ew = warp - kEpiWarp0, q = ew & 3, half = ew >> 2;
+        // ---- sums: a warp may read the 32 lanes of its number modulo 4; it holds those of half ew / 4 of a tile's columns ----
+        const int ew = warp - kEpiWarp0, q = warp & 3, half = ew >> 2;
         const uint32_t lane_addr = sh.tmem + ((uint32_t)(32 * q) << 16);
         int chunk = 0;
         bool ok = true;
@@ -418,34 +464,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             const GroupWeights* gw = L.weights + sg.g;
             const float* xs = nullptr;
             const float* ws[2] = {nullptr, nullptr};
-            float next_x[4], next_w[2];
-            auto fetch = [&](int k) {  // e4m3: the scales of a stage
+            // The scales of a stage are copied kScaleSlots - 1 stages ahead: an L2 access takes longer than a stage's MMAs.
+            auto fetch = [&](int k) {
+                if (k < sg.k1) {
+                    const int slot = k & (kScaleSlots - 1);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = lane + 32 * i;
-                    next_x[i] = c < cols && c0 + c < sg.rows ? __ldg(xs + (size_t)k * L.ld_scale + c) : 0.0f;
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = lane + 32 * i;
+                        if (c < cols) cp4(&sh.scale[ew][slot][c], xs + (size_t)k * L.ld_scale + c, c0 + c < sg.rows);
+                    }
+                    if (lane < (GATED ? 2 : 1)) cp4(&sh.wscale[ew][slot][lane], ws[lane] + k, true);
                 }
-                next_w[0] = __ldg(ws[0] + k);
-                if (GATED) next_w[1] = __ldg(ws[1] + k);
+                cp_commit();
             };
             if constexpr (E8) {
                 const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
                 xs = L.x_scale + sg.row0 + c0;
                 ws[0] = gw->ws + (size_t)block * steps;
-                if (GATED) ws[1] = gw->us + (size_t)block * steps;
-                fetch(sg.k0);
+                ws[1] = GATED ? gw->us + (size_t)block * steps : nullptr;
+                for (int i = 0; i < kScaleSlots - 1; ++i) fetch(sg.k0 + i);
             }
             for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
                 const int buf = chunk & 1;
-                float* mine = sh.scale[ew][buf];
+                const float* mine = sh.scale[ew][k & (kScaleSlots - 1)];
                 f32x2 w2[2];
                 if constexpr (E8) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mine[lane + 32 * i] = next_x[i];
-                    w2[0] = pack2(__float_as_uint(next_w[0]), __float_as_uint(next_w[0]));
-                    w2[1] = GATED ? pack2(__float_as_uint(next_w[1]), __float_as_uint(next_w[1])) : w2[0];
+                    cp_wait<kScaleSlots - 2>();
                     __syncwarp();
-                    if (k + 1 < sg.k1) fetch(k + 1);
+                    const float* w = sh.wscale[ew][k & (kScaleSlots - 1)];
+                    w2[0] = pack2(__float_as_uint(w[0]), __float_as_uint(w[0]));
+                    w2[1] = GATED ? pack2(__float_as_uint(w[1]), __float_as_uint(w[1])) : w2[0];
+                    fetch(k + kScaleSlots - 1);  // into the slot of the stage before, which all lanes have read
                 }
                 ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> 1) & 1, sh));
                 if (!ok) break;
@@ -515,44 +564,83 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             }
             // outputs: [16 lanes h][8 lanes r] of each 8 columns
             const int mlane = lane >> 2, n0 = GATED ? sg.wt * 128 + (int)rank * 64 + q * 16 : sg.wt * 256 + (int)rank * 128 + q * 32;
+            if constexpr (GATED) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (64 * c >= cols) break;
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                    for (int i = 0; i < 16; ++i) {
+                        const float g0 = lo2(acc[0][c][i]), g1 = hi2(acc[0][c][i]), u0 = lo2(acc[1][c][i]), u1 = hi2(acc[1][c][i]);
+                        acc[0][c][i] = pack2(__float_as_uint(g0 > 0.0f && u0 > 0.0f ? g0 * u0 : 0.0f),
+                                             __float_as_uint(g1 > 0.0f && u1 > 0.0f ? g1 * u1 : 0.0f));
+                    }
+            }
+            constexpr int kN = GATED ? 16 : 32;  // outputs of a warp
+            if (L.y_f32) {
+                float* y = static_cast<float*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
 #pragma unroll
-                    for (int h = 0; h < (GATED ? 1 : 2); ++h) {
-                        float v0 = lo2(acc[h][c][i]), v1 = hi2(acc[h][c][i]);
-                        if constexpr (GATED) {
-                            const float u0 = lo2(acc[1][c][i]), u1 = hi2(acc[1][c][i]);
-                            v0 = v0 > 0.0f && u0 > 0.0f ? v0 * u0 : 0.0f;
-                            v1 = v1 > 0.0f && u1 > 0.0f ? v1 * u1 : 0.0f;
-                        }
-                        const int n = n0 + 16 * h + 8 * (i & 1) + mlane;
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
                         if (8 * (8 * c + (i >> 1)) >= cols) continue;
-                        if (L.y_f32) {
-                            float* y = static_cast<float*>(L.y) + (size_t)(sg.row0 + col) * L.ldy + n;
-                            if (n < L.n && col < sg.rows) y[0] = v0;
-                            if (n < L.n && col + 1 < sg.rows) y[L.ldy] = v1;
-                        } else {
-                            // lanes l and l ^ 4 hold neighbouring outputs: each takes both of one row
-                            const bool odd = mlane & 1;
-                            const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 4);
-                            const float a = odd ? other : v0, b = odd ? v1 : other;
-                            const int row = col + (odd ? 1 : 0), m = n - (odd ? 1 : 0);
-                            __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + row) * L.ldy + m;
-                            if (row < sg.rows) {
-                                if (L.y_pairs && m + 1 < L.n) {
-                                    *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(a, b);
-                                } else {
-                                    if (m < L.n) y[0] = __float2bfloat16_rn(a);
-                                    if (m + 1 < L.n) y[1] = __float2bfloat16_rn(b);
-                                }
-                            }
+                        const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        float* at = y + (size_t)col * L.ldy + 8 * (i & 1);
+#pragma unroll
+                        for (int h = 0; h < kN / 16; ++h) {
+                            const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
+                            if (in && col < sg.rows) at[16 * h] = lo2(acc[h][c][i]);
+                            if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = hi2(acc[h][c][i]);
                         }
                     }
-                }
+            } else if (L.y_vec && n0 + kN <= L.n) {
+                // bf16: 16 rows of y at a time are turned round in the warp's own shared memory (its scales' place, idle here),
+                // so that a store writes whole sectors: 64 bytes of a row (gated: 32). Two bytes of 16 rows each instead,
+                // straight from the registers, held the tiles up: 8192 x 8192 x 4096 took 323 us against XXX.
+                constexpr int kPitch = 2 * kN + 16;
+                unsigned char* turn = reinterpret_cast<unsigned char*>(&sh.scale[ew][0][0]);
+                const uint32_t to = smem_u32(turn) + (GATED ? ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16
+                                                            : (lane & 7) * kPitch + (lane >> 3) * 16);
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + c0) * L.ldy + n0;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {  // 16 columns
+                        if (64 * c + 16 * p >= cols) continue;
+                        const f32x2* v0 = &acc[0][c][4 * p];  // 8 columns: lanes 0-7, 8-15; the next 8
+                        const f32x2* v1 = &acc[1][c][4 * p];
+                        __syncwarp();
+                        if constexpr (GATED) {
+                            stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v0[2]), bf16x2(v0[3]));
+                        } else {
+                            stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v1[0]), bf16x2(v1[1]));
+                            stmatrix(to + 8 * kPitch, bf16x2(v0[2]), bf16x2(v0[3]), bf16x2(v1[2]), bf16x2(v1[3]));
+                        }
+                        __syncwarp();
+                        constexpr int kLanes = kN / 8;  // lanes of a row
+#pragma unroll
+                        for (int r0 = 0; r0 < 16; r0 += 32 / kLanes) {
+                            const int r = r0 + lane / kLanes, col = 64 * c + 16 * p + r;
+                            const uint4 v = lds128(turn + r * kPitch + (lane % kLanes) * 16);
+                            if (col < cols && c0 + col < sg.rows)
+                                *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane % kLanes) * 8) = v;
+                        }
+                    }
+                __syncwarp();  // the next tile's scales go there
+            } else {
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (8 * (8 * c + (i >> 1)) >= cols) continue;
+                        const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        __nv_bfloat16* at = y + (size_t)col * L.ldy + 8 * (i & 1);
+#pragma unroll
+                        for (int h = 0; h < kN / 16; ++h) {
+                            const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
+                            if (in && col < sg.rows) at[16 * h] = __float2bfloat16_rn(lo2(acc[h][c][i]));
+                            if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = __float2bfloat16_rn(hi2(acc[h][c][i]));
+                        }
+                    }
             }
         }
     }

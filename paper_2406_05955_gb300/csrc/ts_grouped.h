@@ -66,7 +66,7 @@ struct GroupedLaunch {
     void* y;
     int64_t ldy;
     int y_f32;
-    int y_pairs;                  // bf16 rows of y start on 4-byte boundaries
+    int y_vec;                    // bf16 rows of y start on 16-byte boundaries
     int pairs;                    // CTA pairs of the grid
     int part_chunks;              // 64-column chunks of a warp's part in `partial`: 1 or 2
     float* partial;               // [pairs][2][2 CTAs][kEpiWarps][part_chunks * 2048]

@@ -194,7 +194,7 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     a.y = y;
     a.ldy = ldy;
     a.y_f32 = ydtype == TS_F32;
-    a.y_pairs = ldy % 2 == 0 && ((uintptr_t)y & 3u) == 0;
+    a.y_vec = ldy % 8 == 0 && aligned16(y);
     a.pairs = h->pairs;
     a.part_chunks = h->part_chunks;
     a.partial = h->partial;
