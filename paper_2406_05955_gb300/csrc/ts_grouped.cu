@@ -34,14 +34,16 @@ constexpr int kMinSteps = 4;                    // fewest stages of a part of a 
 
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
+    uint64_t met[kEpiWarps / 2];                // gated: a gate and an up warp
+    unsigned before[kEpiWarps / 2];
     uint32_t tmem;
     int fail;
     int max_cols;                               // widest tile
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
-    // e4m3: scales of a warp's rows of x and of its weights (gate and up), for this stage and the next ones
+    // e4m3: scales of a warp's rows of x and of its weights, for this stage and the next ones
     alignas(16) float scale[kEpiWarps][kScaleSlots][128];
-    float wscale[kEpiWarps][kScaleSlots][2];
+    float wscale[kEpiWarps][kScaleSlots];
 };
 
 // ---- cluster and tcgen05 helpers (pairs of CTAs) ---------------------------
@@ -256,7 +258,7 @@ struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
     static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
     static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
-    static constexpr int kBoxes = GATED ? 8 : KN ? 2 : 1;  // boxes of weights of a CTA's stage
+    static constexpr int kBoxes = GATED || KN ? 2 : 1;    // boxes of weights of a CTA's stage
     static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
 };
 
@@ -326,6 +328,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             mbar_init(&sh.tfull[b], 1);
             mbar_init(&sh.tempty[b], 2 * kEpiWarps);
         }
+        for (int b = 0; b < kEpiWarps / 2; ++b) mbar_init(&sh.met[b], 2);
         sh.fail = 0;
         mbar_fence_init();
     } else if (warp == 2) {
@@ -361,10 +364,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 uint32_t off = kStageW;
                 int cy = sg.row0 + (int)rank * (sg.cols / 2), cx = 0;  // coordinate of the box besides k's
                 if (lane < K::kBoxes) {
-                    if constexpr (GATED) {  // 16 gate rows and 16 up rows in turn
-                        map = lane & 1 ? &gw->u : &gw->w;
-                        off = lane * 2048;
-                        cy = sg.wt * 128 + (int)rank * 64 + (lane >> 1) * 16;
+                    if constexpr (GATED) {  // 64 gate rows, then the same neurons' up rows
+                        map = lane ? &gw->u : &gw->w;
+                        off = lane * 8192;
+                        cy = sg.wt * 128 + (int)rank * 64;
                     } else if constexpr (KN) {
                         map = &gw->w;
                         off = lane * 8192;
@@ -456,6 +459,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         const uint32_t lane_addr = sh.tmem + ((uint32_t)(32 * q) << 16);
         int chunk = 0;
         bool ok = true;
+        // gated: a gate warp and the up warp of the same neurons wait for each other
+        const int both = half * 2 + (q & 1);
+        unsigned met = 0;
+        auto meet = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.met[both]);
+            const bool here = __all_sync(0xffffffffu, wait_for(&sh.met[both], met & 1u, sh));
+            ++met;
+            return here;
+        };
         while (ok && walk.next(sg)) {
             const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8
             f32x2 acc[2][2][16];  // [16 lanes][64 columns][of 8 columns: lanes t / 4, lanes t / 4 + 8]
@@ -463,7 +476,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             for (int i = 0; i < 64; ++i) acc[i >> 5][(i >> 4) & 1][i & 15] = 0ull;
             const GroupWeights* gw = L.weights + sg.g;
             const float* xs = nullptr;
-            const float* ws[2] = {nullptr, nullptr};
+            const float* ws = nullptr;
             // The scales of a stage are copied kScaleSlots - 1 stages ahead: an L2 access takes longer than a stage's MMAs.
             auto fetch = [&](int k) {
                 if (k < sg.k1) {
@@ -473,27 +486,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         const int c = lane + 32 * i;
                         if (c < cols) cp4(&sh.scale[ew][slot][c], xs + (size_t)k * L.ld_scale + c, c0 + c < sg.rows);
                     }
-                    if (lane < (GATED ? 2 : 1)) cp4(&sh.wscale[ew][slot][lane], ws[lane] + k, true);
+                    if (lane == 0) cp4(&sh.wscale[ew][slot], ws + k, true);
                 }
                 cp_commit();
             };
             if constexpr (E8) {
                 const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
                 xs = L.x_scale + sg.row0 + c0;
-                ws[0] = gw->ws + (size_t)block * steps;
-                ws[1] = GATED ? gw->us + (size_t)block * steps : nullptr;
+                ws = (GATED && q >= 2 ? gw->us : gw->ws) + (size_t)block * steps;
                 for (int i = 0; i < kScaleSlots - 1; ++i) fetch(sg.k0 + i);
             }
             for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
                 const int buf = chunk & 1;
                 const float* mine = sh.scale[ew][k & (kScaleSlots - 1)];
-                f32x2 w2[2];
+                f32x2 w2;
                 if constexpr (E8) {
                     cp_wait<kScaleSlots - 2>();
                     __syncwarp();
-                    const float* w = sh.wscale[ew][k & (kScaleSlots - 1)];
-                    w2[0] = pack2(__float_as_uint(w[0]), __float_as_uint(w[0]));
-                    w2[1] = GATED ? pack2(__float_as_uint(w[1]), __float_as_uint(w[1])) : w2[0];
+                    const uint32_t w = __float_as_uint(sh.wscale[ew][k & (kScaleSlots - 1)]);
+                    w2 = pack2(w, w);
                     fetch(k + kScaleSlots - 1);  // into the slot of the stage before, which all lanes have read
                 }
                 ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> 1) & 1, sh));
@@ -510,7 +521,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         for (int j = 0; j < 8; ++j) {
                             if constexpr (E8) {
                                 const float2 s = *reinterpret_cast<const float2*>(&mine[64 * c + 8 * j + 2 * (lane & 3)]);
-                                const f32x2 s2 = mul2(pack2(__float_as_uint(s.x), __float_as_uint(s.y)), w2[h]);
+                                const f32x2 s2 = mul2(pack2(__float_as_uint(s.x), __float_as_uint(s.y)), w2);
                                 acc[h][c][2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), s2, acc[h][c][2 * j]);
                                 acc[h][c][2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), s2, acc[h][c][2 * j + 1]);
                             } else {
@@ -545,11 +556,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 __syncwarp();
                 unsigned* count = L.arrived + ((size_t)sg.rest * 2 + rank) * kEpiWarps + ew;
                 unsigned before = 0;
-                if (lane == 0) before = atomicAdd(count, 1u);
-                before = __shfl_sync(0xffffffffu, before, 0);
+                if constexpr (GATED) {  // a gate and an up warp finish a tile together, so they are counted as one
+                    ok = meet();
+                    if (q < 2 && lane == 0) sh.before[both] = atomicAdd(count, 1u);
+                    ok = ok && meet();
+                    if (!ok) break;
+                    before = sh.before[both];
+                } else {
+                    if (lane == 0) before = atomicAdd(count, 1u);
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                }
                 if ((int)before != p1 - p0) continue;
                 __threadfence();
-                if (lane == 0) *count = 0u;
+                if (lane == 0 && (!GATED || q < 2)) *count = 0u;
                 for (int p = p0; p <= p1; ++p) {
                     const f32x2* from = part_of(p);
 #pragma unroll
@@ -563,85 +582,95 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 }
             }
             // outputs: [16 lanes h][8 lanes r] of each 8 columns
-            const int mlane = lane >> 2, n0 = GATED ? sg.wt * 128 + (int)rank * 64 + q * 16 : sg.wt * 256 + (int)rank * 128 + q * 32;
+            const int mlane = lane >> 2;
+            int n0 = sg.wt * 256 + (int)rank * 128 + q * 32, cb = c0;  // the warp's first output and first column
+            unsigned char* turn = reinterpret_cast<unsigned char*>(&sh.scale[ew][0][0]);  // 2 KB of its own, idle here
             if constexpr (GATED) {
+                // Warp q < 2 holds the gate values and warp q + 2 the up values of the same neurons: the first finishes
+                // columns 0-63, the second 64-127, each with what the other sends it, 16 columns at a time.
+                n0 = sg.wt * 128 + (int)rank * 64 + (q & 1) * 32;
+                cb = c0 + 64 * (q >> 1);
+                f32x2* mine = reinterpret_cast<f32x2*>(turn) + lane;
+                const f32x2* theirs = reinterpret_cast<const f32x2*>(&sh.scale[ew ^ 2][0][0]) + lane;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int p = 0; p < 4; ++p) {
+                    if (16 * p >= cols) break;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float g0 = lo2(acc[0][c][i]), g1 = hi2(acc[0][c][i]), u0 = lo2(acc[1][c][i]), u1 = hi2(acc[1][c][i]);
-                        acc[0][c][i] = pack2(__float_as_uint(g0 > 0.0f && u0 > 0.0f ? g0 * u0 : 0.0f),
-                                             __float_as_uint(g1 > 0.0f && u1 > 0.0f ? g1 * u1 : 0.0f));
+                    for (int i = 0; i < 8; ++i) mine[i * kWarp] = q < 2 ? acc[i >> 2][1][4 * p + (i & 3)] : acc[i >> 2][0][4 * p + (i & 3)];
+                    ok = ok && meet();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const f32x2 a = q < 2 ? acc[i >> 2][0][4 * p + (i & 3)] : acc[i >> 2][1][4 * p + (i & 3)], b = theirs[i * kWarp];
+                        acc[i >> 2][0][4 * p + (i & 3)] =
+                            pack2(__float_as_uint(lo2(a) > 0.0f && lo2(b) > 0.0f ? lo2(a) * lo2(b) : 0.0f),
+                                  __float_as_uint(hi2(a) > 0.0f && hi2(b) > 0.0f ? hi2(a) * hi2(b) : 0.0f));
                     }
+                    ok = ok && meet();  // both have read before either writes there again
+                }
+                if (!ok) break;
             }
-            constexpr int kN = GATED ? 16 : 32;  // outputs of a warp
+            const int n_cols = cols - (cb - c0);  // of the warp's columns, those that it finishes: none where it is not above 0
+            constexpr int kC = GATED ? 1 : 2;     // in chunks of 64
             if (L.y_f32) {
                 float* y = static_cast<float*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if (8 * (8 * c + (i >> 1)) >= cols) continue;
-                        const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        if (64 * c + 8 * (i >> 1) >= n_cols) continue;
+                        const int col = cb + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
                         float* at = y + (size_t)col * L.ldy + 8 * (i & 1);
 #pragma unroll
-                        for (int h = 0; h < kN / 16; ++h) {
+                        for (int h = 0; h < 2; ++h) {
                             const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
                             if (in && col < sg.rows) at[16 * h] = lo2(acc[h][c][i]);
                             if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = hi2(acc[h][c][i]);
                         }
                     }
-            } else if (L.y_vec && n0 + kN <= L.n) {
-                // bf16: 16 rows of y at a time are turned round in the warp's own shared memory (its scales' place, idle here),
-                // so that a store writes whole sectors: 64 bytes of a row (gated: 32). Two bytes of 16 rows each instead,
-                // straight from the registers, held the tiles up: 8192 x 8192 x 4096 took 323 us against XXX.
-                constexpr int kPitch = 2 * kN + 16;
-                unsigned char* turn = reinterpret_cast<unsigned char*>(&sh.scale[ew][0][0]);
-                const uint32_t to = smem_u32(turn) + (GATED ? ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16
-                                                            : (lane & 7) * kPitch + (lane >> 3) * 16);
-                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + c0) * L.ldy + n0;
+            } else if (L.y_vec && n0 + 32 <= L.n) {
+                // bf16: 16 rows of y at a time are turned round in shared memory, so that a store writes whole sectors, 64
+                // bytes of a row. (Two bytes of 16 rows each, straight from the registers, held the tiles up: 8192 rows
+                // through an 8192 x 4096 matrix took 323 us against 289.)
+                constexpr int kPitch = 80;
+                const uint32_t to = smem_u32(turn) + (lane & 7) * kPitch + (lane >> 3) * 16;
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + cb) * L.ldy + n0;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < kC; ++c)
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {  // 16 columns
-                        if (64 * c + 16 * p >= cols) continue;
-                        const f32x2* v0 = &acc[0][c][4 * p];  // 8 columns: lanes 0-7, 8-15; the next 8
+                    for (int p = 0; p < 4; ++p) {  // 16 columns: lanes 0-7 and 8-15 of the first 8, of the next 8
+                        if (64 * c + 16 * p >= n_cols) continue;
+                        const f32x2* v0 = &acc[0][c][4 * p];
                         const f32x2* v1 = &acc[1][c][4 * p];
                         __syncwarp();
-                        if constexpr (GATED) {
-                            stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v0[2]), bf16x2(v0[3]));
-                        } else {
-                            stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v1[0]), bf16x2(v1[1]));
-                            stmatrix(to + 8 * kPitch, bf16x2(v0[2]), bf16x2(v0[3]), bf16x2(v1[2]), bf16x2(v1[3]));
-                        }
+                        stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v1[0]), bf16x2(v1[1]));
+                        stmatrix(to + 8 * kPitch, bf16x2(v0[2]), bf16x2(v0[3]), bf16x2(v1[2]), bf16x2(v1[3]));
                         __syncwarp();
-                        constexpr int kLanes = kN / 8;  // lanes of a row
 #pragma unroll
-                        for (int r0 = 0; r0 < 16; r0 += 32 / kLanes) {
-                            const int r = r0 + lane / kLanes, col = 64 * c + 16 * p + r;
-                            const uint4 v = lds128(turn + r * kPitch + (lane % kLanes) * 16);
-                            if (col < cols && c0 + col < sg.rows)
-                                *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane % kLanes) * 8) = v;
+                        for (int r0 = 0; r0 < 16; r0 += 8) {
+                            const int r = r0 + (lane >> 2), col = 64 * c + 16 * p + r;
+                            const uint4 v = lds128(turn + r * kPitch + (lane & 3) * 16);
+                            if (col < n_cols && cb + col < sg.rows)
+                                *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane & 3) * 8) = v;
                         }
                     }
-                __syncwarp();  // the next tile's scales go there
             } else {
                 __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if (8 * (8 * c + (i >> 1)) >= cols) continue;
-                        const int col = c0 + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        if (64 * c + 8 * (i >> 1) >= n_cols) continue;
+                        const int col = cb + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
                         __nv_bfloat16* at = y + (size_t)col * L.ldy + 8 * (i & 1);
 #pragma unroll
-                        for (int h = 0; h < kN / 16; ++h) {
+                        for (int h = 0; h < 2; ++h) {
                             const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
                             if (in && col < sg.rows) at[16 * h] = __float2bfloat16_rn(lo2(acc[h][c][i]));
                             if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = __float2bfloat16_rn(hi2(acc[h][c][i]));
                         }
                     }
             }
+            __syncwarp();  // the next tile's scales go where the rows were turned
         }
     }
 

@@ -82,7 +82,7 @@ inline size_t grouped_arrived(int pairs) { return (size_t)pairs * 2 * 2 * kEpiWa
 // Tensor map of a [rows][cols] matrix (ld elements apart) whose boxes are 128 bytes wide and box_rows high, with the
 // 128-byte swizzle; false where it cannot be made.
 bool grouped_map(CUtensorMap* m, const void* p, bool e4m3, int64_t cols, int64_t rows, int64_t ld, int box_rows);
-constexpr int grouped_w_box(bool gated, bool kn) { return gated ? 16 : kn ? 64 : 128; }
+constexpr int grouped_w_box(bool gated, bool kn) { return gated || kn ? 64 : 128; }
 cudaError_t prepare_grouped();
 // CTA pairs that can be resident at once.
 int grouped_pairs(bool e4m3, bool gated, bool kn);
