@@ -26,14 +26,15 @@ constexpr int kEpiWarp0 = 4;
 constexpr int kCtaThreads = (kEpiWarp0 + kEpiWarps) * kWarp;
 constexpr int kStageW = 16384;                  // weights of a stage: 128 rows of 128 bytes
 constexpr int kMaxStages = 12;
-constexpr int kStageMem = 204 * 1024;           // bytes of all stages
+constexpr int kStageMem = 200 * 1024;           // bytes of all stages
+constexpr int kMaxBufs = 4;                     // accumulators in tensor memory
 constexpr int kBand = 8;                        // tiles of x that one sweep over the weights serves
-constexpr int kScaleSlots = 4;
+constexpr int kScaleWarps = 2;
 constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
 
 struct Shared {
-    uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], tfull[kMaxBufs], tempty[kMaxBufs], sempty[kMaxBufs];
     uint64_t met[kEpiWarps / 2];                // gated: a gate and an up warp
     unsigned before[kEpiWarps / 2];
     uint32_t tmem;
@@ -41,9 +42,8 @@ struct Shared {
     int max_cols;                               // widest tile
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
-    // e4m3: scales of a warp's rows of x and of its weights, for this stage and the next ones
-    alignas(16) float scale[kEpiWarps][kScaleSlots][128];
-    float wscale[kEpiWarps][kScaleSlots];
+    alignas(16) float scale[kMaxBufs][2][2][64];  // e4m3: of an accumulator, [gate, up][CTA of x][column]: row times weight
+    alignas(16) unsigned char turn[kEpiWarps][2048];
 };
 
 // ---- cluster and tcgen05 helpers (pairs of CTAs) ---------------------------
@@ -72,15 +72,6 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
             dst),
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
-}
-// 4-byte copy global -> shared, 0 where not `take`
-__device__ __forceinline__ void cp4(float* dst, const float* src, bool take) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(take ? 4u : 0u) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
@@ -118,14 +109,23 @@ __device__ __forceinline__ void pair_commit(uint64_t* bar) {
 __device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
           "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr)
         : "memory");
+}
+// the values of the loads before: not to be used earlier
+__device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
 }
 // shared-memory descriptors with the 128-byte swizzle: k along the 128-byte rows (atoms of 8 rows, 1024 bytes apart) ...
 __device__ __forceinline__ uint64_t desc_k(uint32_t saddr) {
@@ -151,11 +151,6 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     f32x2 d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 
@@ -253,10 +248,20 @@ struct Walk {
     __device__ static int tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 15) / 16 * 16; }
 };
 
+// The columns of a tile that a warp holds (half of them) in two chunks: the first, of at most 64. For e4m3 the chunks are
+// accumulators of their own, as equal as they can be: with a step's sums in four small accumulators instead of two of
+// 256 columns, the MMAs go on while the last ones are read (a hand-over to the other CTA and back takes 0.4 us).
+template <bool E8>
+__device__ __forceinline__ int first_chunk(int cols) {
+    return cols <= 64 ? cols : E8 ? (cols / 2 + 7) / 8 * 8 : 64;
+}
+
 template <bool E8, bool GATED, bool KN>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
-    static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
+    [[maybe_unused]] static constexpr int kChunk = 16;    // bf16: stages of an accumulator
+    static constexpr int kBufs = E8 ? 4 : 2;             // accumulators, of 512 / kBufs columns
+    static constexpr int kBufCols = 512 / kBufs;
     static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
     static constexpr int kBoxes = GATED || KN ? 2 : 1;    // boxes of weights of a CTA's stage
     static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
@@ -324,8 +329,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             mbar_init(&sh.full[s], 1);
             mbar_init(&sh.empty[s], 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&sh.tfull[b], 1);
+        for (int b = 0; b < kMaxBufs; ++b) {
+            mbar_init(&sh.tfull[b], E8 ? 1 + kScaleWarps : 1);
+            mbar_init(&sh.sempty[b], kEpiWarps);
             mbar_init(&sh.tempty[b], 2 * kEpiWarps);
         }
         for (int b = 0; b < kEpiWarps / 2; ++b) mbar_init(&sh.met[b], 2);
@@ -418,39 +424,121 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 unsigned ph = 0;
                 bool ok = true;
                 while (ok && walk.next(sg)) {
-                    const uint32_t idesc = K::kIdesc | (uniform((uint32_t)sg.cols) >> 3) << 17;
+                    const int half = (int)uniform((uint32_t)sg.cols) / 2;
                     const int k_end = (int)uniform((uint32_t)sg.k1);
-                    for (int k = (int)uniform((uint32_t)sg.k0); ok && k < k_end;) {
-                        const int kc = min(k_end, k + K::kChunk);
-                        const int buf = chunk & 1;
-                        if (chunk >= 2) ok = wait_for(&sh.tempty[buf], ((chunk >> 1) & 1) ^ 1u, sh);
+                    int k = (int)uniform((uint32_t)sg.k0);
+                    auto next_buf = [&]() {  // waits until accumulator `chunk` may be overwritten
+                        const int buf = chunk % K::kBufs;
+                        if (chunk >= K::kBufs) ok = wait_for(&sh.tempty[buf], ((chunk / K::kBufs) & 1) ^ 1u, sh);
                         tc_after();
-                        const uint32_t d = tmem + buf * 256;
-                        for (int first = k; ok && k < kc; ++k) {
+                        return buf;
+                    };
+                    auto next_stage = [&]() {
+                        if (++st == n_st) {
+                            st = 0;
+                            ph ^= 1u;
+                        }
+                    };
+                    if constexpr (E8) {
+                        const int w0 = first_chunk<E8>(half), w1 = half - w0;
+                        const uint32_t id0 = K::kIdesc | (uint32_t)(2 * w0 >> 3) << 17, id1 = K::kIdesc | (uint32_t)(2 * w1 >> 3) << 17;
+                        for (; ok && k < k_end; ++k) {
                             ok = wait_for(&sh.full[st], ph, sh);
-                            if (!ok) break;
-                            tc_after();
                             const uint32_t a0 = base + st * size;
-                            const uint64_t bd = desc_k(a0 + kStageW);
-                            const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
-                            if (elect_one()) {
+                            for (int c = 0; ok && c < (w1 > 0 ? 2 : 1); ++c, ++chunk) {
+                                const int buf = next_buf();
+                                if (!ok) break;
+                                const uint64_t ad = desc_k(a0), bd = desc_k(a0 + kStageW + c * w0 * 128);
+                                const uint32_t d = tmem + buf * K::kBufCols, idesc = c ? id1 : id0;
+                                if (elect_one()) {
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
-                                pair_commit(&sh.empty[st]);
-                                if (k + 1 == kc) pair_commit(&sh.tfull[buf]);
+                                    for (int i = 0; i < 4; ++i) pair_mma<E8>(d, ad + 2 * i, bd + 2 * i, idesc, i > 0);
+                                    pair_commit(&sh.tfull[buf]);
+                                    if (c == 1 || w1 == 0) pair_commit(&sh.empty[st]);
+                                }
+                                __syncwarp();
                             }
-                            __syncwarp();
-                            if (++st == n_st) {
-                                st = 0;
-                                ph ^= 1u;
+                            next_stage();
+                        }
+                    } else {
+                        const uint32_t idesc = K::kIdesc | (uint32_t)(2 * half >> 3) << 17;
+                        for (; ok && k < k_end; ++chunk) {
+                            const int kc = min(k_end, k + K::kChunk), buf = next_buf();
+                            const uint32_t d = tmem + buf * K::kBufCols;
+                            for (int first = k; ok && k < kc; ++k) {
+                                ok = wait_for(&sh.full[st], ph, sh);
+                                if (!ok) break;
+                                tc_after();
+                                const uint32_t a0 = base + st * size;
+                                const uint64_t bd = desc_k(a0 + kStageW);
+                                const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
+                                if (elect_one()) {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
+                                    pair_commit(&sh.empty[st]);
+                                    if (k + 1 == kc) pair_commit(&sh.tfull[buf]);
+                                }
+                                __syncwarp();
+                                next_stage();
                             }
                         }
-                        ++chunk;
                     }
                 }
             }
             __syncwarp();
+        } else if constexpr (E8) {
+            // ---- scales, by a warp for each CTA's half of the rows of x: those of an accumulator's columns times that of the
+            // weights, two stages ahead (an L2 access takes longer than a stage's MMAs) ----
+            const int half = warp - 2;
+            int chunk = 0;
+            bool ok = true;
+            while (ok && walk.next(sg)) {
+                const int cols = sg.cols / 2, c0 = half * cols, w0 = first_chunk<E8>(cols), w1 = cols - w0;
+                const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
+                const GroupWeights* gw = L.weights + sg.g;
+                const float* ws = gw->ws + (size_t)block * steps;
+                const float* us = GATED ? gw->us + (size_t)block * steps : nullptr;
+                const float* xs = L.x_scale + sg.row0 + c0 + lane;
+                struct Step {
+                    float x[4], w, u;
+                } now, next, then;
+                auto fetch = [&](Step& s, int k) {
+                    if (k >= sg.k1) return;
+                    const float* from = xs + (size_t)k * L.ld_scale;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int col = (i >> 1) * w0 + 32 * (i & 1);  // + lane, of chunk i / 2
+                        const bool in = 32 * (i & 1) + lane < (i < 2 ? w0 : w1) && c0 + col + lane < sg.rows;
+                        s.x[i] = in ? __ldg(from + col) : 0.0f;
+                    }
+                    s.w = __ldg(ws + k);
+                    if (GATED) s.u = __ldg(us + k);
+                };
+                fetch(now, sg.k0);
+                fetch(next, sg.k0 + 1);
+                for (int k = sg.k0; ok && k < sg.k1; ++k) {
+                    fetch(then, k + 2);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (c == 1 && w1 == 0) break;
+                        const int buf = chunk % K::kBufs;
+                        if (chunk >= K::kBufs)
+                            ok = __all_sync(0xffffffffu, wait_for(&sh.sempty[buf], ((chunk / K::kBufs) & 1) ^ 1u, sh));
+                        if (!ok) break;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            sh.scale[buf][0][half][lane + 32 * i] = now.x[2 * c + i] * now.w;
+                            if (GATED) sh.scale[buf][1][half][lane + 32 * i] = now.x[2 * c + i] * now.u;
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.tfull[buf]);
+                        ++chunk;
+                    }
+                    now = next;
+                    next = then;
+                }
+            }
         }
     } else {
         regs_grow();
@@ -470,70 +558,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             return here;
         };
         while (ok && walk.next(sg)) {
-            const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8
+            const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8 ...
+            const int w0 = first_chunk<E8>(cols), w1 = cols - w0;  // ... in two chunks
             f32x2 acc[2][2][16];  // [16 lanes][64 columns][of 8 columns: lanes t / 4, lanes t / 4 + 8]
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i >> 5][(i >> 4) & 1][i & 15] = 0ull;
-            const GroupWeights* gw = L.weights + sg.g;
-            const float* xs = nullptr;
-            const float* ws = nullptr;
-            // The scales of a stage are copied kScaleSlots - 1 stages ahead: an L2 access takes longer than a stage's MMAs.
-            auto fetch = [&](int k) {
-                if (k < sg.k1) {
-                    const int slot = k & (kScaleSlots - 1);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = lane + 32 * i;
-                        if (c < cols) cp4(&sh.scale[ew][slot][c], xs + (size_t)k * L.ld_scale + c, c0 + c < sg.rows);
-                    }
-                    if (lane == 0) cp4(&sh.wscale[ew][slot], ws + k, true);
-                }
-                cp_commit();
+            auto release = [&](int buf) {
+                tc_before();
+                __syncwarp();
+                if (lane == 0) arrive_at(in_cta(&sh.tempty[buf], 0));
+            };
+            auto filled = [&](int buf) {
+                ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk / K::kBufs) & 1, sh));
+                tc_after();
+                return ok;
             };
             if constexpr (E8) {
-                const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
-                xs = L.x_scale + sg.row0 + c0;
-                ws = (GATED && q >= 2 ? gw->us : gw->ws) + (size_t)block * steps;
-                for (int i = 0; i < kScaleSlots - 1; ++i) fetch(sg.k0 + i);
-            }
-            for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
-                const int buf = chunk & 1;
-                const float* mine = sh.scale[ew][k & (kScaleSlots - 1)];
-                f32x2 w2;
-                if constexpr (E8) {
-                    cp_wait<kScaleSlots - 2>();
-                    __syncwarp();
-                    const uint32_t w = __float_as_uint(sh.wscale[ew][k & (kScaleSlots - 1)]);
-                    w2 = pack2(w, w);
-                    fetch(k + kScaleSlots - 1);  // into the slot of the stage before, which all lanes have read
-                }
-                ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> 1) & 1, sh));
-                if (!ok) break;
-                tc_after();
+                const float* scale = &sh.scale[0][GATED ? q >> 1 : 0][half][2 * (lane & 3)];
+                for (int k = sg.k0; ok && k < sg.k1; ++k) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (64 * c >= cols) break;
+                    for (int c = 0; c < 2; ++c) {
+                        if (c == 1 && w1 == 0) break;
+                        const int buf = chunk % K::kBufs;
+                        if (!filled(buf)) break;
+                        const uint32_t from = lane_addr + buf * K::kBufCols + half * (c ? w1 : w0);
+                        uint32_t r0[32], r1[32];
+                        tc_ld64(from, r0);
+                        tc_ld64(from + (16u << 16), r1);
+                        f32x2 s2[8];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t r[32];
-                        tc_ld64(lane_addr + ((uint32_t)(16 * h) << 16) + buf * 256 + c0 + 64 * c, r);
+                        for (int j = 0; j < 8; ++j) s2[j] = *reinterpret_cast<const f32x2*>(scale + buf * 256 + 8 * j);
+                        tc_ld_wait(r0);
+                        tc_ld_wait(r1);
+                        release(buf);
+                        if (lane == 0) mbar_arrive(&sh.sempty[buf]);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            if constexpr (E8) {
-                                const float2 s = *reinterpret_cast<const float2*>(&mine[64 * c + 8 * j + 2 * (lane & 3)]);
-                                const f32x2 s2 = mul2(pack2(__float_as_uint(s.x), __float_as_uint(s.y)), w2);
-                                acc[h][c][2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), s2, acc[h][c][2 * j]);
-                                acc[h][c][2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), s2, acc[h][c][2 * j + 1]);
-                            } else {
+                            acc[0][c][2 * j] = fma2(pack2(r0[4 * j], r0[4 * j + 1]), s2[j], acc[0][c][2 * j]);
+                            acc[0][c][2 * j + 1] = fma2(pack2(r0[4 * j + 2], r0[4 * j + 3]), s2[j], acc[0][c][2 * j + 1]);
+                            acc[1][c][2 * j] = fma2(pack2(r1[4 * j], r1[4 * j + 1]), s2[j], acc[1][c][2 * j]);
+                            acc[1][c][2 * j + 1] = fma2(pack2(r1[4 * j + 2], r1[4 * j + 3]), s2[j], acc[1][c][2 * j + 1]);
+                        }
+                        ++chunk;
+                    }
+                }
+            } else {
+                for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
+                    const int buf = chunk % K::kBufs;
+                    if (!filled(buf)) break;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (c == 1 && w1 == 0) break;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t r[32];
+                            tc_ld64(lane_addr + ((uint32_t)(16 * h) << 16) + buf * K::kBufCols + c0 + c * w0, r);
+                            tc_ld_wait(r);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
                                 acc[h][c][2 * j] = add2(acc[h][c][2 * j], pack2(r[4 * j], r[4 * j + 1]));
                                 acc[h][c][2 * j + 1] = add2(acc[h][c][2 * j + 1], pack2(r[4 * j + 2], r[4 * j + 3]));
                             }
                         }
                     }
+                    release(buf);
                 }
-                tc_before();
-                __syncwarp();
-                if (lane == 0) arrive_at(in_cta(&sh.tempty[buf], 0));
             }
             if (!ok) break;
             if (sg.k1 - sg.k0 < steps) {
@@ -549,7 +638,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 f32x2* to = part_of(pair);
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    if (64 * c < cols)
+                    if (c == 0 || w1 > 0)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) __stcg(to + (c * 32 + i) * kWarp, acc[i >> 4][c][i & 15]);
                 __threadfence();
@@ -573,7 +662,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     const f32x2* from = part_of(p);
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
-                        if (64 * c < cols)
+                        if (c == 0 || w1 > 0)
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
                                 const f32x2 v = __ldcg(from + (c * 32 + i) * kWarp);
@@ -584,17 +673,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             // outputs: [16 lanes h][8 lanes r] of each 8 columns
             const int mlane = lane >> 2;
             int n0 = sg.wt * 256 + (int)rank * 128 + q * 32, cb = c0;  // the warp's first output and first column
-            unsigned char* turn = reinterpret_cast<unsigned char*>(&sh.scale[ew][0][0]);  // 2 KB of its own, idle here
+            unsigned char* turn = sh.turn[ew];
             if constexpr (GATED) {
                 // Warp q < 2 holds the gate values and warp q + 2 the up values of the same neurons: the first finishes
-                // columns 0-63, the second 64-127, each with what the other sends it, 16 columns at a time.
+                // the first chunk of columns, the second the other, each with what the other sends it, 16 columns at a time.
                 n0 = sg.wt * 128 + (int)rank * 64 + (q & 1) * 32;
-                cb = c0 + 64 * (q >> 1);
+                cb = q < 2 ? c0 : c0 + w0;
                 f32x2* mine = reinterpret_cast<f32x2*>(turn) + lane;
-                const f32x2* theirs = reinterpret_cast<const f32x2*>(&sh.scale[ew ^ 2][0][0]) + lane;
+                const f32x2* theirs = reinterpret_cast<const f32x2*>(sh.turn[ew ^ 2]) + lane;
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    if (16 * p >= cols) break;
+                    if (16 * p >= w0) break;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) mine[i * kWarp] = q < 2 ? acc[i >> 2][1][4 * p + (i & 3)] : acc[i >> 2][0][4 * p + (i & 3)];
                     ok = ok && meet();
@@ -609,16 +698,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 }
                 if (!ok) break;
             }
-            const int n_cols = cols - (cb - c0);  // of the warp's columns, those that it finishes: none where it is not above 0
-            constexpr int kC = GATED ? 1 : 2;     // in chunks of 64
+            constexpr int kC = GATED ? 1 : 2;
+            const int width[2] = {GATED && q >= 2 ? w1 : w0, GATED ? 0 : w1};  // columns of chunk 0 and 1 that the warp finishes
             if (L.y_f32) {
                 float* y = static_cast<float*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
 #pragma unroll
                 for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if (64 * c + 8 * (i >> 1) >= n_cols) continue;
-                        const int col = cb + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        if (8 * (i >> 1) >= width[c]) continue;
+                        const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
                         float* at = y + (size_t)col * L.ldy + 8 * (i & 1);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
@@ -638,7 +727,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {  // 16 columns: lanes 0-7 and 8-15 of the first 8, of the next 8
-                        if (64 * c + 16 * p >= n_cols) continue;
+                        if (16 * p >= width[c]) continue;
                         const f32x2* v0 = &acc[0][c][4 * p];
                         const f32x2* v1 = &acc[1][c][4 * p];
                         __syncwarp();
@@ -647,9 +736,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         __syncwarp();
 #pragma unroll
                         for (int r0 = 0; r0 < 16; r0 += 8) {
-                            const int r = r0 + (lane >> 2), col = 64 * c + 16 * p + r;
+                            const int r = r0 + (lane >> 2), col = c * w0 + 16 * p + r;
                             const uint4 v = lds128(turn + r * kPitch + (lane & 3) * 16);
-                            if (col < n_cols && cb + col < sg.rows)
+                            if (16 * p + r < width[c] && cb + col < sg.rows)
                                 *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane & 3) * 8) = v;
                         }
                     }
@@ -659,8 +748,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if (64 * c + 8 * (i >> 1) >= n_cols) continue;
-                        const int col = cb + 64 * c + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                        if (8 * (i >> 1) >= width[c]) continue;
+                        const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
                         __nv_bfloat16* at = y + (size_t)col * L.ldy + 8 * (i & 1);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
@@ -670,7 +759,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         }
                     }
             }
-            __syncwarp();  // the next tile's scales go where the rows were turned
         }
     }
 
