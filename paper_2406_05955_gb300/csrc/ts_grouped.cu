@@ -26,10 +26,10 @@ constexpr int kEpiWarp0 = 4;
 constexpr int kCtaThreads = (kEpiWarp0 + kEpiWarps) * kWarp;
 constexpr int kStageW = 16384;                  // weights of a stage: 128 rows of 128 bytes
 constexpr int kMaxStages = 12;
-constexpr int kStageMem = 200 * 1024;           // bytes of all stages
+constexpr int kStageMem = 192 * 1024;           // bytes of all stages
 constexpr int kMaxBufs = 4;                     // accumulators in tensor memory
 constexpr int kBand = 8;                        // tiles of x that one sweep over the weights serves
-constexpr int kScaleWarps = 2;
+constexpr int kScaleWarps = 2, kScaleSlots = 4;
 constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
 
@@ -43,6 +43,7 @@ struct Shared {
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
     alignas(16) float scale[kMaxBufs][2][2][64];  // e4m3: of an accumulator, [gate, up][CTA of x][column]: row times weight
+    float raw[kScaleSlots][kScaleWarps][6][kWarp];  // and what they are made of, as it was copied
     alignas(16) unsigned char turn[kEpiWarps][2048];
 };
 
@@ -72,6 +73,15 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
             dst),
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
+}
+// 4-byte copy global -> shared (bytes = 0: zero)
+__device__ __forceinline__ void cp4(float* dst, const float* src, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
@@ -489,54 +499,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             __syncwarp();
         } else if constexpr (E8) {
             // ---- scales, by a warp for each CTA's half of the rows of x: those of an accumulator's columns times that of the
-            // weights, two stages ahead (an L2 access takes longer than a stage's MMAs) ----
+            // weights. They are copied kScaleSlots - 1 stages ahead: an L2 access takes longer than a stage's MMAs. ----
             const int half = warp - 2;
             int chunk = 0;
+            unsigned stage = 0;
             bool ok = true;
             while (ok && walk.next(sg)) {
-                const int cols = sg.cols / 2, c0 = half * cols, w0 = first_chunk<E8>(cols), w1 = cols - w0;
+                const int cols = sg.cols / 2, w0 = first_chunk<E8>(cols), w1 = cols - w0;
                 const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
                 const GroupWeights* gw = L.weights + sg.g;
-                const float* ws = gw->ws + (size_t)block * steps;
-                const float* us = GATED ? gw->us + (size_t)block * steps : nullptr;
-                const float* xs = L.x_scale + sg.row0 + c0 + lane;
-                struct Step {
-                    float x[4], w, u;
-                } now, next, then;
-                auto fetch = [&](Step& s, int k) {
-                    if (k >= sg.k1) return;
-                    const float* from = xs + (size_t)k * L.ld_scale;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = (i >> 1) * w0 + 32 * (i & 1);  // + lane, of chunk i / 2
-                        const bool in = 32 * (i & 1) + lane < (i < 2 ? w0 : w1) && c0 + col + lane < sg.rows;
-                        s.x[i] = in ? __ldg(from + col) : 0.0f;
+                const float* ws = gw->ws + (size_t)block * steps + sg.k0;
+                const float* us = GATED ? gw->us + (size_t)block * steps + sg.k0 : nullptr;
+                const float* xs = L.x_scale + (size_t)sg.k0 * L.ld_scale + sg.row0 + half * cols + lane;
+                const int mine = sg.rows - half * cols;  // rows of the tile from this half on
+                const uint32_t t0 = lane < min(w0, mine) ? 4 : 0, t1 = lane + 32 < min(w0, mine) ? 4 : 0;
+                const uint32_t t2 = lane < min(w1, mine - w0) ? 4 : 0, t3 = lane + 32 < min(w1, mine - w0) ? 4 : 0;
+                int ahead = sg.k0;
+                unsigned slot = stage;
+                auto fetch = [&]() {
+                    if (ahead < sg.k1) {
+                        float* to = &sh.raw[slot & (kScaleSlots - 1)][half][0][lane];
+                        cp4(to, t0 ? xs : L.x_scale, t0);
+                        cp4(to + 32, t1 ? xs + 32 : L.x_scale, t1);
+                        cp4(to + 64, t2 ? xs + w0 : L.x_scale, t2);
+                        cp4(to + 96, t3 ? xs + w0 + 32 : L.x_scale, t3);
+                        cp4(to + 128, ws, 4);
+                        if (GATED) cp4(to + 160, us++, 4);
+                        ++ws;
+                        xs += L.ld_scale;
                     }
-                    s.w = __ldg(ws + k);
-                    if (GATED) s.u = __ldg(us + k);
+                    cp_commit();
+                    ++ahead;
+                    ++slot;
                 };
-                fetch(now, sg.k0);
-                fetch(next, sg.k0 + 1);
-                for (int k = sg.k0; ok && k < sg.k1; ++k) {
-                    fetch(then, k + 2);
+                for (int i = 0; i < kScaleSlots - 1; ++i) fetch();
+                for (int k = sg.k0; ok && k < sg.k1; ++k, ++stage) {
+                    fetch();  // (what a lane copies it reads itself)
+                    cp_wait<kScaleSlots - 1>();
+                    const float* raw = &sh.raw[stage & (kScaleSlots - 1)][half][0][lane];
+                    const float g = raw[128], u = GATED ? raw[160] : 0.0f;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (c == 1 && w1 == 0) break;
+                        const float x0 = raw[64 * c], x1 = raw[64 * c + 32];
                         const int buf = chunk % K::kBufs;
                         if (chunk >= K::kBufs)
                             ok = __all_sync(0xffffffffu, wait_for(&sh.sempty[buf], ((chunk / K::kBufs) & 1) ^ 1u, sh));
                         if (!ok) break;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            sh.scale[buf][0][half][lane + 32 * i] = now.x[2 * c + i] * now.w;
-                            if (GATED) sh.scale[buf][1][half][lane + 32 * i] = now.x[2 * c + i] * now.u;
+                        float* to = &sh.scale[buf][0][half][lane];
+                        to[0] = x0 * g;
+                        to[32] = x1 * g;
+                        if (GATED) {
+                            to[128] = x0 * u;
+                            to[160] = x1 * u;
                         }
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&sh.tfull[buf]);
                         ++chunk;
                     }
-                    now = next;
-                    next = then;
                 }
             }
         }
