@@ -570,6 +570,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         // gated: a gate warp and the up warp of the same neurons wait for each other
         const int both = half * 2 + (q & 1);
         unsigned met = 0;
+        const uint32_t t_empty = in_cta(&sh.tempty[0], 0);
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.met[both]);
@@ -586,7 +587,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             auto release = [&](int buf) {
                 tc_before();
                 __syncwarp();
-                if (lane == 0) arrive_at(in_cta(&sh.tempty[buf], 0));
+                if (lane == 0) {
+                    arrive_at(t_empty + buf * 8);
+                    if (E8) mbar_arrive(&sh.sempty[buf]);
+                }
             };
             auto filled = [&](int buf) {
                 ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk / K::kBufs) & 1, sh));
@@ -611,7 +615,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         tc_ld_wait(r0);
                         tc_ld_wait(r1);
                         release(buf);
-                        if (lane == 0) mbar_arrive(&sh.sempty[buf]);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             acc[0][c][2 * j] = fma2(pack2(r0[4 * j], r0[4 * j + 1]), s2[j], acc[0][c][2 * j]);

@@ -18,27 +18,41 @@ _LAYOUTS = {"nk": TS_NK, "kn": TS_KN}
 BLOCK = 128  # elements of one scale
 
 
-def _tensor(t, what: str, dtypes, dim: int, rows_apart: bool = False) -> torch.Tensor:
-    """``t``, checked: on the current device, its type and dimensions, contiguous (or only each row of it)."""
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream  # (torch.cuda.current_stream() takes 1-2 us to make its object)
+
+
+def _refuse(t, what: str, dtypes, dim: int, rows_apart: bool):
+    """The error for a tensor that ``_tensor`` does not take."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != _current_device():
         raise ValueError(f"{what} is on {t.device}, not on the current device")
     if t.dtype not in dtypes:
         raise TypeError(f"{what} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
     if t.dim() != dim:
         raise ValueError(f"{what} must have {dim} dimensions")
-    if rows_apart:
-        if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
-            raise ValueError(f"{what} must have contiguous rows")
-    elif not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
+    raise ValueError(f"{what} must have contiguous rows" if rows_apart else f"{what} must be contiguous")
+
+
+def _rows_apart(t) -> bool:
+    """Whether each row of a matrix is contiguous, and the next one behind it."""
+    s0, s1 = t.stride()
+    n0, n1 = t.shape
+    return (s1 == 1 or n1 <= 1) and (s0 >= n1 or n0 <= 1)
+
+
+def _tensor(t, what: str, dtypes, dim: int, rows_apart: bool = False) -> torch.Tensor:
+    """``t``, checked: on the current device, its type and dimensions, contiguous (or only each row of it)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != _current_device() or \
+            t.dtype not in dtypes or t.dim() != dim or not (t.is_contiguous() or (rows_apart and _rows_apart(t))):
+        _refuse(t, what, dtypes, dim, rows_apart)
     return t
 
 
 def _shaped(t, what: str, dtype, shape) -> torch.Tensor:
     _tensor(t, what, (dtype,), len(shape))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
     return t
 
@@ -48,21 +62,18 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-class _On:
-    """The stream of a call: its handle, and allocation on it."""
+def _handle(stream) -> int:
+    if stream is None:
+        return _raw_stream(_current_device())
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
-    def __init__(self, stream):
-        if stream is None:
-            self.stream, self.handle = None, torch.cuda.current_stream().cuda_stream
-        else:
-            self.stream = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
-            self.handle = self.stream.cuda_stream
 
-    def empty(self, *shape, dtype):
-        if self.stream is None:
-            return torch.empty(*shape, dtype=dtype, device="cuda")
-        with torch.cuda.stream(self.stream):
-            return torch.empty(*shape, dtype=dtype, device="cuda")
+def _empty(stream, *shape, dtype) -> torch.Tensor:
+    """An output, allocated on the stream of the call."""
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
 
 
 class Routing(NamedTuple):
@@ -78,14 +89,14 @@ def route(logits: torch.Tensor, top_k: int, sel=None, w=None, offsets=None, rows
     """``ts_route``: each token's ``top_k`` experts by fp32 ``logits [tokens][experts]``, and each expert's tokens."""
     _tensor(logits, "logits", (torch.float32,), 2)
     t, e = logits.shape
-    k, on, i32 = int(top_k), _On(stream), torch.int32
-    sel = on.empty(t, k, dtype=i32) if sel is None else _shaped(sel, "sel", i32, (t, k))
-    w = on.empty(t, k, dtype=torch.float32) if w is None else _shaped(w, "w", torch.float32, (t, k))
-    offsets = on.empty(e + 1, dtype=i32) if offsets is None else _shaped(offsets, "offsets", i32, (e + 1,))
-    rows = on.empty(t * k, dtype=i32) if rows is None else _shaped(rows, "rows", i32, (t * k,))
-    slots = on.empty(t, k, dtype=i32) if slots is None else _shaped(slots, "slots", i32, (t, k))
+    k, i32 = int(top_k), torch.int32
+    sel = _empty(stream, t, k, dtype=i32) if sel is None else _shaped(sel, "sel", i32, (t, k))
+    w = _empty(stream, t, k, dtype=torch.float32) if w is None else _shaped(w, "w", torch.float32, (t, k))
+    offsets = _empty(stream, e + 1, dtype=i32) if offsets is None else _shaped(offsets, "offsets", i32, (e + 1,))
+    rows = _empty(stream, t * k, dtype=i32) if rows is None else _shaped(rows, "rows", i32, (t * k,))
+    slots = _empty(stream, t, k, dtype=i32) if slots is None else _shaped(slots, "slots", i32, (t, k))
     _check(lib().ts_route(logits.data_ptr(), t, e, k, sel.data_ptr(), w.data_ptr(), offsets.data_ptr(),
-                          rows.data_ptr(), slots.data_ptr(), on.handle), "ts_route")
+                          rows.data_ptr(), slots.data_ptr(), _handle(stream)), "ts_route")
     return Routing(sel, w, offsets, rows, slots)
 
 
@@ -112,10 +123,9 @@ def gather_rows(x: torch.Tensor, rows: torch.Tensor, n=None, out=None, stream=No
     without); the other rows of ``out`` are left as they were."""
     _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
     rp, np_, m = _row_list(x, rows, n, None if out is None else out.shape[0])
-    on = _On(stream)
-    out = on.empty(m, x.shape[1], dtype=x.dtype) if out is None else _shaped(out, "out", x.dtype, (m, x.shape[1]))
+    out = _empty(stream, m, x.shape[1], dtype=x.dtype) if out is None else _shaped(out, "out", x.dtype, (m, x.shape[1]))
     _check(lib().ts_gather_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], x.shape[1], rp, np_, m,
-                                out.data_ptr(), on.handle), "ts_gather_rows")
+                                out.data_ptr(), _handle(stream)), "ts_gather_rows")
     return out
 
 
@@ -125,11 +135,11 @@ def quant_rows(x: torch.Tensor, rows=None, n=None, q=None, scale=None, stream=No
     _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
     k = x.shape[1]
     rp, np_, m = _row_list(x, rows, n, None if q is None else q.shape[0])
-    on, kb = _On(stream), -(-k // BLOCK)
-    q = on.empty(m, k, dtype=torch.float8_e4m3fn) if q is None else _shaped(q, "q", torch.float8_e4m3fn, (m, k))
-    scale = on.empty(kb, m, dtype=torch.float32) if scale is None else _shaped(scale, "scale", torch.float32, (kb, m))
+    kb = -(-k // BLOCK)
+    q = _empty(stream, m, k, dtype=torch.float8_e4m3fn) if q is None else _shaped(q, "q", torch.float8_e4m3fn, (m, k))
+    scale = _empty(stream, kb, m, dtype=torch.float32) if scale is None else _shaped(scale, "scale", torch.float32, (kb, m))
     _check(lib().ts_quant_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], k, rp, np_, m, q.data_ptr(),
-                               scale.data_ptr(), on.handle), "ts_quant_rows")
+                               scale.data_ptr(), _handle(stream)), "ts_quant_rows")
     return q, scale
 
 
@@ -139,11 +149,10 @@ def combine_rows(src: torch.Tensor, slots: torch.Tensor, w: torch.Tensor, out=No
     _tensor(slots, "slots", (torch.int32,), 2)
     t, k = slots.shape
     _shaped(w, "w", torch.float32, (t, k))
-    on = _On(stream)
-    out = on.empty(t, src.shape[1], dtype=torch.float32) if out is None else \
+    out = _empty(stream, t, src.shape[1], dtype=torch.float32) if out is None else \
         _shaped(out, "out", torch.float32, (t, src.shape[1]))
     _check(lib().ts_combine_rows(src.data_ptr(), _CODES[src.dtype], src.shape[0], src.shape[1], slots.data_ptr(),
-                                 w.data_ptr(), t, k, out.data_ptr(), on.handle), "ts_combine_rows")
+                                 w.data_ptr(), t, k, out.data_ptr(), _handle(stream)), "ts_combine_rows")
     return out
 
 
@@ -220,25 +229,24 @@ class Grouped:
             if x_scale.shape[0] != -(-self.k // BLOCK) or x_scale.shape[1] < rows:
                 raise ValueError(f"x_scale must be [{-(-self.k // BLOCK)}][rows]")
             sp, ld = x_scale.data_ptr(), _ld(x_scale)
-        on = _On(stream)
         if y is None:
-            y = on.empty(rows, self.n, dtype=torch.bfloat16)
+            y = _empty(stream, rows, self.n, dtype=torch.bfloat16)
         else:
             _tensor(y, "y", (torch.bfloat16, torch.float32), 2, rows_apart=True)
             if tuple(y.shape) != (rows, self.n):
                 raise ValueError(f"y must be [{rows}][{self.n}]")
         _check(lib().ts_grouped_forward(self.handle, x.data_ptr(), _ld(x), sp, ld, op, rows, y.data_ptr(), _ld(y),
-                                        _CODES[y.dtype], on.handle), "ts_grouped_forward")
+                                        _CODES[y.dtype], _handle(stream)), "ts_grouped_forward")
         return y
 
     __call__ = forward
 
     def get_error(self, stream=None) -> int:
-        return int(lib().ts_grouped_get_error(self.handle, _On(stream).handle))
+        return int(lib().ts_grouped_get_error(self.handle, _handle(stream)))
 
     def check_scratch(self, stream=None) -> int:
         """Status of the scratch guard zones (as Ffn.check_scratch)."""
-        return int(lib().ts_grouped_check_scratch(self.handle, _On(stream).handle))
+        return int(lib().ts_grouped_check_scratch(self.handle, _handle(stream)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None:
