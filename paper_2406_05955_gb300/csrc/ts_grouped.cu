@@ -33,6 +33,37 @@ constexpr int kScaleWarps = 2, kScaleSlots = 4;
 constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
 
+// ---- tiles and their parts --------------------------------------------------
+// The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
+// are dealt out evenly, in order, so that all pairs end together: a pair's share begins and ends anywhere in a tile.
+struct Parts {
+    long long total;       // steps of the rest
+    int pairs, steps;      // CTA pairs, stages of a tile
+    int whole;             // rounds of whole tiles
+    int sharers;           // pairs that get some of the rest
+    __device__ void set(int tiles, int pairs_, int steps_) {
+        pairs = pairs_;
+        steps = steps_;
+        whole = tiles % pairs == 0 ? tiles / pairs : max(0, tiles / pairs - 1);
+        total = (long long)(tiles - whole * pairs) * steps;
+        sharers = (int)max(1ll, min((long long)pairs, total / kMinSteps));
+    }
+    __device__ long long begin(int q) const { return total * q / sharers; }
+    // the pair that has step s
+    __device__ int owner(long long s) const {
+        int q = (int)(s * sharers / total);
+        while (begin(q) > s) --q;
+        while (begin(q + 1) <= s) ++q;
+        return q;
+    }
+};
+
+struct Seg {
+    int tile, k0, k1;       // stages [k0, k1) of a tile
+    int rest;               // its number among the tiles that are shared, -1: a whole one
+    int g, wt, row0, rows, cols;  // group, tile of weights, first row of x, rows, and their number rounded up to 16
+};
+
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages], tfull[kMaxBufs], tempty[kMaxBufs], sempty[kMaxBufs];
     uint64_t met[kEpiWarps / 2];                // gated: a gate and an up warp
@@ -40,6 +71,8 @@ struct Shared {
     uint32_t tmem;
     int fail;
     int max_cols;                               // widest tile
+    Parts parts;
+    Seg seg[kEpiWarps];                         // what a warp works on (its registers are for the sums)
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
     alignas(16) float scale[kMaxBufs][2][2][64];  // e4m3: of an accumulator, [gate, up][CTA of x][column]: row times weight
@@ -180,59 +213,32 @@ __device__ __forceinline__ void stmatrix(uint32_t to, uint32_t a, uint32_t b, ui
                  : "memory");
 }
 
-// ---- tiles and their parts --------------------------------------------------
-// The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
-// are dealt out evenly, in order, so that all pairs end together: a pair's share begins and ends anywhere in a tile.
-struct Parts {
-    int pairs, steps;      // CTA pairs, stages of a tile
-    int whole;             // rounds of whole tiles
-    long long total;       // steps of the rest
-    int sharers;           // pairs that get some of them
-    __device__ Parts(int tiles, int pairs_, int steps_) : pairs(pairs_), steps(steps_) {
-        whole = tiles % pairs == 0 ? tiles / pairs : max(0, tiles / pairs - 1);
-        total = (long long)(tiles - whole * pairs) * steps;
-        sharers = (int)max(1ll, min((long long)pairs, total / kMinSteps));
-    }
-    __device__ long long begin(int q) const { return total * q / sharers; }
-    // the pair that has step s
-    __device__ int owner(long long s) const {
-        int q = (int)(s * sharers / total);
-        while (begin(q) > s) --q;
-        while (begin(q + 1) <= s) ++q;
-        return q;
-    }
-};
+// Tiles of a group of n rows, and rows of each.
+__device__ __forceinline__ int tiles_of(int n) { return (n + kMaxTileRows - 1) / kMaxTileRows; }
+__device__ __forceinline__ int tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 15) / 16 * 16; }
 
-struct Seg {
-    int tile, k0, k1;       // stages [k0, k1) of a tile
-    int rest;               // its number among the tiles that are shared, -1: a whole one
-    int g, wt, row0, rows, cols;  // group, tile of weights, first row of x, rows, and their number rounded up to 16
-};
-
+// A pair's way through its tiles and parts of tiles.
 struct Walk {
-    const Shared& sh;
-    const Parts parts;
-    const int pair, n_groups, w_tiles;
     int round = 0;
-    long long at, end;
-    __device__ Walk(const Shared& s, const GroupedLaunch& L, int pair_, int w_tiles_, int steps)
-        : sh(s), parts(s.first[L.n_groups], L.pairs, steps), pair(pair_), n_groups(L.n_groups), w_tiles(w_tiles_) {
-        at = pair < parts.sharers ? parts.begin(pair) : 0;
-        end = pair < parts.sharers ? parts.begin(pair + 1) : 0;
-    }
-    __device__ bool next(Seg& s) {
-        if (round < parts.whole) {
-            s.tile = round * parts.pairs + pair;
+    long long at = -1;
+    __device__ bool next(const Shared& sh, int n_groups, int w_tiles, Seg& s) {
+        const Parts& P = sh.parts;
+        const int pair = blockIdx.x >> 1;
+        if (round < P.whole) {
+            s.tile = round * P.pairs + pair;
             s.rest = -1;
             s.k0 = 0;
-            s.k1 = parts.steps;
+            s.k1 = P.steps;
             ++round;
         } else {
+            if (pair >= P.sharers) return false;
+            if (at < 0) at = P.begin(pair);
+            const long long end = P.begin(pair + 1);
             if (at >= end) return false;
-            s.rest = (int)(at / parts.steps);
-            s.tile = parts.whole * parts.pairs + s.rest;
-            s.k0 = (int)(at - (long long)s.rest * parts.steps);
-            s.k1 = (int)min((long long)parts.steps, s.k0 + (end - at));
+            s.rest = (int)(at / P.steps);
+            s.tile = P.whole * P.pairs + s.rest;
+            s.k0 = (int)(at - (long long)s.rest * P.steps);
+            s.k1 = (int)min((long long)P.steps, s.k0 + (end - at));
             at += s.k1 - s.k0;
         }
         int lo = 0, hi = n_groups;  // the last group whose first tile is not behind
@@ -243,7 +249,7 @@ struct Walk {
         }
         s.g = lo;
         int t = s.tile - sh.first[lo];
-        const int n = sh.rows[lo], tiles = (n + kMaxTileRows - 1) / kMaxTileRows;
+        const int n = sh.rows[lo], tiles = tiles_of(n);
         const int band = t / (kBand * w_tiles), width = min(kBand, tiles - band * kBand);
         t -= band * kBand * w_tiles;
         s.wt = t / width;
@@ -254,8 +260,6 @@ struct Walk {
         s.cols = high;
         return true;
     }
-    // rows of each of the tiles that n rows are cut into
-    __device__ static int tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 15) / 16 * 16; }
 };
 
 // The columns of a tile that a warp holds (half of them) in two chunks: the first, of at most 64. For e4m3 the chunks are
@@ -299,7 +303,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
     __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cta_rank();
-    const int pair = blockIdx.x >> 1;
     const int steps = (L.k + K::kStep - 1) / K::kStep, w_tiles = (L.n + K::kTileN - 1) / K::kTileN;
 
     // ---- set-up: barriers, tensor memory, the groups' tiles ----
@@ -317,8 +320,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 sh.row0[e] = a;
                 sh.rows[e] = n;
             }
-            const int tiles = (n + kMaxTileRows - 1) / kMaxTileRows;
-            if (n > 0) widest = max(widest, Walk::tile_rows(n, tiles));
+            const int tiles = tiles_of(n);
+            if (n > 0) widest = max(widest, tile_rows(n, tiles));
             int sum = tiles * w_tiles;
 #pragma unroll
             for (int o = 1; o < kWarp; o <<= 1) {
@@ -333,6 +336,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         if (lane == 0) {
             sh.first[0] = 0;
             sh.max_cols = widest;
+            sh.parts.set(tiles_before, L.pairs, steps);
         }
     } else if (warp == 1 && lane == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
@@ -362,8 +366,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
     const int x_rows_max = max(8, 1 << (32 - __clz(sh.max_cols / 2 - 1)));
     const uint32_t stage_bytes = kStageW + x_rows_max * 128;
     const int stages = min(kMaxStages, kStageMem / (int)stage_bytes);
-    Walk walk(sh, L, pair, w_tiles, steps);
-    Seg sg;
+    Walk walk;
 
     if (warp < kEpiWarp0) {
         regs_shrink();
@@ -372,7 +375,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             int st = 0, n_loaded = 0;
             unsigned ph = 0;
             bool ok = true;
-            while (ok && walk.next(sg)) {
+            Seg sg;
+            while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
                 const GroupWeights* gw = L.weights + sg.g;
                 const int x_rows = max(8, 1 << (32 - __clz(sg.cols / 2 - 1))), xi = __ffs(x_rows) - 4;
                 const uint32_t bytes = 2u * (kStageW + x_rows * 128);
@@ -433,7 +437,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 int st = 0, chunk = 0;
                 unsigned ph = 0;
                 bool ok = true;
-                while (ok && walk.next(sg)) {
+                Seg sg;
+                while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
                     const int half = (int)uniform((uint32_t)sg.cols) / 2;
                     const int k_end = (int)uniform((uint32_t)sg.k1);
                     int k = (int)uniform((uint32_t)sg.k0);
@@ -504,7 +509,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             int chunk = 0;
             unsigned stage = 0;
             bool ok = true;
-            while (ok && walk.next(sg)) {
+            Seg sg;
+            while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
                 const int cols = sg.cols / 2, w0 = first_chunk<E8>(cols), w1 = cols - w0;
                 const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
                 const GroupWeights* gw = L.weights + sg.g;
@@ -578,7 +584,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             ++met;
             return here;
         };
-        while (ok && walk.next(sg)) {
+        const Seg& sg = sh.seg[ew];
+        while (ok) {
+            {
+                Seg now;
+                if (!walk.next(sh, L.n_groups, w_tiles, now)) break;
+                __syncwarp();
+                if (lane == 0) sh.seg[ew] = now;
+                __syncwarp();
+            }
             const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8 ...
             const int w0 = first_chunk<E8>(cols), w1 = cols - w0;  // ... in two chunks
             f32x2 acc[2][2][16];  // [16 lanes][64 columns][of 8 columns: lanes t / 4, lanes t / 4 + 8]
@@ -599,7 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             };
             if constexpr (E8) {
                 const float* scale = &sh.scale[0][GATED ? q >> 1 : 0][half][2 * (lane & 3)];
-                for (int k = sg.k0; ok && k < sg.k1; ++k) {
+                for (int left = sg.k1 - sg.k0; ok && left > 0; --left) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (c == 1 && w1 == 0) break;
@@ -626,7 +640,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     }
                 }
             } else {
-                for (int k = sg.k0; k < sg.k1; k += K::kChunk, ++chunk) {
+                for (int left = sg.k1 - sg.k0; left > 0; left -= K::kChunk, ++chunk) {
                     const int buf = chunk % K::kBufs;
                     if (!filled(buf)) break;
 #pragma unroll
@@ -650,7 +664,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             if (!ok) break;
             if (sg.k1 - sg.k0 < steps) {
                 // A part of a tile: left in global memory; the warp that comes last adds the parts in the order of k.
-                const Parts& P = walk.parts;
+                const Parts& P = sh.parts;
+                const int pair = blockIdx.x >> 1;
                 const long long s0 = (long long)sg.rest * steps;
                 const int p0 = P.owner(s0), p1 = P.owner(s0 + steps - 1);
                 auto part_of = [&](int p) {  // a pair's first tile is in its slot 0, its last one in slot 1
@@ -658,12 +673,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     return reinterpret_cast<f32x2*>(L.partial) +
                            ((size_t)((p * 2 + slot) * 2 + (int)rank) * kEpiWarps + ew) * (L.part_chunks * 1024) + lane;
                 };
+                // value i of a chunk of `width` columns: whether its 8 columns are any of the tile's
+                auto in = [](int i, int width) { return 8 * ((i & 15) >> 1) < width; };
                 f32x2* to = part_of(pair);
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    if (c == 0 || w1 > 0)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) __stcg(to + (c * 32 + i) * kWarp, acc[i >> 4][c][i & 15]);
+                    for (int i = 0; i < 32; ++i)
+                        if (in(i, c ? w1 : w0)) __stcg(to + (c * 32 + i) * kWarp, acc[i >> 4][c][i & 15]);
                 __threadfence();
                 __syncwarp();
                 unsigned* count = L.arrived + ((size_t)sg.rest * 2 + rank) * kEpiWarps + ew;
@@ -681,16 +698,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 if ((int)before != p1 - p0) continue;
                 __threadfence();
                 if (lane == 0 && (!GATED || q < 2)) *count = 0u;
-                for (int p = p0; p <= p1; ++p) {
-                    const f32x2* from = part_of(p);
+                if (cols <= 16) {
+                    // few columns: the parts of several pairs at a time, as each access takes as long as all of them
+                    constexpr int kAtOnce = 2;
+                    for (int p = p0; p <= p1; p += kAtOnce) {
+                        f32x2 v[kAtOnce][8];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        if (c == 0 || w1 > 0)
+                        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                v[u][i] = p + u <= p1 && in(i & 3, cols) ? __ldcg(part_of(p + u) + (16 * (i >> 2) + (i & 3)) * kWarp) : 0ull;
+#pragma unroll
+                        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                f32x2& a = acc[i >> 2][0][i & 3];
+                                if (p + u <= p1) a = p + u == p0 ? v[u][i] : add2(a, v[u][i]);
+                            }
+                    }
+                } else {
+                    for (int p = p0; p <= p1; ++p) {
+                        const f32x2* from = part_of(p);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            if (c == 0 || w1 > 0)
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
                                 const f32x2 v = __ldcg(from + (c * 32 + i) * kWarp);
                                 acc[i >> 4][c][i & 15] = p == p0 ? v : add2(acc[i >> 4][c][i & 15], v);
                             }
+                    }
                 }
             }
             // outputs: [16 lanes h][8 lanes r] of each 8 columns
