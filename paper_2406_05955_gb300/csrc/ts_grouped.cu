@@ -72,10 +72,10 @@ struct Shared {
     int fail;
     int max_cols;                               // widest tile
     Parts parts;
-    Seg seg[kEpiWarps];                         // what a warp works on (its registers are for the sums)
+    Seg seg[kEpiWarps];
     int first[kMaxGroups + 1];                  // tiles before each group
     int row0[kMaxGroups], rows[kMaxGroups];
-    alignas(16) float scale[kMaxBufs][2][2][64];  // e4m3: of an accumulator, [gate, up][CTA of x][column]: row times weight
+    alignas(16) float scale[2][512];            // e4m3, [gate, up]: row times weight, of each accumulator's columns
     float raw[kScaleSlots][kScaleWarps][6][kWarp];  // and what they are made of, as it was copied
     alignas(16) unsigned char turn[kEpiWarps][2048];
 };
@@ -159,6 +159,19 @@ __device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[32]) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr)
         : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[8]) {  // 16 columns
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_ld_wait16(uint32_t (&a)[8], uint32_t (&b)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(a[0]), "+r"(a[1]), "+r"(a[2]), "+r"(a[3]), "+r"(a[4]), "+r"(a[5]), "+r"(a[6]), "+r"(a[7]),
+                   "+r"(b[0]), "+r"(b[1]), "+r"(b[2]), "+r"(b[3]), "+r"(b[4]), "+r"(b[5]), "+r"(b[6]), "+r"(b[7])
+                 :
+                 : "memory");
 }
 // the values of the loads before: not to be used earlier
 __device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[32]) {
@@ -262,20 +275,10 @@ struct Walk {
     }
 };
 
-// The columns of a tile that a warp holds (half of them) in two chunks: the first, of at most 64. For e4m3 the chunks are
-// accumulators of their own, as equal as they can be: with a step's sums in four small accumulators instead of two of
-// 256 columns, the MMAs go on while the last ones are read (a hand-over to the other CTA and back takes 0.4 us).
-template <bool E8>
-__device__ __forceinline__ int first_chunk(int cols) {
-    return cols <= 64 ? cols : E8 ? (cols / 2 + 7) / 8 * 8 : 64;
-}
-
 template <bool E8, bool GATED, bool KN>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
-    [[maybe_unused]] static constexpr int kChunk = 16;    // bf16: stages of an accumulator
-    static constexpr int kBufs = E8 ? 4 : 2;             // accumulators, of 512 / kBufs columns
-    static constexpr int kBufCols = 512 / kBufs;
+    static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
     static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
     static constexpr int kBoxes = GATED || KN ? 2 : 1;    // boxes of weights of a CTA's stage
     static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
@@ -366,6 +369,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
     const int x_rows_max = max(8, 1 << (32 - __clz(sh.max_cols / 2 - 1)));
     const uint32_t stage_bytes = kStageW + x_rows_max * 128;
     const int stages = min(kMaxStages, kStageMem / (int)stage_bytes);
+    // tensor memory holds two accumulators, or four where the widest tile has at most 128 columns (a warp's loads are of 64
+    // columns from the first that it holds on, so that narrower accumulators would have to end before the last ones do)
+    const int lg_bufs = sh.max_cols <= 128 ? 2 : 1, n_bufs = 1 << lg_bufs, buf_cols = 512 >> lg_bufs;
     Walk walk;
 
     if (warp < kEpiWarp0) {
@@ -376,7 +382,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             unsigned ph = 0;
             bool ok = true;
             Seg sg;
-            while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
+ while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
                 const GroupWeights* gw = L.weights + sg.g;
                 const int x_rows = max(8, 1 << (32 - __clz(sg.cols / 2 - 1))), xi = __ffs(x_rows) - 4;
                 const uint32_t bytes = 2u * (kStageW + x_rows * 128);
@@ -433,69 +439,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             // is known to be the same for all lanes and stays in uniform registers. ----
             if (rank == 0) {
                 const uint32_t tmem = uniform(sh.tmem), base = uniform(sm0), size = uniform(stage_bytes);
-                const int n_st = (int)uniform((uint32_t)stages);
+                const int n_st = (int)uniform((uint32_t)stages), lg = (int)uniform((uint32_t)lg_bufs), bufs = 1 << lg;
                 int st = 0, chunk = 0;
                 unsigned ph = 0;
                 bool ok = true;
                 Seg sg;
-                while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
+ while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
                     const int half = (int)uniform((uint32_t)sg.cols) / 2;
                     const int k_end = (int)uniform((uint32_t)sg.k1);
                     int k = (int)uniform((uint32_t)sg.k0);
-                    auto next_buf = [&]() {  // waits until accumulator `chunk` may be overwritten
-                        const int buf = chunk % K::kBufs;
-                        if (chunk >= K::kBufs) ok = wait_for(&sh.tempty[buf], ((chunk / K::kBufs) & 1) ^ 1u, sh);
+                    const uint32_t idesc = K::kIdesc | (uint32_t)(2 * half >> 3) << 17;
+                    for (; ok && k < k_end; ++chunk) {
+                        const int kc = min(k_end, k + K::kChunk), buf = chunk & (bufs - 1);
+                        if (chunk >= bufs) ok = wait_for(&sh.tempty[buf], ((chunk >> lg) & 1) ^ 1u, sh);
                         tc_after();
-                        return buf;
-                    };
-                    auto next_stage = [&]() {
-                        if (++st == n_st) {
-                            st = 0;
-                            ph ^= 1u;
-                        }
-                    };
-                    if constexpr (E8) {
-                        const int w0 = first_chunk<E8>(half), w1 = half - w0;
-                        const uint32_t id0 = K::kIdesc | (uint32_t)(2 * w0 >> 3) << 17, id1 = K::kIdesc | (uint32_t)(2 * w1 >> 3) << 17;
-                        for (; ok && k < k_end; ++k) {
+                        const uint32_t d = tmem + (buf << (9 - lg));
+                        for (int first = k; ok && k < kc; ++k) {
                             ok = wait_for(&sh.full[st], ph, sh);
+                            if (!ok) break;
+                            tc_after();
                             const uint32_t a0 = base + st * size;
-                            for (int c = 0; ok && c < (w1 > 0 ? 2 : 1); ++c, ++chunk) {
-                                const int buf = next_buf();
-                                if (!ok) break;
-                                const uint64_t ad = desc_k(a0), bd = desc_k(a0 + kStageW + c * w0 * 128);
-                                const uint32_t d = tmem + buf * K::kBufCols, idesc = c ? id1 : id0;
-                                if (elect_one()) {
+                            const uint64_t bd = desc_k(a0 + kStageW);
+                            const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
+                            if (elect_one()) {
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) pair_mma<E8>(d, ad + 2 * i, bd + 2 * i, idesc, i > 0);
-                                    pair_commit(&sh.tfull[buf]);
-                                    if (c == 1 || w1 == 0) pair_commit(&sh.empty[st]);
-                                }
-                                __syncwarp();
+                                for (int i = 0; i < 4; ++i)
+                                    pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
+                                if (k + 1 == kc) pair_commit(&sh.tfull[buf]);
+                                pair_commit(&sh.empty[st]);
                             }
-                            next_stage();
-                        }
-                    } else {
-                        const uint32_t idesc = K::kIdesc | (uint32_t)(2 * half >> 3) << 17;
-                        for (; ok && k < k_end; ++chunk) {
-                            const int kc = min(k_end, k + K::kChunk), buf = next_buf();
-                            const uint32_t d = tmem + buf * K::kBufCols;
-                            for (int first = k; ok && k < kc; ++k) {
-                                ok = wait_for(&sh.full[st], ph, sh);
-                                if (!ok) break;
-                                tc_after();
-                                const uint32_t a0 = base + st * size;
-                                const uint64_t bd = desc_k(a0 + kStageW);
-                                const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
-                                if (elect_one()) {
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i)
-                                        pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
-                                    pair_commit(&sh.empty[st]);
-                                    if (k + 1 == kc) pair_commit(&sh.tfull[buf]);
-                                }
-                                __syncwarp();
-                                next_stage();
+                            __syncwarp();
+                            if (++st == n_st) {
+                                st = 0;
+                                ph ^= 1u;
                             }
                         }
                     }
@@ -507,31 +483,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             // weights. They are copied kScaleSlots - 1 stages ahead: an L2 access takes longer than a stage's MMAs. ----
             const int half = warp - 2;
             int chunk = 0;
-            unsigned stage = 0;
             bool ok = true;
             Seg sg;
             while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
-                const int cols = sg.cols / 2, w0 = first_chunk<E8>(cols), w1 = cols - w0;
+                const int cols = sg.cols / 2, c0 = half * cols;
                 const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
                 const GroupWeights* gw = L.weights + sg.g;
                 const float* ws = gw->ws + (size_t)block * steps + sg.k0;
                 const float* us = GATED ? gw->us + (size_t)block * steps + sg.k0 : nullptr;
-                const float* xs = L.x_scale + (size_t)sg.k0 * L.ld_scale + sg.row0 + half * cols + lane;
-                const int mine = sg.rows - half * cols;  // rows of the tile from this half on
-                const uint32_t t0 = lane < min(w0, mine) ? 4 : 0, t1 = lane + 32 < min(w0, mine) ? 4 : 0;
-                const uint32_t t2 = lane < min(w1, mine - w0) ? 4 : 0, t3 = lane + 32 < min(w1, mine - w0) ? 4 : 0;
-                int ahead = sg.k0;
-                unsigned slot = stage;
+                const float* xs = L.x_scale + (size_t)sg.k0 * L.ld_scale + sg.row0 + c0 + lane;
+                const int in = min(cols, sg.rows - c0) - lane;  // this lane copies columns lane + 32 i, 32 i < in
+                int ahead = sg.k0, slot = chunk;
                 auto fetch = [&]() {
                     if (ahead < sg.k1) {
                         float* to = &sh.raw[slot & (kScaleSlots - 1)][half][0][lane];
-                        cp4(to, t0 ? xs : L.x_scale, t0);
-                        cp4(to + 32, t1 ? xs + 32 : L.x_scale, t1);
-                        cp4(to + 64, t2 ? xs + w0 : L.x_scale, t2);
-                        cp4(to + 96, t3 ? xs + w0 + 32 : L.x_scale, t3);
-                        cp4(to + 128, ws, 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) cp4(to + 32 * i, 32 * i < in ? xs + 32 * i : L.x_scale, 32 * i < in ? 4 : 0);
+                        cp4(to + 128, ws++, 4);
                         if (GATED) cp4(to + 160, us++, 4);
-                        ++ws;
                         xs += L.ld_scale;
                     }
                     cp_commit();
@@ -539,30 +508,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     ++slot;
                 };
                 for (int i = 0; i < kScaleSlots - 1; ++i) fetch();
-                for (int k = sg.k0; ok && k < sg.k1; ++k, ++stage) {
+                for (int k = sg.k0; k < sg.k1; ++k, ++chunk) {
                     fetch();  // (what a lane copies it reads itself)
                     cp_wait<kScaleSlots - 1>();
-                    const float* raw = &sh.raw[stage & (kScaleSlots - 1)][half][0][lane];
+                    const float* raw = &sh.raw[chunk & (kScaleSlots - 1)][half][0][lane];
                     const float g = raw[128], u = GATED ? raw[160] : 0.0f;
+                    const int buf = chunk & (n_bufs - 1);
+                    if (chunk >= n_bufs)
+                        ok = __all_sync(0xffffffffu, wait_for(&sh.sempty[buf], ((chunk >> lg_bufs) & 1) ^ 1u, sh));
+                    if (!ok) break;
+                    float* to = &sh.scale[0][buf * buf_cols + c0 + lane];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (c == 1 && w1 == 0) break;
-                        const float x0 = raw[64 * c], x1 = raw[64 * c + 32];
-                        const int buf = chunk % K::kBufs;
-                        if (chunk >= K::kBufs)
-                            ok = __all_sync(0xffffffffu, wait_for(&sh.sempty[buf], ((chunk / K::kBufs) & 1) ^ 1u, sh));
-                        if (!ok) break;
-                        float* to = &sh.scale[buf][0][half][lane];
-                        to[0] = x0 * g;
-                        to[32] = x1 * g;
-                        if (GATED) {
-                            to[128] = x0 * u;
-                            to[160] = x1 * u;
+                    for (int i = 0; i < 4; ++i)
+                        if (32 * i + lane < cols) {
+                            to[32 * i] = raw[32 * i] * g;
+                            if (GATED) to[512 + 32 * i] = raw[32 * i] * u;
                         }
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.tfull[buf]);
-                        ++chunk;
-                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.tfull[buf]);
                 }
             }
         }
@@ -575,8 +538,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         bool ok = true;
         // gated: a gate warp and the up warp of the same neurons wait for each other
         const int both = half * 2 + (q & 1);
-        unsigned met = 0;
         const uint32_t t_empty = in_cta(&sh.tempty[0], 0);
+        unsigned met = 0;
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.met[both]);
@@ -594,7 +557,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 __syncwarp();
             }
             const int cols = sg.cols / 2, c0 = half * cols;  // this warp's columns, a multiple of 8 ...
-            const int w0 = first_chunk<E8>(cols), w1 = cols - w0;  // ... in two chunks
+            const int w0 = min(cols, 64), w1 = cols - w0;  // ... in two chunks
             f32x2 acc[2][2][16];  // [16 lanes][64 columns][of 8 columns: lanes t / 4, lanes t / 4 + 8]
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i >> 5][(i >> 4) & 1][i & 15] = 0ull;
@@ -602,46 +565,60 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 tc_before();
                 __syncwarp();
                 if (lane == 0) {
-                    arrive_at(t_empty + buf * 8);
-                    if (E8) mbar_arrive(&sh.sempty[buf]);
-                }
+ arrive_at(t_empty + buf * 8);
+ if (E8) mbar_arrive(&sh.sempty[buf]);
+ }
             };
             auto filled = [&](int buf) {
-                ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk / K::kBufs) & 1, sh));
+                ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> lg_bufs) & 1, sh));
                 tc_after();
                 return ok;
             };
             if constexpr (E8) {
-                const float* scale = &sh.scale[0][GATED ? q >> 1 : 0][half][2 * (lane & 3)];
-                for (int left = sg.k1 - sg.k0; ok && left > 0; --left) {
+                const float* scale = &sh.scale[GATED ? q >> 1 : 0][c0 + 2 * (lane & 3)];
+                for (int left = sg.k1 - sg.k0; left > 0; --left, ++chunk) {
+                    const int buf = chunk & (n_bufs - 1);
+                    if (!filled(buf)) break;
+                    const uint32_t from = lane_addr + buf * buf_cols + c0;
+                    const f32x2* s2 = reinterpret_cast<const f32x2*>(scale + buf * buf_cols);
+                    if (cols <= 16) {  // both halves of the lanes at once
+                        uint32_t r0[8], r1[8];
+                        tc_ld16(from, r0);
+                        tc_ld16(from + (16u << 16), r1);
+                        const f32x2 sa = s2[0], sb = s2[4];
+                        tc_ld_wait16(r0, r1);
+                        release(buf);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            acc[0][0][i] = fma2(pack2(r0[2 * i], r0[2 * i + 1]), i < 2 ? sa : sb, acc[0][0][i]);
+                            acc[1][0][i] = fma2(pack2(r1[2 * i], r1[2 * i + 1]), i < 2 ? sa : sb, acc[1][0][i]);
+                        }
+                        continue;
+                    }
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (c == 1 && w1 == 0) break;
-                        const int buf = chunk % K::kBufs;
-                        if (!filled(buf)) break;
-                        const uint32_t from = lane_addr + buf * K::kBufCols + half * (c ? w1 : w0);
-                        uint32_t r0[32], r1[32];
-                        tc_ld64(from, r0);
-                        tc_ld64(from + (16u << 16), r1);
-                        f32x2 s2[8];
+                        uint32_t r[32];
+                        tc_ld64(from + 64 * c, r);
+                        f32x2 sc[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) s2[j] = *reinterpret_cast<const f32x2*>(scale + buf * 256 + 8 * j);
-                        tc_ld_wait(r0);
-                        tc_ld_wait(r1);
-                        release(buf);
+                        for (int j = 0; j < 8; ++j) sc[j] = s2[32 * c + 4 * j];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            acc[0][c][2 * j] = fma2(pack2(r0[4 * j], r0[4 * j + 1]), s2[j], acc[0][c][2 * j]);
-                            acc[0][c][2 * j + 1] = fma2(pack2(r0[4 * j + 2], r0[4 * j + 3]), s2[j], acc[0][c][2 * j + 1]);
-                            acc[1][c][2 * j] = fma2(pack2(r1[4 * j], r1[4 * j + 1]), s2[j], acc[1][c][2 * j]);
-                            acc[1][c][2 * j + 1] = fma2(pack2(r1[4 * j + 2], r1[4 * j + 3]), s2[j], acc[1][c][2 * j + 1]);
+                        for (int h = 0; h < 2; ++h) {
+                            tc_ld_wait(r);
+                            if (h == 1 && (c == 1 || w1 == 0)) release(buf);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                acc[h][c][2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), sc[j], acc[h][c][2 * j]);
+                                acc[h][c][2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), sc[j], acc[h][c][2 * j + 1]);
+                            }
+                            if (h == 0) tc_ld64(from + 64 * c + (16u << 16), r);
                         }
-                        ++chunk;
                     }
                 }
             } else {
                 for (int left = sg.k1 - sg.k0; left > 0; left -= K::kChunk, ++chunk) {
-                    const int buf = chunk % K::kBufs;
+                    const int buf = chunk & (n_bufs - 1);
                     if (!filled(buf)) break;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -649,7 +626,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t r[32];
-                            tc_ld64(lane_addr + ((uint32_t)(16 * h) << 16) + buf * K::kBufCols + c0 + c * w0, r);
+                            tc_ld64(lane_addr + ((uint32_t)(16 * h) << 16) + buf * buf_cols + c0 + 64 * c, r);
                             tc_ld_wait(r);
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
