@@ -450,12 +450,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     int k = (int)uniform((uint32_t)sg.k0);
                     const uint32_t idesc = K::kIdesc | (uint32_t)(2 * half >> 3) << 17;
                     for (; ok && k < k_end; ++chunk) {
-                        const int kc = min(k_end, k + K::kChunk), buf = chunk & (bufs - 1);
-                        if (chunk >= bufs) ok = wait_for(&sh.tempty[buf], ((chunk >> lg) & 1) ^ 1u, sh);
-                        tc_after();
+                        const int first = k, kc = min(k_end, k + K::kChunk), buf = chunk & (bufs - 1);
                         const uint32_t d = tmem + (buf << (9 - lg));
-                        for (int first = k; ok && k < kc; ++k) {
+                        for (; ok && k < kc; ++k) {
+                            // the accumulator is what is waited for longest: its barrier last
                             ok = wait_for(&sh.full[st], ph, sh);
+                            if (ok && k == first && chunk >= bufs) ok = wait_for(&sh.tempty[buf], ((chunk >> lg) & 1) ^ 1u, sh);
                             if (!ok) break;
                             tc_after();
                             const uint32_t a0 = base + st * size;
