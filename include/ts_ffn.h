@@ -388,7 +388,7 @@ void ts_graph_destroy(ts_graph* g);
 /*
  * Routing of `tokens` tokens from the router's logits.
  *   logits     device [tokens][n_experts] fp32
- *   n_experts  1..256, top_k 1..min(8, n_experts)
+ *   n_experts  1..256, top_k 1..min(8, n_experts); tokens * top_k below 2^30
  *   sel, w     device [tokens][top_k]: the picked experts, largest logit first (the
  *              lower index wins a tie), and the softmax over the picked logits
  *   offsets    device [n_experts + 1]: expert e has rows offsets[e] .. offsets[e + 1] - 1
@@ -487,6 +487,48 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
 /* As ts_ffn_get_error and ts_ffn_check_scratch. */
 ts_status ts_grouped_get_error(ts_grouped* h, cudaStream_t stream);
 ts_status ts_grouped_check_scratch(ts_grouped* h, cudaStream_t stream);
+
+typedef struct ts_experts ts_experts; /* the weights of one layer of experts, for many tokens */
+typedef struct ts_prompt ts_prompt;   /* scratch of layers over many tokens                    */
+
+/*
+ * One layer over many tokens: top_k of n_experts dReLU FFNs (Sec. 4), or a single one.
+ *   d, m       model width and neurons of an expert; multiples of 8 (TS_BF16) or 16 (TS_E4M3)
+ *   n_experts  1..256, top_k 1..min(8, n_experts)
+ *   wdtype     TS_BF16 or TS_E4M3; activations x are bf16 either way
+ *   w_router   device [n_experts][d] bf16; NULL with one expert, which then has weight 1
+ *   w_gate, w_up   host arrays of n_experts device pointers, each [m][d]
+ *   w_down     the same, each [m][d] (by neuron, as ts_ffn_create) for TS_BF16, [d][m] for TS_E4M3
+ *   s_gate, s_up, s_down   TS_E4M3: host arrays of device pointers to scales as in ts_grouped_create,
+ *              [ceil(m / 128)][ceil(d / 128)] twice and [ceil(d / 128)][ceil(m / 128)]. NULL for TS_BF16.
+ * All weights are borrowed. The handle has no scratch: it may be used by forwards with different ts_prompt at once.
+ */
+ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int top_k, ts_dtype wdtype,
+                            const void* w_router, const void* const* w_gate, const void* const* w_up,
+                            const void* const* w_down, const float* const* s_gate, const float* const* s_up,
+                            const float* const* s_down);
+void ts_experts_destroy(ts_experts* e);
+
+/* Scratch for forwards of up to max_tokens tokens through any layers of these sizes (arguments as
+   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle. */
+ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top_k, ts_dtype wdtype, int max_tokens);
+void ts_prompt_destroy(ts_prompt* p);
+
+/*
+ * y[t] = sum over the picked experts of w * FFN_e(x[t]) (one expert: FFN(x[t])), as ts_moe_forward and
+ * ts_ffn_forward compute it for few tokens, with c = max(0, g) max(0, u) rounded to bf16 before the down product
+ * (a GEMM operand), and for TS_E4M3 x and c rounded to e4m3 by ts_quant_rows.
+ *   x       device [tokens][d] bf16, 0 <= tokens <= max_tokens
+ *   y       device [tokens][d] fp32, overwritten (a token with no expert, all of its router logits NaN: 0)
+ */
+ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int tokens, float* y, cudaStream_t stream);
+
+/* Routing of the last forward (of its top_k), to host memory (synchronises `stream`): sel and w [tokens][top_k].
+   TS_ERR_INVALID_ARG after a layer of one expert without a router. */
+ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel, float* w);
+/* As ts_ffn_get_error and ts_ffn_check_scratch. */
+ts_status ts_prompt_get_error(ts_prompt* p, cudaStream_t stream);
+ts_status ts_prompt_check_scratch(ts_prompt* p, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

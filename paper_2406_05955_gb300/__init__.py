@@ -6,4 +6,5 @@ the seeded synthetic inputs; ``build`` compiles the sm_103a library in-tree.
 """
 from .binding import (Ffn, Graph, Moe, Predictor, TsError, lib, moe_stack_forward,  # noqa: F401
                       stack_forward, stack_forward_predicted)
-from .prompt import Grouped, Routing, combine_rows, gather_rows, quant_rows, route  # noqa: F401
+from .prompt import (Experts, Grouped, Prompt, Routing, combine_rows, gather_rows, quant_rows,  # noqa: F401
+                     route)

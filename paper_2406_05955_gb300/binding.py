@@ -80,6 +80,14 @@ SIGNATURES = {
     "ts_grouped_forward": (I, [P, P, L64, P, L64, P, I, P, L64, I, P]),
     "ts_grouped_get_error": (I, [P, P]),
     "ts_grouped_check_scratch": (I, [P, P]),
+    "ts_experts_create": (I, [PP, I, I, I, I, I, P, P, P, P, P, P, P]),
+    "ts_experts_destroy": (None, [P]),
+    "ts_prompt_create": (I, [PP, I, I, I, I, I, I]),
+    "ts_prompt_destroy": (None, [P]),
+    "ts_prompt_forward": (I, [P, P, P, I, P, P]),
+    "ts_prompt_get_routing": (I, [P, P, P, P]),
+    "ts_prompt_get_error": (I, [P, P]),
+    "ts_prompt_check_scratch": (I, [P, P]),
 }
 
 

@@ -877,7 +877,7 @@ void configure(cudaLaunchConfig_t* cfg, int pairs, cudaStream_t stream) {
 }
 }  // namespace
 
-int grouped_pairs(bool e4m3, bool gated, bool kn) {
+int grouped_pairs() {
     cudaLaunchConfig_t cfg{};
     configure(&cfg, 1, nullptr);
     cudaLaunchAttribute at{};
@@ -886,7 +886,7 @@ int grouped_pairs(bool e4m3, bool gated, bool kn) {
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, pick(e4m3, gated, kn), &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, pick(true, true, false), &cfg) != cudaSuccess) {
         cudaGetLastError();
         return 0;
     }

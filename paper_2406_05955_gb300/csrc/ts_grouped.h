@@ -84,8 +84,8 @@ inline size_t grouped_arrived(int pairs) { return (size_t)pairs * 2 * 2 * kEpiWa
 bool grouped_map(CUtensorMap* m, const void* p, bool e4m3, int64_t cols, int64_t rows, int64_t ld, int box_rows);
 constexpr int grouped_w_box(bool gated, bool kn) { return gated || kn ? 64 : 128; }
 cudaError_t prepare_grouped();
-// CTA pairs that can be resident at once.
-int grouped_pairs(bool e4m3, bool gated, bool kn);
+// CTA pairs that can be resident at once (the kernels take the same shared memory and threads).
+int grouped_pairs();
 
 cudaError_t launch_route(const RouteLaunch& a, cudaStream_t stream);
 cudaError_t launch_gather_rows(const RowsLaunch& a, int elem_bytes, cudaStream_t stream);

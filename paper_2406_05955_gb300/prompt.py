@@ -9,9 +9,10 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
+import numpy as np
 import torch
 
-from .binding import (TS_BF16, TS_E4M3, TS_F32, TS_KN, TS_NK, _check, lib)
+from .binding import TS_BF16, TS_E4M3, TS_F32, TS_KN, TS_NK, Ffn, Moe, P, _check, lib
 
 _CODES = {torch.float32: TS_F32, torch.bfloat16: TS_BF16, torch.float8_e4m3fn: TS_E4M3}
 _LAYOUTS = {"nk": TS_NK, "kn": TS_KN}
@@ -156,6 +157,16 @@ def combine_rows(src: torch.Tensor, slots: torch.Tensor, w: torch.Tensor, out=No
     return out
 
 
+def _matrices(t) -> list:
+    """A matrix, a list of them, or a stacked tensor, as a list."""
+    if isinstance(t, torch.Tensor):
+        t = [t] if t.dim() == 2 else list(t.unbind(0)) if t.dim() == 3 else []
+    t = list(t)
+    if not t:
+        raise ValueError("weights are a matrix, a list of them, or a stacked tensor")
+    return t
+
+
 def _pointers(ts):
     return None if ts is None else ctypes.cast((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]), ctypes.c_void_p)
 
@@ -166,7 +177,7 @@ class Grouped:
     ``scale[e] [ceil(n / 128)][ceil(k / 128)]``. ``w`` is a tensor (one group), a list of them, or a stacked one."""
 
     def __init__(self, w, layout: str = "nk", scale=None, max_rows: int = 1, _up=None, _scale_up=None):
-        w, up, scale, scale_up = (None if t is None else self._matrices(t) for t in (w, _up, scale, _scale_up))
+        w, up, scale, scale_up = (None if t is None else _matrices(t) for t in (w, _up, scale, _scale_up))
         if layout not in _LAYOUTS:
             raise ValueError('layout must be "nk" or "kn"')
         for t in w + (up or []):
@@ -197,15 +208,6 @@ class Grouped:
     def gated(cls, w_gate, w_up, scale_gate=None, scale_up=None, max_rows: int = 1) -> "Grouped":
         """``y[r] = max(0, x[r] G_e^T) * max(0, x[r] U_e^T)``: the dReLU products of Eq. 2."""
         return cls(w_gate, scale=scale_gate, max_rows=max_rows, _up=w_up, _scale_up=scale_up)
-
-    @staticmethod
-    def _matrices(t):
-        if isinstance(t, torch.Tensor):
-            t = [t] if t.dim() == 2 else list(t.unbind(0)) if t.dim() == 3 else []
-        t = list(t)
-        if not t:
-            raise ValueError("weights are a matrix, a list of them, or a stacked tensor")
-        return t
 
     @property
     def handle(self) -> ctypes.c_void_p:
@@ -251,6 +253,129 @@ class Grouped:
     def close(self) -> None:
         if getattr(self, "_h", None) is not None:
             lib().ts_grouped_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Experts:
+    """The weights of one layer over many tokens: ``top_k`` of the dReLU FFNs ``w_gate[e], w_up[e] [m][d]`` and ``w_down[e]``
+    (bf16: ``[m][d]``, by neuron, as in ``Ffn``; e4m3: ``[d][m]``, with the three ``scale_*`` lists of ``Grouped``), picked by
+    ``w_router [experts][d]`` (bf16), or a single one without it. Weights are borrowed."""
+
+    def __init__(self, w_gate, w_up, w_down, w_router=None, top_k: int = 1, scale_gate=None, scale_up=None,
+                 scale_down=None):
+        ws = [_matrices(t) for t in (w_gate, w_up, w_down)]
+        for t in ws[0] + ws[1] + ws[2]:
+            _tensor(t, "weights", (torch.bfloat16, torch.float8_e4m3fn), 2)
+        self.dtype, self.n_experts, self.top_k = ws[0][0].dtype, len(ws[0]), int(top_k)
+        self.m, self.d = (int(v) for v in ws[0][0].shape)
+        e8 = self.dtype == torch.float8_e4m3fn
+        down = (self.d, self.m) if e8 else (self.m, self.d)
+        for w, shape in zip(ws, ((self.m, self.d), (self.m, self.d), down)):
+            if len(w) != self.n_experts or any(tuple(t.shape) != shape or t.dtype != self.dtype for t in w):
+                raise ValueError(f"w_gate and w_up must be [{self.m}][{self.d}], w_down {list(down)}, of one type and number")
+        scales = [None if t is None else _matrices(t) for t in (scale_gate, scale_up, scale_down)]
+        for s, w in zip(scales, ws):
+            if (s is not None) != e8 or (e8 and len(s) != self.n_experts):
+                raise ValueError("e4m3 weights need scales, and only they have any")
+            for t in s or []:
+                _shaped(t, "scale", torch.float32, tuple(-(-v // BLOCK) for v in w[0].shape))
+        if w_router is not None:
+            _shaped(w_router, "w_router", torch.bfloat16, (self.n_experts, self.d))
+        self.routed = w_router is not None
+        self._keep = (ws, scales, w_router)
+        h = ctypes.c_void_p()
+        self._h = None
+        _check(lib().ts_experts_create(ctypes.byref(h), self.d, self.m, self.n_experts, self.top_k, _CODES[self.dtype],
+                                       None if w_router is None else w_router.data_ptr(), *map(_pointers, ws),
+                                       *map(_pointers, scales)), "ts_experts_create")
+        self._h = h
+
+    @classmethod
+    def of(cls, layer) -> "Experts":
+        """The same weights as a bf16 ``Ffn`` or ``Moe`` layer."""
+        if isinstance(layer, Moe):
+            ws = list(zip(*(e._keep for e in layer.experts)))
+            return cls(*map(list, ws), w_router=layer._keep[0], top_k=layer.top_k)
+        if isinstance(layer, Ffn):
+            return cls(*layer._keep)
+        raise TypeError("layer must be an Ffn or a Moe")
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if self._h is None:
+            raise RuntimeError("handle is closed")
+        return self._h
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None:
+            lib().ts_experts_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Prompt:
+    """Forwards of up to ``max_tokens`` tokens through ``experts``, or through any other layer of its sizes: the scratch of
+    all of them (``ts_prompt_*``)."""
+
+    def __init__(self, experts: Experts, max_tokens: int):
+        self.experts, self.max_tokens = experts, int(max_tokens)
+        h = ctypes.c_void_p()
+        self._h = None
+        _check(lib().ts_prompt_create(ctypes.byref(h), experts.d, experts.m, experts.n_experts, experts.top_k,
+                                      _CODES[experts.dtype], self.max_tokens), "ts_prompt_create")
+        self._h = h
+        self._last = None
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if self._h is None:
+            raise RuntimeError("handle is closed")
+        return self._h
+
+    def forward(self, x: torch.Tensor, experts=None, y=None, stream=None) -> torch.Tensor:
+        """fp32 ``y [tokens][d]`` of bf16 ``x [tokens][d]``, as ``Moe.forward`` (or ``Ffn.forward``) of few tokens."""
+        layer = self.experts if experts is None else experts
+        _tensor(x, "x", (torch.bfloat16,), 2)
+        if x.shape[1] != layer.d:
+            raise ValueError(f"x must be [tokens][{layer.d}]")
+        t = x.shape[0]
+        y = _empty(stream, t, layer.d, dtype=torch.float32) if y is None else _shaped(y, "y", torch.float32, (t, layer.d))
+        _check(lib().ts_prompt_forward(self.handle, layer.handle, x.data_ptr(), t, y.data_ptr(), _handle(stream)),
+               "ts_prompt_forward")
+        self._last = (t, layer.top_k)
+        return y
+
+    __call__ = forward
+
+    def get_routing(self, stream=None):
+        """(sel, w) of the last forward, as numpy [tokens][top_k]; -1: no expert."""
+        t, k = self._last or (0, 1)
+        sel, w = np.zeros((t, k), np.int32), np.zeros((t, k), np.float32)
+        _check(lib().ts_prompt_get_routing(self.handle, _handle(stream), sel.ctypes.data_as(P), w.ctypes.data_as(P)),
+               "ts_prompt_get_routing")
+        return sel, w
+
+    def get_error(self, stream=None) -> int:
+        return int(lib().ts_prompt_get_error(self.handle, _handle(stream)))
+
+    def check_scratch(self, stream=None) -> int:
+        """Status of the scratch guard zones (as Ffn.check_scratch)."""
+        return int(lib().ts_prompt_check_scratch(self.handle, _handle(stream)))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None:
+            lib().ts_prompt_destroy(self._h)
             self._h = None
 
     def __del__(self):

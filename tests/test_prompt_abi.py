@@ -102,3 +102,37 @@ def test_binding_refuses_cpu_tensors():
                  lambda: ts.combine_rows(w, torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, 1))):
         with pytest.raises(TypeError):
             call()
+
+
+def test_experts_and_prompt_arguments(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_INT4)
+
+    h = ctypes.c_void_p()
+    two, none = _array(GOOD, GOOD), _array(GOOD, None)
+
+    def experts(out=ctypes.byref(h), d=64, m=64, e=2, k=1, dt=TS_BF16, r=GOOD, g=two, u=two, dn=two, sg=None, su=None,
+                sd=None):
+        return lib.ts_experts_create(out, d, m, e, k, dt, r, g, u, dn, sg, su, sd)
+
+    for kw in ({"out": None}, {"d": 0}, {"m": 0}, {"d": 60}, {"m": 60}, {"e": 0}, {"e": 257}, {"k": 0}, {"k": 3}, {"dt": 9},
+               {"r": None}, {"r": GOOD + 2}, {"g": None}, {"u": None}, {"dn": None}, {"g": none}, {"u": none},
+               {"dn": none}, {"sg": two}, {"sd": two}, {"dt": TS_E4M3}, {"dt": TS_E4M3, "sg": two, "su": two},
+               {"dt": TS_E4M3, "sg": two, "su": two, "sd": two, "d": 72}):
+        assert experts(**kw) == BAD, kw
+    for dt in (TS_F32, TS_INT4):
+        assert experts(dt=dt) == UNSUPPORTED
+
+    def prompt(out=ctypes.byref(h), d=64, m=64, e=2, k=1, dt=TS_BF16, t=8):
+        return lib.ts_prompt_create(out, d, m, e, k, dt, t)
+
+    for kw in ({"out": None}, {"d": 0}, {"m": 60}, {"e": 0}, {"k": 3}, {"dt": 9}, {"t": 0}, {"t": 2 ** 30}):
+        assert prompt(**kw) == BAD, kw
+    assert prompt(dt=TS_INT4) == UNSUPPORTED
+    assert h.value is None
+    assert lib.ts_prompt_forward(None, None, GOOD, 4, GOOD, None) == BAD
+    assert lib.ts_prompt_get_routing(None, None, None, None) == BAD
+    assert lib.ts_prompt_get_error(None, None) == BAD
+    assert lib.ts_prompt_check_scratch(None, None) == BAD
+    lib.ts_experts_destroy(None)
+    lib.ts_prompt_destroy(None)
