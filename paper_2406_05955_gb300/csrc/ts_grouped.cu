@@ -33,6 +33,10 @@ constexpr int kScaleWarps = 2, kScaleSlots = 4;
 constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
 
 
+__device__ __forceinline__ void sts128(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
 // ---- tiles and their parts --------------------------------------------------
 // The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
 // are dealt out evenly, in order, so that all pairs end together: a pair's share begins and ends anywhere in a tile.
@@ -173,6 +177,17 @@ __device__ __forceinline__ void tc_ld_wait16(uint32_t (&a)[8], uint32_t (&b)[8])
                  :
                  : "memory");
 }
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32]) {  // 32 lanes x 32 columns, a lane a thread
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
 // the values of the loads before: not to be used earlier
 __device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -234,6 +249,7 @@ __device__ __forceinline__ int tile_rows(int n, int tiles) { return ((n + tiles 
 struct Walk {
     int round = 0;
     long long at = -1;
+    template <bool XM>
     __device__ bool next(const Shared& sh, int n_groups, int w_tiles, Seg& s) {
         const Parts& P = sh.parts;
         const int pair = blockIdx.x >> 1;
@@ -267,7 +283,7 @@ struct Walk {
         t -= band * kBand * w_tiles;
         s.wt = t / width;
         const int j = band * kBand + t % width;
-        const int high = tile_rows(n, tiles);
+        const int high = XM ? kMaxTileRows : tile_rows(n, tiles);
         s.row0 = sh.row0[lo] + j * high;
         s.rows = max(0, min(high, n - j * high));
         s.cols = high;
@@ -275,12 +291,17 @@ struct Walk {
     }
 };
 
-template <bool E8, bool GATED, bool KN>
+// XM (e4m3): the rows of x are the MMA's M, always 256 of them, and the weights its N. What a lane of tensor memory holds
+// then belongs to one row of x, with one scale, and 32 lanes can be read at a time: a load of 16 lanes (of columns that
+// have scales of their own) takes as long, and for wide tiles the reading is what bounds e4m3 products: 8192 rows through
+// a 14336 x 4096 matrix 424 -> 346 us. Narrow tiles would be mostly zeros.
+template <bool E8, bool GATED, bool KN, bool XM>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
     static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
     static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
-    static constexpr int kBoxes = GATED || KN ? 2 : 1;    // boxes of weights of a CTA's stage
+    static constexpr int kBoxes = GATED || KN ? 2 : 1;   // boxes of weights of a CTA's stage
+    static constexpr int kOffW = XM ? kStageW : 0, kOffX = XM ? 0 : kStageW;  // in a stage: M's operand, then N's
     static constexpr uint32_t kIdesc = (1u << 4) | (E8 ? 0u : (1u << 7) | (1u << 10)) | (KN ? 1u << 15 : 0u) | (16u << 24);
 };
 
@@ -299,9 +320,10 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, unsigned parity, Shared&
     return true;
 }
 
-template <bool E8, bool GATED, bool KN>
+template <bool E8, bool GATED, bool KN, bool XM>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_grouped(const __grid_constant__ GroupedLaunch L) {
-    using K = Kind<E8, GATED, KN>;
+    using K = Kind<E8, GATED, KN, XM>;
+    static_assert(!XM || (E8 && !KN), "");
     extern __shared__ __align__(1024) unsigned char sm_raw[];
     __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -324,7 +346,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 sh.rows[e] = n;
             }
             const int tiles = tiles_of(n);
-            if (n > 0) widest = max(widest, tile_rows(n, tiles));
+            if (n > 0) widest = XM ? kMaxTileRows : max(widest, tile_rows(n, tiles));
             int sum = tiles * w_tiles;
 #pragma unroll
             for (int o = 1; o < kWarp; o <<= 1) {
@@ -382,15 +404,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             unsigned ph = 0;
             bool ok = true;
             Seg sg;
- while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
+ while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
                 const GroupWeights* gw = L.weights + sg.g;
                 const int x_rows = max(8, 1 << (32 - __clz(sg.cols / 2 - 1))), xi = __ffs(x_rows) - 4;
                 const uint32_t bytes = 2u * (kStageW + x_rows * 128);
                 const CUtensorMap* map = &L.x[xi];
-                uint32_t off = kStageW;
+                uint32_t off = K::kOffX;
                 int cy = sg.row0 + (int)rank * (sg.cols / 2), cx = 0;  // coordinate of the box besides k's
                 if (lane < K::kBoxes) {
-                    if constexpr (GATED) {  // 64 gate rows, then the same neurons' up rows
+                    if constexpr (GATED && XM) {  // 128 gate rows by one CTA, the same neurons' up rows by the other
+                        map = rank ? &gw->u : &gw->w;
+                        off = K::kOffW + lane * 8192;
+                        cy = sg.wt * 128 + lane * 64;
+                    } else if constexpr (GATED) {  // 64 gate rows, then the same neurons' up rows
                         map = lane ? &gw->u : &gw->w;
                         off = lane * 8192;
                         cy = sg.wt * 128 + (int)rank * 64;
@@ -400,7 +426,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         cx = sg.wt * 256 + (int)rank * 128 + lane * 64;
                     } else {
                         map = &gw->w;
-                        off = 0;
+                        off = K::kOffW;
                         cy = sg.wt * 256 + (int)rank * 128;
                     }
                 }
@@ -444,7 +470,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 unsigned ph = 0;
                 bool ok = true;
                 Seg sg;
- while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
+ while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
                     const int half = (int)uniform((uint32_t)sg.cols) / 2;
                     const int k_end = (int)uniform((uint32_t)sg.k1);
                     int k = (int)uniform((uint32_t)sg.k0);
@@ -485,14 +511,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             int chunk = 0;
             bool ok = true;
             Seg sg;
-            while (ok && walk.next(sh, L.n_groups, w_tiles, sg)) {
-                const int cols = sg.cols / 2, c0 = half * cols;
-                const int block = GATED ? sg.wt : min(2 * sg.wt + (int)rank, (L.n + kScaleBlock - 1) / kScaleBlock - 1);
+            while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
+                // this warp's part: columns [c0, c0 + cols) of an accumulator, XM: lanes of it
+                const int cols = XM ? 64 : sg.cols / 2, c0 = half * cols, first = XM ? (int)rank * 128 + c0 : c0;
+                const int last_block = (L.n + kScaleBlock - 1) / kScaleBlock - 1;
                 const GroupWeights* gw = L.weights + sg.g;
-                const float* ws = gw->ws + (size_t)block * steps + sg.k0;
-                const float* us = GATED ? gw->us + (size_t)block * steps + sg.k0 : nullptr;
-                const float* xs = L.x_scale + (size_t)sg.k0 * L.ld_scale + sg.row0 + c0 + lane;
-                const int in = min(cols, sg.rows - c0) - lane;  // this lane copies columns lane + 32 i, 32 i < in
+                // one scale of the weights (XM: two) for all outputs of a tile, and one for the up product
+                const float* ws = gw->ws + (size_t)(GATED ? sg.wt : min(2 * sg.wt + (XM ? 0 : (int)rank), last_block)) * steps + sg.k0;
+                const float* us = GATED ? gw->us + (size_t)sg.wt * steps + sg.k0
+                                  : XM  ? gw->ws + (size_t)min(2 * sg.wt + 1, last_block) * steps + sg.k0
+                                        : nullptr;
+                const float* xs = L.x_scale + (size_t)sg.k0 * L.ld_scale + sg.row0 + first + lane;
+                const int in = min(cols, sg.rows - first) - lane;  // this lane copies columns lane + 32 i, 32 i < in
                 int ahead = sg.k0, slot = chunk;
                 auto fetch = [&]() {
                     if (ahead < sg.k1) {
@@ -500,7 +530,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
 #pragma unroll
                         for (int i = 0; i < 4; ++i) cp4(to + 32 * i, 32 * i < in ? xs + 32 * i : L.x_scale, 32 * i < in ? 4 : 0);
                         cp4(to + 128, ws++, 4);
-                        if (GATED) cp4(to + 160, us++, 4);
+                        if (GATED || XM) cp4(to + 160, us++, 4);
                         xs += L.ld_scale;
                     }
                     cp_commit();
@@ -512,7 +542,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     fetch();  // (what a lane copies it reads itself)
                     cp_wait<kScaleSlots - 1>();
                     const float* raw = &sh.raw[chunk & (kScaleSlots - 1)][half][0][lane];
-                    const float g = raw[128], u = GATED ? raw[160] : 0.0f;
+                    const float g = raw[128], u = GATED || XM ? raw[160] : 0.0f;
                     const int buf = chunk & (n_bufs - 1);
                     if (chunk >= n_bufs)
                         ok = __all_sync(0xffffffffu, wait_for(&sh.sempty[buf], ((chunk >> lg_bufs) & 1) ^ 1u, sh));
@@ -522,7 +552,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     for (int i = 0; i < 4; ++i)
                         if (32 * i + lane < cols) {
                             to[32 * i] = raw[32 * i] * g;
-                            if (GATED) to[512 + 32 * i] = raw[32 * i] * u;
+                            if (GATED || XM) to[512 + 32 * i] = raw[32 * i] * u;
                         }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.tfull[buf]);
@@ -551,7 +581,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         while (ok) {
             {
                 Seg now;
-                if (!walk.next(sh, L.n_groups, w_tiles, now)) break;
+                if (!walk.next<XM>(sh, L.n_groups, w_tiles, now)) break;
                 __syncwarp();
                 if (lane == 0) sh.seg[ew] = now;
                 __syncwarp();
@@ -565,16 +595,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 tc_before();
                 __syncwarp();
                 if (lane == 0) {
- arrive_at(t_empty + buf * 8);
- if (E8) mbar_arrive(&sh.sempty[buf]);
- }
+                    arrive_at(t_empty + buf * 8);
+                    if (E8) mbar_arrive(&sh.sempty[buf]);
+                }
             };
             auto filled = [&](int buf) {
                 ok = __all_sync(0xffffffffu, wait_for(&sh.tfull[buf], (chunk >> lg_bufs) & 1, sh));
                 tc_after();
                 return ok;
             };
-            if constexpr (E8) {
+            if constexpr (XM) {
+                // lane = row of x; acc[b][c]: columns 32 b .. + 31 of chunk c. Plain: the two chunks follow on one another, from
+                // column 128 half on; gated: chunk 0 gate values, chunk 1 the up values of the same 64 neurons.
+                const float* scale = &sh.scale[GATED ? 0 : half][32 * q + lane];
+                for (int left = sg.k1 - sg.k0; left > 0; --left, ++chunk) {
+                    const int buf = chunk & 1;
+                    if (!filled(buf)) break;
+                    const uint32_t s0 = __float_as_uint(scale[buf * 256]), s1 = GATED ? __float_as_uint(scale[512 + buf * 256]) : s0;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const f32x2 sc = c ? pack2(s1, s1) : pack2(s0, s0);
+                        const uint32_t from = lane_addr + buf * 256 + (GATED ? 64 * half + 128 * c : 128 * half + 64 * c);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            uint32_t r[32];
+                            tc_ld32(from + 32 * b, r);
+                            tc_ld_wait(r);
+                            if (b == 1 && c == 1) release(buf);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[b][c][j] = fma2(pack2(r[2 * j], r[2 * j + 1]), sc, acc[b][c][j]);
+                        }
+                    }
+                }
+            } else if constexpr (E8) {
                 const float* scale = &sh.scale[GATED ? q >> 1 : 0][c0 + 2 * (lane & 3)];
                 for (int left = sg.k1 - sg.k0; left > 0; --left, ++chunk) {
                     const int buf = chunk & (n_bufs - 1);
@@ -662,7 +715,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 __syncwarp();
                 unsigned* count = L.arrived + ((size_t)sg.rest * 2 + rank) * kEpiWarps + ew;
                 unsigned before = 0;
-                if constexpr (GATED) {  // a gate and an up warp finish a tile together, so they are counted as one
+                if constexpr (GATED && !XM) {  // a gate and an up warp finish a tile together, so they are counted as one
                     ok = meet();
                     if (q < 2 && lane == 0) sh.before[both] = atomicAdd(count, 1u);
                     ok = ok && meet();
@@ -674,8 +727,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 }
                 if ((int)before != p1 - p0) continue;
                 __threadfence();
-                if (lane == 0 && (!GATED || q < 2)) *count = 0u;
-                if (cols <= 16) {
+                if (lane == 0 && (!GATED || XM || q < 2)) *count = 0u;
+                if (!XM && cols <= 16) {
                     // few columns: the parts of several pairs at a time, as each access takes as long as all of them
                     constexpr int kAtOnce = 2;
                     for (int p = p0; p <= p1; p += kAtOnce) {
@@ -707,6 +760,76 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     }
                 }
             }
+            if constexpr (XM) {
+                // a thread's row of y, `kOut` outputs from n0 on, in pieces of 64 bytes that are turned round in shared memory
+                // so that 4 lanes write one row's, as whole sectors
+                constexpr int kOut = GATED ? 64 : 128;
+                const int row = (int)rank * 128 + 32 * q, n0 = GATED ? sg.wt * 128 + 64 * half : sg.wt * 256 + 128 * half;
+                if constexpr (GATED) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        f32x2& a = acc[i >> 4][0][i & 15];
+                        const f32x2 u = acc[i >> 4][1][i & 15];
+                        a = pack2(__float_as_uint(lo2(a) > 0.0f && lo2(u) > 0.0f ? lo2(a) * lo2(u) : 0.0f),
+                                  __float_as_uint(hi2(a) > 0.0f && hi2(u) > 0.0f ? hi2(a) * hi2(u) : 0.0f));
+                    }
+                }
+                const int rows = sg.rows - row;  // of this warp's 32
+                if (L.y_vec && n0 + kOut <= L.n) {
+                    unsigned char* turn = sh.turn[ew];
+                    const int swz = (lane >> 1) & 3, r8 = lane >> 2;  // chunk c of row r lies at c ^ (r / 2 % 4)
+                    const uint32_t at = smem_u32(turn) + lane * 64;
+                    const size_t size = L.y_f32 ? 4 : 2;
+                    char* y = static_cast<char*>(L.y) + ((size_t)(sg.row0 + row) * L.ldy + n0) * size + (lane & 3) * 16;
+                    auto write_out = [&](int piece) {
+                        __syncwarp();
+#pragma unroll
+                        for (int r0 = 0; r0 < 32; r0 += 8) {
+                            const int r = r0 + r8;
+                            const uint4 v = lds128(turn + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+                            if (r < rows) *reinterpret_cast<uint4*>(y + (size_t)r * L.ldy * size + piece * 64) = v;
+                        }
+                        __syncwarp();
+                    };
+                    if (L.y_f32) {
+#pragma unroll
+                        for (int p = 0; p < kOut / 16; ++p) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const f32x2 a = acc[(p >> 1) & 1][p >> 2][(p & 1) * 8 + 2 * c], b = acc[(p >> 1) & 1][p >> 2][(p & 1) * 8 + 2 * c + 1];
+                                sts128(at + ((c ^ swz) << 4), (uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
+                            }
+                            write_out(p);
+                        }
+                    } else {
+#pragma unroll
+                        for (int p = 0; p < kOut / 32; ++p) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const f32x2* v = &acc[p & 1][p >> 1][4 * c];
+                                sts128(at + ((c ^ swz) << 4), bf16x2(v[0]), bf16x2(v[1]), bf16x2(v[2]), bf16x2(v[3]));
+                            }
+                            write_out(p);
+                        }
+                    }
+                } else if (lane < rows) {
+#pragma unroll
+                    for (int i = 0; i < kOut / 2; ++i) {
+                        const f32x2 v = acc[(i >> 4) & 1][i >> 5][i & 15];
+                        const int n = n0 + 2 * i;
+                        const size_t at = (size_t)(sg.row0 + row + lane) * L.ldy + n;
+                        if (L.y_f32) {
+                            if (n < L.n) static_cast<float*>(L.y)[at] = lo2(v);
+                            if (n + 1 < L.n) static_cast<float*>(L.y)[at + 1] = hi2(v);
+                        } else {
+                            if (n < L.n) static_cast<__nv_bfloat16*>(L.y)[at] = __float2bfloat16_rn(lo2(v));
+                            if (n + 1 < L.n) static_cast<__nv_bfloat16*>(L.y)[at + 1] = __float2bfloat16_rn(hi2(v));
+                        }
+                    }
+                }
+                __syncwarp();
+                continue;
+            } else {
             // outputs: [16 lanes h][8 lanes r] of each 8 columns
             const int mlane = lane >> 2;
             int n0 = sg.wt * 256 + (int)rank * 128 + q * 32, cb = c0;  // the warp's first output and first column
@@ -796,6 +919,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         }
                     }
             }
+            }
         }
     }
 
@@ -817,21 +941,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
 
 constexpr int kDynSmem = kStageMem + 1024;
 
+using Kernel = void (*)(GroupedLaunch);
+
 template <typename F>
 cudaError_t each_kernel(F&& f) {
-    cudaError_t e = f(k_grouped<false, false, false>);
-    if (e == cudaSuccess) e = f(k_grouped<false, false, true>);
-    if (e == cudaSuccess) e = f(k_grouped<false, true, false>);
-    if (e == cudaSuccess) e = f(k_grouped<true, false, false>);
-    if (e == cudaSuccess) e = f(k_grouped<true, true, false>);
-    return e;
+    for (Kernel k : {k_grouped<false, false, false, false>, k_grouped<false, false, true, false>,
+                     k_grouped<false, true, false, false>, k_grouped<true, false, false, false>,
+                     k_grouped<true, true, false, false>, k_grouped<true, false, false, true>, k_grouped<true, true, false, true>}) {
+        const cudaError_t e = f(k);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
-using Kernel = void (*)(GroupedLaunch);
-Kernel pick(bool e4m3, bool gated, bool kn) {
-    if (e4m3) return gated ? k_grouped<true, true, false> : k_grouped<true, false, false>;
-    if (gated) return k_grouped<false, true, false>;
-    return kn ? k_grouped<false, false, true> : k_grouped<false, false, false>;
+Kernel pick(bool e4m3, bool gated, bool kn, bool xm) {
+    if (e4m3 && xm) return gated ? k_grouped<true, true, false, true> : k_grouped<true, false, false, true>;
+    if (e4m3) return gated ? k_grouped<true, true, false, false> : k_grouped<true, false, false, false>;
+    if (gated) return k_grouped<false, true, false, false>;
+    return kn ? k_grouped<false, false, true, false> : k_grouped<false, false, false, false>;
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -886,7 +1013,7 @@ int grouped_pairs() {
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, pick(true, true, false), &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, pick(true, true, false, true), &cfg) != cudaSuccess) {
         cudaGetLastError();
         return 0;
     }
@@ -896,7 +1023,8 @@ int grouped_pairs() {
 cudaError_t launch_grouped(const GroupedLaunch& a, bool e4m3, bool gated, bool kn, cudaStream_t stream) {
     cudaLaunchConfig_t cfg{};
     configure(&cfg, a.pairs, stream);
-    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn), a);
+    const bool xm = e4m3 && a.rows > 128 * (a.offsets != nullptr ? a.n_groups : 1);
+    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn, xm), a);
 }
 
 }  // namespace tsffn
