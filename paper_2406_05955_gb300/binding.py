@@ -100,6 +100,8 @@ class TsError(RuntimeError):
 def lib() -> ctypes.CDLL:
     """The loaded libtsffn; raises if it has not been built (no fallback exists)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):

@@ -404,7 +404,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             unsigned ph = 0;
             bool ok = true;
             Seg sg;
- while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
+            while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
                 const GroupWeights* gw = L.weights + sg.g;
                 const int x_rows = max(8, 1 << (32 - __clz(sg.cols / 2 - 1))), xi = __ffs(x_rows) - 4;
                 const uint32_t bytes = 2u * (kStageW + x_rows * 128);
@@ -470,7 +470,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 unsigned ph = 0;
                 bool ok = true;
                 Seg sg;
- while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
+                while (ok && walk.next<XM>(sh, L.n_groups, w_tiles, sg)) {
                     const int half = (int)uniform((uint32_t)sg.cols) / 2;
                     const int k_end = (int)uniform((uint32_t)sg.k1);
                     int k = (int)uniform((uint32_t)sg.k0);
@@ -728,24 +728,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 if ((int)before != p1 - p0) continue;
                 __threadfence();
                 if (lane == 0 && (!GATED || XM || q < 2)) *count = 0u;
-                if (!XM && cols <= 16) {
-                    // few columns: the parts of several pairs at a time, as each access takes as long as all of them
-                    constexpr int kAtOnce = 2;
+                // few columns: the parts of several pairs at a time, as each access takes as long as all of them
+                auto join_few = [&](auto groups, auto at_once) {  // of 8 columns; parts
+                    constexpr int kG = decltype(groups)::value, kAtOnce = decltype(at_once)::value;
                     for (int p = p0; p <= p1; p += kAtOnce) {
-                        f32x2 v[kAtOnce][8];
+                        f32x2 v[kAtOnce][4 * kG];
 #pragma unroll
                         for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                v[u][i] = p + u <= p1 && in(i & 3, cols) ? __ldcg(part_of(p + u) + (16 * (i >> 2) + (i & 3)) * kWarp) : 0ull;
+                            for (int i = 0; i < 4 * kG; ++i)
+                                v[u][i] = p + u <= p1 ? __ldcg(part_of(p + u) + (16 * (i / (2 * kG)) + i % (2 * kG)) * kWarp) : 0ull;
 #pragma unroll
                         for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                f32x2& a = acc[i >> 2][0][i & 3];
+                            for (int i = 0; i < 4 * kG; ++i) {
+                                f32x2& a = acc[i / (2 * kG)][0][i % (2 * kG)];
                                 if (p + u <= p1) a = p + u == p0 ? v[u][i] : add2(a, v[u][i]);
                             }
                     }
+                };
+                if (!XM && cols == 8) {
+                    join_few(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+                } else if (!XM && cols == 16) {
+                    join_few(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
                 } else {
                     for (int p = p0; p <= p1; ++p) {
                         const f32x2* from = part_of(p);
@@ -1023,8 +1028,7 @@ int grouped_pairs() {
 cudaError_t launch_grouped(const GroupedLaunch& a, bool e4m3, bool gated, bool kn, cudaStream_t stream) {
     cudaLaunchConfig_t cfg{};
     configure(&cfg, a.pairs, stream);
-    const bool xm = e4m3 && a.rows > 128 * (a.offsets != nullptr ? a.n_groups : 1);
-    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn, xm), a);
+    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn, grouped_x_is_m(e4m3, gated, a.rows, a.n_groups)), a);
 }
 
 }  // namespace tsffn

@@ -74,8 +74,15 @@ struct GroupedLaunch {
     unsigned* status;
 };
 
+// Whether an e4m3 product takes the rows of x as the MMA's M (see Kind in ts_grouped.cu): where the groups have enough of
+// them on average to fill a tile of 256 reasonably. Over 8 groups of 65 rows (d = 4096, m = 14336) gated products take 202
+// us so and 207 otherwise, of 49 201 and 195; down products of 128 rows 110 and 101.
+inline bool grouped_x_is_m(bool e4m3, bool gated, long long rows, int groups) {
+    return e4m3 && rows > (gated ? 64ll : 128ll) * groups;
+}
+
 // Bytes of GroupedLaunch::partial for tiles of up to `rows` rows, and entries of `arrived`.
-inline int grouped_part_chunks(int rows) { return rows > 128 ? 2 : 1; }
+inline int grouped_part_chunks(int rows) { return rows > 64 ? 2 : 1; }  // (rows as M have two from 65 rows on)
 inline size_t grouped_partial_bytes(int pairs, int chunks) { return (size_t)pairs * 2 * 2 * kEpiWarps * chunks * 2048 * 4; }
 inline size_t grouped_arrived(int pairs) { return (size_t)pairs * 2 * 2 * kEpiWarps; }
 

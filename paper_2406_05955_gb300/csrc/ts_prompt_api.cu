@@ -102,7 +102,8 @@ ts_status run_products(const Products& P, const ProductScratch& S, const void* x
     const bool e8 = P.dt == TS_E4M3;
     GroupedLaunch a;
     // boxes of up to half of the widest tile that so many rows can give
-    const int widest = std::min(kMaxTileRows, (rows + 15) / 16 * 16);
+    const int widest = grouped_x_is_m(e8, P.gated, rows, P.n_groups) ? kMaxTileRows
+                                                                     : std::min(kMaxTileRows, (rows + 15) / 16 * 16);
     for (int i = 0; i < kXMaps; ++i) {
         if (!grouped_map(&a.x[i], x, e8, P.k, rows, ldx, 8 << i)) return TS_ERR_CUDA;
         if ((8 << i) >= widest / 2) break;

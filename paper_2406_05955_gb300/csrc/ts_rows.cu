@@ -38,11 +38,25 @@ __global__ void __launch_bounds__(kRowThreads) k_gather_rows(const RowsLaunch L,
         if (at + 16 * kWarp * i < row_bytes) *reinterpret_cast<uint4*>(to + 16 * kWarp * i) = v[i];
 }
 
-// e4m3 of the quotient x / scale, for inv = 1 / scale: the product with inv, corrected once by its remainder (Markstein's
-// division, correctly rounded but for rare last bits), which takes 3 instructions where a division takes about 10
-__device__ __forceinline__ float quotient(float x, float scale, float inv) {
-    const float q = __fmul_rn(x, inv);
-    return __fmaf_rn(__fmaf_rn(-q, scale, x), inv, q);
+// Two quotients x / scale, for inv = 1 / scale: the products with inv, corrected once by their remainders (Markstein's
+// division, correctly rounded but for rare last bits), 3 instructions for both where a division takes about 10.
+__device__ __forceinline__ float2 quotients(float a, float b, float scale, float inv) {
+    const float2 x = make_float2(a, b), i = make_float2(inv, inv), q = __fmul2_rn(x, i);
+    return __ffma2_rn(__ffma2_rn(q, make_float2(-scale, -scale), x), i, q);
+}
+
+// Largest magnitude of a 16-byte load's elements (NaN left out; a maximum in bf16 is exact).
+template <typename T>
+__device__ __forceinline__ float largest(const uint4& v) {
+    if constexpr (sizeof(T) == 2) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(__habs2(h[0]), __habs2(h[1])), __hmax2(__habs2(h[2]), __habs2(h[3])));
+        return fmaxf(__low2float(m), __high2float(m));
+    } else {
+        float f[4];
+        Vec<T>::unpack(v, f);
+        return fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
+    }
 }
 
 // A warp takes 8 (bf16) or 4 (fp32) blocks of 128 elements of a row, 16 or 32 lanes a block; a CTA the same blocks of 8
@@ -66,10 +80,8 @@ __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const RowsLaunch L) 
             raw[i] = at + N * kWarp * i < L.k ? ld_stream(from + N * kWarp * i) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            float v[N], top = 0.0f;
+            float v[N], top = largest<T>(raw[i]);
             Vec<T>::unpack(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));  // (leaves NaN out)
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             const float scale = top > 0.0f ? fmaxf(__fdiv_rn(top, kE4m3Max), kMinScale) : 1.0f, inv = __frcp_rn(scale);
@@ -77,8 +89,8 @@ __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const RowsLaunch L) 
             uint32_t q[N / 4];
 #pragma unroll
             for (int j = 0; j < N; j += 4) {
-                const float2 a = make_float2(quotient(v[j], scale, inv), quotient(v[j + 1], scale, inv));
-                const float2 b = make_float2(quotient(v[j + 2], scale, inv), quotient(v[j + 3], scale, inv));
+                const float2 a = quotients(v[j], v[j + 1], scale, inv);
+                const float2 b = quotients(v[j + 2], v[j + 3], scale, inv);
                 q[j / 4] = (uint32_t)__nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3) |
                            (uint32_t)__nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3) << 16;
             }
@@ -96,30 +108,30 @@ __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const RowsLaunch L) 
 }
 
 // A thread sums 16 bytes' elements of a token (VEC), its rows' loads on their way together, or one element. 4096 tokens
-// of 2 rows, n = 4096, fp32: 36 us (5.6 TB/s); 4 elements a thread without the streaming loads and stores 48, two or four
-// times 16 bytes a thread 41 and 46 (fewer threads). bf16: 23.6 us, 46 with 8 bytes a thread.
-template <typename T, bool VEC>
+// of 2 rows, n = 4096, fp32: 36 us (5.6 TB/s); without the streaming loads and stores 48, with registers for 8 rows (fewer
+// threads on an SM) 41, with two or four times 16 bytes a thread 41 and 46. bf16: 23.6 us, 46 with 8 bytes a thread.
+template <typename T, bool VEC, int K>  // K: top_k rounded up to 2, 4 or 8
 __global__ void __launch_bounds__(kRowThreads) k_combine(const CombineLaunch L) {
     constexpr int N = VEC ? Vec<T>::N : 1;
     const int t = blockIdx.y, i = (blockIdx.x * kRowThreads + threadIdx.x) * N;
     if (i >= L.n) return;
-    int s[kMaxRouteK];
-    float w[kMaxRouteK], sum[N] = {};
+    int s[K];
+    float w[K], sum[N] = {};
 #pragma unroll
-    for (int j = 0; j < kMaxRouteK; ++j) {
+    for (int j = 0; j < K; ++j) {
         s[j] = j < L.top_k ? __ldg(L.slots + (size_t)t * L.top_k + j) : -1;
         w[j] = j < L.top_k ? __ldg(L.w + (size_t)t * L.top_k + j) : 0.0f;
     }
-    uint4 raw[kMaxRouteK];
+    uint4 raw[K];
 #pragma unroll
-    for (int j = 0; j < kMaxRouteK; ++j) {
+    for (int j = 0; j < K; ++j) {
         if ((unsigned)s[j] >= (unsigned)L.n_rows) continue;
         const T* from = static_cast<const T*>(L.src) + (size_t)s[j] * L.n + i;
         if constexpr (VEC) raw[j] = ld_stream(from);
         else raw[j].x = __float_as_uint(Vec<T>::load1(from, 0));
     }
 #pragma unroll
-    for (int j = 0; j < kMaxRouteK; ++j) {
+    for (int j = 0; j < K; ++j) {
         if ((unsigned)s[j] >= (unsigned)L.n_rows) continue;
         float v[N];
         if constexpr (VEC) Vec<T>::unpack(raw[j], v);
@@ -135,6 +147,17 @@ __global__ void __launch_bounds__(kRowThreads) k_combine(const CombineLaunch L) 
     } else {
         y[0] = sum[0];
     }
+}
+
+template <typename T>
+void combine(const CombineLaunch& a, bool vec, dim3 grid, cudaStream_t stream) {
+    auto run = [&](auto v) {
+        constexpr bool kVec = decltype(v)::value;
+        if (a.top_k <= 2) k_combine<T, kVec, 2><<<grid, kRowThreads, 0, stream>>>(a);
+        else if (a.top_k <= 4) k_combine<T, kVec, 4><<<grid, kRowThreads, 0, stream>>>(a);
+        else k_combine<T, kVec, kMaxRouteK><<<grid, kRowThreads, 0, stream>>>(a);
+    };
+    vec ? run(std::true_type()) : run(std::false_type());
 }
 
 dim3 row_grid(const RowsLaunch& a, int row, int per_cta) {
@@ -166,12 +189,7 @@ cudaError_t launch_combine(const CombineLaunch& a, bool f32, cudaStream_t stream
         b.w += (size_t)t * a.top_k;
         b.y += (size_t)t * a.n;
         const dim3 grid(gx, (unsigned)(a.tokens - t < 65535 ? a.tokens - t : 65535));
-        if (f32)
-            vec ? k_combine<float, true><<<grid, kRowThreads, 0, stream>>>(b)
-                : k_combine<float, false><<<grid, kRowThreads, 0, stream>>>(b);
-        else
-            vec ? k_combine<__nv_bfloat16, true><<<grid, kRowThreads, 0, stream>>>(b)
-                : k_combine<__nv_bfloat16, false><<<grid, kRowThreads, 0, stream>>>(b);
+        f32 ? combine<float>(b, vec, grid, stream) : combine<__nv_bfloat16>(b, vec, grid, stream);
     }
     return cudaGetLastError();
 }

@@ -51,10 +51,13 @@ def _tensor(t, what: str, dtypes, dim: int, rows_apart: bool = False) -> torch.T
     return t
 
 
-def _shaped(t, what: str, dtype, shape) -> torch.Tensor:
-    _tensor(t, what, (dtype,), len(shape))
-    if t.shape != shape:
-        raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
+def _shaped(t, what: str, dtype, shape, dev=None) -> torch.Tensor:
+    """``t``, checked: on device ``dev`` (the current one), contiguous, of this type and shape."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or \
+            t.get_device() != dev:
+        _tensor(t, what, (dtype,), len(shape))
+        if t.shape != shape:
+            raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
     return t
 
 
@@ -90,12 +93,12 @@ def route(logits: torch.Tensor, top_k: int, sel=None, w=None, offsets=None, rows
     """``ts_route``: each token's ``top_k`` experts by fp32 ``logits [tokens][experts]``, and each expert's tokens."""
     _tensor(logits, "logits", (torch.float32,), 2)
     t, e = logits.shape
-    k, i32 = int(top_k), torch.int32
-    sel = _empty(stream, t, k, dtype=i32) if sel is None else _shaped(sel, "sel", i32, (t, k))
-    w = _empty(stream, t, k, dtype=torch.float32) if w is None else _shaped(w, "w", torch.float32, (t, k))
-    offsets = _empty(stream, e + 1, dtype=i32) if offsets is None else _shaped(offsets, "offsets", i32, (e + 1,))
-    rows = _empty(stream, t * k, dtype=i32) if rows is None else _shaped(rows, "rows", i32, (t * k,))
-    slots = _empty(stream, t, k, dtype=i32) if slots is None else _shaped(slots, "slots", i32, (t, k))
+    k, i32, dev = int(top_k), torch.int32, logits.get_device()
+    sel = _empty(stream, t, k, dtype=i32) if sel is None else _shaped(sel, "sel", i32, (t, k), dev)
+    w = _empty(stream, t, k, dtype=torch.float32) if w is None else _shaped(w, "w", torch.float32, (t, k), dev)
+    offsets = _empty(stream, e + 1, dtype=i32) if offsets is None else _shaped(offsets, "offsets", i32, (e + 1,), dev)
+    rows = _empty(stream, t * k, dtype=i32) if rows is None else _shaped(rows, "rows", i32, (t * k,), dev)
+    slots = _empty(stream, t, k, dtype=i32) if slots is None else _shaped(slots, "slots", i32, (t, k), dev)
     _check(lib().ts_route(logits.data_ptr(), t, e, k, sel.data_ptr(), w.data_ptr(), offsets.data_ptr(),
                           rows.data_ptr(), slots.data_ptr(), _handle(stream)), "ts_route")
     return Routing(sel, w, offsets, rows, slots)
@@ -124,7 +127,8 @@ def gather_rows(x: torch.Tensor, rows: torch.Tensor, n=None, out=None, stream=No
     without); the other rows of ``out`` are left as they were."""
     _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
     rp, np_, m = _row_list(x, rows, n, None if out is None else out.shape[0])
-    out = _empty(stream, m, x.shape[1], dtype=x.dtype) if out is None else _shaped(out, "out", x.dtype, (m, x.shape[1]))
+    out = _empty(stream, m, x.shape[1], dtype=x.dtype) if out is None else \
+        _shaped(out, "out", x.dtype, (m, x.shape[1]), x.get_device())
     _check(lib().ts_gather_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], x.shape[1], rp, np_, m,
                                 out.data_ptr(), _handle(stream)), "ts_gather_rows")
     return out
@@ -136,9 +140,10 @@ def quant_rows(x: torch.Tensor, rows=None, n=None, q=None, scale=None, stream=No
     _tensor(x, "x", (torch.bfloat16, torch.float32), 2, rows_apart=True)
     k = x.shape[1]
     rp, np_, m = _row_list(x, rows, n, None if q is None else q.shape[0])
-    kb = -(-k // BLOCK)
-    q = _empty(stream, m, k, dtype=torch.float8_e4m3fn) if q is None else _shaped(q, "q", torch.float8_e4m3fn, (m, k))
-    scale = _empty(stream, kb, m, dtype=torch.float32) if scale is None else _shaped(scale, "scale", torch.float32, (kb, m))
+    kb, dev, f8 = -(-k // BLOCK), x.get_device(), torch.float8_e4m3fn
+    q = _empty(stream, m, k, dtype=f8) if q is None else _shaped(q, "q", f8, (m, k), dev)
+    scale = _empty(stream, kb, m, dtype=torch.float32) if scale is None else \
+        _shaped(scale, "scale", torch.float32, (kb, m), dev)
     _check(lib().ts_quant_rows(x.data_ptr(), _ld(x), _CODES[x.dtype], x.shape[0], k, rp, np_, m, q.data_ptr(),
                                scale.data_ptr(), _handle(stream)), "ts_quant_rows")
     return q, scale
@@ -148,10 +153,10 @@ def combine_rows(src: torch.Tensor, slots: torch.Tensor, w: torch.Tensor, out=No
     """``ts_combine_rows``: fp32 ``out[t] = sum_j w[t][j] src[slots[t][j]]``; a slot outside ``src`` adds nothing."""
     _tensor(src, "src", (torch.bfloat16, torch.float32), 2)
     _tensor(slots, "slots", (torch.int32,), 2)
-    t, k = slots.shape
-    _shaped(w, "w", torch.float32, (t, k))
+    (t, k), dev = slots.shape, src.get_device()
+    _shaped(w, "w", torch.float32, (t, k), dev)
     out = _empty(stream, t, src.shape[1], dtype=torch.float32) if out is None else \
-        _shaped(out, "out", torch.float32, (t, src.shape[1]))
+        _shaped(out, "out", torch.float32, (t, src.shape[1]), dev)
     _check(lib().ts_combine_rows(src.data_ptr(), _CODES[src.dtype], src.shape[0], src.shape[1], slots.data_ptr(),
                                  w.data_ptr(), t, k, out.data_ptr(), _handle(stream)), "ts_combine_rows")
     return out
@@ -168,7 +173,9 @@ def _matrices(t) -> list:
 
 
 def _pointers(ts):
-    return None if ts is None else ctypes.cast((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]), ctypes.c_void_p)
+    if ts is None:
+        return None
+    return ctypes.cast((ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts]), ctypes.c_void_p)
 
 
 class Grouped:
@@ -216,15 +223,15 @@ class Grouped:
         return self._h
 
     def forward(self, x: torch.Tensor, offsets=None, x_scale=None, y=None, stream=None) -> torch.Tensor:
-        """``y`` (bf16 or fp32, bf16 without one) of the groups of rows ``offsets[e] .. offsets[e + 1] - 1`` of ``x``; rows
-        that no group has are left as they were. e4m3 rows come with ``x_scale``, as ``quant_rows`` gives it."""
+        """``y`` (bf16 or fp32, bf16 without one) of the groups of rows ``offsets[e] .. offsets[e + 1] - 1`` of ``x``;
+        rows that no group has are left as they were. e4m3 rows come with ``x_scale``, as ``quant_rows`` gives it."""
         _tensor(x, "x", (self.dtype,), 2, rows_apart=True)
         rows = x.shape[0]
         if x.shape[1] != self.k:
             raise ValueError(f"x must be [rows][{self.k}]")
         op = sp = None
         if offsets is not None:
-            op = _shaped(offsets, "offsets", torch.int32, (self.groups + 1,)).data_ptr()
+            op = _shaped(offsets, "offsets", torch.int32, (self.groups + 1,), x.get_device()).data_ptr()
         ld = 0
         if x_scale is not None:
             _tensor(x_scale, "x_scale", (torch.float32,), 2, rows_apart=True)
@@ -263,9 +270,9 @@ class Grouped:
 
 
 class Experts:
-    """The weights of one layer over many tokens: ``top_k`` of the dReLU FFNs ``w_gate[e], w_up[e] [m][d]`` and ``w_down[e]``
-    (bf16: ``[m][d]``, by neuron, as in ``Ffn``; e4m3: ``[d][m]``, with the three ``scale_*`` lists of ``Grouped``), picked by
-    ``w_router [experts][d]`` (bf16), or a single one without it. Weights are borrowed."""
+    """The weights of one layer over many tokens: ``top_k`` of the dReLU FFNs ``w_gate[e], w_up[e] [m][d]`` and
+    ``w_down[e]`` (bf16: ``[m][d]``, by neuron, as in ``Ffn``; e4m3: ``[d][m]``, with three lists of scales as in
+    ``Grouped``), picked by ``w_router [experts][d]`` (bf16), or a single one without it. Weights are borrowed."""
 
     def __init__(self, w_gate, w_up, w_down, w_router=None, top_k: int = 1, scale_gate=None, scale_up=None,
                  scale_down=None):
@@ -278,7 +285,7 @@ class Experts:
         down = (self.d, self.m) if e8 else (self.m, self.d)
         for w, shape in zip(ws, ((self.m, self.d), (self.m, self.d), down)):
             if len(w) != self.n_experts or any(tuple(t.shape) != shape or t.dtype != self.dtype for t in w):
-                raise ValueError(f"w_gate and w_up must be [{self.m}][{self.d}], w_down {list(down)}, of one type and number")
+                raise ValueError(f"w_gate and w_up must be [{self.m}][{self.d}], w_down {list(down)}, as many of each")
         scales = [None if t is None else _matrices(t) for t in (scale_gate, scale_up, scale_down)]
         for s, w in zip(scales, ws):
             if (s is not None) != e8 or (e8 and len(s) != self.n_experts):
@@ -325,8 +332,8 @@ class Experts:
 
 
 class Prompt:
-    """Forwards of up to ``max_tokens`` tokens through ``experts``, or through any other layer of its sizes: the scratch of
-    all of them (``ts_prompt_*``)."""
+    """Forwards of up to ``max_tokens`` tokens through ``experts``, or through any other layer of its sizes: the scratch
+    of all of them (``ts_prompt_*``)."""
 
     def __init__(self, experts: Experts, max_tokens: int):
         self.experts, self.max_tokens = experts, int(max_tokens)
@@ -350,7 +357,8 @@ class Prompt:
         if x.shape[1] != layer.d:
             raise ValueError(f"x must be [tokens][{layer.d}]")
         t = x.shape[0]
-        y = _empty(stream, t, layer.d, dtype=torch.float32) if y is None else _shaped(y, "y", torch.float32, (t, layer.d))
+        y = _empty(stream, t, layer.d, dtype=torch.float32) if y is None else \
+            _shaped(y, "y", torch.float32, (t, layer.d), x.get_device())
         _check(lib().ts_prompt_forward(self.handle, layer.handle, x.data_ptr(), t, y.data_ptr(), _handle(stream)),
                "ts_prompt_forward")
         self._last = (t, layer.top_k)
