@@ -460,7 +460,7 @@ typedef enum {
  *   scale, scale_up  TS_E4M3: host arrays of device pointers, each [ceil(n / 128)][ceil(k / 128)]
  *              fp32: a scale for each 128 x 128 block of weights. NULL for TS_BF16.
  *   max_rows   largest number of rows of a forward
- * k must be a multiple of 8 (TS_BF16) or 16 (TS_E4M3), n of 8 for TS_KN.
+ * k must be a multiple of 8 (TS_BF16) or 16 (TS_E4M3), at most 2^28, n a multiple of 8 for TS_KN.
  * Products are exact, sums are held in fp32. Returns TS_ERR_INVALID_ARG,
  * TS_ERR_UNSUPPORTED (wdtype or layout without a kernel), TS_ERR_OOM or TS_ERR_CUDA.
  */

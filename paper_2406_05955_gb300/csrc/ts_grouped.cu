@@ -30,7 +30,9 @@ constexpr int kStageMem = 192 * 1024;           // bytes of all stages
 constexpr int kMaxBufs = 4;                     // accumulators in tensor memory
 constexpr int kBand = 8;                        // tiles of x that one sweep over the weights serves
 constexpr int kScaleWarps = 2, kScaleSlots = 4;
-constexpr int kMinSteps = 4;                    // fewest stages of a part of a tile
+// Fewest stages of a part of a tile. A part costs its pair about 3 us (written, made visible, counted and read again): with
+// 16 rows through a 4096 x 4096 bf16 matrix, 4 stages take 18.5 us, 16 16.8, 24 18.1; 300 rows, 1024 x 512, 18.2, 11.1, 16.2.
+constexpr int kMinSteps = 16;
 
 
 __device__ __forceinline__ void sts128(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -41,24 +43,24 @@ __device__ __forceinline__ void sts128(uint32_t to, uint32_t a, uint32_t b, uint
 // The tiles [0, whole * pairs) go round the pairs whole. The steps of the others (as many tiles as one to two rounds)
 // are dealt out evenly, in order, so that all pairs end together: a pair's share begins and ends anywhere in a tile.
 struct Parts {
-    long long total;       // steps of the rest
-    int pairs, steps;      // CTA pairs, stages of a tile
-    int whole;             // rounds of whole tiles
-    int sharers;           // pairs that get some of the rest
+    int pairs, steps;   // CTA pairs, stages of a tile
+    int whole;          // rounds of whole tiles
+    int sharers;        // pairs that get some of the rest
+    int base, more;     // steps of each of them; the first `more` have one more
     __device__ void set(int tiles, int pairs_, int steps_) {
         pairs = pairs_;
         steps = steps_;
         whole = tiles % pairs == 0 ? tiles / pairs : max(0, tiles / pairs - 1);
-        total = (long long)(tiles - whole * pairs) * steps;
-        sharers = (int)max(1ll, min((long long)pairs, total / kMinSteps));
+        const int total = (tiles - whole * pairs) * steps;  // fewer than two rounds of at most 2^22 steps: below 2^31
+        sharers = max(1, min(pairs, total / kMinSteps));
+        base = total / sharers;
+        more = total % sharers;
     }
-    __device__ long long begin(int q) const { return total * q / sharers; }
+    __device__ int begin(int q) const { return q * base + min(q, more); }
     // the pair that has step s
-    __device__ int owner(long long s) const {
-        int q = (int)(s * sharers / total);
-        while (begin(q) > s) --q;
-        while (begin(q + 1) <= s) ++q;
-        return q;
+    __device__ int owner(int s) const {
+        const int first = more * (base + 1);  // steps of the pairs that have one more
+        return s < first ? s / (base + 1) : more + (s - first) / base;
     }
 };
 
@@ -247,8 +249,7 @@ __device__ __forceinline__ int tile_rows(int n, int tiles) { return ((n + tiles 
 
 // A pair's way through its tiles and parts of tiles.
 struct Walk {
-    int round = 0;
-    long long at = -1;
+    int round = 0, at = -1;
     template <bool XM>
     __device__ bool next(const Shared& sh, int n_groups, int w_tiles, Seg& s) {
         const Parts& P = sh.parts;
@@ -262,12 +263,12 @@ struct Walk {
         } else {
             if (pair >= P.sharers) return false;
             if (at < 0) at = P.begin(pair);
-            const long long end = P.begin(pair + 1);
+            const int end = P.begin(pair + 1);
             if (at >= end) return false;
-            s.rest = (int)(at / P.steps);
+            s.rest = at / P.steps;
             s.tile = P.whole * P.pairs + s.rest;
-            s.k0 = (int)(at - (long long)s.rest * P.steps);
-            s.k1 = (int)min((long long)P.steps, s.k0 + (end - at));
+            s.k0 = at - s.rest * P.steps;
+            s.k1 = min(P.steps, s.k0 + (end - at));
             at += s.k1 - s.k0;
         }
         int lo = 0, hi = n_groups;  // the last group whose first tile is not behind
@@ -568,7 +569,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         bool ok = true;
         // gated: a gate warp and the up warp of the same neurons wait for each other
         const int both = half * 2 + (q & 1);
-        const uint32_t t_empty = in_cta(&sh.tempty[0], 0);
         unsigned met = 0;
         auto meet = [&]() {
             __syncwarp();
@@ -594,8 +594,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             auto release = [&](int buf) {
                 tc_before();
                 __syncwarp();
-                if (lane == 0) {
-                    arrive_at(t_empty + buf * 8);
+                if (elect_one()) {
+                    arrive_at(in_cta(&sh.tempty[buf], 0));
                     if (E8) mbar_arrive(&sh.sempty[buf]);
                 }
             };
@@ -696,7 +696,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 // A part of a tile: left in global memory; the warp that comes last adds the parts in the order of k.
                 const Parts& P = sh.parts;
                 const int pair = blockIdx.x >> 1;
-                const long long s0 = (long long)sg.rest * steps;
+                const int s0 = sg.rest * steps;
                 const int p0 = P.owner(s0), p1 = P.owner(s0 + steps - 1);
                 auto part_of = [&](int p) {  // a pair's first tile is in its slot 0, its last one in slot 1
                     const int slot = P.begin(p) >= s0 ? 0 : 1;
@@ -728,40 +728,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 if ((int)before != p1 - p0) continue;
                 __threadfence();
                 if (lane == 0 && (!GATED || XM || q < 2)) *count = 0u;
-                // few columns: the parts of several pairs at a time, as each access takes as long as all of them
-                auto join_few = [&](auto groups, auto at_once) {  // of 8 columns; parts
-                    constexpr int kG = decltype(groups)::value, kAtOnce = decltype(at_once)::value;
-                    for (int p = p0; p <= p1; p += kAtOnce) {
-                        f32x2 v[kAtOnce][4 * kG];
 #pragma unroll
-                        for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-                            for (int i = 0; i < 4 * kG; ++i)
-                                v[u][i] = p + u <= p1 ? __ldcg(part_of(p + u) + (16 * (i / (2 * kG)) + i % (2 * kG)) * kWarp) : 0ull;
-#pragma unroll
-                        for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-                            for (int i = 0; i < 4 * kG; ++i) {
-                                f32x2& a = acc[i / (2 * kG)][0][i % (2 * kG)];
-                                if (p + u <= p1) a = p + u == p0 ? v[u][i] : add2(a, v[u][i]);
-                            }
-                    }
-                };
-                if (!XM && cols == 8) {
-                    join_few(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-                } else if (!XM && cols == 16) {
-                    join_few(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
-                } else {
+                for (int i = 0; i < 64; ++i) acc[i >> 5][(i >> 4) & 1][i & 15] = 0ull;
+                auto join_few = [&](auto groups) {  // of 8 columns
+                    constexpr int kG = decltype(groups)::value;
                     for (int p = p0; p <= p1; ++p) {
                         const f32x2* from = part_of(p);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c)
-                            if (c == 0 || w1 > 0)
+                        for (int i = 0; i < 4 * kG; ++i) {
+                            f32x2& a = acc[i / (2 * kG)][0][i % (2 * kG)];
+                            a = add2(a, __ldcg(from + (16 * (i / (2 * kG)) + i % (2 * kG)) * kWarp));
+                        }
+                    }
+                };
+                if (!XM && cols == 8) {
+                    join_few(std::integral_constant<int, 1>());
+                } else if (!XM && cols == 16) {
+                    join_few(std::integral_constant<int, 2>());
+                } else {
+#pragma unroll 1
+                    for (int p = p0; p <= p1; ++p) {
+                        const f32x2* from = part_of(p);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const f32x2 v = __ldcg(from + (c * 32 + i) * kWarp);
-                                acc[i >> 4][c][i & 15] = p == p0 ? v : add2(acc[i >> 4][c][i & 15], v);
+                        for (int c = 0; c < 2; ++c) {
+                            if (c == 1 && w1 == 0) break;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                f32x2 v[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v[i] = __ldcg(from + (c * 32 + h * 16 + i) * kWarp);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) acc[h][c][i] = add2(acc[h][c][i], v[i]);
+                                asm volatile("" ::: "memory");  // no more loads at once than there are registers for
                             }
+                        }
                     }
                 }
             }

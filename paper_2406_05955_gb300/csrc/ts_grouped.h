@@ -10,6 +10,7 @@ namespace tsffn {
 constexpr int kMaxRouteExperts = 256;
 constexpr int kMaxRouteK = 8;
 constexpr int kMaxGroups = 256;
+constexpr int kMaxGroupedK = 1 << 28;  // 32-bit counts of the kernel's steps hold up to it
 constexpr int kScaleBlock = 128;  // elements of one scale, along k and along n
 
 struct RouteLaunch {

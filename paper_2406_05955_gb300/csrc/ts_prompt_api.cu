@@ -143,6 +143,7 @@ ts_status check_experts(int d, int m, int n_experts, int top_k, ts_dtype wdtype)
         return TS_ERR_INVALID_ARG;
     if (wdtype == TS_F32 || wdtype == TS_INT4) return TS_ERR_UNSUPPORTED;
     if (wdtype != TS_BF16 && wdtype != TS_E4M3) return TS_ERR_INVALID_ARG;
+    if (d > kMaxGroupedK || m > kMaxGroupedK) return TS_ERR_UNSUPPORTED;
     const int step = wdtype == TS_E4M3 ? 16 : 8;
     return d % step == 0 && m % step == 0 ? TS_OK : TS_ERR_INVALID_ARG;
 }
@@ -232,6 +233,7 @@ ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dty
     if (wdtype == TS_F32 || wdtype == TS_INT4) return TS_ERR_UNSUPPORTED;
     if (wdtype != TS_BF16 && wdtype != TS_E4M3) return TS_ERR_INVALID_ARG;
     const bool e8 = wdtype == TS_E4M3, gated = w_up != nullptr;
+    if (k > kMaxGroupedK) return TS_ERR_UNSUPPORTED;
     if (k % (e8 ? 16 : 8) != 0 || (layout == TS_KN && n % 8 != 0)) return TS_ERR_INVALID_ARG;
     if (layout == TS_KN && (e8 || gated)) return TS_ERR_UNSUPPORTED;
     if (!weights_ok(n_groups, e8, w, scale) || (gated && !weights_ok(n_groups, e8, w_up, scale_up)) || (!gated && scale_up))
