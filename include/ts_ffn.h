@@ -410,7 +410,7 @@ ts_status ts_route(const float* logits, int tokens, int n_experts, int top_k, in
  *             0..n_src-1 leaves its row of `out` as it was.
  *   n         device int32 (as &offsets[n_experts] of ts_route), NULL: max_rows
  *   out       device [max_rows][k], same type
- * Rows of x and out start on 16-byte boundaries.
+ * Rows of x and out start on 16-byte boundaries. TS_ERR_UNSUPPORTED: k above 2^24 or max_rows above 2^30.
  */
 ts_status ts_gather_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, const int32_t* rows,
                          const int32_t* n, int max_rows, void* out, cudaStream_t stream);
@@ -432,7 +432,7 @@ ts_status ts_quant_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, i
  * y[t][:] = sum over j < top_k of w[t][j] * src[slots[t][j]][:], in order of j, in fp32.
  *   src       device [n_rows][n] TS_F32 or TS_BF16
  *   slots, w  device [tokens][top_k]; a slot outside 0..n_rows-1 adds nothing
- *   top_k     1..8; n >= 1
+ *   top_k     1..8; n 1..2^30, at most 2^30 tokens
  *   y         device [tokens][n] fp32, overwritten
  */
 ts_status ts_combine_rows(const void* src, ts_dtype dtype, int n_rows, int n, const int32_t* slots, const float* w,
@@ -451,7 +451,7 @@ typedef enum {
  *     y[r] = max(0, x[r] . W_e) * max(0, x[r] . U_e)         (gated: Eq. 1 with the dReLU of Eq. 2)
  * for offsets[e] <= r < offsets[e + 1]. One group is an ordinary matrix product.
  *   n_groups   1..256
- *   n, k       outputs and inputs of a weight matrix
+ *   n, k       outputs (at most 2^30) and inputs of a weight matrix
  *   wdtype     TS_BF16 (x bf16) or TS_E4M3 (x e4m3)
  *   layout     TS_NK, or TS_KN for plain TS_BF16 products
  *   w          host array of n_groups device pointers (borrowed, 16-byte aligned), each
@@ -459,7 +459,7 @@ typedef enum {
  *   w_up       NULL, or the same for U (gated)
  *   scale, scale_up  TS_E4M3: host arrays of device pointers, each [ceil(n / 128)][ceil(k / 128)]
  *              fp32: a scale for each 128 x 128 block of weights. NULL for TS_BF16.
- *   max_rows   largest number of rows of a forward
+ *   max_rows   largest number of rows of a forward, at most 2^30
  * k must be a multiple of 8 (TS_BF16) or 16 (TS_E4M3), at most 2^28, n a multiple of 8 for TS_KN.
  * Products are exact, sums are held in fp32. Returns TS_ERR_INVALID_ARG,
  * TS_ERR_UNSUPPORTED (wdtype or layout without a kernel), TS_ERR_OOM or TS_ERR_CUDA.
@@ -479,7 +479,7 @@ void ts_grouped_destroy(ts_grouped* h);
  *              skipped and recorded (ts_grouped_get_error: TS_ERR_BAD_INDEX).
  *   y, ldy     device, rows of n elements ldy apart (ydtype TS_BF16, rounded once, or TS_F32); rows
  *              that no group has are left as they were
- * One forward may be in flight per handle.
+ * One forward may be in flight per handle, and its device is the current one (else TS_ERR_INVALID_ARG).
  */
 ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const float* x_scale, int64_t ld_scale,
                              const int32_t* offsets, int rows, void* y, int64_t ldy, ts_dtype ydtype,
@@ -493,7 +493,7 @@ typedef struct ts_prompt ts_prompt;   /* scratch of layers over many tokens     
 
 /*
  * One layer over many tokens: top_k of n_experts dReLU FFNs (Sec. 4), or a single one.
- *   d, m       model width and neurons of an expert; multiples of 8 (TS_BF16) or 16 (TS_E4M3)
+ *   d, m       model width and neurons of an expert; multiples of 8 (TS_BF16) or 16 (TS_E4M3), at most 2^24
  *   n_experts  1..256, top_k 1..min(8, n_experts)
  *   wdtype     TS_BF16 or TS_E4M3; activations x are bf16 either way
  *   w_router   device [n_experts][d] bf16; NULL with one expert, which then has weight 1
@@ -510,7 +510,8 @@ ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int t
 void ts_experts_destroy(ts_experts* e);
 
 /* Scratch for forwards of up to max_tokens tokens through any layers of these sizes (arguments as
-   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle. */
+   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle; scratch, layer and the
+   current device are one device (else TS_ERR_INVALID_ARG). */
 ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top_k, ts_dtype wdtype, int max_tokens);
 void ts_prompt_destroy(ts_prompt* p);
 

@@ -10,7 +10,10 @@ namespace tsffn {
 constexpr int kMaxRouteExperts = 256;
 constexpr int kMaxRouteK = 8;
 constexpr int kMaxGroups = 256;
-constexpr int kMaxGroupedK = 1 << 28;  // 32-bit counts of the kernel's steps hold up to it
+// Up to these sizes the kernels' 32-bit counts and the grids' second dimension hold.
+constexpr int kMaxGroupedK = 1 << 28;
+constexpr int kMaxRowElems = 1 << 24;  // of a row that is copied or rounded
+constexpr int kMaxRows = 1 << 30;      // rows, and outputs of a product
 constexpr int kScaleBlock = 128;  // elements of one scale, along k and along n
 
 struct RouteLaunch {

@@ -23,6 +23,7 @@ int elem_size(ts_dtype dt) { return dt == TS_F32 ? 4 : dt == TS_BF16 ? 2 : 1; }
 ts_status check_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, int max_rows, const void* out) {
     if (dtype != TS_F32 && dtype != TS_BF16) return TS_ERR_INVALID_ARG;
     if (n_src < 0 || k < 1 || max_rows < 0 || ldx < k) return TS_ERR_INVALID_ARG;
+    if (k > kMaxRowElems || max_rows > kMaxRows) return TS_ERR_UNSUPPORTED;
     if (max_rows == 0) return TS_OK;
     if (!out || (!x && n_src > 0)) return TS_ERR_INVALID_ARG;
     const int64_t size = elem_size(dtype);
@@ -45,9 +46,11 @@ struct ProductScratch {
     float* partial = nullptr;
     unsigned* arrived = nullptr;
     unsigned* status = nullptr;
+    int device = -1;
 
     // False where the kernels cannot be resident.
     bool plan(Arena* ar, int max_rows) {
+        if (cudaGetDevice(&device) != cudaSuccess) return false;
         pairs = grouped_pairs();
         part_chunks = grouped_part_chunks(max_rows);
         if (pairs < 1) return false;
@@ -62,6 +65,12 @@ struct ProductScratch {
         partial = ar.at<float>(o_partial);
     }
 };
+
+// Whether a handle's device is the current one.
+bool here(int device) {
+    int now = -1;
+    return cudaGetDevice(&now) == cudaSuccess && now == device;
+}
 
 // Whether the weights and scales that a product of n_groups groups needs are there, aligned.
 bool weights_ok(int n_groups, bool e8, const void* const* w, const float* const* scale) {
@@ -128,10 +137,14 @@ ts_status run_products(const Products& P, const ProductScratch& S, const void* x
     return launched(launch_grouped(a, e8, P.gated, P.kn, stream));
 }
 
-ts_status read_status(unsigned* status, cudaStream_t stream) {
+ts_status read_status(const ProductScratch& S, cudaStream_t stream) {
     unsigned bits = 0;
-    if (cudaMemcpyAsync(&bits, status, sizeof bits, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
-        cudaMemsetAsync(status, 0, sizeof bits, stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
+    if (cudaMemcpyAsync(&bits, S.status, sizeof bits, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
+        cudaMemsetAsync(S.status, 0, sizeof bits, stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
+        return TS_ERR_CUDA;
+    // a launch that gave up may have left tiles half counted
+    if ((bits & kStatusTimeout) &&
+        cudaMemsetAsync(S.arrived, 0, grouped_arrived(S.pairs) * sizeof(unsigned), stream) != cudaSuccess)
         return TS_ERR_CUDA;
     return bits & kStatusTimeout ? TS_ERR_TIMEOUT : bits & kStatusBadIndex ? TS_ERR_BAD_INDEX : TS_OK;
 }
@@ -143,7 +156,7 @@ ts_status check_experts(int d, int m, int n_experts, int top_k, ts_dtype wdtype)
         return TS_ERR_INVALID_ARG;
     if (wdtype == TS_F32 || wdtype == TS_INT4) return TS_ERR_UNSUPPORTED;
     if (wdtype != TS_BF16 && wdtype != TS_E4M3) return TS_ERR_INVALID_ARG;
-    if (d > kMaxGroupedK || m > kMaxGroupedK) return TS_ERR_UNSUPPORTED;
+    if (d > kMaxRowElems || m > kMaxRowElems) return TS_ERR_UNSUPPORTED;
     const int step = wdtype == TS_E4M3 ? 16 : 8;
     return d % step == 0 && m % step == 0 ? TS_OK : TS_ERR_INVALID_ARG;
 }
@@ -161,6 +174,7 @@ struct ts_experts {
     int d = 0, m = 0, n_experts = 0, top_k = 0;
     ts_dtype dt = TS_BF16;
     bool routed = false;
+    int device = -1;
     Products router, gate_up, down;
     Arena arena;
 };
@@ -217,6 +231,7 @@ ts_status ts_combine_rows(const void* src, ts_dtype dtype, int n_rows, int n, co
                           int tokens, int top_k, float* y, cudaStream_t stream) {
     if ((dtype != TS_F32 && dtype != TS_BF16) || n_rows < 0 || n < 1 || tokens < 0 || top_k < 1 || top_k > kMaxRouteK)
         return TS_ERR_INVALID_ARG;
+    if (n > kMaxRows || tokens > kMaxRows) return TS_ERR_UNSUPPORTED;
     if (tokens == 0) return TS_OK;
     if ((!src && n_rows > 0) || !slots || !w || !y) return TS_ERR_INVALID_ARG;
     return launched(launch_combine({src, n_rows, n, slots, w, tokens, top_k, y}, dtype == TS_F32, stream));
@@ -233,7 +248,7 @@ ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dty
     if (wdtype == TS_F32 || wdtype == TS_INT4) return TS_ERR_UNSUPPORTED;
     if (wdtype != TS_BF16 && wdtype != TS_E4M3) return TS_ERR_INVALID_ARG;
     const bool e8 = wdtype == TS_E4M3, gated = w_up != nullptr;
-    if (k > kMaxGroupedK) return TS_ERR_UNSUPPORTED;
+    if (k > kMaxGroupedK || n > kMaxRows || max_rows > kMaxRows) return TS_ERR_UNSUPPORTED;
     if (k % (e8 ? 16 : 8) != 0 || (layout == TS_KN && n % 8 != 0)) return TS_ERR_INVALID_ARG;
     if (layout == TS_KN && (e8 || gated)) return TS_ERR_UNSUPPORTED;
     if (!weights_ok(n_groups, e8, w, scale) || (gated && !weights_ok(n_groups, e8, w_up, scale_up)) || (!gated && scale_up))
@@ -283,14 +298,14 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     if (!h || rows < 0 || rows > h->max_rows || (ydtype != TS_F32 && ydtype != TS_BF16)) return TS_ERR_INVALID_ARG;
     if (!offsets && h->p.n_groups != 1) return TS_ERR_INVALID_ARG;
     if (rows == 0) return TS_OK;
-    if (!x || !y || !aligned16(x) || ldx < h->p.k || ldx * elem_size(h->p.dt) % 16 != 0 || ldy < h->p.n)
+    if (!here(h->s.device) || !x || !y || !aligned16(x) || ldx < h->p.k || ldx * elem_size(h->p.dt) % 16 != 0 || ldy < h->p.n)
         return TS_ERR_INVALID_ARG;
     if (h->p.dt == TS_E4M3 ? (!x_scale || ld_scale < rows) : x_scale != nullptr) return TS_ERR_INVALID_ARG;
     return run_products(h->p, h->s, x, ldx, x_scale, ld_scale, offsets, rows, y, ldy, ydtype == TS_F32, stream);
 }
 
 ts_status ts_grouped_get_error(ts_grouped* h, cudaStream_t stream) {
-    return h ? read_status(h->s.status, stream) : TS_ERR_INVALID_ARG;
+    return h ? read_status(h->s, stream) : TS_ERR_INVALID_ARG;
 }
 
 ts_status ts_grouped_check_scratch(ts_grouped* h, cudaStream_t stream) {
@@ -322,6 +337,7 @@ ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int t
         h->top_k = top_k;
         h->dt = wdtype;
         h->routed = w_router != nullptr;
+        cudaGetDevice(&h->device);
         auto set = [](Products& p, int groups, int n, int k, ts_dtype dt, bool gated, bool kn) {
             p.n_groups = groups;
             p.n = n;
@@ -429,7 +445,7 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
         tokens < 0 || tokens > p->max_tokens)
         return TS_ERR_INVALID_ARG;
     if (tokens == 0) return TS_OK;
-    if (!x || !y || !aligned16(x)) return TS_ERR_INVALID_ARG;
+    if (!here(p->s.device) || e->device != p->s.device || !x || !y || !aligned16(x)) return TS_ERR_INVALID_ARG;
     const int d = p->d, m = p->m, rows = e->routed ? tokens * e->top_k : tokens;
     const bool e8 = p->dt == TS_E4M3;
     const int32_t *offsets = nullptr, *count = nullptr, *list = nullptr;
@@ -483,7 +499,7 @@ ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel,
 }
 
 ts_status ts_prompt_get_error(ts_prompt* p, cudaStream_t stream) {
-    return p ? read_status(p->s.status, stream) : TS_ERR_INVALID_ARG;
+    return p ? read_status(p->s, stream) : TS_ERR_INVALID_ARG;
 }
 
 ts_status ts_prompt_check_scratch(ts_prompt* p, cudaStream_t stream) {

@@ -271,6 +271,38 @@ def test_repeated_calls_give_the_same_bits(ts, form):
     check(y, y.clone(), [0, 100, 120, 150], xd, wd, gated, layout, k)
 
 
+WIDE = [f for f in FORMS if f[0] == E4M3]
+
+
+@pytest.mark.parametrize("form", WIDE, ids=["plain", "gated"])
+@pytest.mark.parametrize("out", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,k,pad", [(1, 16, 0), (3, 128, 0), (127, 272, 1), (257, 144, 0), (264, 1040, 4), (1000, 64, 8),
+                                     (520, 2064, 0)])
+def test_many_e4m3_rows(ts, form, out, n, k, pad):
+    """Enough rows a group for the rows to be the MMA's M; short ones, tiles' edges, an empty group, rows behind."""
+    run(ts, E4M3, [300, 0, 1, 257, 511], n, k, form[1], "nk", out, 7, seed=n + k, pad_x=16 * (pad > 0), pad_y=pad)
+
+
+@pytest.mark.parametrize("form", WIDE, ids=["plain", "gated"])
+def test_many_e4m3_rows_with_bad_ones(ts, form):
+    """Non-finite rows of the same tile, of the next group and of no group, and bad offsets."""
+    n, k, off = 200, 256, [0, 300, 290, 560, 700]
+    x, xs, w, ss, xd, wd = make(E4M3, 4, n, k, 720, form[1], "nk", seed=14)
+    bad = [5, 130, 299, 300, 559, 560, 700, 719]
+    x.view(torch.uint8)[bad, 7] = 0x7F
+    mm = handle(ts, w, ss, form[1], "nk", 720)
+    y = torch.full((720, n), 7.0, device="cuda")
+    mm.forward(x, torch.tensor(off, dtype=torch.int32, device="cuda"), xs, y)
+    assert mm.get_error() == 4 and mm.check_scratch() == 0
+    assert (y[700:] == 7.0).all()
+    xd[bad] = 0.0
+    got = y.clone()
+    got[bad] = 0.0
+    for e in (0, 2, 3):  # (rows 290 to 299 belong to two groups: either may have them)
+        a, b = (off[e], 290) if e == 0 else (max(off[e], 300), off[e + 1])
+        check(got[a:b], got[a:b], [0, b - a], xd[a:b], [[ws[e]] for ws in wd], form[1], "nk", k)
+
+
 def test_refusals(ts):
     dev = "cuda"
     w = [torch.zeros(64, 64, dtype=BF16, device=dev) for _ in range(2)]

@@ -136,3 +136,24 @@ def test_experts_and_prompt_arguments(lib):
     assert lib.ts_prompt_check_scratch(None, None) == BAD
     lib.ts_experts_destroy(None)
     lib.ts_prompt_destroy(None)
+
+
+def test_sizes_beyond_the_kernels_counts(lib):
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_KN, TS_NK
+
+    g, h, two = GOOD, ctypes.c_void_p(), _array(GOOD, GOOD)
+    for k, m in ((2 ** 24 + 16, 4), (64, 2 ** 30 + 1)):
+        assert lib.ts_gather_rows(g, k, TS_BF16, 4, k, None, None, m, g, None) == UNSUPPORTED
+        assert lib.ts_quant_rows(g, k, TS_F32, 4, k, None, None, m, g, g, None) == UNSUPPORTED
+    for n, t in ((2 ** 30 + 1, 2), (8, 2 ** 30 + 1)):
+        assert lib.ts_combine_rows(g, TS_F32, 4, n, g, g, t, 2, g, None) == UNSUPPORTED
+    for n, k, rows in ((64, 2 ** 28 + 16, 8), (2 ** 30 + 8, 64, 8), (64, 64, 2 ** 30 + 1)):
+        for layout in (TS_NK, TS_KN):
+            assert lib.ts_grouped_create(ctypes.byref(h), 2, n, k, TS_BF16, layout, two, None, None, None,
+                                         rows) == UNSUPPORTED
+        assert lib.ts_grouped_create(ctypes.byref(h), 2, n, k, TS_E4M3, TS_NK, two, two, two, two, rows) == UNSUPPORTED
+    for d, m in ((2 ** 24 + 16, 64), (64, 2 ** 24 + 16)):
+        assert lib.ts_experts_create(ctypes.byref(h), d, m, 2, 1, TS_BF16, g, two, two, two, None, None,
+                                     None) == UNSUPPORTED
+        assert lib.ts_prompt_create(ctypes.byref(h), d, m, 2, 1, TS_BF16, 8) == UNSUPPORTED
+    assert h.value is None
