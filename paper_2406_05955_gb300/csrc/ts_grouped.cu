@@ -5,6 +5,7 @@
 // A tile is D[i][t] = W[i] . x_t for 256 weight rows i (gated: 128 neurons, gate and up rows) and up to 256 rows t of
 // one group. The weights are the MMA's M and the rows of x its N, which may be any multiple of 16: a group's rows are
 // cut into equal tiles, so ragged groups waste at most 15 rows a tile, and one kernel serves one row and thousands.
+// (e4m3 products of many rows are taken the other way round: XM below.)
 //
 // A tile belongs to a pair of CTAs (tcgen05 cta_group::2): each loads its 128 weight rows and half of the rows of x, and
 // the MMA reads both halves of x, so that a pair moves 64 KB for 2 x 256 x 256 x 64 flop and not 96 (one CTA
@@ -14,6 +15,13 @@
 // sums out of tensor memory, where two accumulators take turns. They keep running sums in fp32 registers and add an
 // accumulator to them every kChunk stages: the tensor cores truncate when they accumulate, which 64 steps do not show,
 // and each 128 of k of e4m3 products has scales of its own, which enter there.
+//
+// What bounds it, and what it measured (d = 4096, m = 14336): few rows, reading the weights (gated bf16, 16 rows over
+// 8 groups: 281 us, 6.7 TB/s); many rows of bf16, the tensor cores under the power cap (8192 rows: plain 495 us, gated
+// 1020-1090 us, 1.75-1.9 PFLOP/s; a library's plain product takes 471-484); many rows of e4m3, reading tensor memory at
+// every 128 of k (8192 rows: plain 330-350 us, gated over 8 groups 688 us, 2.8 PFLOP/s; 2000 rows over 8 groups 208 us, of
+// which reading the weights is 139); one row, latency (1 x 4096 x 14336 e4m3: 23 us, of which reading the weights is 9:
+// launch, set-up, the first load, the join of a tile's parts and the stores come one after another).
 #include <cuda_fp8.h>
 
 #include "ts_grouped.h"
@@ -33,7 +41,6 @@ constexpr int kScaleWarps = 2, kScaleSlots = 4;
 // Fewest stages of a part of a tile. A part costs its pair about 3 us (written, made visible, counted and read again): with
 // 16 rows through a 4096 x 4096 bf16 matrix, 4 stages take 18.5 us, 16 16.8, 24 18.1; 300 rows, 1024 x 512, 18.2, 11.1, 16.2.
 constexpr int kMinSteps = 16;
-
 
 __device__ __forceinline__ void sts128(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -297,8 +304,8 @@ struct Walk {
 
 // XM (e4m3): the rows of x are the MMA's M, always 256 of them, and the weights its N. What a lane of tensor memory holds
 // then belongs to one row of x, with one scale, and 32 lanes can be read at a time: a load of 16 lanes (of columns that
-// have scales of their own) takes as long, and for wide tiles the reading is what bounds e4m3 products: 8192 rows through
-// a 14336 x 4096 matrix 424 -> 346 us. Narrow tiles would be mostly zeros.
+// have scales of their own) takes as long, and for wide tiles the reading is what bounds e4m3 products: 8192 rows,
+// 4096 x 14336, 424 -> 346 us. Narrow tiles would be mostly zeros.
 template <bool E8, bool GATED, bool KN, bool XM>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
@@ -838,95 +845,95 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 __syncwarp();
                 continue;
             } else {
-            // outputs: [16 lanes h][8 lanes r] of each 8 columns
-            const int mlane = lane >> 2;
-            int n0 = sg.wt * 256 + (int)rank * 128 + q * 32, cb = c0;  // the warp's first output and first column
-            unsigned char* turn = sh.turn[ew];
-            if constexpr (GATED) {
-                // Warp q < 2 holds the gate values and warp q + 2 the up values of the same neurons: the first finishes
-                // the first chunk of columns, the second the other, each with what the other sends it, 16 columns at a time.
-                n0 = sg.wt * 128 + (int)rank * 64 + (q & 1) * 32;
-                cb = q < 2 ? c0 : c0 + w0;
-                f32x2* mine = reinterpret_cast<f32x2*>(turn) + lane;
-                const f32x2* theirs = reinterpret_cast<const f32x2*>(sh.turn[ew ^ 2]) + lane;
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    if (16 * p >= w0) break;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) mine[i * kWarp] = q < 2 ? acc[i >> 2][1][4 * p + (i & 3)] : acc[i >> 2][0][4 * p + (i & 3)];
-                    ok = ok && meet();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const f32x2 a = q < 2 ? acc[i >> 2][0][4 * p + (i & 3)] : acc[i >> 2][1][4 * p + (i & 3)], b = theirs[i * kWarp];
-                        acc[i >> 2][0][4 * p + (i & 3)] =
-                            pack2(__float_as_uint(lo2(a) > 0.0f && lo2(b) > 0.0f ? lo2(a) * lo2(b) : 0.0f),
-                                  __float_as_uint(hi2(a) > 0.0f && hi2(b) > 0.0f ? hi2(a) * hi2(b) : 0.0f));
+                // outputs: [16 lanes h][8 lanes r] of each 8 columns
+                const int mlane = lane >> 2;
+                int n0 = sg.wt * 256 + (int)rank * 128 + q * 32, cb = c0;  // the warp's first output and first column
+                unsigned char* turn = sh.turn[ew];
+                if constexpr (GATED) {
+                    // Warp q < 2 holds the gate values and warp q + 2 the up values of the same neurons: the first finishes
+                    // the first chunk of columns, the second the other, each with what the other sends it, 16 columns at a time.
+                    n0 = sg.wt * 128 + (int)rank * 64 + (q & 1) * 32;
+                    cb = q < 2 ? c0 : c0 + w0;
+                    f32x2* mine = reinterpret_cast<f32x2*>(turn) + lane;
+                    const f32x2* theirs = reinterpret_cast<const f32x2*>(sh.turn[ew ^ 2]) + lane;
+    #pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        if (16 * p >= w0) break;
+    #pragma unroll
+                        for (int i = 0; i < 8; ++i) mine[i * kWarp] = q < 2 ? acc[i >> 2][1][4 * p + (i & 3)] : acc[i >> 2][0][4 * p + (i & 3)];
+                        ok = ok && meet();
+    #pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const f32x2 a = q < 2 ? acc[i >> 2][0][4 * p + (i & 3)] : acc[i >> 2][1][4 * p + (i & 3)], b = theirs[i * kWarp];
+                            acc[i >> 2][0][4 * p + (i & 3)] =
+                                pack2(__float_as_uint(lo2(a) > 0.0f && lo2(b) > 0.0f ? lo2(a) * lo2(b) : 0.0f),
+                                      __float_as_uint(hi2(a) > 0.0f && hi2(b) > 0.0f ? hi2(a) * hi2(b) : 0.0f));
+                        }
+                        ok = ok && meet();  // both have read before either writes there again
                     }
-                    ok = ok && meet();  // both have read before either writes there again
+                    if (!ok) break;
                 }
-                if (!ok) break;
-            }
-            constexpr int kC = GATED ? 1 : 2;
-            const int width[2] = {GATED && q >= 2 ? w1 : w0, GATED ? 0 : w1};  // columns of chunk 0 and 1 that the warp finishes
-            if (L.y_f32) {
-                float* y = static_cast<float*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (8 * (i >> 1) >= width[c]) continue;
-                        const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
-                        float* at = y + (size_t)col * L.ldy + 8 * (i & 1);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
-                            if (in && col < sg.rows) at[16 * h] = lo2(acc[h][c][i]);
-                            if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = hi2(acc[h][c][i]);
+                constexpr int kC = GATED ? 1 : 2;
+                const int width[2] = {GATED && q >= 2 ? w1 : w0, GATED ? 0 : w1};  // columns of chunk 0 and 1 that the warp finishes
+                if (L.y_f32) {
+                    float* y = static_cast<float*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
+    #pragma unroll
+                    for (int c = 0; c < kC; ++c)
+    #pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (8 * (i >> 1) >= width[c]) continue;
+                            const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                            float* at = y + (size_t)col * L.ldy + 8 * (i & 1);
+    #pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
+                                if (in && col < sg.rows) at[16 * h] = lo2(acc[h][c][i]);
+                                if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = hi2(acc[h][c][i]);
+                            }
                         }
-                    }
-            } else if (L.y_vec && n0 + 32 <= L.n) {
-                // bf16: 16 rows of y at a time are turned round in shared memory, so that a store writes whole sectors, 64
-                // bytes of a row. (Two bytes of 16 rows each, straight from the registers, held the tiles up: 8192 rows
-                // through an 8192 x 4096 matrix took 323 us against 289.)
-                constexpr int kPitch = 80;
-                const uint32_t to = smem_u32(turn) + (lane & 7) * kPitch + (lane >> 3) * 16;
-                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + cb) * L.ldy + n0;
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {  // 16 columns: lanes 0-7 and 8-15 of the first 8, of the next 8
-                        if (16 * p >= width[c]) continue;
-                        const f32x2* v0 = &acc[0][c][4 * p];
-                        const f32x2* v1 = &acc[1][c][4 * p];
-                        __syncwarp();
-                        stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v1[0]), bf16x2(v1[1]));
-                        stmatrix(to + 8 * kPitch, bf16x2(v0[2]), bf16x2(v0[3]), bf16x2(v1[2]), bf16x2(v1[3]));
-                        __syncwarp();
-#pragma unroll
-                        for (int r0 = 0; r0 < 16; r0 += 8) {
-                            const int r = r0 + (lane >> 2), col = c * w0 + 16 * p + r;
-                            const uint4 v = lds128(turn + r * kPitch + (lane & 3) * 16);
-                            if (16 * p + r < width[c] && cb + col < sg.rows)
-                                *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane & 3) * 8) = v;
+                } else if (L.y_vec && n0 + 32 <= L.n) {
+                    // bf16: 16 rows of y at a time are turned round in shared memory, so that a store writes whole sectors, 64
+                    // bytes of a row. (Two bytes of 16 rows each, straight from the registers, held the tiles up: 8192 rows
+                    // through an 8192 x 4096 matrix took 323 us against 289.)
+                    constexpr int kPitch = 80;
+                    const uint32_t to = smem_u32(turn) + (lane & 7) * kPitch + (lane >> 3) * 16;
+                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)(sg.row0 + cb) * L.ldy + n0;
+    #pragma unroll
+                    for (int c = 0; c < kC; ++c)
+    #pragma unroll
+                        for (int p = 0; p < 4; ++p) {  // 16 columns: lanes 0-7 and 8-15 of the first 8, of the next 8
+                            if (16 * p >= width[c]) continue;
+                            const f32x2* v0 = &acc[0][c][4 * p];
+                            const f32x2* v1 = &acc[1][c][4 * p];
+                            __syncwarp();
+                            stmatrix(to, bf16x2(v0[0]), bf16x2(v0[1]), bf16x2(v1[0]), bf16x2(v1[1]));
+                            stmatrix(to + 8 * kPitch, bf16x2(v0[2]), bf16x2(v0[3]), bf16x2(v1[2]), bf16x2(v1[3]));
+                            __syncwarp();
+    #pragma unroll
+                            for (int r0 = 0; r0 < 16; r0 += 8) {
+                                const int r = r0 + (lane >> 2), col = c * w0 + 16 * p + r;
+                                const uint4 v = lds128(turn + r * kPitch + (lane & 3) * 16);
+                                if (16 * p + r < width[c] && cb + col < sg.rows)
+                                    *reinterpret_cast<uint4*>(y + (size_t)col * L.ldy + (lane & 3) * 8) = v;
+                            }
                         }
-                    }
-            } else {
-                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (8 * (i >> 1) >= width[c]) continue;
-                        const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
-                        __nv_bfloat16* at = y + (size_t)col * L.ldy + 8 * (i & 1);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
-                            if (in && col < sg.rows) at[16 * h] = __float2bfloat16_rn(lo2(acc[h][c][i]));
-                            if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = __float2bfloat16_rn(hi2(acc[h][c][i]));
+                } else {
+                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(L.y) + (size_t)sg.row0 * L.ldy + n0 + mlane;
+    #pragma unroll
+                    for (int c = 0; c < kC; ++c)
+    #pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (8 * (i >> 1) >= width[c]) continue;
+                            const int col = cb + c * w0 + 8 * (i >> 1) + 2 * (lane & 3);  // and + 1
+                            __nv_bfloat16* at = y + (size_t)col * L.ldy + 8 * (i & 1);
+    #pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const bool in = n0 + mlane + 8 * (i & 1) + 16 * h < L.n;
+                                if (in && col < sg.rows) at[16 * h] = __float2bfloat16_rn(lo2(acc[h][c][i]));
+                                if (in && col + 1 < sg.rows) at[16 * h + L.ldy] = __float2bfloat16_rn(hi2(acc[h][c][i]));
+                            }
                         }
-                    }
-            }
+                }
             }
         }
     }
