@@ -343,6 +343,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
 
     // ---- set-up: barriers, tensor memory, the groups' tiles ----
     if (warp == 0) {
+        pdl_wait();
         int tiles_before = 0, widest = 16;
         for (int e0 = 0; e0 < L.n_groups; e0 += kWarp) {
             const int e = e0 + lane;
@@ -388,10 +389,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         sh.fail = 0;
         mbar_fence_init();
     } else if (warp == 2) {
+        pdl_wait();  // (a CTA of the launch before may hold tensor memory)
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
+    pdl_wait();
     tc_before();
     __syncthreads();
     cluster_sync();
@@ -1011,17 +1014,15 @@ cudaError_t prepare_grouped() {
 }
 
 namespace {
-void configure(cudaLaunchConfig_t* cfg, int pairs, cudaStream_t stream) {
-    cfg->gridDim = dim3(2 * pairs);
-    cfg->blockDim = dim3(kCtaThreads);
-    cfg->dynamicSmemBytes = kDynSmem;
-    cfg->stream = stream;
+cudaLaunchConfig_t configure(int pairs, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = launch_shape(dim3(2 * pairs), kCtaThreads, stream);
+    cfg.dynamicSmemBytes = kDynSmem;
+    return cfg;
 }
 }  // namespace
 
 int grouped_pairs() {
-    cudaLaunchConfig_t cfg{};
-    configure(&cfg, 1, nullptr);
+    cudaLaunchConfig_t cfg = configure(1, nullptr);
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {2, 1, 1};
@@ -1036,9 +1037,7 @@ int grouped_pairs() {
 }
 
 cudaError_t launch_grouped(const GroupedLaunch& a, bool e4m3, bool gated, bool kn, cudaStream_t stream) {
-    cudaLaunchConfig_t cfg{};
-    configure(&cfg, a.pairs, stream);
-    return cudaLaunchKernelEx(&cfg, pick(e4m3, gated, kn, grouped_x_is_m(e4m3, gated, a.rows, a.n_groups)), a);
+    return launch_after(pick(e4m3, gated, kn, grouped_x_is_m(e4m3, gated, a.rows, a.n_groups)), configure(a.pairs, stream), a);
 }
 
 }  // namespace tsffn

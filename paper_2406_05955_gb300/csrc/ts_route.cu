@@ -89,6 +89,7 @@ __device__ __forceinline__ void pick(const RouteLaunch& L, int t, int sub) {
 template <int G>
 __global__ void __launch_bounds__(kPickThreads) k_route_pick(const RouteLaunch L) {
     pdl_launch_dependents();  // the placing CTAs set up meanwhile
+    pdl_wait();
     const long long i = (long long)blockIdx.x * kPickThreads + threadIdx.x;
     pick<G>(L, (int)(i / G), (int)(i % G));
 }
@@ -140,6 +141,7 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
     __shared__ int total_here[kMaxRouteExperts], first[kMaxRouteExperts], sums[kMaxRouteExperts / kWarp];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = L.n_experts;
     if constexpr (G > 0) {
+        pdl_wait();
         for (int i = tid; i - tid < L.tokens * G; i += kPlaceThreads) pick<G>(L, i / G, i % G);
         __syncthreads();  // (orders the picks' stores before the loads below)
     }
@@ -233,22 +235,18 @@ cudaError_t launch(const RouteLaunch& a, cudaStream_t stream) {
     // One launch as long as the one CTA picks in one round: 4 tokens of 8 experts 3.7 us (two launches
     // 5.1), 1024 5.8 (6.6), 2048 8.1 (6.6); 128 tokens of 64 experts 7.9 (7.5), 512 25.0 (8.3).
     const bool fused = (long long)a.tokens * G <= kPlaceThreads;
-    if (fused) {
-        k_route_place<G><<<1, kPlaceThreads, 0, stream>>>(a);
-        return cudaGetLastError();
-    }
+    if (fused) return launch_after(k_route_place<G>, launch_shape(dim3(1), kPlaceThreads, stream), a);
     const long long lanes = (long long)a.tokens * G;
-    k_route_pick<G><<<(unsigned)((lanes + kPickThreads - 1) / kPickThreads), kPickThreads, 0, stream>>>(a);
+    const cudaError_t picked = launch_after(
+        k_route_pick<G>, launch_shape(dim3((unsigned)((lanes + kPickThreads - 1) / kPickThreads)), kPickThreads, stream), a);
+    if (picked != cudaSuccess) return picked;
     // 16 CTAs from 16384 picks on: 8192 tokens, 6 of 64 experts, 14.5 -> 11.9 us; 4096 tokens, 2 of 8, 6.8 -> 7.1.
     const unsigned ctas = (long long)a.tokens * a.top_k >= 16384 ? kPlaceMost : kPlaceCtas;
     if (ctas > kPlaceCtas) {
         const cudaError_t e = cudaFuncSetAttribute(k_route_place<0>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
     }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kPlaceThreads);
-    cfg.stream = stream;
+    cudaLaunchConfig_t cfg = launch_shape(dim3(ctas), kPlaceThreads, stream);
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim = {ctas, 1, 1};

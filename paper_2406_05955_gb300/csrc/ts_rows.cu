@@ -24,6 +24,7 @@ __device__ __forceinline__ int source_row(const RowsLaunch& L, int r) {
 
 // A warp copies 2 KB of a row.
 __global__ void __launch_bounds__(kRowThreads) k_gather_rows(const RowsLaunch L, int64_t src_bytes, int row_bytes) {
+    pdl_wait();
     const int r = blockIdx.x * kRowsPerCta + (threadIdx.x >> 5), lane = threadIdx.x & 31, s = source_row(L, r);
     if (s < 0) return;
     const int at = blockIdx.y * (16 * kLoads * kWarp) + 16 * lane;
@@ -68,6 +69,7 @@ __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const RowsLaunch L) 
     __shared__ float scales[kBlocks][kRowsPerCta];
     __shared__ bool live[kRowsPerCta];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_wait();
     const int r = blockIdx.x * kRowsPerCta + warp, s = source_row(L, r);
     if (lane == 0) live[warp] = s >= 0;
     if (s >= 0) {
@@ -114,13 +116,14 @@ template <typename T, bool VEC, int K>  // K: top_k rounded up to 2, 4 or 8
 __global__ void __launch_bounds__(kRowThreads) k_combine(const CombineLaunch L) {
     constexpr int N = VEC ? Vec<T>::N : 1;
     const int t = blockIdx.y, i = (blockIdx.x * kRowThreads + threadIdx.x) * N;
+    pdl_wait();
     if (i >= L.n) return;
     int s[K];
     float w[K], sum[N] = {};
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        s[j] = j < L.top_k ? __ldg(L.slots + (size_t)t * L.top_k + j) : -1;
-        w[j] = j < L.top_k ? __ldg(L.w + (size_t)t * L.top_k + j) : 0.0f;
+        s[j] = j < L.top_k ? L.slots[(size_t)t * L.top_k + j] : -1;
+        w[j] = j < L.top_k ? L.w[(size_t)t * L.top_k + j] : 0.0f;
     }
     uint4 raw[K];
 #pragma unroll
@@ -149,15 +152,9 @@ __global__ void __launch_bounds__(kRowThreads) k_combine(const CombineLaunch L) 
     }
 }
 
-template <typename T>
-void combine(const CombineLaunch& a, bool vec, dim3 grid, cudaStream_t stream) {
-    auto run = [&](auto v) {
-        constexpr bool kVec = decltype(v)::value;
-        if (a.top_k <= 2) k_combine<T, kVec, 2><<<grid, kRowThreads, 0, stream>>>(a);
-        else if (a.top_k <= 4) k_combine<T, kVec, 4><<<grid, kRowThreads, 0, stream>>>(a);
-        else k_combine<T, kVec, kMaxRouteK><<<grid, kRowThreads, 0, stream>>>(a);
-    };
-    vec ? run(std::true_type()) : run(std::false_type());
+template <typename T, bool VEC>
+auto pick_combine(int top_k) {
+    return top_k <= 2 ? k_combine<T, VEC, 2> : top_k <= 4 ? k_combine<T, VEC, 4> : k_combine<T, VEC, kMaxRouteK>;
 }
 
 dim3 row_grid(const RowsLaunch& a, int row, int per_cta) {
@@ -168,14 +165,13 @@ dim3 row_grid(const RowsLaunch& a, int row, int per_cta) {
 
 cudaError_t launch_gather_rows(const RowsLaunch& a, int elem_bytes, cudaStream_t stream) {
     const int bytes = a.k * elem_bytes;
-    k_gather_rows<<<row_grid(a, bytes, 16 * kLoads * kWarp), kRowThreads, 0, stream>>>(a, a.ldx * elem_bytes, bytes);
-    return cudaGetLastError();
+    return launch_after(k_gather_rows, launch_shape(row_grid(a, bytes, 16 * kLoads * kWarp), kRowThreads, stream), a,
+                        a.ldx * elem_bytes, bytes);
 }
 
 cudaError_t launch_quant_rows(const RowsLaunch& a, bool f32, cudaStream_t stream) {
-    if (f32) k_quant_rows<float><<<row_grid(a, a.k, 4 * kLoads * kWarp), kRowThreads, 0, stream>>>(a);
-    else k_quant_rows<__nv_bfloat16><<<row_grid(a, a.k, 8 * kLoads * kWarp), kRowThreads, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch_after(f32 ? k_quant_rows<float> : k_quant_rows<__nv_bfloat16>,
+                        launch_shape(row_grid(a, a.k, (f32 ? 4 : 8) * kLoads * kWarp), kRowThreads, stream), a);
 }
 
 cudaError_t launch_combine(const CombineLaunch& a, bool f32, cudaStream_t stream) {
@@ -183,15 +179,18 @@ cudaError_t launch_combine(const CombineLaunch& a, bool f32, cudaStream_t stream
     const bool vec = a.n % size == 0 && (((uintptr_t)a.src | (uintptr_t)a.y) & 15u) == 0;
     const int per = kRowThreads * (vec ? size : 1);
     const unsigned gx = (unsigned)((a.n + per - 1) / per);
+    const auto kernel = f32 ? (vec ? pick_combine<float, true>(a.top_k) : pick_combine<float, false>(a.top_k))
+                            : (vec ? pick_combine<__nv_bfloat16, true>(a.top_k) : pick_combine<__nv_bfloat16, false>(a.top_k));
     for (int t = 0; t < a.tokens; t += 65535) {  // the grid's second dimension ends there
         CombineLaunch b = a;
         b.slots += (size_t)t * a.top_k;
         b.w += (size_t)t * a.top_k;
         b.y += (size_t)t * a.n;
         const dim3 grid(gx, (unsigned)(a.tokens - t < 65535 ? a.tokens - t : 65535));
-        f32 ? combine<float>(b, vec, grid, stream) : combine<__nv_bfloat16>(b, vec, grid, stream);
+        const cudaError_t e = launch_after(kernel, launch_shape(grid, kRowThreads, stream), b);
+        if (e != cudaSuccess) return e;
     }
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 }  // namespace tsffn

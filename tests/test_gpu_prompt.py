@@ -224,6 +224,51 @@ def test_layers_share_scratch_on_a_stream_and_in_a_graph(ts):
 
 
 @pytest.mark.parametrize("e8", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("t", [1, 40, 700])
+def test_calls_wait_for_what_is_before_them(ts, t, e8):
+    """Inputs that long work writes just before a call, overwritten just after it; also in a graph whose stream joins
+    another one before the call."""
+    d, m = 256, 512
+    layer = Layer(ts, 8, d, m, 2, seed=5, e8=e8)
+    p = ts.Prompt(layer.experts, t)
+    xs = [wl.tokens(t, d, seed=s).cuda() for s in range(4)]
+    want = [p.forward(x).clone() for x in xs]
+    big = torch.randn(4096, 4096, device="cuda")
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(x, x_in, y, out):
+        a = big @ big                              # holds the next copy up
+        x_in.copy_(x + (a[0, 0] * 0).to(x.dtype))
+        p.forward(x_in, y=y)
+        x_in.fill_(float("nan"))
+        out.copy_(y)
+        y.fill_(float("nan"))
+
+    x_in, y = torch.empty_like(xs[0]), torch.empty_like(want[0])
+    got = [torch.empty_like(y) for _ in xs]
+    for _ in range(3):
+        for x, out in zip(xs, got):
+            step(x, x_in, y, out)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for x, out in zip(xs, got):
+            other.wait_stream(side)
+            with torch.cuda.stream(other):
+                x_in.copy_(x)
+            side.wait_stream(other)                # the call comes after two things
+            p.forward(x_in, y=out)
+            p.forward(x_in, y=y)                   # and after another call
+    for out in got:
+        out.zero_()
+    for _ in range(3):
+        graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(y, want[-1]) and p.get_error() == 0
+
+
+@pytest.mark.parametrize("e8", [False, True], ids=["bf16", "e4m3"])
 def test_tokens_without_an_expert_give_zero(ts, e8):
     """Padding whose router logits are NaN: no expert, y = 0; the other tokens as without it."""
     d, m, t = 256, 256, 90
