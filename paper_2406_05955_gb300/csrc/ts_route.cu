@@ -6,6 +6,9 @@
 // warps and, through distributed shared memory, over the CTAs, and a pick's row is its expert's first row plus the
 // picks of that expert before it. Nothing is atomic, so rows do not depend on timing, and no scratch is needed.
 // Few tokens are picked by the CTA that places them: one launch instead of two.
+//
+// Latency bounds it: logits and lists are 2.9 MB for 8192 tokens of 64 experts, 0.4 us of memory time; picking and the
+// placing's chain of counts, cluster barrier and scan take 10.3 us (4 tokens of 8 experts: 4.2).
 #include "ts_grouped.h"
 #include "ts_kernels.cuh"
 
