@@ -268,6 +268,30 @@ def test_calls_wait_for_what_is_before_them(ts, t, e8):
     assert torch.equal(y, want[-1]) and p.get_error() == 0
 
 
+def test_two_forwards_at_once(ts):
+    """One layer through two scratches, and a layer of few tokens, on three streams at once."""
+    d, m = 256, 1024
+    layer = Layer(ts, 8, d, m, 2, seed=6)
+    sizes = (37, 600)
+    ps = [ts.Prompt(layer.experts, t) for t in sizes]
+    xs = [wl.tokens(t, d, seed=t).cuda() for t in sizes]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = [(torch.randn(m, d, generator=g, device="cuda") / 16).to(torch.bfloat16) for _ in range(3)]
+    few = ts.Ffn(*w)
+    want = [p.forward(x).clone() for p, x in zip(ps, xs)] + [few.forward(xs[0][:1]).clone()]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    ys = [[torch.empty_like(v) for _ in range(20)] for v in want]
+    for i in range(20):
+        for p, x, y, st in zip(ps, xs, ys, streams):
+            p.forward(x, y=y[i], stream=st)
+        ys[2][i] = few.forward(xs[0][:1], stream=streams[2])
+    torch.cuda.synchronize()
+    for y, v in zip(ys, want):
+        assert all(torch.equal(a, v) for a in y)
+    assert all(p.get_error() == 0 and p.check_scratch() == 0 for p in ps)
+
+
 @pytest.mark.parametrize("e8", [False, True], ids=["bf16", "e4m3"])
 def test_tokens_without_an_expert_give_zero(ts, e8):
     """Padding whose router logits are NaN: no expert, y = 0; the other tokens as without it."""
