@@ -450,6 +450,7 @@ typedef enum {
  *     y[r] = x[r] . W_e                                      (plain)
  *     y[r] = max(0, x[r] . W_e) * max(0, x[r] . U_e)         (gated: Eq. 1 with the dReLU of Eq. 2)
  * for offsets[e] <= r < offsets[e + 1]. One group is an ordinary matrix product.
+ * A gated product is 0 unless both factors are positive (so where either is NaN).
  *   n_groups   1..256
  *   n, k       outputs (at most 2^30) and inputs of a weight matrix
  *   wdtype     TS_BF16 (x bf16) or TS_E4M3 (x e4m3)

@@ -306,7 +306,7 @@ ts_status ts_ffn_create(ts_ffn** out, int d, int m, ts_dtype wdtype, const void*
 
 void ts_ffn_destroy(ts_ffn* h) {
     if (!h) return;
-    if (h->arena.base) cudaFree(h->arena.base);
+    free_arena(&h->arena);
     delete h;
 }
 
@@ -789,7 +789,7 @@ ts_status ts_moe_create(ts_moe** out, int d, int n_experts, int top_k, ts_dtype 
 
 void ts_moe_destroy(ts_moe* h) {
     if (!h) return;
-    if (h->arena.base) cudaFree(h->arena.base);
+    free_arena(&h->arena);
     delete h;
 }
 
@@ -989,7 +989,7 @@ ts_status ts_predictor_create(ts_predictor** out, int d, int r, int m, ts_dtype 
 
 void ts_predictor_destroy(ts_predictor* p) {
     if (!p) return;
-    if (p->arena.base) cudaFree(p->arena.base);
+    free_arena(&p->arena);
     delete p;
 }
 
@@ -1216,6 +1216,7 @@ ts_status ts_graph_launch(ts_graph* g, cudaStream_t stream) {
 
 void ts_graph_destroy(ts_graph* g) {
     if (!g) return;
+    const WhileCapturing may_free;
     if (g->exec) cudaGraphExecDestroy(g->exec);
     if (g->graph) cudaGraphDestroy(g->graph);
     if (g->mem) cudaFree(g->mem);

@@ -52,6 +52,26 @@ inline ts_status alloc_arena(Arena* ar) {
     return TS_OK;
 }
 
+// Handles are also destroyed while some stream is being captured (a garbage collector picks its time): what is freed
+// under this, which no captured work depends on, does not end that capture.
+class WhileCapturing {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    bool relaxed = cudaThreadExchangeStreamCaptureMode(&mode) == cudaSuccess;
+
+public:
+    WhileCapturing() = default;
+    WhileCapturing(const WhileCapturing&) = delete;
+    ~WhileCapturing() {
+        if (relaxed) cudaThreadExchangeStreamCaptureMode(&mode);
+    }
+};
+inline void free_arena(Arena* ar) {
+    if (!ar->base) return;
+    const WhileCapturing may_free;
+    cudaFree(ar->base);
+    ar->base = nullptr;
+}
+
 // Synchronise `stream` and compare every guard zone with its fill.
 inline ts_status check_arena(const Arena& ar, cudaStream_t stream) {
     if (!ar.base) return TS_ERR_INVALID_ARG;

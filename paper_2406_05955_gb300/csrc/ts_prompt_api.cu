@@ -288,7 +288,7 @@ ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dty
 
 void ts_grouped_destroy(ts_grouped* h) {
     if (!h) return;
-    if (h->arena.base) cudaFree(h->arena.base);
+    free_arena(&h->arena);
     delete h;
 }
 
@@ -377,7 +377,7 @@ ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int t
 
 void ts_experts_destroy(ts_experts* h) {
     if (!h) return;
-    if (h->arena.base) cudaFree(h->arena.base);
+    free_arena(&h->arena);
     delete h;
 }
 
@@ -436,7 +436,7 @@ ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top
 
 void ts_prompt_destroy(ts_prompt* p) {
     if (!p) return;
-    if (p->arena.base) cudaFree(p->arena.base);
+    free_arena(&p->arena);
     delete p;
 }
 

@@ -292,6 +292,24 @@ def test_two_forwards_at_once(ts):
     assert all(p.get_error() == 0 and p.check_scratch() == 0 for p in ps)
 
 
+@pytest.mark.parametrize("what", ["grouped", "experts", "prompt", "ffn"])
+def test_a_handle_is_destroyed_during_a_capture(ts, what):
+    """As a garbage collection may do at any time: the capture goes on."""
+    w = torch.randn(64, 64, device="cuda").to(torch.bfloat16)
+    experts = ts.Experts(w, w, w)
+    other = {"grouped": ts.Grouped(w), "experts": ts.Experts(w, w, w), "prompt": ts.Prompt(experts, 4),
+             "ffn": ts.Ffn(w, w, w)}[what]
+    p, x, y = ts.Prompt(experts, 8), torch.randn(8, 64, device="cuda").to(torch.bfloat16), torch.zeros(8, 64, device="cuda")
+    want = p.forward(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        p.forward(x, y=y)
+        other.close()
+    graph.replay()
+    assert torch.equal(y, want) and p.get_error() == 0 and p.check_scratch() == 0
+
+
 @pytest.mark.parametrize("e8", [False, True], ids=["bf16", "e4m3"])
 def test_tokens_without_an_expert_give_zero(ts, e8):
     """Padding whose router logits are NaN: no expert, y = 0; the other tokens as without it."""
