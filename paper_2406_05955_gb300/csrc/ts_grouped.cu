@@ -18,10 +18,11 @@
 //
 // What bounds it, and what it measured (d = 4096, m = 14336): few rows, reading the weights (gated bf16, 16 rows over
 // 8 groups: 281 us, 6.7 TB/s); many rows of bf16, the tensor cores under the power cap (8192 rows: plain 495 us, gated
-// 1020-1090 us, 1.75-1.9 PFLOP/s; a library's plain product takes 471-484); many rows of e4m3, reading tensor memory at
-// every 128 of k (8192 rows: plain 330-350 us, gated over 8 groups 688 us, 2.8 PFLOP/s; 2000 rows over 8 groups 208 us, of
-// which reading the weights is 139); one row, latency (1 x 4096 x 14336 e4m3: 23 us, of which reading the weights is 9:
-// launch, set-up, the first load, the join of a tile's parts and the stores come one after another).
+// 1020-1090 us, 1.75-1.9 PFLOP/s; a library's plain product takes 471-484); many rows of e4m3, handing an accumulator to the
+// summing warps and back at every 128 of k, 0.44 us where its MMAs take 0.27 (8192 rows: plain 330-360 us, gated over 8 groups
+// 688 us, 2.8 PFLOP/s; 2000 rows over 8 groups 208 us, of which reading the weights is 139); one row, latency (1 x 4096 x 14336
+// e4m3: 23 us, of which reading the weights is 9: launch, set-up, the first load, the join of a tile's parts and the stores
+// come one after another).
 #include <cuda_fp8.h>
 
 #include "ts_grouped.h"
@@ -306,8 +307,8 @@ struct Walk {
 
 // XM (e4m3): the rows of x are the MMA's M, always 256 of them, and the weights its N. What a lane of tensor memory holds
 // then belongs to one row of x, with one scale, and 32 lanes can be read at a time: a load of 16 lanes (of columns that
-// have scales of their own) takes as long, and for wide tiles the reading is what bounds e4m3 products: 8192 rows,
-// 4096 x 14336, 424 -> 346 us. Narrow tiles would be mostly zeros.
+// have scales of their own) takes as long, and for wide tiles that is what bound e4m3 products: 8192 rows, 4096 x 14336,
+// 424 -> 346 us. Narrow tiles would be mostly zeros.
 template <bool E8, bool GATED, bool KN, bool XM>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
