@@ -480,7 +480,8 @@ void ts_grouped_destroy(ts_grouped* h);
  *              skipped and recorded (ts_grouped_get_error: TS_ERR_BAD_INDEX).
  *   y, ldy     device, rows of n elements ldy apart (ydtype TS_BF16, rounded once, or TS_F32); rows
  *              that no group has are left as they were
- * One forward may be in flight per handle, and its device is the current one (else TS_ERR_INVALID_ARG).
+ * One forward may be in flight per handle (a replay of a graph that holds one counts), and its device is the current
+ * one (else TS_ERR_INVALID_ARG).
  */
 ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const float* x_scale, int64_t ld_scale,
                              const int32_t* offsets, int rows, void* y, int64_t ldy, ts_dtype ydtype,
@@ -511,8 +512,8 @@ ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int t
 void ts_experts_destroy(ts_experts* e);
 
 /* Scratch for forwards of up to max_tokens tokens through any layers of these sizes (arguments as
-   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle; scratch, layer and the
-   current device are one device (else TS_ERR_INVALID_ARG). */
+   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle (a replay of a graph that
+   holds one counts); scratch, layer and the current device are one device (else TS_ERR_INVALID_ARG). */
 ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top_k, ts_dtype wdtype, int max_tokens);
 void ts_prompt_destroy(ts_prompt* p);
 

@@ -181,7 +181,8 @@ def _pointers(ts):
 class Grouped:
     """Products of ragged groups of rows, each group with its own weights (``ts_grouped_*``): ``y[r] = x[r] W_e^T``
     over borrowed ``w[e] [n][k]`` (``layout="kn"``: ``x[r] W_e`` over ``[k][n]``), bf16, or e4m3 with fp32
-    ``scale[e] [ceil(n / 128)][ceil(k / 128)]``. ``w`` is a tensor (one group), a list of them, or a stacked one."""
+    ``scale[e] [ceil(n / 128)][ceil(k / 128)]``. ``w`` is a tensor (one group), a list of them, or a stacked one.
+    One forward may be in flight at a time, replays of graphs that hold one included."""
 
     def __init__(self, w, layout: str = "nk", scale=None, max_rows: int = 1, _up=None, _scale_up=None):
         w, up, scale, scale_up = (None if t is None else _matrices(t) for t in (w, _up, scale, _scale_up))
@@ -333,7 +334,7 @@ class Experts:
 
 class Prompt:
     """Forwards of up to ``max_tokens`` tokens through ``experts``, or through any other layer of its sizes: the scratch
-    of all of them (``ts_prompt_*``)."""
+    of all of them (``ts_prompt_*``). One forward may be in flight at a time, replays of graphs that hold one included."""
 
     def __init__(self, experts: Experts, max_tokens: int):
         self.experts, self.max_tokens = experts, int(max_tokens)
