@@ -512,8 +512,9 @@ ts_status ts_experts_create(ts_experts** out, int d, int m, int n_experts, int t
 void ts_experts_destroy(ts_experts* e);
 
 /* Scratch for forwards of up to max_tokens tokens through any layers of these sizes (arguments as
-   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per handle (a replay of a graph that
-   holds one counts); scratch, layer and the current device are one device (else TS_ERR_INVALID_ARG). */
+   ts_experts_create; n_experts and top_k may be smaller in a layer). One forward may be in flight per
+   handle (a replay of a graph that holds one counts); scratch, layer and the current device are one
+   device (else TS_ERR_INVALID_ARG). */
 ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top_k, ts_dtype wdtype, int max_tokens);
 void ts_prompt_destroy(ts_prompt* p);
 
