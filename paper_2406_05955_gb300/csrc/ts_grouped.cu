@@ -126,6 +126,11 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// What the host has copied to a map in global memory is what this thread's later boxes go by, and no map that lay at the
+// same address before. (A map that is a parameter needs no such fence.)
+__device__ __forceinline__ void map_acquire(const CUtensorMap* map) {
+    asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(map) : "memory");
+}
 // 4-byte copy global -> shared (bytes = 0: zero)
 __device__ __forceinline__ void cp4(float* dst, const float* src, uint32_t bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
@@ -417,7 +422,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
         regs_shrink();
         if (warp == 0) {
             // ---- loads: lane i < kBoxes a box of weights, the next one the rows of x ----
-            int st = 0, n_loaded = 0;
+            int st = 0, n_loaded = 0, group = -1;
             unsigned ph = 0;
             bool ok = true;
             Seg sg;
@@ -446,7 +451,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                         off = K::kOffW;
                         cy = sg.wt * 256 + (int)rank * 128;
                     }
+                    if (sg.g != group) map_acquire(map);
                 }
+                group = sg.g;
                 for (int k = sg.k0; k < sg.k1; ++k) {
                     if (n_loaded >= stages) ok = wait_for(&sh.empty[st], ph ^ 1u, sh);
                     ok = __all_sync(0xffffffffu, ok);

@@ -271,6 +271,29 @@ def test_repeated_calls_give_the_same_bits(ts, form):
     check(y, y.clone(), [0, 100, 120, 150], xd, wd, gated, layout, k)
 
 
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_handles_made_and_closed_in_turn(ts, form):
+    """Their scratch has one size, so that one handle's maps of weights lie where another's lay. (All weights stay.)"""
+    dtype, gated, layout = form
+    shapes = [(64, 128), (256, 64), (520, 256), (128, 512)]
+    made = [make(dtype, 3, n, k, 50, gated, layout, seed=n + k) for n, k in shapes]
+    off = [0, 20, 21, 50]
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    want = [None] * len(shapes)
+    for turn in range(24):
+        i = turn * 7 % 4 if turn < 12 else turn % 4
+        (n, k), (x, xs, w, ss, xd, wd) = shapes[i], made[i]
+        mm = handle(ts, w, ss, gated, layout, 50)
+        y = torch.zeros(50, n, device="cuda")
+        mm.forward(x, o, xs, y)
+        assert mm.get_error() == 0
+        mm.close()
+        if want[i] is None:
+            check(y, y.clone(), off, xd, wd, gated, layout, k)
+            want[i] = y
+        assert torch.equal(y, want[i])
+
+
 WIDE = [f for f in FORMS if f[0] == E4M3]
 
 
