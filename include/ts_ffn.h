@@ -527,8 +527,9 @@ void ts_prompt_destroy(ts_prompt* p);
  */
 ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int tokens, float* y, cudaStream_t stream);
 
-/* Routing of the last forward (of its top_k), to host memory (synchronises `stream`): sel and w [tokens][top_k].
-   TS_ERR_INVALID_ARG after a layer of one expert without a router. */
+/* Routing of the last forward (of its top_k), to host memory (synchronises `stream`): sel and w [tokens][top_k],
+   which is nothing after a forward of no tokens. TS_ERR_INVALID_ARG before any forward, after one that failed on
+   its way, and after a layer of one expert without a router. */
 ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel, float* w);
 /* As ts_ffn_get_error and ts_ffn_check_scratch. */
 ts_status ts_prompt_get_error(ts_prompt* p, cudaStream_t stream);

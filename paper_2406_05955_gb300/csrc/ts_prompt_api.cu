@@ -196,7 +196,7 @@ struct ts_prompt {
     void* cq = nullptr;               // [rows][m] e4m3
     float* c_scale = nullptr;         // [m / 128][rows]
     float* y = nullptr;               // [rows][d]
-    int last_tokens = 0, last_k = 0;  // of the last forward with a router
+    int last_tokens = 0, last_k = 0;  // of the last forward; last_k 0: none, without a router, or failed
 };
 
 extern "C" {
@@ -444,7 +444,11 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
     if (!p || !e || e->d != p->d || e->m != p->m || e->dt != p->dt || e->n_experts > p->n_experts || e->top_k > p->top_k ||
         tokens < 0 || tokens > p->max_tokens)
         return TS_ERR_INVALID_ARG;
-    if (tokens == 0) return TS_OK;
+    if (tokens == 0) {
+        p->last_tokens = 0;
+        p->last_k = e->routed ? e->top_k : 0;
+        return TS_OK;
+    }
     if (!here(p->s.device) || e->device != p->s.device || !x || !y || !aligned16(x)) return TS_ERR_INVALID_ARG;
     const int d = p->d, m = p->m, rows = e->routed ? tokens * e->top_k : tokens;
     const bool e8 = p->dt == TS_E4M3;
@@ -482,8 +486,10 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
                          stream);
     if (s == TS_OK && e->routed) {
         s = launched(launch_combine({p->y, rows, d, p->slots, p->w, tokens, e->top_k, y}, true, stream));
-        p->last_tokens = tokens;
-        p->last_k = e->top_k;
+        if (s == TS_OK) {
+            p->last_tokens = tokens;
+            p->last_k = e->top_k;
+        }
     }
     return s;
 }

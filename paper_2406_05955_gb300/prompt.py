@@ -337,7 +337,7 @@ class Prompt:
     of all of them (``ts_prompt_*``). One forward may be in flight at a time, replays of graphs that hold one included."""
 
     def __init__(self, experts: Experts, max_tokens: int):
-        self.experts, self.max_tokens = experts, int(max_tokens)
+        self.experts, self.max_tokens, self._most = experts, int(max_tokens), int(max_tokens) * experts.top_k
         h = ctypes.c_void_p()
         self._h = None
         _check(lib().ts_prompt_create(ctypes.byref(h), experts.d, experts.m, experts.n_experts, experts.top_k,
@@ -369,11 +369,11 @@ class Prompt:
 
     def get_routing(self, stream=None):
         """(sel, w) of the last forward, as numpy [tokens][top_k]; -1: no expert."""
-        t, k = self._last or (0, 1)
-        sel, w = np.zeros((t, k), np.int32), np.zeros((t, k), np.float32)
+        sel, w = np.zeros(self._most, np.int32), np.zeros(self._most, np.float32)  # room for any forward's
         _check(lib().ts_prompt_get_routing(self.handle, _handle(stream), sel.ctypes.data_as(P), w.ctypes.data_as(P)),
                "ts_prompt_get_routing")
-        return sel, w
+        t, k = self._last
+        return sel[:t * k].reshape(t, k), w[:t * k].reshape(t, k)
 
     def get_error(self, stream=None) -> int:
         return int(lib().ts_prompt_get_error(self.handle, _handle(stream)))

@@ -182,6 +182,29 @@ def test_single_ffn(ts, tokens, e8):
         p.get_routing()
 
 
+def test_routing_has_the_tokens_of_the_last_forward(ts):
+    """None after a forward of no tokens: nothing is written behind a caller's buffers of that size."""
+    import ctypes
+
+    layer = Layer(ts, 8, 128, 128, 2, seed=2)
+    p = ts.Prompt(layer.experts, 40)
+    with pytest.raises(ts.TsError):
+        p.get_routing()
+    x = wl.tokens(40, 128, seed=2).cuda()
+    for t in (40, 0, 3, 0, 17):
+        p(x[:t])
+        sel, w = (torch.full((80,), -77, dtype=d) for d in (torch.int32, torch.float32))
+        status = ts.lib().ts_prompt_get_routing(p.handle, None, *(ctypes.c_void_p(v.data_ptr()) for v in (sel, w)))
+        assert status == 0
+        assert (sel[2 * t:] == -77).all() and (w[2 * t:] == -77).all(), "written behind the last forward's tokens"
+        got = p.get_routing()
+        assert got[0].shape == got[1].shape == (t, 2)
+        assert np.array_equal(got[0].reshape(-1), sel[:2 * t].numpy()) and (got[0] >= 0).all()
+    with pytest.raises(ts.TsError):
+        p(torch.cat([x, x]))                     # refused: the forward before it is still the last one
+    assert p.get_routing()[0].shape == (17, 2)
+
+
 def test_same_as_the_layers_of_few_tokens(ts):
     """Experts.of(Moe) and Experts.of(Ffn) over the tokens that those layers take; c alone is rounded differently."""
     d, m, e = 512, 1024, 8
