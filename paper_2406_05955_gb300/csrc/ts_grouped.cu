@@ -499,19 +499,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     const int k_end = (int)uniform((uint32_t)sg.k1);
                     int k = (int)uniform((uint32_t)sg.k0);
                     const uint32_t idesc = K::kIdesc | (uint32_t)(2 * half >> 3) << 17;
-                    for (; ok && k < k_end; ++chunk) {
+                    // A lane whose limit has passed goes on with the others to the tile's end, without waiting: the limit may
+                    // pass for some lanes alone, and all of them have to take part in the election. (A vote at every
+                    // stage instead: 8192 rows, 4096 x 14336 e4m3, 366 us for 360.)
+                    for (; k < k_end; ++chunk) {
                         const int first = k, kc = min(k_end, k + K::kChunk), buf = chunk & (bufs - 1);
                         const uint32_t d = tmem + (buf << (9 - lg));
-                        for (; ok && k < kc; ++k) {
+                        for (; k < kc; ++k) {
                             // the accumulator is what is waited for longest: its barrier last
-                            ok = wait_for(&sh.full[st], ph, sh);
+                            if (ok) ok = wait_for(&sh.full[st], ph, sh);
                             if (ok && k == first && chunk >= bufs) ok = wait_for(&sh.tempty[buf], ((chunk >> lg) & 1) ^ 1u, sh);
-                            if (!ok) break;
                             tc_after();
                             const uint32_t a0 = base + st * size;
                             const uint64_t bd = desc_k(a0 + kStageW);
                             const uint64_t ad = KN ? desc_mn(a0, 8192) : desc_k(a0);
-                            if (elect_one()) {
+                            if (elect_one() && ok) {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i)
                                     pair_mma<E8>(d, ad + (KN ? 128 : 2) * i, bd + 2 * i, idesc, k > first || i > 0);
@@ -525,6 +527,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                             }
                         }
                     }
+                    ok = __all_sync(0xffffffffu, ok);
                 }
             }
             __syncwarp();
