@@ -489,6 +489,8 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
 /* As ts_ffn_get_error and ts_ffn_check_scratch. */
 ts_status ts_grouped_get_error(ts_grouped* h, cudaStream_t stream);
 ts_status ts_grouped_check_scratch(ts_grouped* h, cudaStream_t stream);
+/* As ts_ffn_set_test_stall: one warp that keeps sums, after its last tile, of every CTA of the next forwards. */
+ts_status ts_grouped_set_test_stall(ts_grouped* h, int on);
 
 typedef struct ts_experts ts_experts; /* the weights of one layer of experts, for many tokens */
 typedef struct ts_prompt ts_prompt;   /* scratch of layers over many tokens                    */

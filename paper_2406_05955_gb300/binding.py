@@ -80,6 +80,7 @@ SIGNATURES = {
     "ts_grouped_forward": (I, [P, P, L64, P, L64, P, I, P, L64, I, P]),
     "ts_grouped_get_error": (I, [P, P]),
     "ts_grouped_check_scratch": (I, [P, P]),
+    "ts_grouped_set_test_stall": (I, [P, I]),
     "ts_experts_create": (I, [PP, I, I, I, I, I, P, P, P, P, P, P, P]),
     "ts_experts_destroy": (None, [P]),
     "ts_prompt_create": (I, [PP, I, I, I, I, I, I]),

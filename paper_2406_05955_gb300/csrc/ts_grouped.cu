@@ -86,6 +86,7 @@ struct Seg {
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages], tfull[kMaxBufs], tempty[kMaxBufs], sempty[kMaxBufs];
     uint64_t met[kEpiWarps / 2];                // gated: a gate and an up warp
+    uint64_t never;                             // nothing arrives here (GroupedLaunch::test_stall)
     unsigned before[kEpiWarps / 2];
     uint32_t tmem;
     int fail;
@@ -394,6 +395,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
             mbar_init(&sh.tempty[b], 2 * kEpiWarps);
         }
         for (int b = 0; b < kEpiWarps / 2; ++b) mbar_init(&sh.met[b], 2);
+        mbar_init(&sh.never, 1);
         sh.fail = 0;
         mbar_fence_init();
     } else if (warp == 2) {
@@ -952,15 +954,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                 }
             }
         }
+        if (L.test_stall && ew == 0) wait_for(&sh.never, 0u, sh);
     }
 
     // ---- the end: no CTA leaves while the other may still signal or read it ----
-    if (*reinterpret_cast<volatile int*>(&sh.fail)) {  // copies may be in flight: give them time to land
+    __syncthreads();  // no wait of the CTA can give up after this
+    if (sh.fail) {    // copies may be in flight: give them time to land
         if (tid == 0) atomicOr(L.status, kStatusTimeout);
         const unsigned long long t0 = global_ns();
         while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
-    __syncthreads();
     tc_before();
     __syncwarp();
     cluster_sync();

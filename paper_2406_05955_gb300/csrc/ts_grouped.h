@@ -76,6 +76,7 @@ struct GroupedLaunch {
     float* partial;               // [pairs][2][2 CTAs][kEpiWarps][part_chunks * 2048]
     unsigned* arrived;            // [2 * pairs][2 CTAs][kEpiWarps], zero between calls
     unsigned* status;
+    int test_stall;               // ts_grouped_set_test_stall
 };
 
 // Whether an e4m3 product takes the rows of x as the MMA's M (see Kind in ts_grouped.cu): where the groups have enough of

@@ -107,7 +107,7 @@ ts_status copy_in(void* to, const void* from, size_t bytes) {
 
 ts_status run_products(const Products& P, const ProductScratch& S, const void* x, int64_t ldx, const float* x_scale,
                        int64_t ld_scale, const int32_t* offsets, int rows, void* y, int64_t ldy, bool y_f32,
-                       cudaStream_t stream) {
+                       cudaStream_t stream, bool test_stall = false) {
     const bool e8 = P.dt == TS_E4M3;
     GroupedLaunch a;
     // boxes of up to half of the widest tile that so many rows can give
@@ -134,6 +134,7 @@ ts_status run_products(const Products& P, const ProductScratch& S, const void* x
     a.partial = S.partial;
     a.arrived = S.arrived;
     a.status = S.status;
+    a.test_stall = test_stall;
     return launched(launch_grouped(a, e8, P.gated, P.kn, stream));
 }
 
@@ -168,6 +169,7 @@ struct ts_grouped {
     ProductScratch s;
     Arena arena;
     int max_rows = 0;
+    bool test_stall = false;  // ts_grouped_set_test_stall
 };
 
 struct ts_experts {
@@ -301,11 +303,17 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     if (!here(h->s.device) || !x || !y || !aligned16(x) || ldx < h->p.k || ldx * elem_size(h->p.dt) % 16 != 0 || ldy < h->p.n)
         return TS_ERR_INVALID_ARG;
     if (h->p.dt == TS_E4M3 ? (!x_scale || ld_scale < rows) : x_scale != nullptr) return TS_ERR_INVALID_ARG;
-    return run_products(h->p, h->s, x, ldx, x_scale, ld_scale, offsets, rows, y, ldy, ydtype == TS_F32, stream);
+    return run_products(h->p, h->s, x, ldx, x_scale, ld_scale, offsets, rows, y, ldy, ydtype == TS_F32, stream, h->test_stall);
 }
 
 ts_status ts_grouped_get_error(ts_grouped* h, cudaStream_t stream) {
     return h ? read_status(h->s, stream) : TS_ERR_INVALID_ARG;
+}
+
+ts_status ts_grouped_set_test_stall(ts_grouped* h, int on) {
+    if (!h) return TS_ERR_INVALID_ARG;
+    h->test_stall = on != 0;
+    return TS_OK;
 }
 
 ts_status ts_grouped_check_scratch(ts_grouped* h, cudaStream_t stream) {

@@ -258,6 +258,10 @@ class Grouped:
         """Status of the scratch guard zones (as Ffn.check_scratch)."""
         return int(lib().ts_grouped_check_scratch(self.handle, _handle(stream)))
 
+    def set_test_stall(self, on: bool) -> None:
+        """Failure-detection test hook: the next forwards' bounded waits run out."""
+        _check(lib().ts_grouped_set_test_stall(self.handle, int(bool(on))), "ts_grouped_set_test_stall")
+
     def close(self) -> None:
         if getattr(self, "_h", None) is not None:
             lib().ts_grouped_destroy(self._h)

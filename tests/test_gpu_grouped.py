@@ -326,6 +326,23 @@ def test_many_e4m3_rows_with_bad_ones(ts, form):
         check(got[a:b], got[a:b], [0, b - a], xd[a:b], [[ws[e]] for ws in wd], form[1], "nk", k)
 
 
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_a_wait_that_gives_up_last_is_reported(ts, form):
+    """A summing warp's wait runs out when the CTA's loads have long ended; the context and the handle stay usable."""
+    dtype, gated, layout = form
+    x, xs, w, ss, xd, wd = make(dtype, 2, 256, 512, 40, gated, layout, seed=31)
+    mm = handle(ts, w, ss, gated, layout, 40)
+    o = torch.tensor([0, 11, 40], dtype=torch.int32, device="cuda")
+    want = mm.forward(x, o, xs, torch.zeros(40, 256, device="cuda")).clone()
+    assert mm.get_error() == 0
+    mm.set_test_stall(True)
+    mm.forward(x, o, xs, torch.zeros(40, 256, device="cuda"))
+    assert mm.get_error() == 5  # TS_ERR_TIMEOUT
+    mm.set_test_stall(False)
+    assert torch.equal(mm.forward(x, o, xs, torch.zeros(40, 256, device="cuda")), want)
+    assert mm.get_error() == 0 and mm.check_scratch() == 0
+
+
 def test_refusals(ts):
     dev = "cuda"
     w = [torch.zeros(64, 64, dtype=BF16, device=dev) for _ in range(2)]

@@ -157,3 +157,9 @@ def test_sizes_beyond_the_kernels_counts(lib):
                                      None) == UNSUPPORTED
         assert lib.ts_prompt_create(ctypes.byref(h), d, m, 2, 1, TS_BF16, 8) == UNSUPPORTED
     assert h.value is None
+
+
+def test_the_stall_hook_wants_a_handle(lib):
+    from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD
+
+    assert lib.ts_grouped_set_test_stall(None, 1) == BAD
