@@ -462,7 +462,8 @@ typedef enum {
  *              fp32: a scale for each 128 x 128 block of weights. NULL for TS_BF16.
  *   max_rows   largest number of rows of a forward, at most 2^30
  * k must be a multiple of 8 (TS_BF16) or 16 (TS_E4M3), at most 2^28, n a multiple of 8 for TS_KN.
- * Products are exact, sums are held in fp32. Returns TS_ERR_INVALID_ARG,
+ * Products are exact, sums are held in fp32; those of bf16 weights are truncated at every 16 of k within 256 of k, for
+ * TS_BF16 outputs within 1024 (over Gaussian rows, relative in 2-norm, 2.4e-7 and, before the rounding, 1e-6). Returns TS_ERR_INVALID_ARG,
  * TS_ERR_UNSUPPORTED (wdtype or layout without a kernel), TS_ERR_OOM or TS_ERR_CUDA.
  */
 ts_status ts_grouped_create(ts_grouped** out, int n_groups, int n, int k, ts_dtype wdtype, ts_layout layout,

@@ -13,8 +13,8 @@
 //
 // Roles of a CTA's warps: 0 loads stages of 128 bytes of k by TMA, 1 (of the first CTA) issues the MMAs, 4-11 take the
 // sums out of tensor memory, where two accumulators take turns. They keep running sums in fp32 registers and add an
-// accumulator to them every kChunk stages: the tensor cores truncate when they accumulate, which 64 steps do not show,
-// and each 128 of k of e4m3 products has scales of its own, which enter there.
+// accumulator to them every few stages (Kind): the tensor cores truncate when they accumulate, and each 128 of k of
+// e4m3 products has scales of its own, which enter there.
 //
 // What bounds it, and what it measured (d = 4096, m = 14336): few rows, reading the weights (gated bf16, 16 rows over
 // 8 groups: 281 us, 6.7 TB/s); many rows of bf16, the tensor cores under the power cap (8192 rows: plain 495 us, gated
@@ -318,7 +318,12 @@ struct Walk {
 template <bool E8, bool GATED, bool KN, bool XM>
 struct Kind {
     static constexpr int kStep = E8 ? 128 : 64;          // elements of k of a stage
-    static constexpr int kChunk = E8 ? 1 : 16;           // stages of an accumulator
+    // Stages of an accumulator, for bf16 outputs and for fp32 ones. A step of 16 of k takes off up to 2^-24 of the bf16 sum,
+    // always toward 0: Gaussian rows are off by 9.9e-7 (2-norm) after 16 stages, 64 steps, which an output rounded to
+    // bf16 (1.7e-3) does not show; after 8, 4 and 2 by 4.8e-7, 2.4e-7 and 1.6e-7. More hand-overs cost time where the tensor cores
+    // bound: 16, 8, 4 and 2 stages, 8192 rows, 14336 x 4096, bf16 outputs 496, 514, 541 and 592 us, fp32 ones 548, 608, 635
+    // and 653; 4096 x 14336 by rows of k, fp32 ones 532, 547, 554 and 605; of 40 to 2400 rows the same within 2% down to 4.
+    static constexpr int kChunk = E8 ? 1 : 16, kChunkF32 = E8 ? 1 : 4;
     static constexpr int kTileN = GATED ? 128 : 256;     // outputs of a tile
     static constexpr int kBoxes = GATED || KN ? 2 : 1;   // boxes of weights of a CTA's stage
     static constexpr int kOffW = XM ? kStageW : 0, kOffX = XM ? 0 : kStageW;  // in a stage: M's operand, then N's
@@ -348,6 +353,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
     __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cta_rank();
+    const int chunk_stages = L.y_f32 ? K::kChunkF32 : K::kChunk;
     const int steps = (L.k + K::kStep - 1) / K::kStep, w_tiles = (L.n + K::kTileN - 1) / K::kTileN;
 
     // ---- set-up: barriers, tensor memory, the groups' tiles ----
@@ -505,7 +511,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     // pass for some lanes alone, and all of them have to take part in the election. (A vote at every
                     // stage instead: 8192 rows, 4096 x 14336 e4m3, 366 us for 360.)
                     for (; k < k_end; ++chunk) {
-                        const int first = k, kc = min(k_end, k + K::kChunk), buf = chunk & (bufs - 1);
+                        const int first = k, kc = min(k_end, k + chunk_stages), buf = chunk & (bufs - 1);
                         const uint32_t d = tmem + (buf << (9 - lg));
                         for (; k < kc; ++k) {
                             // the accumulator is what is waited for longest: its barrier last
@@ -698,7 +704,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCtaThreads, 1) k_gr
                     }
                 }
             } else {
-                for (int left = sg.k1 - sg.k0; left > 0; left -= K::kChunk, ++chunk) {
+                for (int left = sg.k1 - sg.k0; left > 0; left -= chunk_stages, ++chunk) {
                     const int buf = chunk & (n_bufs - 1);
                     if (!filled(buf)) break;
 #pragma unroll

@@ -171,6 +171,26 @@ def test_layer_sizes(ts, form, rows):
     run(ts, dtype, [rows, rows // 2], n, k, gated, layout, F32, 0, seed=rows)
 
 
+@pytest.mark.parametrize("rows", [40, 700])
+@pytest.mark.parametrize("n,k", [(1024, 4096), (520, 14336)])
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_fp32_outputs_are_as_exact_as_sums_in_fp32(ts, form, n, k, rows):
+    """2-norm of the error of Gaussian sums. The tensor cores truncate at 2^-24 of the power of two below a sum: half of that
+    on average, 2.15e-8 of the sum (a mantissa's mean square reciprocal is 0.72^2), at each of 16 steps of 16 of k, during which
+    the sum is 0.69 of its last size on average: 2.4e-7, all toward 0. An addition of k / 256 such sums in fp32 rounds
+    at random, 2^-24 / sqrt 3 times 0.74 of a sum that grows with its root: 2.5e-8 sqrt(k / 512), 1.34e-7 at the most. Together
+    (2.4^2 + 1.34^2)^(1/2) = 2.8e-7. e4m3: 4 steps of 32 of k are truncated, 0.6e-7, there are k / 128 additions, 1.9e-7 at the
+    most, and a rounded product of two scales each, which k / 128 of them average out. Bounded by 3.3e-7, and twice that for a
+    product of two. (Accumulators of 1024 of k: 9.9e-7 and 1.8e-6.)"""
+    dtype, gated, layout = form
+    x, xs, w, ss, xd, wd = make(dtype, 1, n, k, rows, gated, layout, seed=n + rows)
+    mm = handle(ts, w, ss, gated, layout, rows)
+    y = mm.forward(x, None, xs, torch.empty(rows, n, device="cuda")).double()
+    p = [xd @ (m[0] if layout == "kn" else m[0].t()) for m in wd]
+    want = p[0].clamp(min=0) * p[1].clamp(min=0) if gated else p[0]
+    assert float((y - want).norm() / want.norm()) <= (6.6e-7 if gated else 3.3e-7)
+
+
 @pytest.mark.parametrize("form", FORMS, ids=IDS)
 def test_many_groups(ts, form):
     dtype, gated, layout = form
