@@ -532,7 +532,8 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
 
 /* Routing of the last forward (of its top_k), to host memory (synchronises `stream`): sel and w [tokens][top_k],
    which is nothing after a forward of no tokens. TS_ERR_INVALID_ARG before any forward, after one that failed on
-   its way, and after a layer of one expert without a router. */
+   its way, after a layer of one expert without a router, and where what ran last on the GPU had another number of
+   tokens or another top_k than the last call: the call was captured and not replayed yet, or an earlier one replayed. */
 ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel, float* w);
 /* As ts_ffn_get_error and ts_ffn_check_scratch. */
 ts_status ts_prompt_get_error(ts_prompt* p, cudaStream_t stream);

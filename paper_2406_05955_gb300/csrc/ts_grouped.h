@@ -24,6 +24,7 @@ struct RouteLaunch {
     int32_t* offsets;     // [n_experts + 1]
     int32_t* rows;        // [tokens * top_k]
     int32_t* slots;       // [tokens][top_k]
+    int32_t* shape;       // nullptr, or {tokens, top_k} of what sel and w hold
 };
 
 struct RowsLaunch {

@@ -192,13 +192,14 @@ struct ts_prompt {
     int32_t* slots = nullptr;
     int32_t* rows = nullptr;          // [max_tokens * top_k]
     int32_t* offsets = nullptr;       // [n_experts + 1]
+    int32_t* shape = nullptr;         // {tokens, top_k} of sel and w, by the forward that ran last (of a call or a replay)
     void* x = nullptr;                // [rows][d] in the experts' order, bf16 or e4m3
     float* x_scale = nullptr;         // [d / 128][rows]
     __nv_bfloat16* c = nullptr;       // [rows][m]
     void* cq = nullptr;               // [rows][m] e4m3
     float* c_scale = nullptr;         // [m / 128][rows]
     float* y = nullptr;               // [rows][d]
-    int last_tokens = 0, last_k = 0;  // of the last forward; last_k 0: none, without a router, or failed
+    int last_tokens = 0, last_k = 0;  // of the last call; last_k 0: none, without a router, or failed
 };
 
 extern "C" {
@@ -209,7 +210,7 @@ ts_status ts_route(const float* logits, int tokens, int n_experts, int top_k, in
         top_k > n_experts || !offsets || (long long)tokens * top_k >= 1ll << 30)
         return TS_ERR_INVALID_ARG;
     if (tokens > 0 && (!logits || !sel || !w || !rows || !slots)) return TS_ERR_INVALID_ARG;
-    return launched(launch_route({logits, tokens, n_experts, top_k, sel, w, offsets, rows, slots}, stream));
+    return launched(launch_route({logits, tokens, n_experts, top_k, sel, w, offsets, rows, slots, nullptr}, stream));
 }
 
 ts_status ts_gather_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, const int32_t* rows,
@@ -410,7 +411,7 @@ ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top
         const size_t tokens = (size_t)max_tokens, rows = tokens * (size_t)top_k, db = ((size_t)d + 127) / 128,
                      mb = ((size_t)m + 127) / 128;
         const size_t o_logits = ar.take(tokens * (size_t)n_experts * 4), o_sel = ar.take(rows * 4), o_w = ar.take(rows * 4),
-                     o_slots = ar.take(rows * 4), o_rows = ar.take(rows * 4), o_off = ar.take(((size_t)n_experts + 1) * 4),
+                     o_slots = ar.take(rows * 4), o_rows = ar.take(rows * 4), o_off = ar.take(((size_t)n_experts + 1) * 4), o_shape = ar.take(8),
                      o_x = ar.take(rows * (size_t)d * (e8 ? 1 : 2)), o_c = ar.take(rows * (size_t)m * 2),
                      o_y = ar.take(rows * (size_t)d * 4), o_xs = ar.take(e8 ? db * rows * 4 : 0),
                      o_cq = ar.take(e8 ? rows * (size_t)m : 0), o_cs = ar.take(e8 ? mb * rows * 4 : 0);
@@ -424,6 +425,7 @@ ts_status ts_prompt_create(ts_prompt** out, int d, int m, int n_experts, int top
             p->slots = ar.at<int32_t>(o_slots);
             p->rows = ar.at<int32_t>(o_rows);
             p->offsets = ar.at<int32_t>(o_off);
+            p->shape = ar.at<int32_t>(o_shape);
             p->x = ar.at<char>(o_x);
             p->c = ar.at<__nv_bfloat16>(o_c);
             p->y = ar.at<float>(o_y);
@@ -467,7 +469,7 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
         s = run_products(e->router, p->s, x, d, nullptr, 0, nullptr, tokens, p->logits, e->n_experts, true, stream);
         if (s == TS_OK)
             s = launched(launch_route(
-                {p->logits, tokens, e->n_experts, e->top_k, p->sel, p->w, p->offsets, p->rows, p->slots}, stream));
+                {p->logits, tokens, e->n_experts, e->top_k, p->sel, p->w, p->offsets, p->rows, p->slots, p->shape}, stream));
         if (s != TS_OK) return s;
         offsets = p->offsets;
         count = p->offsets + e->n_experts;
@@ -505,6 +507,12 @@ ts_status ts_prompt_forward(ts_prompt* p, ts_experts* e, const void* x, int toke
 ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel, float* w) {
     if (!p || p->last_k == 0 || !sel || !w) return TS_ERR_INVALID_ARG;
     const size_t bytes = (size_t)p->last_tokens * (size_t)p->last_k * 4;
+    if (bytes == 0) return cudaStreamSynchronize(stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
+    int32_t shape[2] = {0, 0};
+    if (cudaMemcpyAsync(shape, p->shape, sizeof shape, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
+        cudaStreamSynchronize(stream) != cudaSuccess)
+        return TS_ERR_CUDA;
+    if (shape[0] != p->last_tokens || shape[1] != p->last_k) return TS_ERR_INVALID_ARG;
     if (cudaMemcpyAsync(sel, p->sel, bytes, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
         cudaMemcpyAsync(w, p->w, bytes, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
         cudaStreamSynchronize(stream) != cudaSuccess)

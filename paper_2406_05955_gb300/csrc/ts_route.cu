@@ -209,7 +209,10 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
             first[tid] = scan - all + before;
             if (rank == 0) L.offsets[tid + 1] = scan;
         }
-        if (tid == 0 && rank == 0) L.offsets[0] = 0;
+        if (tid == 0 && rank == 0) {
+            L.offsets[0] = 0;
+            if (L.shape != nullptr) L.shape[0] = L.tokens, L.shape[1] = L.top_k;
+        }
     }
     __syncthreads();
     for (int i0 = begin; i0 < end; i0 += kAhead * kWarp) {

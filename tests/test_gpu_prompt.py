@@ -205,6 +205,36 @@ def test_routing_has_the_tokens_of_the_last_forward(ts):
     assert p.get_routing()[0].shape == (17, 2)
 
 
+def test_routing_of_captured_and_replayed_forwards(ts):
+    """That of the forward that ran last, or a refusal; never a mixture of two."""
+    layer = Layer(ts, 8, 128, 128, 2, seed=7)
+    p = ts.Prompt(layer.experts, 300)
+    x = wl.tokens(300, 128, seed=7).cuda()
+    p(x[:30])
+    long, _ = p.get_routing()
+    few, y = x[30:34].clone(), torch.zeros(4, 128, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        p.forward(few, y=y)
+    with pytest.raises(ts.TsError):
+        p.get_routing()                          # not replayed yet
+    graph.replay()
+    got, _ = p.get_routing()
+    assert got.shape == (4, 2)
+    p(few)
+    assert np.array_equal(p.get_routing()[0], got)
+    few.copy_(x[:4])
+    graph.replay()                               # as many tokens as the last call had
+    assert np.array_equal(p.get_routing()[0], long[:4])
+    for t in (30, 300):                          # (few and many tokens are routed by one and by two kernels)
+        p(x[:t])
+        assert np.array_equal(p.get_routing()[0][:30], long)
+        graph.replay()
+        with pytest.raises(ts.TsError):
+            p.get_routing()
+
+
 def test_same_as_the_layers_of_few_tokens(ts):
     """Experts.of(Moe) and Experts.of(Ffn) over the tokens that those layers take; c alone is rounded differently."""
     d, m, e = 512, 1024, 8
