@@ -430,7 +430,7 @@ ts_status ts_quant_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, i
 
 /*
  * y[t][:] = sum over j < top_k of w[t][j] * src[slots[t][j]][:], in order of j, in fp32.
- *   src       device [n_rows][n] TS_F32 or TS_BF16
+ *   src       device [n_rows][n] TS_F32 or TS_BF16, on a boundary of its elements
  *   slots, w  device [tokens][top_k]; a slot outside 0..n_rows-1 adds nothing
  *   top_k     1..8; n 1..2^30, at most 2^30 tokens
  *   y         device [tokens][n] fp32, overwritten
@@ -479,8 +479,8 @@ void ts_grouped_destroy(ts_grouped* h);
  *   offsets    device [n_groups + 1] int32, ascending, within 0..rows; NULL with one
  *              group: all rows. A group whose bounds are descending or out of range is
  *              skipped and recorded (ts_grouped_get_error: TS_ERR_BAD_INDEX).
- *   y, ldy     device, rows of n elements ldy apart (ydtype TS_BF16, rounded once, or TS_F32); rows
- *              that no group has are left as they were
+ *   y, ldy     device, rows of n elements ldy apart (ydtype TS_BF16, rounded once, or TS_F32), on a boundary
+ *              of its elements; rows that no group has are left as they were
  * One forward may be in flight per handle (a replay of a graph that holds one counts), and its device is the current
  * one (else TS_ERR_INVALID_ARG).
  */

@@ -18,6 +18,7 @@ namespace {
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 ts_status launched(cudaError_t e) { return e == cudaSuccess ? TS_OK : TS_ERR_CUDA; }
 int elem_size(ts_dtype dt) { return dt == TS_F32 ? 4 : dt == TS_BF16 ? 2 : 1; }
+bool aligned_for(const void* p, ts_dtype dt) { return (uintptr_t)p % (unsigned)elem_size(dt) == 0; }
 
 // Arguments that ts_gather_rows and ts_quant_rows share.
 ts_status check_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, int k, int max_rows, const void* out) {
@@ -236,7 +237,7 @@ ts_status ts_combine_rows(const void* src, ts_dtype dtype, int n_rows, int n, co
         return TS_ERR_INVALID_ARG;
     if (n > kMaxRows || tokens > kMaxRows) return TS_ERR_UNSUPPORTED;
     if (tokens == 0) return TS_OK;
-    if ((!src && n_rows > 0) || !slots || !w || !y) return TS_ERR_INVALID_ARG;
+    if ((!src && n_rows > 0) || !aligned_for(src, dtype) || !slots || !w || !y) return TS_ERR_INVALID_ARG;
     return launched(launch_combine({src, n_rows, n, slots, w, tokens, top_k, y}, dtype == TS_F32, stream));
 }
 
@@ -301,7 +302,8 @@ ts_status ts_grouped_forward(ts_grouped* h, const void* x, int64_t ldx, const fl
     if (!h || rows < 0 || rows > h->max_rows || (ydtype != TS_F32 && ydtype != TS_BF16)) return TS_ERR_INVALID_ARG;
     if (!offsets && h->p.n_groups != 1) return TS_ERR_INVALID_ARG;
     if (rows == 0) return TS_OK;
-    if (!here(h->s.device) || !x || !y || !aligned16(x) || ldx < h->p.k || ldx * elem_size(h->p.dt) % 16 != 0 || ldy < h->p.n)
+    if (!here(h->s.device) || !x || !y || !aligned16(x) || ldx < h->p.k || ldx * elem_size(h->p.dt) % 16 != 0 ||
+        ldy < h->p.n || !aligned_for(y, ydtype))
         return TS_ERR_INVALID_ARG;
     if (h->p.dt == TS_E4M3 ? (!x_scale || ld_scale < rows) : x_scale != nullptr) return TS_ERR_INVALID_ARG;
     return run_products(h->p, h->s, x, ldx, x_scale, ld_scale, offsets, rows, y, ldy, ydtype == TS_F32, stream, h->test_stall);

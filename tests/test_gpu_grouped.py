@@ -363,6 +363,26 @@ def test_a_wait_that_gives_up_last_is_reported(ts, form):
     assert mm.get_error() == 0 and mm.check_scratch() == 0
 
 
+def test_outputs_on_a_boundary_of_their_elements(ts):
+    """Others are refused by the host; these need not lie on one of 16 bytes."""
+    import ctypes
+
+    mm = ts.Grouped(torch.randn(72, 64, device="cuda").to(BF16), max_rows=4)
+    x = torch.randn(4, 64, device="cuda").to(BF16)
+    want = mm.forward(x, y=torch.zeros(4, 72, device="cuda"))
+    raw = torch.zeros(4 * 72 * 4 + 64, dtype=torch.uint8, device="cuda")
+    for size, code, bad, good in ((4, 0, (1, 2, 3, 6), (0, 4, 12)), (2, 1, (1, 3, 7), (0, 2, 6))):
+        def call(at):
+            return ts.lib().ts_grouped_forward(mm.handle, ctypes.c_void_p(x.data_ptr()), 64, None, 0, None, 4,
+                                               ctypes.c_void_p(raw.data_ptr() + at), 72, code, None)
+        for at in bad:
+            assert call(at) == 1, "TS_ERR_INVALID_ARG"
+        for at in good:
+            assert call(at) == 0
+            got = raw[at:at + 4 * 72 * size].clone().view(F32 if size == 4 else BF16).view(4, 72)
+            assert torch.equal(got, want.to(got.dtype))
+
+
 def test_refusals(ts):
     dev = "cuda"
     w = [torch.zeros(64, 64, dtype=BF16, device=dev) for _ in range(2)]

@@ -163,3 +163,12 @@ def test_the_stall_hook_wants_a_handle(lib):
     from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD
 
     assert lib.ts_grouped_set_test_stall(None, 1) == BAD
+
+
+def test_sums_by_token_want_whole_elements(lib):
+    """Rows that do not start on a boundary of their elements, which no load of an element takes."""
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_ERR_INVALID_ARG as BAD, TS_F32
+
+    g = GOOD
+    for src, dt in ((g + 1, TS_BF16), (g + 3, TS_BF16), (g + 1, TS_F32), (g + 2, TS_F32), (g + 6, TS_F32)):
+        assert lib.ts_combine_rows(src, dt, 4, 8, g, g, 2, 2, g, None) == BAD, (src, dt)
