@@ -473,11 +473,12 @@ class Moe:
     __call__ = forward
 
     def get_routing(self, batch: int, stream=None):
-        sel = np.zeros((batch, self.top_k), np.int32)
-        w = np.zeros((batch, self.top_k), np.float32)
+        room = max(batch, self.max_batch)  # the call writes as many tokens as the last forward had
+        sel = np.zeros((room, self.top_k), np.int32)
+        w = np.zeros((room, self.top_k), np.float32)
         _check(lib().ts_moe_get_routing(self.handle, _stream(stream), sel.ctypes.data_as(P),
                                         w.ctypes.data_as(P)), "ts_moe_get_routing")
-        return sel, w
+        return sel[:batch], w[:batch]
 
     def get_active(self, expert: int, token: int = -1, stream=None):
         g = np.zeros(self.m, np.int32)

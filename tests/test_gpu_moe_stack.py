@@ -223,3 +223,18 @@ def test_mistral_stack_32_layers_graph(ts):
     err = rel_l2(dy_gpu, dy_ref)
     print(f"free-running 32-layer divergence of h_32 - h_0: rel L2 {err:.3e} (reported, not gated)")
     assert np.isfinite(err)
+
+
+def test_routing_of_fewer_tokens_than_the_last_forward(ts):
+    """The first of them; what the call writes for the others lies in the binding's own buffers."""
+    d, m, e = 256, 256, 4
+    layers = [wl.ffn_layer(d, m, activation=0.25, dtype=torch.bfloat16, seed=i, device="cuda") for i in range(e)]
+    moe = ts.Moe(wl.router(e, d, seed=1).cuda(), [ts.Ffn(w.w_gate, w.w_up, w.w_down, max_batch=8) for w in layers],
+                 top_k=2, max_batch=8)
+    moe.forward(wl.tokens(8, d, seed=2).cuda())
+    sel, w = moe.get_routing(8)
+    for batch in (0, 1, 5):
+        few = moe.get_routing(batch)
+        assert few[0].base.shape[0] >= 8 and few[1].base.shape[0] >= 8
+        assert few[0].shape == (batch, 2)
+        assert (few[0] == sel[:batch]).all() and (few[1] == w[:batch]).all()
