@@ -192,6 +192,23 @@ def test_fp32_outputs_are_as_exact_as_sums_in_fp32(ts, form, n, k, rows):
 
 
 @pytest.mark.parametrize("form", FORMS, ids=IDS)
+@pytest.mark.parametrize("sizes", [[4097, 30], [30, 9000], [4096 + 300], [8192, 1]])
+def test_groups_of_several_sweeps(ts, form, sizes):
+    """More than the 4096 rows of a group that one sweep over its weights serves, the last sweep narrower than the others."""
+    dtype, gated, layout = form
+    run(ts, dtype, sizes, 520, 144, gated, layout, F32, 3, seed=sizes[0])
+    run(ts, dtype, sizes, 520, 144, gated, layout, BF16, 0, seed=sizes[0])
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+def test_one_long_group_among_many_empty_ones(ts, gated):
+    """Few rows for so many groups: the weights are the MMA's M, with several sweeps."""
+    sizes = [0] * 90
+    sizes[41], sizes[42], sizes[89] = 5000, 1, 20
+    run(ts, E4M3, sizes, 264, 272, gated, "nk", F32, 2, seed=3)
+
+
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
 def test_many_groups(ts, form):
     dtype, gated, layout = form
     sizes = [(i * 37) % 61 if i % 5 else 0 for i in range(256)]

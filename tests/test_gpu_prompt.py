@@ -396,6 +396,18 @@ def test_layer_sizes(ts):
     assert float((y.double() - want).norm() / want.norm()) <= 2.0 ** -8
 
 
+def test_e4m3_layer_sizes(ts):
+    """d = 4096, m = 14336, 2 of 4 experts: few rows, and enough of them to be the MMA's M. (Bound: test_e4m3_experts.)"""
+    layer = Layer(ts, 4, 4096, 14336, 2, seed=78, e8=True)
+    p = ts.Prompt(layer.experts, 600)
+    for tokens in (3, 600):
+        x = wl.tokens(tokens, 4096, seed=79).cuda()
+        y = p(x)
+        want, _ = layer.exact(x, *check_routing(layer, x, *p.get_routing()))
+        assert float((y.double() - want).norm() / want.norm()) <= 2.0 ** -3 + 2.0 ** -7
+        assert p.get_error() == 0 and p.check_scratch() == 0
+
+
 def test_refusals(ts):
     layer = Layer(ts, 4, 128, 128, 2, seed=1)
     p = ts.Prompt(layer.experts, 10)

@@ -228,6 +228,22 @@ def test_combine_rows(ts, dtype, t, k, n):
     assert ((got - terms.sum(1)).abs() <= 16 * 2.0 ** -24 * terms.abs().sum(1)).all()
 
 
+@pytest.mark.parametrize("t", [65535, 65536, 131071, 131073])
+@pytest.mark.parametrize("dtype,n", [(BF16, 8), (F32, 5)])
+def test_combine_rows_of_many_tokens(ts, t, dtype, n):
+    """More tokens than one launch's grid holds."""
+    g = gen(t)
+    src = torch.randn(1000, n, generator=g, device="cuda").to(dtype)
+    slots = torch.randint(-1, 1001, (t, 2), generator=g, device="cuda").to(torch.int32)
+    w = torch.randn(t, 2, generator=g, device="cuda")
+    out = torch.full((t + 1, n), 7.0, device="cuda")
+    ts.combine_rows(src, slots, w, out=out[:t])
+    ok = ((slots >= 0) & (slots < 1000))[..., None]
+    terms = torch.where(ok, w.double()[..., None] * src.double()[slots.clamp(0, 999).long()], 0.0)
+    assert ((out[:t].double() - terms.sum(1)).abs() <= 16 * 2.0 ** -24 * terms.abs().sum(1)).all()
+    assert (out[t] == 7.0).all()
+
+
 def test_combine_rows_without_rows(ts):
     src = torch.zeros(0, 64, device="cuda")
     y = ts.combine_rows(src, torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.ones(4, 2, device="cuda"))
