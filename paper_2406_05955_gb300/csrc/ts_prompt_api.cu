@@ -144,9 +144,10 @@ ts_status read_status(const ProductScratch& S, cudaStream_t stream) {
     if (cudaMemcpyAsync(&bits, S.status, sizeof bits, cudaMemcpyDeviceToHost, stream) != cudaSuccess ||
         cudaMemsetAsync(S.status, 0, sizeof bits, stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
         return TS_ERR_CUDA;
-    // a launch that gave up may have left tiles half counted
+    // a launch that gave up may have left tiles half counted (and the next one may be on another stream)
     if ((bits & kStatusTimeout) &&
-        cudaMemsetAsync(S.arrived, 0, grouped_arrived(S.pairs) * sizeof(unsigned), stream) != cudaSuccess)
+        (cudaMemsetAsync(S.arrived, 0, grouped_arrived(S.pairs) * sizeof(unsigned), stream) != cudaSuccess ||
+         cudaStreamSynchronize(stream) != cudaSuccess))
         return TS_ERR_CUDA;
     return bits & kStatusTimeout ? TS_ERR_TIMEOUT : bits & kStatusBadIndex ? TS_ERR_BAD_INDEX : TS_OK;
 }

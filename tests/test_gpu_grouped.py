@@ -380,6 +380,26 @@ def test_a_wait_that_gives_up_last_is_reported(ts, form):
     assert mm.get_error() == 0 and mm.check_scratch() == 0
 
 
+@pytest.mark.parametrize("form", [FORMS[0], FORMS[3]], ids=["bf16", "e4m3"])
+def test_a_forward_on_another_stream_after_a_timeout(ts, form):
+    """What get_error clears is clear when it returns."""
+    dtype, gated, layout = form
+    x, xs, w, ss, xd, wd = make(dtype, 1, 300, 8192, 20, gated, layout, seed=32)  # tiles in several parts
+    mm = handle(ts, w, ss, gated, layout, 20)
+    want = mm.forward(x, None, xs, torch.zeros(20, 300, device="cuda")).clone()
+    torch.cuda.synchronize()
+    mm.set_test_stall(True)
+    mm.forward(x, None, xs, torch.zeros(20, 300, device="cuda"))
+    torch.cuda.synchronize()
+    mm.set_test_stall(False)
+    assert mm.get_error() == 5
+    y, side = torch.zeros(20, 300, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    mm.forward(x, None, xs, y, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want) and mm.get_error() == 0
+
+
 def test_outputs_on_a_boundary_of_their_elements(ts):
     """Others are refused by the host; these need not lie on one of 16 bytes."""
     import ctypes
