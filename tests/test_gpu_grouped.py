@@ -209,6 +209,26 @@ def test_one_long_group_among_many_empty_ones(ts, gated):
 
 
 @pytest.mark.parametrize("form", FORMS, ids=IDS)
+@pytest.mark.parametrize("n,k", [(40, 32768), (32768, 64)])
+def test_rows_beyond_32_bits_of_elements(ts, form, n, k):
+    """x, or y, of more than 2^31 elements: the first rows, and the last ones, which are a group of their own."""
+    dtype, gated, layout = form
+    r, few = 65900, 60
+    _, _, w, ss, _, wd = make(dtype, 2, n, k, 1, gated, layout, seed=k)
+    x = torch.randn(r, k, generator=gen(3), device="cuda", dtype=BF16).to(dtype)
+    xs = torch.rand(-(-k // 128), r, generator=gen(4), device="cuda") + 0.5 if dtype == E4M3 else None
+    y = torch.zeros(r, n, device="cuda", dtype=BF16)
+    mm = handle(ts, w, ss, gated, layout, r)
+    mm.forward(x, torch.tensor([0, r - few, r], dtype=torch.int32, device="cuda"), xs, y)
+    assert mm.get_error() == 0
+    for at, e in ((slice(0, few), 0), (slice(r - few, r), 1)):
+        xd = x[at].double()
+        if xs is not None:
+            xd = xd * xs[:, at].double().repeat_interleave(128, 0)[:k].t()
+        check(y[at], y[at], [0, few], xd, [[ws[e]] for ws in wd], gated, layout, k)
+
+
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
 def test_many_groups(ts, form):
     dtype, gated, layout = form
     sizes = [(i * 37) % 61 if i % 5 else 0 for i in range(256)]

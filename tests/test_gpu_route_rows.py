@@ -244,6 +244,24 @@ def test_combine_rows_of_many_tokens(ts, t, dtype, n):
     assert (out[t] == 7.0).all()
 
 
+def test_rows_beyond_32_bits_of_elements(ts):
+    """Inputs and outputs of more than 2^31 elements: what lies at their ends."""
+    r, k = 65900, 32768
+    x = torch.randn(r, k, generator=gen(1), device="cuda", dtype=BF16)
+    order = torch.arange(r - 1, -1, -1, device="cuda").to(torch.int32)
+    assert torch.equal(ts.gather_rows(x, order), x.flip(0))
+    q, s = ts.quant_rows(x)
+    few_q, few_s = ts.quant_rows(x[-50:])
+    assert torch.equal(q[-50:].view(torch.uint8), few_q.view(torch.uint8)) and torch.equal(s[:, -50:], few_s)
+    del q, s
+    slots = torch.stack([order, order.flip(0)], 1).contiguous()
+    w = torch.rand(r, 2, generator=gen(2), device="cuda")
+    y = ts.combine_rows(x, slots, w)
+    for t in (0, 7, r - 1):
+        terms = w[t].double()[:, None] * x[slots[t].long()].double()
+        assert ((y[t].double() - terms.sum(0)).abs() <= 16 * 2.0 ** -24 * terms.abs().sum(0)).all()
+
+
 def test_combine_rows_without_rows(ts):
     src = torch.zeros(0, 64, device="cuda")
     y = ts.combine_rows(src, torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.ones(4, 2, device="cuda"))
