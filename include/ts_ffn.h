@@ -418,8 +418,8 @@ ts_status ts_gather_rows(const void* x, int64_t ldx, ts_dtype dtype, int n_src, 
 /*
  * Rows rounded to TS_E4M3 with an fp32 scale for each block of 128 elements:
  *     scale[b][r] = max |x[rows[r]][128 b .. 128 b + 127]| / 448
- * (at least 2^-100; 1 where the block is all zero) and q[r][i] = x / scale, rounded to the nearest, ties
- * to even. Arguments as ts_gather_rows (TS_BF16 or TS_F32; k a multiple of 16).
+ * (at least 2^-100; 1 where the block is all zero) and q[r][i] = x / scale (as an fp32 quotient), rounded to the
+ * nearest, ties to even. Arguments as ts_gather_rows (TS_BF16 or TS_F32; k a multiple of 16).
  *   q         device [max_rows][k] e4m3
  *   scale     device [ceil(k / 128)][max_rows] fp32: a block's scales lie together
  * NaN stays NaN in its place; a block that holds an infinity has an infinite scale and

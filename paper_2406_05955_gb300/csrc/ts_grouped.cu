@@ -17,12 +17,13 @@
 // e4m3 products has scales of its own, which enter there.
 //
 // What bounds it, and what it measured (d = 4096, m = 14336): few rows, reading the weights (gated bf16, 16 rows over
-// 8 groups: 281 us, 6.7 TB/s); many rows of bf16, the tensor cores under the power cap (8192 rows: plain 495 us, gated
-// 1020-1090 us, 1.75-1.9 PFLOP/s; a library's plain product takes 471-484); many rows of e4m3, handing an accumulator to the
-// summing warps and back at every 128 of k, 0.44 us where its MMAs take 0.27 (8192 rows: plain 330-360 us, gated over 8 groups
-// 688 us, 2.8 PFLOP/s; 2000 rows over 8 groups 208 us, of which reading the weights is 139); one row, latency (1 x 4096 x 14336
-// e4m3: 23 us, of which reading the weights is 9: launch, set-up, the first load, the join of a tile's parts and the stores
-// come one after another).
+// 8 groups: 281 us, 6.7 TB/s); many rows of bf16, the tensor cores under the power cap (8192 rows: plain 500 us, 1.9 PFLOP/s,
+// where a library's product takes 471-484; gated over 8 equal groups 1053-1165 us, 1.65-1.83 PFLOP/s, over ragged ones 1225-1310);
+// many rows of e4m3, handing an accumulator to the summing warps and back at every 128 of k, 0.44 us where its MMAs take
+// 0.27 (8192 rows: plain 345-374 us, gated over 8 equal groups 700 us, 2.75 PFLOP/s, over ragged ones 780; 2000 rows over 8
+// equal groups 230-254 us, of which reading the weights is 139, over ragged ones 284-333); one row, latency (1 x 4096 x 14336
+// e4m3: 23.8 us, of which reading the weights is 9: launch, set-up, the first load, the join of a tile's parts and the
+// stores come one after another).
 #include <cuda_fp8.h>
 
 #include "ts_grouped.h"
@@ -37,8 +38,8 @@ constexpr int kStageW = 16384;                  // weights of a stage: 128 rows 
 constexpr int kMaxStages = 12;
 constexpr int kStageMem = 192 * 1024;           // bytes of all stages
 constexpr int kMaxBufs = 4;                     // accumulators in tensor memory
-// Tiles of x that one sweep over the weights serves. 8192 rows, 14336 x 4096, gated e4m3: 4 tiles 726 us, 8 722, 16 710, 32 706;
-// plain bf16 523, 505, 502, 532; 16384 rows, gated bf16: 8 tiles 2215, 16 2170, 32 2270.
+// Tiles of x that one sweep over the weights serves. One group, 14336 x 4096, 8192 rows, plain bf16: 8 tiles 506-511 us, 16
+// 501, 32 527-535; 16384 rows, gated bf16: 2215, 2180, 2282; 8192 rows, gated e4m3: 700-740 with each.
 constexpr int kBand = 16;
 constexpr int kScaleWarps = 2, kScaleSlots = 4;
 // Fewest stages of a part of a tile. A part costs its pair about 3 us (written, made visible, counted and read again): with
@@ -73,7 +74,7 @@ struct Parts {
         return s < first ? s / (base + 1) : more + (s - first) / base;
     }
     // The same by a call: in the kernels of wide tiles the join's loop then leaves registers to the sums (gated e4m3, 8192 rows
-    // in 8 groups, 14336 x 4096: 766 -> 688 us); in those of narrow tiles it would cost 1 to 2 us.
+    // in 8 equal groups, 14336 x 4096: 766 -> 688 us); in those of narrow tiles it would cost 1 to 2 us.
     __device__ __noinline__ int begin_called(int q) const { return begin(q); }
 };
 

@@ -82,7 +82,8 @@ struct GroupedLaunch {
 
 // Whether an e4m3 product takes the rows of x as the MMA's M (see Kind in ts_grouped.cu): where the groups have enough of
 // them on average to fill a tile of 256 reasonably. Over 8 groups of 65 rows (d = 4096, m = 14336) gated products take 202
-// us so and 207 otherwise, of 49 201 and 195; down products of 128 rows 110 and 101.
+// us so and 207 otherwise, of 49 201 and 195; down products of 128 rows 110 and 101. All of that is over equal groups: the
+// host knows the buffer's rows and the number of groups, not which groups have rows, nor how many rows lie behind the last one.
 inline bool grouped_x_is_m(bool e4m3, bool gated, long long rows, int groups) {
     return e4m3 && rows > (gated ? 64ll : 128ll) * groups;
 }

@@ -8,7 +8,7 @@
 // Few tokens are picked by the CTA that places them: one launch instead of two.
 //
 // Latency bounds it: logits and lists are 2.9 MB for 8192 tokens of 64 experts, 0.4 us of memory time; picking and the
-// placing's chain of counts, cluster barrier and scan take 10.3 us (4 tokens of 8 experts: 4.2).
+// placing's chain of counts, cluster barrier and scan take 10.1 us (4 tokens of 8 experts: 3.7).
 #include "ts_grouped.h"
 #include "ts_kernels.cuh"
 
@@ -238,8 +238,9 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
 
 template <int G>
 cudaError_t launch(const RouteLaunch& a, cudaStream_t stream) {
-    // One launch as long as the one CTA picks in one round: 4 tokens of 8 experts 3.7 us (two launches
-    // 5.1), 1024 5.8 (6.6), 2048 8.1 (6.6); 128 tokens of 64 experts 7.9 (7.5), 512 25.0 (8.3).
+    // One launch as long as the one CTA picks in one round. Calls among others on a stream, which the caller bounds: 4 and 1024
+    // tokens of 8 experts and 128 of 64 take 6.8 us so and 8.8 in two launches. In a graph: 3.7 us (in two launches 3.9), 5.5 (5.0)
+    // and 6.8 (5.6); beyond one round the CTA falls behind: 2048 tokens of 8 experts 8.5 (5.2), 512 of 64 20.0 (6.5).
     const bool fused = (long long)a.tokens * G <= kPlaceThreads;
     if (fused) return launch_after(k_route_place<G>, launch_shape(dim3(1), kPlaceThreads, stream), a);
     const long long lanes = (long long)a.tokens * G;
