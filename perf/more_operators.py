@@ -222,7 +222,7 @@ def prepare(case, seed):
 # ---------------------------------------------------------------------------
 def _plain_adapt(s):
     """(y and the adapters' share, in the type of y; h)."""
-    case, x, y = s["case"], s["x"], s["y"].float()
+    case, x, y = s["case"], s["x"], s["y"].to(F32, copy=True)
     if "lists" not in s:  # each row times its own matrices
         some = s["ids"] >= 0
         i = s["ids"].clamp(min=0).long()
@@ -240,7 +240,7 @@ def _plain_adapt(s):
 def _plain_tune(s):
     case = s["case"]
     y, h = _plain_adapt(s)
-    dx, dy = s["dx"].float(), s["dy"].float()
+    dx, dy = s["dx"].to(F32, copy=True), s["dy"].float()
     x = s["x"].float() if s["x8"] is None else \
         s["x8"].float() * s["x_scale"].repeat_interleave(BLOCK, 0)[:case["k"]].t()
     for i, rows in enumerate(s["lists"]):
