@@ -539,6 +539,149 @@ ts_status ts_prompt_get_routing(ts_prompt* p, cudaStream_t stream, int32_t* sel,
 ts_status ts_prompt_get_error(ts_prompt* p, cudaStream_t stream);
 ts_status ts_prompt_check_scratch(ts_prompt* p, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Adapted layers: what serving and tuning low-rank adapters of a layer needs beside its frozen weights.
+ *     ts_list_rows              the rows of every adapter
+ *     ts_adapt_rows             each row's share of its adapter, added to a product; its backward pass by rows
+ *     ts_adapter_grads          gradients of the adapters
+ *     ts_drelu_rows             the gated activation of products computed apart, kept in 8 bits
+ *     ts_drelu_rows_backward    its backward pass from what was kept
+ *     ts_balance                loss on uneven routing, with the experts' counts
+ *     ts_route_backward         gradient of the router's logits
+ *     ts_combine_rows_backward  backward pass of ts_combine_rows
+ * The backward pass of the frozen bf16 weights themselves is products that are there: by x, dg . W_gate is ts_grouped_*
+ * with TS_KN, dy . W_down^T with TS_NK; that of ts_gather_rows is ts_combine_rows with weights of 1. All are
+ * asynchronous on `stream`, keep nothing between calls, do not allocate and may be captured in a CUDA graph. No
+ * result depends on timing: the same inputs give the same bits. The paper has no counterpart to any of them (its
+ * training is of all weights): these are readings.
+ */
+
+/*
+ * Rows by group: group i has list entries offsets[i] .. offsets[i + 1] - 1, ascending, and group n_groups the rows of none
+ * (an id outside 0..n_groups-1).
+ *   ids       device [n_rows] int32, n_rows below 2^30
+ *   n_groups  1..255
+ *   rows      device [n_rows] int32
+ *   offsets   device [n_groups + 2] int32; offsets[n_groups + 1] = n_rows
+ */
+ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* rows, int32_t* offsets, cudaStream_t stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared product: with i = ids[t],
+ *     h[t] = scale[i] * x[t] A_i^T,      out[t] = y[t] + h[t] B_i
+ * and h[t] = 0, out[t] = y[t] for a row of no adapter (an id outside 0..n_adapters-1). Given dy, B, A and dx for x, A, B
+ * and y it is the backward pass by rows: dh[t] = scale[i] * dy[t] B_i^T, dx[t] + dh[t] A_i.
+ *   x, ldx     device, rows of k bf16 (a multiple of 8), ldx apart
+ *   a, b       device [n_adapters][r][k] and [n_adapters][r][n] bf16, n a multiple of 8; row j of B_i is what
+ *              component j adds, as row j of w_down is
+ *   scale      device [n_adapters] fp32, NULL: 1
+ *   ranks      device [n_adapters] int32, NULL: r. Components from ranks[i] on count as 0 and are not read.
+ *   n_adapters 1..255, r 1..128
+ *   ids        device [rows] int32; read where there is no list: up to 64 rows
+ *   list, offsets   as ts_list_rows writes them from ids for n_adapters groups, or NULL
+ *   y, ldy     device, rows of n of ydtype (TS_BF16 or TS_F32), ldy apart
+ *   out, ldo   the same; may be y itself. NULL (y as well): h alone
+ *   h          device [rows][r] fp32, or NULL
+ * Rows of x, y and out and the matrices start on 16-byte boundaries. Weights are finite. Products are exact, sums are in
+ * fp32; h enters the second product in 16 (ydtype TS_BF16) or 24 significant bits; out is rounded once.
+ * TS_ERR_UNSUPPORTED: k or n above 2^24, or rows above 2^30.
+ */
+ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void* a, const void* b, const float* scale,
+                        const int32_t* ranks, int n_adapters, int r, int n, const int32_t* ids, const int32_t* list,
+                        const int32_t* offsets, const void* y, int64_t ldy, ts_dtype ydtype, void* out, int64_t ldo, float* h,
+                        cudaStream_t stream);
+
+/*
+ * Gradients of adapters: grad[i] = sum over the rows t of adapter i of h[t]^T x[t], so of B_i from h and dy, and of A_i from
+ * dh and x, with h and dh as ts_adapt_rows gives them.
+ *   h          device [rows][r] fp32
+ *   x, ldx     device, rows of k, ldx apart, TS_BF16 (k a multiple of 8) or TS_E4M3 (of 16)
+ *   x_scale, ld_scale  TS_E4M3: device [ceil(k / 128)][ld_scale] fp32, ld_scale >= rows (as ts_quant_rows writes
+ *              them). NULL for TS_BF16.
+ *   list, offsets   as ts_list_rows writes them
+ *   grad       device [n_adapters][r][k] fp32, on a 16-byte boundary: overwritten (0 for an adapter without rows), or
+ *              added to if accumulate is not 0
+ * Products and sums are in fp32, h in 24 significant bits.
+ */
+ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
+                           int64_t ld_scale, int rows, int k, int n_adapters, const int32_t* list, const int32_t* offsets,
+                           float* grad, int accumulate, cudaStream_t stream);
+
+/*
+ * The gated activation (Eq. 2) of rows whose two products were computed apart: c = max(0, g) max(0, u), 0 unless both are
+ * positive (so where either is NaN), for rows r < min(*n, rows); the others are left as they were. What its backward
+ * pass needs is kept in TS_E4M3: each factor where both are positive and 0 elsewhere, with a scale for each 128 of a row,
+ *     scale = the smallest power of two, at least 2^-100, with max / scale <= 448 (1 where all are 0)
+ *     q     = factor / scale rounded to the nearest, ties to even, but at least 2^-9 where the factor is positive
+ * (a factor above 1.875 * 2^127 is kept as that).
+ *   g, u       device, rows of m (a multiple of 16) of dtype (TS_BF16 or TS_F32), ldg and ldu apart
+ *   n          device int32 (as &offsets[n_experts] of ts_route), NULL: rows
+ *   c, ldc     device, rows of m bf16, ldc apart
+ *   q_gate, q_up   device [rows][m] e4m3, s_gate, s_up device [ceil(m / 128)][rows] fp32; or NULL, all four
+ * All rows start on 16-byte boundaries. TS_ERR_UNSUPPORTED: m above 2^24 or rows above 2^30.
+ */
+ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, ts_dtype dtype, const int32_t* n, int rows,
+                        int m, void* c, int64_t ldc, void* q_gate, void* q_up, float* s_gate, float* s_up,
+                        cudaStream_t stream);
+
+/*
+ * The backward pass of ts_drelu_rows from what it kept, with factors g = s_gate q_gate and u = s_up q_up:
+ *     dg = dc u,  du = dc g,  c = g u  where both are positive, 0 elsewhere (whatever dc is there)
+ * rounded to bf16 (c is exact). Rows from min(*n, rows) on are left as they were.
+ *   dc, ldd    device, rows of m of dtype (TS_BF16 or TS_F32), ldd apart
+ *   dg, du     device, rows of m bf16, ldg and ldu apart
+ *   c, ldc     the same, for the gradient of the down product's weights; or NULL
+ */
+ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, const void* q_gate, const void* q_up,
+                                 const float* s_gate, const float* s_up, const int32_t* n, int rows, int m, void* dg,
+                                 int64_t ldg, void* du, int64_t ldu, void* c, int64_t ldc, cudaStream_t stream);
+
+/*
+ * How evenly tokens are routed. A token is live if any of its logits is above -infinity; p[t] is the softmax over its
+ * logits (-infinity and NaN count as none, equal +infinities share), and over the live tokens and the picks
+ *     share[e] = mean of p[t][e],   loss = n_experts * sum_e (counts[e] / picks) share[e]
+ * which is 1 where both are even, and 0 without picks.
+ *   logits     device [tokens][n_experts] fp32; sel device [tokens][top_k], as ts_route takes and gives them (an
+ *              entry outside 0..n_experts-1 is no pick)
+ *   loss       device [1] fp32
+ *   counts     device [n_experts] int32: picks of each expert
+ *   share      device [n_experts] fp32
+ *   totals     device [2] int32: live tokens, picks
+ *   work       device, ts_balance_work(tokens, n_experts) fp32, not shared by calls in flight at once
+ */
+long long ts_balance_work(int tokens, int n_experts); /* -1: sizes that ts_balance refuses */
+ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32_t* sel, int top_k, float* loss,
+                     int32_t* counts, float* share, int32_t* totals, float* work, cudaStream_t stream);
+
+/*
+ * Gradient of the router's logits, overwritten, from the routing weights' (dw, or NULL) and the balance loss's (dloss with
+ * the counts and totals of ts_balance for these logits, or all three NULL):
+ *     dlogits[t][e] = sum over the picks j of e of w_j (dw_j - sum_i w_i dw_i)
+ *                   + dloss n_experts / (picks * live tokens) p_e (counts[e] - sum_f counts[f] p_f)
+ * The counts have no gradient. A token without a pick, and an expert of logit -infinity or NaN, gets 0.
+ *   logits     device [tokens][n_experts] fp32 (with dloss); sel, w device [tokens][top_k] as ts_route gives them, dw
+ *              the same (with dw)
+ *   dloss      device [1] fp32
+ *   dlogits    device [tokens][n_experts] fp32
+ */
+ts_status ts_route_backward(const float* logits, int tokens, int n_experts, const int32_t* sel, const float* w, int top_k,
+                            const float* dw, const int32_t* counts, const int32_t* totals, const float* dloss, float* dlogits,
+                            cudaStream_t stream);
+
+/*
+ * The backward pass of ts_combine_rows for slots as ts_route gives them, where a row belongs to one token:
+ *     dsrc[r] = (sum over the j with slots[t][j] = r of w[t][j]) dy[t]   for t = rows[r], if slots names r there
+ *     dw[t][j] = sum over i of dy[t][i] src[slots[t][j]][i]              0 for a slot outside 0..n_rows-1
+ * Other rows of dsrc are left as they were.
+ *   dy         device [tokens][n] of dydtype (TS_F32 or TS_BF16)
+ *   src, dsrc  device [n_rows][n] of dtype (TS_F32 or TS_BF16), two buffers
+ *   rows       device [n_rows] int32: token of each row
+ *   slots, w, dw   device [tokens][top_k], top_k 1..8; n 1..2^30, at most 2^30 tokens
+ */
+ts_status ts_combine_rows_backward(const void* dy, ts_dtype dydtype, const void* src, ts_dtype dtype, int n_rows, int n,
+                                   const int32_t* slots, const float* w, const int32_t* rows, int tokens, int top_k,
+                                   void* dsrc, float* dw, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

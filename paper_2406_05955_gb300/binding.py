@@ -89,6 +89,15 @@ SIGNATURES = {
     "ts_prompt_get_routing": (I, [P, P, P, P]),
     "ts_prompt_get_error": (I, [P, P]),
     "ts_prompt_check_scratch": (I, [P, P]),
+    "ts_list_rows": (I, [P, I, I, P, P, P]),
+    "ts_adapt_rows": (I, [P, L64, I, I, P, P, P, P, I, I, I, P, P, P, P, L64, I, P, L64, P, P]),
+    "ts_adapter_grads": (I, [P, I, P, L64, I, P, L64, I, I, I, P, P, P, I, P]),
+    "ts_drelu_rows": (I, [P, L64, P, L64, I, P, I, I, P, L64, P, P, P, P, P]),
+    "ts_drelu_rows_backward": (I, [P, L64, I, P, P, P, P, P, I, I, P, L64, P, L64, P, L64, P]),
+    "ts_balance_work": (ctypes.c_longlong, [I, I]),
+    "ts_balance": (I, [P, I, I, P, I, P, P, P, P, P, P]),
+    "ts_route_backward": (I, [P, I, I, P, P, I, P, P, P, P, P, P]),
+    "ts_combine_rows_backward": (I, [P, I, P, I, I, I, P, P, P, I, I, P, P, P]),
 }
 
 

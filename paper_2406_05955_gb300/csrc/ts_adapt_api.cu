@@ -1,0 +1,168 @@
+// ts_adapt_api.cu -- the C ABI of what an adapted layer needs beside its frozen weights (include/ts_ffn.h): argument checks
+// and launches. None of these operators keeps anything between calls.
+#include <stdint.h>
+
+#include "ts_adapt.h"
+#include "ts_ffn.h"
+#include "ts_grouped.h"
+
+using namespace tsffn;
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+ts_status launched(cudaError_t e) { return e == cudaSuccess ? TS_OK : TS_ERR_CUDA; }
+int elem_size(ts_dtype dt) { return dt == TS_F32 ? 4 : dt == TS_BF16 ? 2 : 1; }
+
+// Rows of `cols` elements, `ld` apart, each on a 16-byte boundary.
+bool rows_ok(const void* p, int64_t ld, int cols, ts_dtype dt) {
+    return p != nullptr && aligned16(p) && ld >= cols && ld * elem_size(dt) % 16 == 0;
+}
+
+// The counts that ts_adapt_rows and ts_adapter_grads share.
+ts_status check_adapters(int rows, int k, int n_adapters, int r) {
+    if (rows < 0 || k < 1 || n_adapters < 1 || n_adapters > kMaxAdapters || r < 1 || r > kMaxRank) return TS_ERR_INVALID_ARG;
+    return rows > kMaxRows || k > kMaxRowElems ? TS_ERR_UNSUPPORTED : TS_OK;
+}
+
+ts_status check_routing(int tokens, int n_experts, int top_k) {
+    return tokens < 0 || n_experts < 1 || n_experts > kMaxRouteExperts || top_k < 1 || top_k > kMaxRouteK ||
+                   top_k > n_experts || (long long)tokens * top_k >= 1ll << 30
+               ? TS_ERR_INVALID_ARG
+               : TS_OK;
+}
+
+// Sizes of the gated activation: rows of e4m3 numbers start on 16-byte boundaries.
+ts_status check_drelu(ts_dtype dtype, int rows, int m) {
+    if ((dtype != TS_F32 && dtype != TS_BF16) || rows < 0 || m < 1 || m % 16 != 0) return TS_ERR_INVALID_ARG;
+    return rows > kMaxRows || m > kMaxRowElems ? TS_ERR_UNSUPPORTED : TS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* rows, int32_t* offsets, cudaStream_t stream) {
+    if (n_rows < 0 || n_rows >= 1 << 30 || n_groups < 1 || n_groups > kMaxAdapters || !aligned4(ids) || !aligned4(rows) ||
+        !offsets || !aligned4(offsets) || (n_rows > 0 && (!ids || !rows)))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_list_rows(ids, n_rows, n_groups, rows, offsets, stream));
+}
+
+ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void* a, const void* b, const float* scale,
+                        const int32_t* ranks, int n_adapters, int r, int n, const int32_t* ids, const int32_t* list,
+                        const int32_t* offsets, const void* y, int64_t ldy, ts_dtype ydtype, void* out, int64_t ldo, float* h,
+                        cudaStream_t stream) {
+    ts_status s = check_adapters(rows, k, n_adapters, r);
+    if (s == TS_OK) s = check_adapters(rows, n, n_adapters, r);
+    if (s != TS_OK) return s;
+    if ((ydtype != TS_F32 && ydtype != TS_BF16) || k % 8 != 0 || n % 8 != 0) return TS_ERR_INVALID_ARG;
+    if (rows == 0) return TS_OK;
+    if (!rows_ok(x, ldx, k, TS_BF16) || !a || !aligned16(a) || !b || !aligned16(b) || !aligned4(scale) || !aligned4(ranks) ||
+        !aligned4(h))
+        return TS_ERR_INVALID_ARG;
+    if (list ? !offsets || !aligned4(list) || !aligned4(offsets) : !ids || !aligned4(ids) || rows > kFewRows)
+        return TS_ERR_INVALID_ARG;
+    if (!out ? y != nullptr || !h : !rows_ok(y, ldy, n, ydtype) || !rows_ok(out, ldo, n, ydtype) || (out == y && ldo != ldy))
+        return TS_ERR_INVALID_ARG;
+    if (prepare_adapt() != cudaSuccess) return TS_ERR_CUDA;
+    return launched(launch_adapt({x, ldx, rows, k, a, b, scale, ranks, n_adapters, r, n, list ? nullptr : ids, list,
+                                  list ? offsets : nullptr, y, ldy, out, ldo, h},
+                                 ydtype == TS_F32, stream));
+}
+
+ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
+                           int64_t ld_scale, int rows, int k, int n_adapters, const int32_t* list, const int32_t* offsets,
+                           float* grad, int accumulate, cudaStream_t stream) {
+    const ts_status s = check_adapters(rows, k, n_adapters, r);
+    if (s != TS_OK) return s;
+    const bool e8 = xdtype == TS_E4M3;
+    if ((!e8 && xdtype != TS_BF16) || k % (e8 ? 16 : 8) != 0 || !grad || !aligned16(grad) || !offsets || !aligned4(offsets))
+        return TS_ERR_INVALID_ARG;
+    if (rows > 0 && (!h || !aligned4(h) || !rows_ok(x, ldx, k, xdtype) || !list || !aligned4(list) ||
+                     (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
+        return TS_ERR_INVALID_ARG;
+    if (prepare_adapt() != cudaSuccess) return TS_ERR_CUDA;
+    return launched(launch_adapter_grads(
+        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0}, e8, stream));
+}
+
+ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, ts_dtype dtype, const int32_t* n, int rows,
+                        int m, void* c, int64_t ldc, void* q_gate, void* q_up, float* s_gate, float* s_up,
+                        cudaStream_t stream) {
+    const ts_status s = check_drelu(dtype, rows, m);
+    if (s != TS_OK || rows == 0) return s;
+    if (!rows_ok(g, ldg, m, dtype) || !rows_ok(u, ldu, m, dtype) || !rows_ok(c, ldc, m, TS_BF16) || !aligned4(n))
+        return TS_ERR_INVALID_ARG;
+    const bool kept = q_gate != nullptr;
+    if (kept != (q_up != nullptr) || kept != (s_gate != nullptr) || kept != (s_up != nullptr) || !aligned16(q_gate) ||
+        !aligned16(q_up) || !aligned4(s_gate) || !aligned4(s_up))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_drelu({g, u, ldg, ldu, n, rows, m, c, ldc, static_cast<uint8_t*>(q_gate),
+                                  static_cast<uint8_t*>(q_up), s_gate, s_up},
+                                 dtype == TS_F32, stream));
+}
+
+ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, const void* q_gate, const void* q_up,
+                                 const float* s_gate, const float* s_up, const int32_t* n, int rows, int m, void* dg,
+                                 int64_t ldg, void* du, int64_t ldu, void* c, int64_t ldc, cudaStream_t stream) {
+    const ts_status s = check_drelu(dtype, rows, m);
+    if (s != TS_OK || rows == 0) return s;
+    if (!rows_ok(dc, ldd, m, dtype) || !rows_ok(dg, ldg, m, TS_BF16) || !rows_ok(du, ldu, m, TS_BF16) || !aligned4(n) ||
+        (c && !rows_ok(c, ldc, m, TS_BF16)) || !q_gate || !aligned16(q_gate) || !q_up || !aligned16(q_up) || !s_gate ||
+        !aligned4(s_gate) || !s_up || !aligned4(s_up))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_drelu_backward({dc, ldd, static_cast<const uint8_t*>(q_gate), static_cast<const uint8_t*>(q_up),
+                                           s_gate, s_up, n, rows, m, dg, du, c, ldg, ldu, ldc},
+                                          dtype == TS_F32, stream));
+}
+
+long long ts_balance_work(int tokens, int n_experts) {
+    return check_routing(tokens, n_experts, 1) == TS_OK ? (long long)balance_work(tokens, n_experts) : -1;
+}
+
+ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32_t* sel, int top_k, float* loss,
+                     int32_t* counts, float* share, int32_t* totals, float* work, cudaStream_t stream) {
+    const ts_status s = check_routing(tokens, n_experts, top_k);
+    if (s != TS_OK) return s;
+    if (!loss || !aligned4(loss) || !counts || !aligned4(counts) || !share || !aligned4(share) || !totals ||
+        !aligned4(totals) || !work || !aligned4(work) || !aligned4(logits) || !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_balance({logits, tokens, n_experts, top_k, sel, loss, counts, share, totals, work}, stream));
+}
+
+ts_status ts_route_backward(const float* logits, int tokens, int n_experts, const int32_t* sel, const float* w, int top_k,
+                            const float* dw, const int32_t* counts, const int32_t* totals, const float* dloss, float* dlogits,
+                            cudaStream_t stream) {
+    const ts_status s = check_routing(tokens, n_experts, top_k);
+    if (s != TS_OK) return s;
+    const bool balance = counts != nullptr;
+    if (balance != (totals != nullptr) || balance != (dloss != nullptr) || !aligned4(counts) || !aligned4(totals) ||
+        !aligned4(dloss))
+        return TS_ERR_INVALID_ARG;
+    if (tokens == 0) return TS_OK;
+    if ((!balance && !dw) || (balance && !logits) || !aligned4(logits) || !dlogits || !aligned4(dlogits) || !aligned4(dw) || !aligned4(sel) ||
+        !aligned4(w) || (dw && (!sel || !w)))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_route_backward({logits, tokens, n_experts, top_k, sel, w, dw, counts, totals, dloss, dlogits}, stream));
+}
+
+ts_status ts_combine_rows_backward(const void* dy, ts_dtype dydtype, const void* src, ts_dtype dtype, int n_rows, int n,
+                                   const int32_t* slots, const float* w, const int32_t* rows, int tokens, int top_k,
+                                   void* dsrc, float* dw, cudaStream_t stream) {
+    if ((dtype != TS_F32 && dtype != TS_BF16) || (dydtype != TS_F32 && dydtype != TS_BF16) || n_rows < 0 || n < 1 ||
+        tokens < 0 || top_k < 1 || top_k > kMaxRouteK)
+        return TS_ERR_INVALID_ARG;
+    if (n > kMaxRows || tokens > kMaxRows) return TS_ERR_UNSUPPORTED;
+    if (tokens == 0) return TS_OK;
+    const unsigned size = (unsigned)elem_size(dtype);
+    if (!dy || (uintptr_t)dy % (unsigned)elem_size(dydtype) != 0 || (uintptr_t)src % size != 0 || (uintptr_t)dsrc % size != 0 ||
+        (n_rows > 0 && (!src || !rows || !dsrc || src == dsrc)) || !aligned4(rows) || !slots || !aligned4(slots) || !w ||
+        !aligned4(w) || !dw || !aligned4(dw))
+        return TS_ERR_INVALID_ARG;
+    return launched(launch_combine_backward({dy, src, n_rows, n, slots, w, rows, tokens, top_k, dsrc, dw}, dydtype == TS_F32,
+                                            dtype == TS_F32, stream));
+}
+
+}  // extern "C"

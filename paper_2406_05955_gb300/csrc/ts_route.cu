@@ -1,4 +1,5 @@
-// ts_route.cu -- routing of many tokens (Sec. 4: top_k of the experts by router logit, softmax over the picked ones).
+// ts_route.cu -- routing of many tokens (Sec. 4: top_k of the experts by router logit, softmax over the picked ones), and
+// the placing alone for rows whose groups are given (ts_list_rows).
 //
 // Picking: as many lanes of a token as give each at most 8 experts hold its logits in registers; top_k rounds of a
 // maximum over them (a lower expert wins a tie). Placing: the picks are sorted by expert, in token order, by a counting
@@ -130,15 +131,22 @@ __device__ __forceinline__ unsigned same_expert(int e, int bits) {
     return same;
 }
 
-// The picks i, i + 32, ... of a lane, all on their way at once; -1 behind the last one.
+// The picks i, i + 32, ... of a lane, all on their way at once; -1 behind the last one. LIST: given ones, which may be out
+// of range: the last group has those.
 constexpr int kAhead = 8;
+template <bool LIST>
 __device__ __forceinline__ void load_picks(const RouteLaunch& L, int i, int end, int (&e)[kAhead]) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) e[u] = i + u * kWarp < end ? L.sel[i + u * kWarp] : -1;
+    if constexpr (LIST) {
+        const unsigned last = (unsigned)L.n_experts - 1u;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) e[u] = i + u * kWarp < end ? (int)min((unsigned)e[u], last) : -1;
+    }
 }
 
-// G > 0: picks first (one CTA).
-template <int G>
+// G > 0: picks first (one CTA). LIST: the rows of given groups (ts_list_rows), one pick a row and no slots.
+template <int G, bool LIST = false>
 __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch L) {
     __shared__ int count[kPlaceWarps][kMaxRouteExperts];
     __shared__ int total_here[kMaxRouteExperts], first[kMaxRouteExperts], sums[kMaxRouteExperts / kWarp];
@@ -159,7 +167,7 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
     if constexpr (G == 0) pdl_wait();  // for the picks
     for (int i0 = begin; i0 < end; i0 += kAhead * kWarp) {
         int es[kAhead];
-        load_picks(L, i0 + lane, end, es);
+        load_picks<LIST>(L, i0 + lane, end, es);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (i0 + u * kWarp >= end) break;
@@ -217,7 +225,7 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
     __syncthreads();
     for (int i0 = begin; i0 < end; i0 += kAhead * kWarp) {
         int es[kAhead];
-        load_picks(L, i0 + lane, end, es);
+        load_picks<LIST>(L, i0 + lane, end, es);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int i = i0 + u * kWarp + lane, e = es[u];
@@ -228,12 +236,29 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
             __syncwarp();
             if (e >= 0) {
                 if (ahead == 0u) count[warp][e] += __popc(same);
-                L.rows[at] = (int32_t)((unsigned)i / (unsigned)L.top_k);
+                L.rows[at] = LIST ? i : (int32_t)((unsigned)i / (unsigned)L.top_k);
             }
-            if (i < end) L.slots[i] = at;
+            if (!LIST && i < end) L.slots[i] = at;
             __syncwarp();
         }
     }
+}
+
+// The placing, by a cluster of `ctas` CTAs.
+cudaError_t launch_place(void (*kernel)(RouteLaunch), const RouteLaunch& a, unsigned ctas, cudaStream_t stream) {
+    if (ctas > kPlaceCtas) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = launch_shape(dim3(ctas), kPlaceThreads, stream);
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {ctas, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <int G>
@@ -248,20 +273,7 @@ cudaError_t launch(const RouteLaunch& a, cudaStream_t stream) {
         k_route_pick<G>, launch_shape(dim3((unsigned)((lanes + kPickThreads - 1) / kPickThreads)), kPickThreads, stream), a);
     if (picked != cudaSuccess) return picked;
     // 16 CTAs from 16384 picks on: 8192 tokens, 6 of 64 experts, 14.5 -> 11.9 us; 4096 tokens, 2 of 8, 6.8 -> 7.1.
-    const unsigned ctas = (long long)a.tokens * a.top_k >= 16384 ? kPlaceMost : kPlaceCtas;
-    if (ctas > kPlaceCtas) {
-        const cudaError_t e = cudaFuncSetAttribute(k_route_place<0>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = launch_shape(dim3(ctas), kPlaceThreads, stream);
-    cudaLaunchAttribute at[2]{};
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {ctas, 1, 1};
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_route_place<0>, a);
+    return launch_place(k_route_place<0>, a, (long long)a.tokens * a.top_k >= 16384 ? kPlaceMost : kPlaceCtas, stream);
 }
 
 }  // namespace
@@ -274,6 +286,14 @@ cudaError_t launch_route(const RouteLaunch& a, cudaStream_t stream) {
     if (lanes <= 8) return launch<8>(a, stream);
     if (lanes <= 16) return launch<16>(a, stream);
     return launch<32>(a, stream);
+}
+
+cudaError_t launch_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* rows, int32_t* offsets,
+                             cudaStream_t stream) {
+    const RouteLaunch a{nullptr, n_rows, n_groups + 1, 1, const_cast<int32_t*>(ids), nullptr, offsets, rows, nullptr, nullptr};
+    // one CTA as long as its warps have one round of rows each
+    const unsigned ctas = n_rows >= 16384 ? kPlaceMost : n_rows > kPlaceThreads ? kPlaceCtas : 1;
+    return launch_place(k_route_place<0, true>, a, ctas, stream);
 }
 
 }  // namespace tsffn

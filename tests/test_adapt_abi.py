@@ -1,0 +1,136 @@
+"""The entry points of adapted layers reject bad arguments before they touch the device (no GPU needed)."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2406_05955_gb300 import binding, build
+
+    build.build()
+    return binding.lib()
+
+
+G = 0x10000
+
+
+def call(fn, defaults, **kw):
+    assert set(kw) <= set(defaults), kw
+    return fn(*{**defaults, **kw}.values())
+
+
+def test_list_rows(lib):
+    from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD
+
+    good = {"ids": G, "n": 4, "groups": 8, "rows": G, "offsets": G, "stream": None}
+    for kw in ({"ids": None}, {"ids": G + 2}, {"n": -1}, {"n": 1 << 30}, {"groups": 0}, {"groups": 256}, {"rows": None},
+               {"rows": G + 1}, {"offsets": None}, {"offsets": G + 2}):
+        assert call(lib.ts_list_rows, good, **kw) == BAD, kw
+
+
+def test_adapt_rows(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_INT4, TS_OK)
+
+    good = {"x": G, "ldx": 64, "rows": 4, "k": 64, "a": G, "b": G, "scale": G, "ranks": None, "adapters": 3, "r": 8, "n": 32,
+            "ids": G, "list": None, "offsets": None, "y": G, "ldy": 32, "dt": TS_BF16, "out": G, "ldo": 32, "h": None,
+            "stream": None}
+    for kw in ({"x": None}, {"x": G + 8}, {"ldx": 63}, {"ldx": 68}, {"rows": -1}, {"k": 0}, {"k": 60}, {"a": None},
+               {"a": G + 2}, {"b": None}, {"b": G + 8}, {"scale": G + 2}, {"ranks": G + 1}, {"adapters": 0},
+               {"adapters": 256}, {"r": 0}, {"r": 129}, {"n": 0}, {"n": 36}, {"ids": None}, {"ids": G + 2},
+               {"rows": 65}, {"list": G}, {"list": G + 2, "offsets": G}, {"list": G, "offsets": G + 2}, {"y": None},
+               {"y": G + 4}, {"ldy": 31}, {"ldy": 36}, {"dt": TS_INT4}, {"dt": TS_E4M3}, {"dt": 9}, {"out": G + 8},
+               {"ldo": 24}, {"ldo": 40}, {"out": None}, {"out": None, "y": None}, {"h": G + 2},
+               {"dt": TS_F32, "y": G + 8}):
+        assert call(lib.ts_adapt_rows, good, **kw) == BAD, kw
+    big = 1 << 24
+    for kw in ({"k": big + 8, "ldx": big + 8}, {"n": big + 8, "ldy": big + 8, "ldo": big + 8},
+               {"rows": (1 << 30) + 1, "list": G, "offsets": G}):
+        assert call(lib.ts_adapt_rows, good, **kw) == UNSUPPORTED, kw
+    assert call(lib.ts_adapt_rows, good, rows=0, x=None, y=None, out=None, ids=None) == TS_OK
+
+
+def test_adapter_grads(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32)
+
+    good = {"h": G, "r": 8, "x": G, "ldx": 64, "dt": TS_BF16, "x_scale": None, "ld_scale": 0, "rows": 4, "k": 64,
+            "adapters": 3, "list": G, "offsets": G, "grad": G, "accumulate": 0, "stream": None}
+    e8 = {"dt": TS_E4M3, "x_scale": G, "ld_scale": 4}
+    for kw in ({"h": None}, {"h": G + 1}, {"r": 0}, {"r": 129}, {"x": None}, {"x": G + 8}, {"ldx": 56}, {"ldx": 68},
+               {"dt": TS_F32}, {"x_scale": G}, {"rows": -1}, {"k": 0}, {"k": 60}, {"adapters": 0}, {"adapters": 256},
+               {"list": None}, {"offsets": None}, {"grad": None}, {"grad": G + 4}, {**e8, "x_scale": None},
+               {**e8, "ld_scale": 3}, {**e8, "k": 56}, {**e8, "ldx": 72}):
+        assert call(lib.ts_adapter_grads, good, **kw) == BAD, kw
+    assert call(lib.ts_adapter_grads, good, k=(1 << 24) + 8, ldx=(1 << 24) + 8) == UNSUPPORTED
+
+
+def test_drelu_rows(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_OK)
+
+    good = {"g": G, "ldg": 64, "u": G, "ldu": 64, "dt": TS_BF16, "n": None, "rows": 4, "m": 64, "c": G, "ldc": 64, "qg": G,
+            "qu": G, "sg": G, "su": G, "stream": None}
+    for kw in ({"g": None}, {"g": G + 8}, {"ldg": 63}, {"ldg": 68}, {"u": None}, {"u": G + 2}, {"ldu": 48}, {"dt": TS_E4M3},
+               {"n": G + 2}, {"rows": -1}, {"m": 0}, {"m": 72}, {"c": None}, {"c": G + 4}, {"ldc": 60}, {"qg": None},
+               {"qu": None}, {"sg": None}, {"su": None}, {"qg": G + 8}, {"su": G + 2}, {"dt": TS_F32, "g": G + 4}):
+        assert call(lib.ts_drelu_rows, good, **kw) == BAD, kw
+    assert call(lib.ts_drelu_rows, good, m=(1 << 24) + 16) == UNSUPPORTED
+    assert call(lib.ts_drelu_rows, good, rows=0, g=None, c=None) == TS_OK
+
+    good = {"dc": G, "ldd": 64, "dt": TS_F32, "qg": G, "qu": G, "sg": G, "su": G, "n": None, "rows": 4, "m": 64, "dg": G,
+            "ldg": 64, "du": G, "ldu": 64, "c": None, "ldc": 0, "stream": None}
+    for kw in ({"dc": None}, {"dc": G + 8}, {"ldd": 62}, {"dt": TS_E4M3}, {"qg": None}, {"qu": G + 8}, {"sg": None},
+               {"su": G + 1}, {"n": G + 2}, {"rows": -1}, {"m": 8}, {"dg": None}, {"ldg": 60}, {"du": G + 4}, {"ldu": 63},
+               {"c": G + 8, "ldc": 64}, {"c": G, "ldc": 56}):
+        assert call(lib.ts_drelu_rows_backward, good, **kw) == BAD, kw
+    assert call(lib.ts_drelu_rows_backward, good, rows=(1 << 30) + 1) == UNSUPPORTED
+
+
+def test_balance(lib):
+    from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD, TS_OK
+
+    good = {"logits": G, "tokens": 4, "experts": 8, "sel": G, "top_k": 2, "loss": G, "counts": G, "share": G, "totals": G,
+            "work": G, "stream": None}
+    for kw in ({"logits": None}, {"logits": G + 2}, {"tokens": -1}, {"tokens": 1 << 29}, {"experts": 0}, {"experts": 257},
+               {"sel": None}, {"top_k": 0}, {"top_k": 9}, {"experts": 1}, {"loss": None}, {"counts": None}, {"share": None},
+               {"totals": None}, {"work": None}, {"work": G + 2}):
+        assert call(lib.ts_balance, good, **kw) == BAD, kw
+    assert lib.ts_balance_work(-1, 8) == -1 and lib.ts_balance_work(4, 257) == -1
+    assert lib.ts_balance_work(0, 1) > 0 and lib.ts_balance_work(1 << 29, 256) > 0
+
+    good = {"logits": G, "tokens": 4, "experts": 8, "sel": G, "w": G, "top_k": 2, "dw": G, "counts": G, "totals": G,
+            "dloss": G, "dlogits": G, "stream": None}
+    for kw in ({"logits": None}, {"tokens": -1}, {"experts": 300}, {"sel": None}, {"w": None}, {"top_k": 9},
+               {"counts": None}, {"totals": None}, {"dloss": None}, {"dlogits": None}, {"dlogits": G + 2}, {"dw": G + 1},
+               {"dw": None, "counts": None, "totals": None, "dloss": None}):
+        assert call(lib.ts_route_backward, good, **kw) == BAD, kw
+    assert call(lib.ts_route_backward, good, tokens=0, dlogits=None) == TS_OK
+
+
+def test_combine_rows_backward(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_OK)
+
+    good = {"dy": G, "ddt": TS_F32, "src": G, "dt": TS_BF16, "n_rows": 8, "n": 64, "slots": G, "w": G, "rows": G, "tokens": 4,
+            "top_k": 2, "dsrc": 2 * G, "dw": G, "stream": None}
+    for kw in ({"dy": None}, {"dy": G + 2}, {"ddt": TS_E4M3}, {"src": None}, {"src": G + 1}, {"dt": TS_E4M3}, {"n_rows": -1},
+               {"n": 0}, {"slots": None}, {"w": None}, {"rows": None}, {"tokens": -1}, {"top_k": 0}, {"top_k": 9},
+               {"dsrc": None}, {"dsrc": G}, {"dw": None}, {"dw": G + 2}):
+        assert call(lib.ts_combine_rows_backward, good, **kw) == BAD, kw
+    assert call(lib.ts_combine_rows_backward, good, n=(1 << 30) + 1) == UNSUPPORTED
+    assert call(lib.ts_combine_rows_backward, good, tokens=0, dy=None, dw=None) == TS_OK
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused():
+    import torch
+
+    import paper_2406_05955_gb300 as ts
+
+    x, i = torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    f, two = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32)
+    for fn in (lambda: ts.Adapters(x[None], x[None]), lambda: ts.list_rows(i, 2), lambda: ts.drelu_rows(x, x),
+               lambda: ts.drelu_rows_backward(x, ts.Kept(x, x, f, f)), lambda: ts.balance(f, two),
+               lambda: ts.route_backward(f, two, f[:, :2], dw=f[:, :2]),
+               lambda: ts.combine_rows_backward(f, x, two, f[:, :2], i)):
+        with pytest.raises(TypeError):
+            fn()

@@ -1,0 +1,374 @@
+"""Low-rank adapters beside a shared product, and their gradients, against plain implementations in 64 bits.
+
+Tolerances. A sum in fp32 whose terms meet at most n roundings on their way (of 2^-24 each; the tensor cores truncate: 2^-23)
+is within n 2^-23 of the sum of the terms' magnitudes. h: at most 8 steps of 16 in a tensor core, a sum for each 128 of k,
+and the warps' and the cluster's joins, 48 in all for k up to 4096, and a product with the scale. out: as many more over
+the r components in up to 3 parts (at most 24 steps), y and the rounding of h to 16 bits (bf16: 2^-16) or 24 (2^-23), then
+the rounding to the type of out (half a step: 2^-8 of it in bf16). A gradient over n rows: n + 16 at most, plus the 2^-23 of h
+in 24 bits."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+U = 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def ts():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    import paper_2406_05955_gb300 as ts
+
+    ts.lib()
+    return ts
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def case(t, k, n, r, adapters, seed=0, dtype=BF16, none=0.2):
+    """x, y, a, b, scale, ids."""
+    g = gen(seed)
+    ids = torch.randint(0, adapters, (t,), generator=g, device="cuda")
+    ids = torch.where(torch.rand(t, generator=g, device="cuda") < none, -1, ids).to(torch.int32)
+    return (randn(g, t, k).to(BF16), randn(g, t, n).to(dtype), (randn(g, adapters, r, k) / math.sqrt(k)).to(BF16),
+            randn(g, adapters, r, n).to(BF16), 0.5 + torch.rand(adapters, generator=g, device="cuda"), ids)
+
+
+def plain(x, a, b, scale, ids, y=None, ranks=None):
+    """(h, its terms' magnitudes, out, its terms' magnitudes) in 64 bits."""
+    t, r = x.shape[0], a.shape[1]
+    h = torch.zeros(t, r, dtype=torch.float64, device="cuda")
+    hm = torch.zeros_like(h)
+    out = mag = None
+    if y is not None:
+        out, mag = y.double(), y.double().abs()
+    for i in range(a.shape[0]):
+        at = torch.nonzero(ids == i)[:, 0]
+        rank = r if ranks is None else min(max(int(ranks[i]), 0), r)
+        if not at.numel() or not rank:
+            continue
+        aa, bb, s = a[i, :rank].double(), b[i, :rank].double(), 1.0 if scale is None else float(scale[i])
+        v = x[at].double()
+        part, pm = s * v @ aa.t(), abs(s) * v.abs() @ aa.abs().t()
+        h[at, :rank], hm[at, :rank] = part, pm
+        if y is not None:
+            out[at] += part @ bb
+            mag[at] += pm @ bb.abs()
+    return h, hm, out, mag
+
+
+def check(ts, x, y, a, b, scale, ids, ranks=None, list_them=False, in_place=False, stream=None):
+    ad = ts.Adapters(a, b, scale=scale, ranks=ranks)
+    given = ad.rows(ids) if list_them else ids
+    h = torch.full((x.shape[0], a.shape[1]), 7.0, device="cuda")
+    want_h, hm, want, mag = plain(x, a, b, scale, ids, y, ranks)
+    if in_place:
+        out = y.clone()
+        assert ad.forward(x, out, given, h=h) is out
+    else:
+        before = y.clone()
+        out = ad.forward(x, y, given, out=torch.full_like(y, 9.0), h=h)
+        assert torch.equal(y, before)
+    assert ((h.double() - want_h).abs() <= 48 * U * hm).all()
+    tol = (76 * U + (2.0 ** -16 if y.dtype == BF16 else U)) * mag
+    if y.dtype == BF16:
+        tol = tol + 2.0 ** -8 * want.abs()
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), float((err - tol).max())
+    return out, h
+
+
+SIZES = [(1, 64, 64, 1, 1), (1, 4096, 1408, 16, 3), (2, 8, 8, 4, 2), (3, 136, 72, 5, 2), (17, 512, 1408, 16, 4),
+         (64, 1024, 264, 32, 64), (64, 520, 4096, 64, 3), (33, 256, 136, 128, 5), (65, 512, 512, 8, 2), (130, 1408, 512, 40, 7),
+         (300, 264, 1032, 12, 20), (1000, 512, 1408, 100, 3), (257, 4096, 128, 16, 1), (500, 128, 4104, 33, 255)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t,k,n,r,adapters", SIZES)
+def test_forward(ts, t, k, n, r, adapters, dtype):
+    c = case(t, k, n, r, adapters, seed=t + k, dtype=dtype)
+    outs = [check(ts, *c, list_them=lists, in_place=place) for lists in (False, True) for place in (False, True)]
+    for o in outs[1:3]:
+        assert torch.equal(o[1], outs[0][1]) or t <= 64  # (few rows without a list are summed in another order)
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[2][0], outs[3][0])
+
+
+@pytest.mark.parametrize("t", [5, 64, 300])
+def test_ids(ts, t):
+    """No row has an adapter, all have the same, ids out of range, sorted ids, the last adapter alone."""
+    x, y, a, b, scale, _ = case(t, 264, 136, 9, 4, seed=t)
+    g = gen(t)
+    for ids in (torch.full((t,), -1), torch.full((t,), 4), torch.full((t,), 2), torch.full((t,), 3),
+                torch.randint(-3, 9, (t,), generator=g, device="cuda"), torch.arange(t) * 4 // t,
+                torch.full((t,), -2 ** 31), torch.full((t,), 2 ** 31 - 1)):
+        for lists in (False, True):
+            check(ts, x, y, a, b, scale, ids.to("cuda", torch.int32), list_them=lists)
+
+
+@pytest.mark.parametrize("t", [16, 200])
+def test_ranks_scales_and_what_is_not_read(ts, t):
+    """Components behind an adapter's rank and adapters without rows are not read; a scale may be absent, 0 or negative."""
+    x, y, a, b, scale, ids = case(t, 256, 264, 24, 6, seed=3, none=0.1)
+    ids = torch.where(ids == 4, 5, ids)
+    ranks = torch.tensor([24, 0, 1, 17, 3, 30], dtype=torch.int32, device="cuda")
+    a, b = a.clone(), b.clone()
+    for i, rank in enumerate(ranks.tolist()):
+        a[i, rank:], b[i, rank:] = math.nan, math.nan
+    a[4], b[4] = math.nan, math.nan
+    scale[0], scale[2], scale[3] = 0.0, -2.0, 1e-3
+    for lists in (False, True):
+        check(ts, x, y, a, b, scale, ids, ranks=ranks, list_them=lists)
+        check(ts, x, y, a, b, None, ids, ranks=ranks, list_them=lists)
+
+
+@pytest.mark.parametrize("t", [20, 150])
+def test_infinities_and_nan_stay_in_their_rows(ts, t):
+    x, y, a, b, scale, ids = case(t, 512, 136, 16, 3, seed=5)
+    for lists in (False, True):
+        want, _ = check(ts, x, y, a, b, scale, ids, list_them=lists)
+        ad = ts.Adapters(a, b, scale=scale)
+        bad = x.clone()
+        bad[7, 3], bad[9, 500], y2 = math.nan, math.inf, y.clone()
+        y2[11, 5] = -math.inf
+        ids2 = ids.clone()
+        ids2[7], ids2[9] = 1, -1
+        got = ad.forward(bad, y2, ad.rows(ids2) if lists else ids2, out=torch.empty_like(y))
+        assert got[7].isnan().all() and torch.equal(got[9], y[9]) and got[11, 5] == -math.inf
+        rest = torch.ones(t, dtype=torch.bool, device="cuda")
+        rest[[7, 9, 11]] = False
+        assert torch.equal(got[rest], want[rest])
+
+
+@pytest.mark.parametrize("t", [30, 100])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_apart(ts, t, dtype):
+    """Rows of x, y and out that lie in wider ones: what is between them is left as it was."""
+    x, y, a, b, scale, ids = case(t, 136, 72, 6, 3, seed=7, dtype=dtype)
+    want, h = check(ts, x, y, a, b, scale, ids)
+    wide_x = torch.full((t, 160), math.nan, dtype=BF16, device="cuda")
+    wide_y, wide_out = (torch.full((t, 96), 5.0, dtype=dtype, device="cuda") for _ in range(2))
+    wide_x[:, 8:144], wide_y[:, 8:80] = x, y
+    ad = ts.Adapters(a, b, scale=scale)
+    got = ad.forward(wide_x[:, 8:144], wide_y[:, 8:80], ids, out=wide_out[:, 16:88])
+    assert torch.equal(got, want) and torch.equal(wide_out[:, 16:88], want)
+    assert (wide_out[:, :16] == 5).all() and (wide_out[:, 88:] == 5).all()
+    ad.forward(wide_x[:, 8:144], wide_y[:, 8:80], ids)
+    assert torch.equal(wide_y[:, 8:80], want) and (wide_y[:, :8] == 5).all() and (wide_y[:, 80:] == 5).all()
+
+
+def test_no_rows(ts):
+    x, y, a, b, scale, ids = case(0, 64, 64, 4, 3)
+    ad = ts.Adapters(a, b, scale=scale)
+    assert ad.forward(x, y, ids).shape == (0, 64)
+    rows = ad.rows(ids)
+    assert rows.offsets.tolist() == [0] * 5
+    da, db = torch.full_like(a, 3.0, dtype=F32), torch.full_like(b, 3.0, dtype=F32)
+    h, dy = torch.empty(0, 4, device="cuda"), torch.empty(0, 64, dtype=BF16, device="cuda")
+    ad.backward(dy, x.clone(), rows, h, x, da=da, db=db, accumulate=True)
+    assert (da == 3).all() and (db == 3).all()
+    ad.backward(dy, x.clone(), rows, h, x, da=da, db=db)
+    assert (da == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("t", [1, 2, 33, 1000, 1025, 5000, 40000])
+@pytest.mark.parametrize("groups", [1, 2, 7, 64, 255])
+def test_list_rows(ts, t, groups):
+    ids = torch.randint(-2, groups + 2, (t,), generator=gen(t + groups), device="cuda").to(torch.int32)
+    if t == 5000:
+        ids.fill_(groups - 1)
+    got = ts.list_rows(ids, groups)
+    of = torch.where((ids >= 0) & (ids < groups), ids, groups).long()
+    assert got.rows.tolist() == torch.sort(of, stable=True).indices.tolist()
+    assert got.offsets.tolist() == [0] + torch.bincount(of, minlength=groups + 1).cumsum(0).tolist()
+
+
+def kept_rows(ts, x):
+    q, s = ts.quant_rows(x)
+    return q, s, q.double() * s.double().repeat_interleave(128, 0)[:x.shape[1]].t()
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("t,k,n,r,adapters", [(1, 64, 64, 1, 1), (3, 144, 72, 5, 2), (64, 512, 1408, 16, 4), (130, 1408, 512, 40, 7),
+                                              (700, 272, 1032, 12, 20), (1000, 512, 136, 100, 3), (2049, 128, 264, 128, 2),
+                                              (90, 16, 8, 33, 255)])
+def test_backward(ts, t, k, n, r, adapters, x8):
+    x, _, a, b, scale, ids = case(t, k, n, r, adapters, seed=t)
+    g = gen(t + 1)
+    dy, dx = (0.1 * randn(g, t, n)).to(BF16), randn(g, t, k).to(F32 if t % 2 else BF16)
+    h = randn(g, t, r)
+    ad = ts.Adapters(a, b, scale=scale)
+    h[(ids < 0)] = 0.0
+    x_scale, wide = None, x.double()
+    if x8:
+        x, x_scale, wide = kept_rows(ts, x)
+    dh, dhm, want, mag = plain(dy, b, a, scale, ids, dx)
+    before = dx.clone()
+    out, da, db = ad.backward(dy, dx, ids, h, x, x_scale=x_scale, out=torch.empty_like(dx))
+    assert torch.equal(dx, before)
+    tol = (76 * U + (2.0 ** -16 if dx.dtype == BF16 else U)) * mag + (2.0 ** -8 * want.abs() if dx.dtype == BF16 else 0.0)
+    assert ((out.double() - want).abs() <= tol).all()
+    for i in range(adapters):
+        at = torch.nonzero(ids == i)[:, 0]
+        m = at.numel()
+        hi, dhi = h[at].double(), dh[at]
+        assert ((db[i].double() - hi.t() @ dy[at].double()).abs() <= (m + 17) * U * (hi.abs().t() @ dy[at].double().abs())).all()
+        tol = (m + 17) * U * (dhi.abs().t() @ wide[at].abs()) + 48 * U * (dhm[at].t() @ wide[at].abs())
+        assert ((da[i].double() - dhi.t() @ wide[at]).abs() <= tol).all()
+        if m == 0:
+            assert (da[i] == 0).all() and (db[i] == 0).all()
+    again = ad.backward(dy, dx, ad.rows(ids), h, x, x_scale=x_scale, out=torch.empty_like(dx))
+    assert all(torch.equal(p, q) for p, q in zip(again, (out, da, db)))
+    # added to: exact where what is there is a power of two far below, so only that it is not overwritten
+    da2, db2 = torch.full_like(da, 2.0), torch.full_like(db, -2.0)
+    ad.backward(dy, None, ids, h, x, x_scale=x_scale, da=da2, db=db2, accumulate=True)
+    assert torch.equal(da2, da + 2.0) and torch.equal(db2, db - 2.0)
+
+
+def test_rows_without_an_adapter_do_not_reach_the_gradients(ts):
+    x, _, a, b, scale, ids = case(200, 256, 128, 8, 3, seed=9, none=0.3)
+    g = gen(10)
+    dy, h = (0.1 * randn(g, 200, 128)).to(BF16), randn(g, 200, 8)
+    ad = ts.Adapters(a, b, scale=scale)
+    _, da, db = ad.backward(dy, None, ids, h, x)
+    off = ids < 0
+    x2, dy2, h2 = x.clone(), dy.clone(), h.clone()
+    x2[off], dy2[off], h2[off] = math.nan, math.inf, math.nan
+    _, da2, db2 = ad.backward(dy2, None, ids, h2, x2)
+    assert torch.equal(da, da2) and torch.equal(db, db2)
+    one = int(torch.nonzero(ids == 1)[0])
+    x2[one, 5] = math.nan
+    _, da3, _ = ad.backward(dy2, None, ids, h2, x2)
+    assert da3[1, :, 5].isnan().all() and torch.equal(da3[[0, 2]], da[[0, 2]])
+    keep = torch.ones(256, dtype=torch.bool, device="cuda")
+    keep[5] = False
+    assert torch.equal(da3[1][:, keep], da[1][:, keep])
+
+
+def test_gradients_against_differences(ts):
+    """<gradient, direction> against central differences of sum(out * weight) in 64 bits: out is linear in each of x, A
+    and B, so the differences are exact but for rounding, and what is left are the kernels' own tolerances."""
+    t, k, n, r, adapters = 120, 128, 72, 8, 3
+    x, y, a, b, scale, ids = case(t, k, n, r, adapters, seed=11, dtype=F32)
+    dy = randn(gen(12), t, n).to(BF16)
+    ad = ts.Adapters(a, b, scale=scale)
+    h = torch.empty(t, r, device="cuda")
+    ad.forward(x, y, ids, out=torch.empty_like(y), h=h)
+    dx, da, db = ad.backward(dy, torch.zeros(t, k, device="cuda"), ids, h, x)
+
+    def value(x, a, b):
+        some = ids >= 0
+        i = ids.clamp(min=0).long()
+        h = torch.einsum("tk,trk->tr", x, a[i]) * torch.where(some, scale[i].double(), 0.0)[:, None]
+        return float((dy.double() * torch.einsum("tr,trn->tn", h, b[i])).sum())
+
+    at = (x.double(), a.double(), b.double())
+    for which, grad in enumerate((dx, da, db)):
+        d = torch.randn(grad.shape, generator=gen(20 + which), device="cuda").double()
+        plus, minus = list(at), list(at)
+        plus[which], minus[which] = at[which] + 0.5 * d, at[which] - 0.5 * d
+        want = value(*plus) - value(*minus)
+        got = float((grad.double() * d).sum())
+        # 200 roundings of 2^-23 on terms of random signs, whose magnitudes' sum is below 64 times the norms' product here
+        assert abs(got - want) <= 200 * U * float(grad.double().norm() * d.norm()) * 64, which
+
+
+def test_streams_graphs_and_calls_at_once(ts):
+    c = case(300, 512, 264, 16, 5, seed=13)
+    few = case(40, 512, 264, 16, 5, seed=14)
+    x, y, a, b, scale, ids = c
+    ad, ad2 = ts.Adapters(a, b, scale=scale), ts.Adapters(few[2], few[3], scale=few[4])
+    want = ad.forward(x, y, ids, out=torch.empty_like(y))
+    want2 = ad2.forward(few[0], few[1], few[5], out=torch.empty_like(few[1]))
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in (s1, s2):
+        s.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(20):  # in flight together
+        outs.append((ad.forward(x, y, ids, out=_like(y, s1), stream=s1), ad2.forward(few[0], few[1], few[5], out=_like(few[1], s2), stream=s2)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, want) and torch.equal(q, want2) for p, q in outs)
+    h, dy = torch.empty(300, 16, device="cuda"), (0.1 * randn(gen(15), 300, 264)).to(BF16)
+    dx, out = randn(gen(16), 300, 512), torch.empty_like(y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s1):
+        rows = ad.rows(ids)
+        ad.forward(x, y, rows, out=out, h=h)
+        got = ad.backward(dy, dx, rows, h, x, out=torch.empty_like(dx))
+    other = case(300, 512, 264, 16, 5, seed=17)
+    x.copy_(other[0])
+    ids.copy_(other[5])
+    graph.replay()
+    graph.replay()
+    h2 = torch.empty_like(h)
+    want = ad.forward(x, y, ids, out=torch.empty_like(y), h=h2)
+    back = ad.backward(dy, dx, ids, h2, x, out=torch.empty_like(dx))
+    assert torch.equal(out, want) and torch.equal(h, h2)
+    assert all(torch.equal(p, q) for p, q in zip(got, back))
+
+
+def _like(t, stream):
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def test_offsets_beyond_32_bits(ts):
+    """Rows whose elements are more than 2^31 apart."""
+    t, k, n = 600, 64, 64
+    ld = 1 << 22
+    x, y, a, b, scale, ids = case(t, k, n, 8, 3, seed=18)
+    want, h = check(ts, x, y, a, b, scale, ids)
+    far = torch.empty(t * ld, dtype=BF16, device="cuda")
+    fx, fy = far.view(t, ld)[:, :k], far.view(t, ld)[:, 1024:1024 + n]
+    fx.copy_(x)
+    fy.copy_(y)
+    ad = ts.Adapters(a, b, scale=scale)
+    assert torch.equal(ad.forward(fx, fy, ids, out=far.view(t, ld)[:, 2048:2048 + n]), want)
+    dy = (0.1 * randn(gen(19), t, n)).to(BF16)
+    far_dy = far.view(t, ld)[:, 4096:4096 + n]
+    far_dy.copy_(dy)
+    near = ad.backward(dy, None, ids, h, x)
+    assert all(torch.equal(p, q) for p, q in zip(near[1:], ad.backward(far_dy, None, ids, h, fx)[1:]))
+
+
+def test_refusals(ts):
+    x, y, a, b, scale, ids = case(70, 64, 72, 4, 3)
+    ad = ts.Adapters(a, b, scale=scale)
+    h, dy = torch.zeros(70, 4, device="cuda"), torch.zeros(70, 72, dtype=BF16, device="cuda")
+    q, s, _ = kept_rows(ts, x)
+    f8 = torch.float8_e4m3fn
+    for error, call in (
+        (TypeError, lambda: ts.Adapters(a.float(), b)), (ValueError, lambda: ts.Adapters(a, b[:2])),
+        (ValueError, lambda: ts.Adapters(a, b[:, :3])), (ValueError, lambda: ts.Adapters(a.transpose(1, 2), b)),
+        (ValueError, lambda: ts.Adapters(a, b, scale=scale[:2])), (TypeError, lambda: ts.Adapters(a, b, scale=scale.double())),
+        (TypeError, lambda: ts.Adapters(a, b, ranks=scale)), (TypeError, lambda: ts.Adapters(a, b.cpu())),
+        (TypeError, lambda: ad.forward(x.float(), y, ids)), (ValueError, lambda: ad.forward(x[:, :56], y, ids)),
+        (ValueError, lambda: ad.forward(x, y[:, :64], ids)), (ValueError, lambda: ad.forward(x, y[:69], ids)),
+        (TypeError, lambda: ad.forward(x, y.half(), ids)), (ValueError, lambda: ad.forward(x, y, ids[:69])),
+        (TypeError, lambda: ad.forward(x, y, ids.long())), (TypeError, lambda: ad.forward(x, y, ids, out=y.float())),
+        (ValueError, lambda: ad.forward(x, y, ids, h=h[:, :3])), (ValueError, lambda: ad.forward(x, y, ts.list_rows(ids, 2))),
+        (TypeError, lambda: ad.backward(dy.float(), None, ids, h, x)), (ValueError, lambda: ad.backward(dy, None, ids, h, x[:, :32])),
+        (ValueError, lambda: ad.backward(dy, None, ids, h, x, x_scale=s)), (ValueError, lambda: ad.backward(dy, None, ids, h, q)),
+        (ValueError, lambda: ad.backward(dy, None, ids, h, q, x_scale=s[:, :69])),
+        (ValueError, lambda: ad.backward(dy, None, ids, h, x, out=x)), (ValueError, lambda: ad.backward(dy, None, ids, h, x, accumulate=True)),
+        (TypeError, lambda: ad.backward(dy, None, ids, h, x.to(torch.float16))), (ValueError, lambda: ts.list_rows(ids[None], 3)),
+        (ts.TsError, lambda: ts.list_rows(ids, 256)), (ts.TsError, lambda: ts.list_rows(ids, 0)),
+        (ts.TsError, lambda: ad.forward(torch.zeros(70, 72, dtype=BF16, device="cuda")[:, 4:68], y, ids)),
+        (ts.TsError, lambda: ts.Adapters(a.new_zeros(3, 129, 64), b.new_zeros(3, 129, 72)).forward(x, y, ids)),
+        (ts.TsError, lambda: ts.Adapters(a.new_zeros(256, 4, 64), b.new_zeros(256, 4, 72)).forward(x[:4], y[:4], ids[:4])),
+        (ts.TsError, lambda: ts.Adapters(a.new_zeros(3, 4, 60), b).forward(x[:, :60].contiguous(), y, ids)),
+    ):
+        with pytest.raises(error):
+            call()
+    assert f8 is E4M3
