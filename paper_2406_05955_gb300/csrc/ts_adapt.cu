@@ -1,6 +1,14 @@
 // ts_adapt.cu -- low-rank adapters of many requests beside a shared projection: h[t] = s_i x[t] A_i^T and
 // out[t] = y[t] + h[t] B_i for the adapter i of row t (ts_adapt_rows), and the sums over rows of h^T x that are the
 // gradients of A and B (ts_adapter_grads). With A and B exchanged the first is also the backward pass by rows.
+//
+// Both products in one launch. A cluster of CTAs has a tile of up to 16 or 64 rows of one adapter: each CTA sums its part
+// of k for the whole tile, the parts of h meet through distributed shared memory, summed in the same order by all, and each
+// CTA adds h B_i to its part of the columns. One ring of chunks, 256 bytes of each row wide, carries x and A_i and then y and B_i: while h is
+// being joined the first chunks of y are already on their way. Rows of a tile are gathered (a list by adapter), so they
+// come by 16-byte asynchronous copies.
+//
+// Memory bounds it: x, y and out are 2 k + 2 n elements a row, the products 2 r flops for each of them.
 #include <cuda_fp8.h>
 
 #include "ts_adapt.h"
@@ -11,77 +19,764 @@ namespace tsffn {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / kWarp;
+constexpr int kChunk = 256;  // bytes of a row of x, A, y or out in a chunk
+constexpr int kMaxCluster = 8;
+constexpr int kResidentCtas = 2 * 152;
 
-template <typename TY>
-__global__ void __launch_bounds__(kThreads) k_adapt(const AdaptLaunch L) {
-    __shared__ float h[kMaxRank];
-    pdl_wait();
-    const int at = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int row = at, id;
-    if (L.list != nullptr) {
-        row = L.list[at];
-        for (id = 0; id < L.n_adapters && L.offsets[id + 1] <= at;) ++id;
-    } else {
-        id = L.ids[row];
-    }
-    if ((unsigned)row >= (unsigned)L.rows) return;
-    const bool some = (unsigned)id < (unsigned)L.n_adapters;
-    const int rank = !some ? 0 : L.ranks != nullptr ? min(max(L.ranks[id], 0), L.r) : L.r;
-    const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(L.x) + row * L.ldx;
-    for (int j = warp; j < L.r; j += kThreads / kWarp) {
-        float sum = 0.0f;
-        if (j < rank) {
-            const __nv_bfloat16* a = static_cast<const __nv_bfloat16*>(L.a) + ((size_t)id * L.r + j) * L.k;
-            for (int i = lane; i < L.k; i += kWarp) sum = fmaf(__bfloat162float(x[i]), __bfloat162float(a[i]), sum);
-            sum = warp_sum(sum) * (L.scale != nullptr ? L.scale[id] : 1.0f);
-        }
-        if (lane == 0) {
-            h[j] = sum;
-            if (L.h != nullptr) L.h[(size_t)row * L.r + j] = sum;
-        }
-    }
-    __syncthreads();
-    if (L.out == nullptr || (rank == 0 && L.out == L.y)) return;
-    const TY* y = static_cast<const TY*>(L.y) + row * L.ldy;
-    TY* out = static_cast<TY*>(L.out) + row * L.ldo;
-    const __nv_bfloat16* b = static_cast<const __nv_bfloat16*>(L.b) + (size_t)(some ? id : 0) * L.r * L.n;
-    for (int i = threadIdx.x; i < L.n; i += kThreads) {
-        float sum = 0.0f;
-        for (int j = 0; j < rank; ++j) sum = fmaf(h[j], __bfloat162float(b[(size_t)j * L.n + i]), sum);
-        Vec<TY>::store1(out, i, Vec<TY>::load1(y, i) + sum);
+// ---- matrix instructions, asynchronous copies, clusters ---------------------------------------
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&v)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_t(uint32_t (&v)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix2_t(uint32_t (&v)[2], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at) : "memory");
+}
+// 16 bytes, or zeros.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t at, uint32_t rank) {
+    uint32_t a;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+// Byte of 16-byte piece `c` of row `row` in rows of PITCH bytes, pieces permuted so that 8 rows' same piece lie in 8 banks.
+template <int PITCH>
+__device__ __forceinline__ int place(int row, int c) {
+    static_assert(PITCH >= 128, "");
+    return row * PITCH + ((c ^ (row & 7)) << 4);
+}
+
+// fp32 as a sum of P bf16 numbers, 8 significant bits each; an infinity or NaN is the first alone.
+template <int P>
+__device__ __forceinline__ void split(float v, __nv_bfloat16 (&p)[P]) {
+    p[0] = __float2bfloat16_rn(v);
+    const bool finite = fabsf(__bfloat162float(p[0])) < INFINITY;
+#pragma unroll
+    for (int i = 1; i < P; ++i) {
+        v -= __bfloat162float(p[i - 1]);
+        p[i] = __float2bfloat16_rn(finite ? v : 0.0f);
     }
 }
 
-template <bool E8>
-__global__ void __launch_bounds__(kThreads) k_adapter_grads(const AdapterGradsLaunch L) {
-    constexpr int kAtOnce = 16;
-    pdl_wait();
-    const int id = blockIdx.y, i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= L.k) return;
-    const int begin = L.offsets[id], end = min(L.offsets[id + 1], L.rows);
-    for (int j0 = 0; j0 < L.r; j0 += kAtOnce) {
-        float sum[kAtOnce] = {};
-        for (int at = begin; at < end; ++at) {
-            const int row = L.list[at];
-            if ((unsigned)row >= (unsigned)L.rows) continue;
-            float v;
-            if constexpr (E8) {
-                const __nv_fp8_e4m3 q = static_cast<const __nv_fp8_e4m3*>(L.x)[row * L.ldx + i];
-                v = (float)q * L.x_scale[(int64_t)(i / kScaleBlock) * L.ld_scale + row];
-            } else {
-                v = __bfloat162float(static_cast<const __nv_bfloat16*>(L.x)[row * L.ldx + i]);
-            }
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j)
-                if (j0 + j < L.r) sum[j] = fmaf(L.h[(size_t)row * L.r + j0 + j], v, sum[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-            if (j0 + j < L.r) {
-                float* g = L.grad + ((size_t)id * L.r + j0 + j) * L.k + i;
-                *g = L.accumulate ? *g + sum[j] : sum[j];
-            }
+// ---------------------------------------------------------------------------
+// h and out
+// ---------------------------------------------------------------------------
+// MT: rows of a tile. RP: r rounded up to 16, 32, 64 or 128.
+template <int MT, int RP, typename TY>
+struct Tile {
+    static constexpr int kCols = kChunk / 2;                          // of x and A in a chunk
+    static constexpr int kOutCols = kChunk / (int)sizeof(TY);         // of y and out
+    static constexpr int kBPitch = kOutCols * 2;                      // bytes of a row of B
+    static constexpr int kParts = sizeof(TY) == 2 ? 2 : 3;            // bf16 numbers that h enters the second product as
+    static constexpr int kStage = (MT + RP) * kChunk;
+    static constexpr int kMTiles = MT / 16;
+    static constexpr int kSides = kWarps / kMTiles;                   // warps that share 16 rows
+    static constexpr int kNSplit = MT == 64 && RP == 128 ? 2 : 1;     // ways that those share r in the first product
+    static constexpr int kSlabs = kSides / kNSplit;                   // and k
+    static constexpr int kNT = RP / 8 / kNSplit;                      // 8-column tiles of a warp in the first product
+    static constexpr int kOT = kOutCols / 8 / kSides;                 // and in the second
+    static constexpr int kHPitch = RP * 2 + 16;
+    static constexpr int kSlabBytes = MT * RP * 4;
+    static constexpr int kPartBytes = MT * kHPitch;
+    // the sums of h of this CTA, one slab a warp that shares k (the first has their sum), and h as bf16 numbers
+    static constexpr int kFixed = kSlabs * kSlabBytes + kParts * kPartBytes;
+    static constexpr int kWish = MT == 16 ? 8 : RP <= 32 ? 3 : 4;
+    static constexpr int kRoom = 226 * 1024 - kFixed;
+    static constexpr int kStages = kWish * kStage <= kRoom ? kWish : kRoom / kStage;
+    static constexpr int kSmem = kStages * kStage + kFixed;
+    static_assert(kStages >= 2, "");
+};
+
+// The tile of a cluster: up to MT rows of one adapter.
+struct TileRows {
+    int id, rank, first, count;
+};
+
+// By the list: tile number `tile` of all groups' in a row, the rows without an adapter last.
+template <int MT>
+__device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, TileRows* found, int* rows) {
+    __shared__ int sums[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int begin = 0, end = 0;
+    if (tid <= L.n_adapters) {
+        begin = min(max(L.offsets[tid], 0), L.rows);
+        end = min(max(L.offsets[tid + 1], begin), L.rows);
     }
+    const int tiles = (end - begin + MT - 1) / MT;
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == kWarp - 1) sums[warp] = upto;
+    if (tid == 0) *found = {-1, 0, 0, 0};
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += sums[w];
+    if (tile < upto && tile >= upto - tiles) {
+        const int first = begin + (tile - (upto - tiles)) * MT;
+        *found = {tid, 0, first, min(MT, end - first)};
+    }
+    __syncthreads();
+    if (tid < MT) {
+        const int row = tid < found->count ? L.list[found->first + tid] : -1;
+        rows[tid] = (unsigned)row < (unsigned)L.rows ? row : -1;
+    }
+}
+
+// Without a list, of up to 64 rows: tile number t is there if row t is the first, 17th, 33rd or 49th of its adapter.
+template <int MT>
+__device__ __forceinline__ void find_few(const AdaptLaunch& L, int t, TileRows* found, int* rows) {
+    static_assert(kFewRows == 64, "");
+    if (threadIdx.x >= kWarp) return;
+    const int lane = threadIdx.x;
+    int id[2];
+    unsigned same[2];
+    const int mine = min((unsigned)L.ids[t], (unsigned)L.n_adapters);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = lane + i * kWarp;
+        id[i] = row < L.rows ? (int)min((unsigned)L.ids[row], (unsigned)L.n_adapters) : -1;
+        same[i] = __ballot_sync(0xffffffffu, id[i] == mine);
+    }
+    const unsigned long long all = (unsigned long long)same[1] << 32 | same[0];
+    const int before = __popcll(all & ((1ull << t) - 1ull));
+    const bool leads = before % MT == 0;
+    if (lane == 0) *found = {leads ? mine : -1, 0, 0, leads ? min(MT, __popcll(all) - before) : 0};
+    for (int i = lane; i < MT; i += kWarp) rows[i] = -1;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = lane + i * kWarp, at = __popcll(all & ((1ull << row) - 1ull)) - before;
+        if (id[i] == mine && at >= 0 && at < MT) rows[at] = row;
+    }
+}
+
+template <int MT, int RP, typename TY>
+__global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ AdaptLaunch L, int ctas) {
+    using T = Tile<MT, RP, TY>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ TileRows found;
+    __shared__ int rows[MT];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t cta = cluster_rank();
+    unsigned char* const slabs = smem + T::kStages * T::kStage;
+    unsigned char* const parts = slabs + T::kSlabs * T::kSlabBytes;
+    const uint32_t smem0 = smem_u32(smem), parts0 = smem_u32(parts);
+    pdl_wait();
+    if (L.list != nullptr) find_listed<MT>(L, (int)(blockIdx.x / ctas), &found, rows);
+    else find_few<MT>(L, (int)(blockIdx.x / ctas), &found, rows);
+    __syncthreads();
+    const int id = found.id, count = found.count;
+    if (id < 0) return;
+    const bool some = id < L.n_adapters;
+    const int rank = !some ? 0 : L.ranks != nullptr ? min(max(L.ranks[id], 0), L.r) : L.r;
+    const __nv_bfloat16* const x = static_cast<const __nv_bfloat16*>(L.x);
+    const __nv_bfloat16* const a = static_cast<const __nv_bfloat16*>(L.a) + (size_t)(some ? id : 0) * L.r * L.k;
+    const __nv_bfloat16* const b = static_cast<const __nv_bfloat16*>(L.b) + (size_t)(some ? id : 0) * L.r * L.n;
+    const TY* const y = static_cast<const TY*>(L.y);
+    TY* const out = static_cast<TY*>(L.out);
+    if (rank == 0) {
+        if (L.h != nullptr && cta == 0)
+            for (int i = tid; i < count * L.r; i += kThreads)
+                if (rows[i / L.r] >= 0) L.h[(size_t)rows[i / L.r] * L.r + i % L.r] = 0.0f;
+        if (out == y) return;  // (of both nullptr too)
+    }
+
+    // this CTA's chunks: of k, then of n
+    const int k_chunks = rank > 0 ? (L.k + T::kCols - 1) / T::kCols : 0;
+    const int n_chunks = out != nullptr ? (L.n + T::kOutCols - 1) / T::kOutCols : 0;
+    const int k0 = (int)((long long)k_chunks * cta / ctas), nk = (int)((long long)k_chunks * (cta + 1) / ctas) - k0;
+    const int n0 = (int)((long long)n_chunks * cta / ctas), nn = (int)((long long)n_chunks * (cta + 1) / ctas) - n0;
+
+    const auto issue = [&](int i) {
+        if (i < nk + nn) {
+            const uint32_t to = smem0 + (uint32_t)(i % T::kStages) * T::kStage;
+            constexpr int kPieces = kChunk / 16;
+            if (i < nk) {
+                const int col0 = (k0 + i) * T::kCols;
+#pragma unroll
+                for (int p = tid; p < MT * kPieces; p += kThreads) {
+                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * 8;
+                    const bool in = rows[row] >= 0 && col < L.k;
+                    copy16(to + place<kChunk>(row, c), in ? x + rows[row] * L.ldx + col : x, in);
+                }
+#pragma unroll
+                for (int p = tid; p < RP * kPieces; p += kThreads) {
+                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * 8;
+                    const bool in = row < rank && col < L.k;
+                    copy16(to + MT * kChunk + place<kChunk>(row, c), in ? a + (size_t)row * L.k + col : a, in);
+                }
+            } else {
+                const int col0 = (n0 + i - nk) * T::kOutCols;
+#pragma unroll
+                for (int p = tid; p < MT * kPieces; p += kThreads) {
+                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * (16 / (int)sizeof(TY));
+                    const bool in = rows[row] >= 0 && col < L.n;
+                    copy16(to + place<kChunk>(row, c), in ? y + rows[row] * L.ldy + col : y, in);
+                }
+                constexpr int kBPieces = T::kBPitch / 16;
+                if (rank > 0) {
+#pragma unroll
+                    for (int p = tid; p < RP * kBPieces; p += kThreads) {
+                        const int row = p / kBPieces, c = p % kBPieces, col = col0 + c * 8;
+                        const bool in = row < rank && col < L.n;
+                        copy16(to + MT * kChunk + place<T::kBPitch>(row, c), in ? b + (size_t)row * L.n + col : b, in);
+                    }
+                }
+            }
+        }
+        copies_commit();
+    };
+
+    const int m0 = (warp % T::kMTiles) * 16, side = warp / T::kMTiles;
+    const bool live = m0 < count;
+    // The tensor cores cut bits off a long sum: `sum` takes over what 8 steps of 16 have added.
+    float acc[T::kNT][4] = {}, sum[T::kNT][4] = {};
+    const auto take_over = [&] {
+#pragma unroll
+        for (int t = 0; t < T::kNT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum[t][e] += acc[t][e];
+                acc[t][e] = 0.0f;
+            }
+    };
+
+    // h of the whole tile: this CTA's sums over its warps, all CTAs' over the cluster.
+    const auto join = [&] {
+        take_over();
+        const int j0 = T::kNSplit == 2 ? side * T::kNT * 8 : 0, slab = T::kNSplit == 2 ? 0 : side;
+        float* const to = reinterpret_cast<float*>(slabs + slab * T::kSlabBytes);
+#pragma unroll
+        for (int t = 0; t < T::kNT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<float2*>(to + (m0 + lane / 4 + e * 4) * RP + j0 + t * 8 + (lane & 3) * 2) =
+                    make_float2(sum[t][e], sum[t][e + 1]);
+        __syncthreads();
+        float4* const mine = reinterpret_cast<float4*>(slabs);
+        if constexpr (T::kSlabs > 1) {
+            for (int i = tid; i < MT * RP / 4; i += kThreads) {
+                float4 s = mine[i];
+#pragma unroll
+                for (int w = 1; w < T::kSlabs; ++w) {
+                    const float4 v = mine[w * (MT * RP / 4) + i];
+                    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+                }
+                mine[i] = s;
+            }
+        }
+        if (ctas > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        const float scale = L.scale != nullptr ? L.scale[id] : 1.0f;
+        const uint32_t at = smem_u32(slabs);
+        for (int i = tid; i < MT * RP / 4; i += kThreads) {
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (ctas > 1) {
+                float4 v[kMaxCluster];
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c)
+                    if (c < ctas) v[c] = cluster_ld4(at + 16 * i, (uint32_t)c);
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c)
+                    if (c < ctas) s.x += v[c].x, s.y += v[c].y, s.z += v[c].z, s.w += v[c].w;
+            } else {
+                s = mine[i];
+            }
+            const int row = i / (RP / 4), j = i % (RP / 4) * 4;
+            const float h[4] = {j < rank ? s.x * scale : 0.0f, j + 1 < rank ? s.y * scale : 0.0f,  // (x may hold NaN)
+                                j + 2 < rank ? s.z * scale : 0.0f, j + 3 < rank ? s.w * scale : 0.0f};
+            __nv_bfloat16 p[4][T::kParts];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split<T::kParts>(h[e], p[e]);
+#pragma unroll
+            for (int q = 0; q < T::kParts; ++q) {
+                __nv_bfloat162 two[2] = {__halves2bfloat162(p[0][q], p[1][q]), __halves2bfloat162(p[2][q], p[3][q])};
+                *reinterpret_cast<uint2*>(parts + q * T::kPartBytes + row * T::kHPitch + j * 2) = *reinterpret_cast<const uint2*>(two);
+            }
+            if (L.h != nullptr && row % ctas == (int)cta && rows[row] >= 0)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < L.r) L.h[(size_t)rows[row] * L.r + j + e] = h[e];
+        }
+        __syncthreads();
+        if (ctas > 1) cluster_arrive();  // (waited for at the end: no CTA leaves while another reads its sums)
+    };
+
+#pragma unroll
+    for (int i = 0; i < T::kStages - 1; ++i) issue(i);
+    for (int i = 0; i < nk + nn; ++i) {
+        copies_wait<T::kStages - 2>();
+        __syncthreads();
+        issue(i + T::kStages - 1);
+        const int stage = (i % T::kStages) * T::kStage;
+        const uint32_t first = smem0 + stage, second = first + MT * kChunk;
+        if (i < nk) {
+            if (live) {
+                constexpr int kSteps = T::kCols / 16, kMySteps = kSteps / T::kSlabs;
+#pragma unroll
+                for (int u = 0; u < kMySteps; ++u) {
+                    const int ks = T::kSlabs > 1 ? side * kMySteps + u : u;
+                    uint32_t xa[4];
+                    ldmatrix4(xa, first + place<kChunk>(m0 + (lane & 15), ks * 2 + (lane >> 4)));
+#pragma unroll
+                    for (int t = 0; t < T::kNT; t += 2) {
+                        uint32_t w[4];
+                        const int j0 = (T::kNSplit == 2 ? side * T::kNT : 0) * 8 + t * 8;
+                        ldmatrix4(w, second + place<kChunk>(j0 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)));
+                        mma(acc[t], xa, w[0], w[1]);
+                        mma(acc[t + 1], xa, w[2], w[3]);
+                    }
+                }
+                if (MT > 16 || (i & 7) == 7) take_over();
+            }
+            continue;
+        }
+        if (i == nk && rank > 0) join();
+        if (live) {
+            float o[T::kOT][4] = {};
+            const int c0 = side * T::kOT * 8;  // this warp's first column in the chunk
+            if (rank > 0) {
+#pragma unroll
+                for (int ks = 0; ks < RP / 16; ++ks) {
+                    uint32_t h[T::kParts][4];
+#pragma unroll
+                    for (int q = 0; q < T::kParts; ++q)
+                        ldmatrix4(h[q], parts0 + q * T::kPartBytes + (m0 + (lane & 15)) * T::kHPitch + ks * 32 + (lane >> 4) * 16);
+                    const int j = ks * 16 + (lane & 15);
+                    if constexpr (T::kOT == 1) {
+                        uint32_t w[2];
+                        ldmatrix2_t(w, second + place<T::kBPitch>(j, c0 / 8));
+#pragma unroll
+                        for (int q = T::kParts - 1; q >= 0; --q) mma(o[0], h[q], w[0], w[1]);
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < T::kOT; t += 2) {
+                            uint32_t w[4];
+                            ldmatrix4_t(w, second + place<T::kBPitch>(j, c0 / 8 + t + (lane >> 4)));
+#pragma unroll
+                            for (int q = T::kParts - 1; q >= 0; --q) {
+                                mma(o[t], h[q], w[0], w[1]);
+                                mma(o[t + 1], h[q], w[2], w[3]);
+                            }
+                        }
+                    }
+                }
+            }
+            unsigned char* const tile = smem + stage;
+            constexpr int kPer = 16 / (int)sizeof(TY);
+#pragma unroll
+            for (int t = 0; t < T::kOT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    const int row = m0 + lane / 4 + e * 4, col = c0 + t * 8 + (lane & 3) * 2;
+                    unsigned char* const p = tile + place<kChunk>(row, col / kPer) + col % kPer * (int)sizeof(TY);
+                    if constexpr (sizeof(TY) == 2) {
+                        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+                        const __nv_bfloat162 s = __floats2bfloat162_rn(bf16lo(v) + o[t][e], bf16hi(v) + o[t][e + 1]);
+                        *reinterpret_cast<__nv_bfloat162*>(p) = s;
+                    } else {
+                        const float2 v = *reinterpret_cast<const float2*>(p);
+                        *reinterpret_cast<float2*>(p) = make_float2(v.x + o[t][e], v.y + o[t][e + 1]);
+                    }
+                }
+            __syncwarp();
+            constexpr int kSeg = T::kOT * 8 / kPer;  // 16-byte pieces of a row of this warp
+            const int col0 = (n0 + i - nk) * T::kOutCols;
+#pragma unroll
+            for (int p = lane; p < 16 * kSeg; p += kWarp) {
+                const int row = m0 + p / kSeg, c = c0 / kPer + p % kSeg, col = col0 + c * kPer;
+                if (rows[row] >= 0 && col < L.n)
+                    *reinterpret_cast<uint4*>(out + rows[row] * L.ldo + col) = *reinterpret_cast<const uint4*>(tile + place<kChunk>(row, c));
+            }
+        }
+    }
+    if (rank > 0) {
+        if (nn == 0) join();
+        if (ctas > 1) cluster_wait();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// gradients
+// ---------------------------------------------------------------------------
+// A CTA has 128 columns of x; the rows of an adapter come in chunks of 64. h is the transposed operand and is split into
+// three bf16 numbers, x is exact in bf16 (e4m3 rows too: the scale that 128 of their columns share is multiplied into h).
+constexpr int kGradCols = 128, kGradRows = 64;
+constexpr int kIdRing = 8;
+
+template <int RP, bool E8>
+struct Grads {
+    static constexpr int kXPitch = kGradCols * (E8 ? 1 : 2);
+    static constexpr int kXBytes = kGradRows * kXPitch, kHBytes = kGradRows * RP * 4, kScaleBytes = E8 ? kGradRows * 4 : 0;
+    static constexpr int kStage = kXBytes + kHBytes + kScaleBytes;
+    static constexpr int kStages = 3;
+    static constexpr int kHPitch = RP * 2 + 16;
+    static constexpr int kPartBytes = kGradRows * kHPitch;
+    static constexpr int kWide = E8 ? kGradRows * kChunk : 0;  // x in bf16
+    static constexpr int kSmem = kStages * kStage + 3 * kPartBytes + kWide;
+    static constexpr int kMGroups = RP == 16 ? 1 : 2;          // ways that the warps share the components
+    static constexpr int kMT = RP / 16 / kMGroups;             // 16-component tiles of a warp
+    static constexpr int kNT = kGradCols / 8 / (kWarps / kMGroups);
+    static_assert(kStages * kStage >= RP * kGradCols * 4 && kStages + 2 <= kIdRing, "");
+};
+
+// Whether an adapter's rows are shared by the CTAs of a cluster: where one CTA would have more than twice the even share.
+__device__ __forceinline__ bool shared_rows(int count, int even) { return count > max(2 * even, kGradRows); }
+
+// First entry of adapter `id` in the list, and their number.
+__device__ __forceinline__ int2 entries(const AdapterGradsLaunch& L, int id) {
+    const int begin = min(max(L.offsets[id], 0), L.rows);
+    return make_int2(begin, min(max(L.offsets[id + 1], begin), L.rows) - begin);
+}
+
+template <int RP, bool E8>
+__global__ void __launch_bounds__(kThreads) k_adapter_grads(const __grid_constant__ AdapterGradsLaunch L, int ctas, int even) {
+    using G = Grads<RP, E8>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int ids[kIdRing][kGradRows];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t cta = cluster_rank();
+    unsigned char* const parts = smem + G::kStages * G::kStage;
+    unsigned char* const wide = parts + 3 * G::kPartBytes;
+    const uint32_t smem0 = smem_u32(smem), parts0 = smem_u32(parts), wide0 = smem_u32(wide);
+    const int col0 = (int)(blockIdx.x / ctas) * kGradCols;
+    const bool h_vec = L.r % 4 == 0 && (reinterpret_cast<uintptr_t>(L.h) & 15u) == 0;
+    pdl_wait();
+
+    // The sums over entries begin .. begin + count - 1 of the list, of which `mine` are this CTA's; shared: the cluster's CTAs
+    // join theirs.
+    const auto sums = [&](int id, int begin, int count, bool join) {
+        const int chunks = (count + kGradRows - 1) / kGradRows, parties = join ? ctas : 1, me = join ? (int)cta : 0;
+        const int c0 = (int)((long long)chunks * me / parties), nc = (int)((long long)chunks * (me + 1) / parties) - c0;
+        const int first = begin + c0 * kGradRows, end = begin + count;
+        const auto listed = [&](int i) {
+            const int at = first + i * kGradRows + tid;
+            const int row = tid < kGradRows && i < nc && at < end ? L.list[at] : -1;
+            return (unsigned)row < (unsigned)L.rows ? row : -1;
+        };
+        const auto issue = [&](int i) {
+            if (i < nc) {
+                const uint32_t to = smem0 + (uint32_t)(i % G::kStages) * G::kStage;
+                const int* const rows = ids[i % kIdRing];
+                constexpr int kPieces = G::kXPitch / 16;
+#pragma unroll
+                for (int p = tid; p < kGradRows * kPieces; p += kThreads) {
+                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * (E8 ? 16 : 8);
+                    const bool in = rows[row] >= 0 && col < L.k;
+                    const char* const from = static_cast<const char*>(L.x) + (in ? (rows[row] * L.ldx + col) * (E8 ? 1 : 2) : 0);
+                    copy16(to + (E8 ? p * 16 : place<kChunk>(row, c)), from, in);
+                }
+                const uint32_t h = to + G::kXBytes;
+                if (h_vec) {
+                    for (int p = tid; p < kGradRows * (RP / 4); p += kThreads) {
+                        const int row = p / (RP / 4), j = p % (RP / 4) * 4;
+                        const bool in = rows[row] >= 0 && j < L.r;
+                        copy16(h + p * 16, in ? L.h + (size_t)rows[row] * L.r + j : L.h, in);
+                    }
+                } else {
+                    for (int p = tid; p < kGradRows * RP; p += kThreads) {
+                        const int row = p / RP, j = p % RP;
+                        const bool in = rows[row] >= 0 && j < L.r;
+                        copy4(h + p * 4, in ? L.h + (size_t)rows[row] * L.r + j : L.h, in);
+                    }
+                }
+                if (E8 && tid < kGradRows) {
+                    const bool in = rows[tid] >= 0;
+                    copy4(h + G::kHBytes + tid * 4,
+                          in ? L.x_scale + (int64_t)(col0 / kScaleBlock) * L.ld_scale + rows[tid] : L.x_scale, in);
+                }
+            }
+            copies_commit();
+        };
+        float acc[G::kMT][G::kNT][4] = {}, sum[G::kMT][G::kNT][4] = {};
+        int next = -1;
+        __syncthreads();  // (of what the last sums have in shared memory)
+        for (int i = 0; i < G::kStages; ++i) {
+            next = listed(i);
+            if (tid < kGradRows) ids[i][tid] = next;
+        }
+        next = listed(G::kStages);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < G::kStages - 1; ++i) issue(i);
+        const int mg = warp % G::kMGroups, n0 = warp / G::kMGroups * G::kNT * 8;
+        for (int i = 0; i < nc; ++i) {
+            copies_wait<G::kStages - 2>();
+            __syncthreads();
+            if (tid < kGradRows) ids[(i + G::kStages) % kIdRing][tid] = next;
+            next = listed(i + G::kStages + 1);
+            issue(i + G::kStages - 1);
+            const unsigned char* const stage = smem + (i % G::kStages) * G::kStage;
+            const float* const h = reinterpret_cast<const float*>(stage + G::kXBytes);
+#pragma unroll 4
+            for (int p = tid; p < kGradRows * (RP / 4); p += kThreads) {
+                const int row = p / (RP / 4), j = p % (RP / 4) * 4;
+                float4 v = reinterpret_cast<const float4*>(h)[p];
+                if constexpr (E8) {
+                    const float s = reinterpret_cast<const float*>(stage + G::kXBytes + G::kHBytes)[row];
+                    v.x *= s, v.y *= s, v.z *= s, v.w *= s;
+                }
+                __nv_bfloat16 q[4][3];
+                split<3>(v.x, q[0]);
+                split<3>(v.y, q[1]);
+                split<3>(v.z, q[2]);
+                split<3>(v.w, q[3]);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) {
+                    __nv_bfloat162 two[2] = {__halves2bfloat162(q[0][t], q[1][t]), __halves2bfloat162(q[2][t], q[3][t])};
+                    *reinterpret_cast<uint2*>(parts + t * G::kPartBytes + row * G::kHPitch + j * 2) = *reinterpret_cast<const uint2*>(two);
+                }
+            }
+            if constexpr (E8) {
+#pragma unroll
+                for (int p = tid; p < kGradRows * kGradCols / 16; p += kThreads) {
+                    const int row = p / (kGradCols / 16), c = p % (kGradCols / 16) * 2;
+                    const uint4 v = reinterpret_cast<const uint4*>(stage)[p];
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t b[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const __half2_raw f = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[e / 2] >> 16 * (e & 1)), __NV_E4M3);
+                        const __nv_bfloat162 t = __float22bfloat162_rn(__half22float2(*reinterpret_cast<const __half2*>(&f)));
+                        b[e] = *reinterpret_cast<const uint32_t*>(&t);
+                    }
+                    *reinterpret_cast<uint4*>(wide + place<kChunk>(row, c)) = make_uint4(b[0], b[1], b[2], b[3]);
+                    *reinterpret_cast<uint4*>(wide + place<kChunk>(row, c + 1)) = make_uint4(b[4], b[5], b[6], b[7]);
+                }
+            }
+            __syncthreads();
+            const uint32_t x0 = E8 ? wide0 : smem0 + (uint32_t)(i % G::kStages) * G::kStage;
+#pragma unroll
+            for (int ks = 0; ks < kGradRows / 16; ++ks) {
+                uint32_t w[G::kNT / 2][4];
+#pragma unroll
+                for (int t = 0; t < G::kNT; t += 2)
+                    ldmatrix4_t(w[t / 2], x0 + place<kChunk>(ks * 16 + (lane & 15), n0 / 8 + t + (lane >> 4)));
+#pragma unroll
+                for (int m = 0; m < G::kMT; ++m)
+#pragma unroll
+                    for (int q = 2; q >= 0; --q) {
+                        uint32_t a[4];
+                        ldmatrix4_t(a, parts0 + q * G::kPartBytes + (ks * 16 + (lane & 7) + (lane >> 4) * 8) * G::kHPitch +
+                                           ((mg * G::kMT + m) * 16 + ((lane >> 3) & 1) * 8) * 2);
+#pragma unroll
+                        for (int t = 0; t < G::kNT; t += 2) {
+                            mma(acc[m][t], a, w[t / 2][0], w[t / 2][1]);
+                            mma(acc[m][t + 1], a, w[t / 2][2], w[t / 2][3]);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int m = 0; m < G::kMT; ++m)
+#pragma unroll
+                for (int t = 0; t < G::kNT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {  // (the tensor cores cut bits off a long sum)
+                        sum[m][t][e] += acc[m][t][e];
+                        acc[m][t][e] = 0.0f;
+                    }
+        }
+        float* const grad = L.grad + (size_t)id * L.r * L.k;
+        if (!join) {
+#pragma unroll
+            for (int m = 0; m < G::kMT; ++m)
+#pragma unroll
+                for (int t = 0; t < G::kNT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const int j = (mg * G::kMT + m) * 16 + lane / 4 + e * 4, col = col0 + n0 + t * 8 + (lane & 3) * 2;
+                        if (j >= L.r || col >= L.k) continue;
+                        float2* const to = reinterpret_cast<float2*>(grad + (size_t)j * L.k + col);
+                        float2 v = make_float2(sum[m][t][e], sum[m][t][e + 1]);
+                        if (L.accumulate) {
+                            const float2 had = *to;
+                            v.x += had.x, v.y += had.y;
+                        }
+                        *to = v;
+                    }
+            return;
+        }
+        copies_wait<0>();
+        __syncthreads();  // the stages hold the sums now
+        float* const mine = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int m = 0; m < G::kMT; ++m)
+#pragma unroll
+            for (int t = 0; t < G::kNT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2)
+                    *reinterpret_cast<float2*>(mine + ((mg * G::kMT + m) * 16 + lane / 4 + e * 4) * kGradCols + n0 + t * 8 + (lane & 3) * 2) =
+                        make_float2(sum[m][t][e], sum[m][t][e + 1]);
+        __syncthreads();
+        cluster_arrive();
+        cluster_wait();
+        constexpr int kQuads = RP * kGradCols / 4;
+        for (int p = (int)cta * kThreads + tid; p < kQuads; p += kThreads * ctas) {
+            const int j = p / (kGradCols / 4), col = col0 + p % (kGradCols / 4) * 4;
+            if (j >= L.r || col >= L.k) continue;
+            float4 v[kMaxCluster];
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c)
+                if (c < ctas) v[c] = cluster_ld4(smem0 + 16 * p, (uint32_t)c);
+            float4* const to = reinterpret_cast<float4*>(grad + (size_t)j * L.k + col);
+            float4 s = v[0];
+#pragma unroll
+            for (int c = 1; c < kMaxCluster; ++c)
+                if (c < ctas) s.x += v[c].x, s.y += v[c].y, s.z += v[c].z, s.w += v[c].w;
+            if (L.accumulate) {
+                const float4 had = *to;
+                s.x += had.x, s.y += had.y, s.z += had.z, s.w += had.w;
+            }
+            *to = s;
+        }
+        __syncthreads();
+        cluster_arrive();
+        cluster_wait();
+    };
+
+    // Adapters whose rows are shared go round by cluster, the others by CTA: thread t looks at adapter t, and the masks say
+    // which ones are this CTA's.
+    __shared__ unsigned bigs[kWarps], smalls[kWarps];
+    const int count_of_mine = tid < L.n_adapters ? entries(L, tid).y : 0;
+    const bool big = ctas > 1 && shared_rows(count_of_mine, even);
+    const bool small = tid < L.n_adapters && !big && !(count_of_mine == 0 && L.accumulate);
+    const unsigned big_here = __ballot_sync(0xffffffffu, big), small_here = __ballot_sync(0xffffffffu, small);
+    if (lane == 0) {
+        bigs[warp] = big_here;
+        smalls[warp] = small_here;
+    }
+    __syncthreads();
+    unsigned nth_big = __popc(big_here & ((1u << lane) - 1u)), nth_small = __popc(small_here & ((1u << lane) - 1u));
+    for (int w = 0; w < warp; ++w) {
+        nth_big += __popc(bigs[w]);
+        nth_small += __popc(smalls[w]);
+    }
+    __syncthreads();
+    const unsigned my_big = __ballot_sync(0xffffffffu, big && nth_big % gridDim.y == blockIdx.y);
+    const unsigned my_small = __ballot_sync(0xffffffffu, small && nth_small % (gridDim.y * ctas) == blockIdx.y * ctas + cta);
+    if (lane == 0) {
+        bigs[warp] = my_big;
+        smalls[warp] = my_small;
+    }
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w)
+        for (unsigned m = bigs[w]; m != 0u; m &= m - 1u) {
+            const int id = w * kWarp + __ffs(m) - 1;
+            const int2 of = entries(L, id);
+            sums(id, of.x, of.y, true);
+        }
+    for (int w = 0; w < kWarps; ++w)
+        for (unsigned m = smalls[w]; m != 0u; m &= m - 1u) {
+            const int id = w * kWarp + __ffs(m) - 1;
+            const int2 of = entries(L, id);
+            sums(id, of.x, of.y, false);
+        }
+}
+
+template <int MT, int RP, typename TY>
+cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
+    const auto kernel = k_adapt<MT, RP, TY>;
+    constexpr int kSmem = Tile<MT, RP, TY>::kSmem;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas)), kThreads, stream);
+    cfg.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {(unsigned)ctas, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, ctas);
+}
+
+template <int MT, typename TY>
+cudaError_t launch_rank(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
+    if (a.r <= 16) return launch_tiles<MT, 16, TY>(a, tiles, ctas, stream);
+    if (a.r <= 32) return launch_tiles<MT, 32, TY>(a, tiles, ctas, stream);
+    if (a.r <= 64) return launch_tiles<MT, 64, TY>(a, tiles, ctas, stream);
+    return launch_tiles<MT, 128, TY>(a, tiles, ctas, stream);
+}
+
+template <typename TY>
+cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
+    if (a.list == nullptr) return launch_rank<16, TY>(a, a.rows, kMaxCluster, stream);
+    // the most tiles that lists of so many rows can have
+    const auto most = [&](int mt) { return (long long)a.rows / mt + (a.rows < a.n_adapters + 1 ? a.rows : a.n_adapters + 1); };
+    const bool small = a.rows < 1024 && a.rows / a.n_adapters <= 24;
+    const int mt = small ? 16 : 64;
+    int ctas = kMaxCluster;
+    while (ctas > 1 && a.rows / mt * ctas > 2 * kResidentCtas) ctas /= 2;
+    return small ? launch_rank<16, TY>(a, most(16), ctas, stream) : launch_rank<64, TY>(a, most(64), ctas, stream);
+}
+
+template <int RP, bool E8>
+cudaError_t launch_grads(const AdapterGradsLaunch& a, cudaStream_t stream) {
+    const auto kernel = k_adapter_grads<RP, E8>;
+    constexpr int kSmem = Grads<RP, E8>::kSmem;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    // about two rounds of CTAs, in clusters of 8: fewer where there are no more adapters or chunks than that
+    const int blocks = (a.k + kGradCols - 1) / kGradCols;
+    int ctas = kMaxCluster;
+    while (ctas > 1 && (long long)ctas * kGradRows / 2 >= a.rows) ctas /= 2;
+    const int wish = (kResidentCtas * 2 + blocks * ctas - 1) / (blocks * ctas);
+    const int ys = wish < a.n_adapters ? wish : a.n_adapters;
+    const int even = (int)((long long)a.rows * blocks / kResidentCtas);
+    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas), (unsigned)ys), kThreads, stream);
+    cfg.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {(unsigned)ctas, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, ctas, even);
+}
+
+template <bool E8>
+cudaError_t launch_grads_rank(const AdapterGradsLaunch& a, cudaStream_t stream) {
+    if (a.r <= 16) return launch_grads<16, E8>(a, stream);
+    if (a.r <= 32) return launch_grads<32, E8>(a, stream);
+    if (a.r <= 64) return launch_grads<64, E8>(a, stream);
+    return launch_grads<128, E8>(a, stream);
 }
 
 }  // namespace
@@ -89,12 +784,11 @@ __global__ void __launch_bounds__(kThreads) k_adapter_grads(const AdapterGradsLa
 cudaError_t prepare_adapt() { return cudaSuccess; }
 
 cudaError_t launch_adapt(const AdaptLaunch& a, bool y_f32, cudaStream_t stream) {
-    return launch_after(y_f32 ? k_adapt<float> : k_adapt<__nv_bfloat16>, launch_shape(dim3((unsigned)a.rows), kThreads, stream), a);
+    return y_f32 ? launch_type<float>(a, stream) : launch_type<__nv_bfloat16>(a, stream);
 }
 
 cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStream_t stream) {
-    return launch_after(e4m3 ? k_adapter_grads<true> : k_adapter_grads<false>,
-                        launch_shape(dim3((unsigned)((a.k + kThreads - 1) / kThreads), (unsigned)a.n_adapters), kThreads, stream), a);
+    return e4m3 ? launch_grads_rank<true>(a, stream) : launch_grads_rank<false>(a, stream);
 }
 
 }  // namespace tsffn
