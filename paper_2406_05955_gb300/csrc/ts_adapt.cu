@@ -107,12 +107,15 @@ struct Tile {
     static constexpr int kHPitch = RP * 2 + 16;
     static constexpr int kSlabBytes = MT * RP * 4;
     static constexpr int kPartBytes = MT * kHPitch;
-    // the sums of h of this CTA, one slab a warp that shares k (the first has their sum), and h as bf16 numbers
-    static constexpr int kFixed = kSlabs * kSlabBytes + kParts * kPartBytes;
-    static constexpr int kWish = MT == 16 ? 8 : RP <= 32 ? 3 : 4;
-    static constexpr int kRoom = 226 * 1024 - kFixed;
-    static constexpr int kStages = kWish * kStage <= kRoom ? kWish : kRoom / kStage;
+    // the sums of h of this CTA (a slab for each warp of 16 rows; 64 rows' two warps add to one), and h as bf16 numbers
+    static constexpr int kFixed = (MT == 16 ? kSlabs : 1) * kSlabBytes + kParts * kPartBytes;
+    // two CTAs on an SM where two stages fit (the loads in flight of two cover the latency, and one works while the other joins)
+    static constexpr int kHalf = 113 * 1024 - kFixed, kWhole = 226 * 1024 - kFixed;
+    static constexpr int kWish = MT == 16 ? 8 : 4;
+    static constexpr int kFit = kHalf >= 2 * kStage ? kHalf / kStage : kWhole / kStage;
+    static constexpr int kStages = kFit < kWish ? kFit : kWish;
     static constexpr int kSmem = kStages * kStage + kFixed;
+    static constexpr int kCtas = kSmem <= 113 * 1024 && RP <= 64 ? 2 : 1;  // on an SM
     static_assert(kStages >= 2, "");
 };
 
@@ -182,15 +185,15 @@ __device__ __forceinline__ void find_few(const AdaptLaunch& L, int t, TileRows* 
 }
 
 template <int MT, int RP, typename TY>
-__global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ AdaptLaunch L, int ctas) {
+__global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(const __grid_constant__ AdaptLaunch L, int ctas) {
     using T = Tile<MT, RP, TY>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ TileRows found;
     __shared__ int rows[MT];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t cta = cluster_rank();
-    unsigned char* const slabs = smem + T::kStages * T::kStage;
-    unsigned char* const parts = slabs + T::kSlabs * T::kSlabBytes;
+    unsigned char* const parts = smem + T::kStages * T::kStage;
+    unsigned char* const slabs = parts + T::kParts * T::kPartBytes;
     const uint32_t smem0 = smem_u32(smem), parts0 = smem_u32(parts);
     pdl_wait();
     if (L.list != nullptr) find_listed<MT>(L, (int)(blockIdx.x / ctas), &found, rows);
@@ -205,54 +208,82 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
     const __nv_bfloat16* const b = static_cast<const __nv_bfloat16*>(L.b) + (size_t)(some ? id : 0) * L.r * L.n;
     const TY* const y = static_cast<const TY*>(L.y);
     TY* const out = static_cast<TY*>(L.out);
+    const float scale = some && L.scale != nullptr ? L.scale[id] : 1.0f;
     if (rank == 0) {
-        if (L.h != nullptr && cta == 0)
+        if (L.h != nullptr && cta == 0 && blockIdx.y == 0)
             for (int i = tid; i < count * L.r; i += kThreads)
                 if (rows[i / L.r] >= 0) L.h[(size_t)rows[i / L.r] * L.r + i % L.r] = 0.0f;
         if (out == y) return;  // (of both nullptr too)
     }
 
-    // this CTA's chunks: of k, then of n
+    // this CTA's chunks: of k, and then of n, which the clusters of a tile share as well
     const int k_chunks = rank > 0 ? (L.k + T::kCols - 1) / T::kCols : 0;
     const int n_chunks = out != nullptr ? (L.n + T::kOutCols - 1) / T::kOutCols : 0;
     const int k0 = (int)((long long)k_chunks * cta / ctas), nk = (int)((long long)k_chunks * (cta + 1) / ctas) - k0;
-    const int n0 = (int)((long long)n_chunks * cta / ctas), nn = (int)((long long)n_chunks * (cta + 1) / ctas) - n0;
+    const int all = ctas * (int)gridDim.y, me = (int)(blockIdx.y * ctas + cta);
+    const int n0 = (int)((long long)n_chunks * me / all), nn = (int)((long long)n_chunks * (me + 1) / all) - n0;
 
+    // A thread copies the same 16-byte piece of every 16th row of a chunk of x or y, and of the rows of A or B: where it
+    // reads moves on by a chunk from one call to the next.
+    constexpr int kPieces = kChunk / 16, kRowStep = kThreads / kPieces, kMine = MT / kRowStep;
+    const int piece = tid % kPieces, row0 = tid / kPieces;
+    const uint32_t to0 = smem0 + place<kChunk>(row0, piece);
+    const char* src[kMine];
+    bool there[kMine];
+#pragma unroll
+    for (int p = 0; p < kMine; ++p) {
+        const int row = rows[row0 + p * kRowStep];
+        there[p] = row >= 0;
+        src[p] = reinterpret_cast<const char*>(x + (there[p] ? row * L.ldx : 0) + k0 * T::kCols + piece * 8);
+    }
+    const char* mat = reinterpret_cast<const char*>(a + (size_t)row0 * L.k + k0 * T::kCols + piece * 8);
+    int col = k0 * T::kCols + piece * 8;
     const auto issue = [&](int i) {
         if (i < nk + nn) {
-            const uint32_t to = smem0 + (uint32_t)(i % T::kStages) * T::kStage;
-            constexpr int kPieces = kChunk / 16;
-            if (i < nk) {
-                const int col0 = (k0 + i) * T::kCols;
+            const uint32_t to = to0 + (uint32_t)(i % T::kStages) * T::kStage;
+            if (i == nk) {
+                col = n0 * T::kOutCols + piece * (16 / (int)sizeof(TY));
 #pragma unroll
-                for (int p = tid; p < MT * kPieces; p += kThreads) {
-                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * 8;
-                    const bool in = rows[row] >= 0 && col < L.k;
-                    copy16(to + place<kChunk>(row, c), in ? x + rows[row] * L.ldx + col : x, in);
-                }
-#pragma unroll
-                for (int p = tid; p < RP * kPieces; p += kThreads) {
-                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * 8;
-                    const bool in = row < rank && col < L.k;
-                    copy16(to + MT * kChunk + place<kChunk>(row, c), in ? a + (size_t)row * L.k + col : a, in);
-                }
-            } else {
-                const int col0 = (n0 + i - nk) * T::kOutCols;
-#pragma unroll
-                for (int p = tid; p < MT * kPieces; p += kThreads) {
-                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * (16 / (int)sizeof(TY));
-                    const bool in = rows[row] >= 0 && col < L.n;
-                    copy16(to + place<kChunk>(row, c), in ? y + rows[row] * L.ldy + col : y, in);
-                }
+                for (int p = 0; p < kMine; ++p)
+                    src[p] = reinterpret_cast<const char*>(y + (there[p] ? rows[row0 + p * kRowStep] * L.ldy : 0) + col);
                 constexpr int kBPieces = T::kBPitch / 16;
+                mat = reinterpret_cast<const char*>(b + (size_t)(tid / kBPieces) * L.n + n0 * T::kOutCols + tid % kBPieces * 8);
+            }
+            const bool in = col < (i < nk ? L.k : L.n);
+#pragma unroll
+            for (int p = 0; p < kMine; ++p) {
+                const bool take = in && there[p];
+                copy16(to + p * kRowStep * kChunk, take ? src[p] : reinterpret_cast<const char*>(x), take);
+                src[p] += kChunk;
+            }
+            if (i < nk) {
+                const int64_t step = (int64_t)kRowStep * L.k * 2;
+                const char* from = mat;
+#pragma unroll
+                for (int p = 0; p < RP / kRowStep; ++p) {
+                    const bool take = in && row0 + p * kRowStep < rank;
+                    copy16(to + MT * kChunk + p * kRowStep * kChunk, take ? from : reinterpret_cast<const char*>(x), take);
+                    from += step;
+                }
+                mat += kChunk;
+                col += T::kCols;
+            } else {
+                constexpr int kBPieces = T::kBPitch / 16, kBStep = kThreads / kBPieces;
+                const int b_row = tid / kBPieces, b_col = col - piece * (16 / (int)sizeof(TY)) + tid % kBPieces * 8;
+                const uint32_t b_to = smem0 + (uint32_t)(i % T::kStages) * T::kStage + MT * kChunk + place<T::kBPitch>(b_row, tid % kBPieces);
+                const int64_t step = (int64_t)kBStep * L.n * 2;
+                const char* from = mat;
                 if (rank > 0) {
 #pragma unroll
-                    for (int p = tid; p < RP * kBPieces; p += kThreads) {
-                        const int row = p / kBPieces, c = p % kBPieces, col = col0 + c * 8;
-                        const bool in = row < rank && col < L.n;
-                        copy16(to + MT * kChunk + place<T::kBPitch>(row, c), in ? b + (size_t)row * L.n + col : b, in);
+                    for (int p = 0; p < (RP + kBStep - 1) / kBStep; ++p) {
+                        const bool take = b_col < L.n && b_row + p * kBStep < rank;
+                        if (RP >= kBStep || b_row < RP)
+                            copy16(b_to + p * kBStep * T::kBPitch, take ? from : reinterpret_cast<const char*>(x), take);
+                        from += step;
                     }
                 }
+                mat += T::kBPitch;
+                col += T::kOutCols;
             }
         }
         copies_commit();
@@ -275,17 +306,21 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
     // h of the whole tile: this CTA's sums over its warps, all CTAs' over the cluster.
     const auto join = [&] {
         take_over();
-        const int j0 = T::kNSplit == 2 ? side * T::kNT * 8 : 0, slab = T::kNSplit == 2 ? 0 : side;
-        float* const to = reinterpret_cast<float*>(slabs + slab * T::kSlabBytes);
-#pragma unroll
-        for (int t = 0; t < T::kNT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2)
-                *reinterpret_cast<float2*>(to + (m0 + lane / 4 + e * 4) * RP + j0 + t * 8 + (lane & 3) * 2) =
-                    make_float2(sum[t][e], sum[t][e + 1]);
-        __syncthreads();
+        const int j0 = T::kNSplit == 2 ? side * T::kNT * 8 : 0;
         float4* const mine = reinterpret_cast<float4*>(slabs);
-        if constexpr (T::kSlabs > 1) {
+        const auto store = [&](float* to, bool add) {
+#pragma unroll
+            for (int t = 0; t < T::kNT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    float2* const p = reinterpret_cast<float2*>(to + (m0 + lane / 4 + e * 4) * RP + j0 + t * 8 + (lane & 3) * 2);
+                    const float2 had = add ? *p : make_float2(0.0f, 0.0f);
+                    *p = make_float2(had.x + sum[t][e], had.y + sum[t][e + 1]);
+                }
+        };
+        if constexpr (MT == 16) {
+            store(reinterpret_cast<float*>(slabs + side * T::kSlabBytes), false);
+            __syncthreads();
             for (int i = tid; i < MT * RP / 4; i += kThreads) {
                 float4 s = mine[i];
 #pragma unroll
@@ -295,14 +330,17 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
                 }
                 mine[i] = s;
             }
+        } else {
+            float* const to = reinterpret_cast<float*>(slabs);
+            if (T::kSlabs == 1 || side == 0) store(to, false);
+            __syncthreads();
+            if (T::kSlabs == 2 && side == 1) store(to, true);
         }
+        __syncthreads();
         if (ctas > 1) {
             cluster_arrive();
             cluster_wait();
-        } else {
-            __syncthreads();
         }
-        const float scale = L.scale != nullptr ? L.scale[id] : 1.0f;
         const uint32_t at = smem_u32(slabs);
         for (int i = tid; i < MT * RP / 4; i += kThreads) {
             float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -328,7 +366,7 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
                 __nv_bfloat162 two[2] = {__halves2bfloat162(p[0][q], p[1][q]), __halves2bfloat162(p[2][q], p[3][q])};
                 *reinterpret_cast<uint2*>(parts + q * T::kPartBytes + row * T::kHPitch + j * 2) = *reinterpret_cast<const uint2*>(two);
             }
-            if (L.h != nullptr && row % ctas == (int)cta && rows[row] >= 0)
+            if (L.h != nullptr && blockIdx.y == 0 && row % ctas == (int)cta && rows[row] >= 0)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (j + e < L.r) L.h[(size_t)rows[row] * L.r + j + e] = h[e];
@@ -368,8 +406,23 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
         }
         if (i == nk && rank > 0) join();
         if (live) {
-            float o[T::kOT][4] = {};
+            float o[T::kOT][4];
             const int c0 = side * T::kOT * 8;  // this warp's first column in the chunk
+            unsigned char* const tile = smem + stage;
+            constexpr int kPer = 16 / (int)sizeof(TY);
+            const auto at = [&](int t, int e) -> unsigned char* {  // of o[t][e] and the next one
+                const int row = m0 + lane / 4 + e * 4, c = c0 + t * 8 + (lane & 3) * 2;
+                return tile + place<kChunk>(row, c / kPer) + c % kPer * (int)sizeof(TY);
+            };
+            // sums for bf16 begin with y; fp32 ones add it last, as the tensor cores cut bits off a long sum
+#pragma unroll
+            for (int t = 0; t < T::kOT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    const uint32_t v = sizeof(TY) == 2 ? *reinterpret_cast<const uint32_t*>(at(t, e)) : 0u;
+                    o[t][e] = bf16lo(v);
+                    o[t][e + 1] = bf16hi(v);
+                }
             if (rank > 0) {
 #pragma unroll
                 for (int ks = 0; ks < RP / 16; ++ks) {
@@ -397,21 +450,15 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
                     }
                 }
             }
-            unsigned char* const tile = smem + stage;
-            constexpr int kPer = 16 / (int)sizeof(TY);
 #pragma unroll
             for (int t = 0; t < T::kOT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    const int row = m0 + lane / 4 + e * 4, col = c0 + t * 8 + (lane & 3) * 2;
-                    unsigned char* const p = tile + place<kChunk>(row, col / kPer) + col % kPer * (int)sizeof(TY);
                     if constexpr (sizeof(TY) == 2) {
-                        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
-                        const __nv_bfloat162 s = __floats2bfloat162_rn(bf16lo(v) + o[t][e], bf16hi(v) + o[t][e + 1]);
-                        *reinterpret_cast<__nv_bfloat162*>(p) = s;
+                        *reinterpret_cast<__nv_bfloat162*>(at(t, e)) = __floats2bfloat162_rn(o[t][e], o[t][e + 1]);
                     } else {
-                        const float2 v = *reinterpret_cast<const float2*>(p);
-                        *reinterpret_cast<float2*>(p) = make_float2(v.x + o[t][e], v.y + o[t][e + 1]);
+                        float2* const p = reinterpret_cast<float2*>(at(t, e));
+                        *p = make_float2(p->x + o[t][e], p->y + o[t][e + 1]);
                     }
                 }
             __syncwarp();
@@ -419,9 +466,9 @@ __global__ void __launch_bounds__(kThreads) k_adapt(const __grid_constant__ Adap
             const int col0 = (n0 + i - nk) * T::kOutCols;
 #pragma unroll
             for (int p = lane; p < 16 * kSeg; p += kWarp) {
-                const int row = m0 + p / kSeg, c = c0 / kPer + p % kSeg, col = col0 + c * kPer;
-                if (rows[row] >= 0 && col < L.n)
-                    *reinterpret_cast<uint4*>(out + rows[row] * L.ldo + col) = *reinterpret_cast<const uint4*>(tile + place<kChunk>(row, c));
+                const int row = m0 + p / kSeg, c = c0 / kPer + p % kSeg, to = col0 + c * kPer;
+                if (rows[row] >= 0 && to < L.n)
+                    *reinterpret_cast<uint4*>(out + rows[row] * L.ldo + to) = *reinterpret_cast<const uint4*>(tile + place<kChunk>(row, c));
             }
         }
     }
@@ -710,11 +757,16 @@ __global__ void __launch_bounds__(kThreads) k_adapter_grads(const __grid_constan
 
 template <int MT, int RP, typename TY>
 cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
+    // Few tiles: several clusters have one, each with its own h and a part of the columns, of 2 chunks a CTA at least.
+    const long long chunks = (a.n + Tile<MT, RP, TY>::kOutCols - 1) / Tile<MT, RP, TY>::kOutCols;
+    long long sharing = a.out != nullptr ? kResidentCtas / (tiles * ctas) : 1;
+    if (sharing > chunks / (2 * ctas)) sharing = chunks / (2 * ctas);
+    if (sharing < 1) sharing = 1;
     const auto kernel = k_adapt<MT, RP, TY>;
     constexpr int kSmem = Tile<MT, RP, TY>::kSmem;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas)), kThreads, stream);
+    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas), (unsigned)sharing), kThreads, stream);
     cfg.dynamicSmemBytes = kSmem;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeClusterDimension;
