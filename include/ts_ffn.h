@@ -591,6 +591,12 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
                         const int32_t* offsets, const void* y, int64_t ldy, ts_dtype ydtype, void* out, int64_t ldo, float* h,
                         cudaStream_t stream);
 
+/* What calls of ts_adapt_rows on the current device have recorded since this was last called (synchronises `stream`): TS_OK,
+   or TS_ERR_TIMEOUT where a bounded wait gave up, after which out and h are not to be used. */
+ts_status ts_adapt_get_error(cudaStream_t stream);
+/* Failure-detection test hook: a bounded wait of the next calls over many rows runs out. */
+void ts_adapt_set_test_stall(int on);
+
 /*
  * Gradients of adapters: grad[i] = sum over the rows t of adapter i of h[t]^T x[t], so of B_i from h and dy, and of A_i from
  * dh and x, with h and dh as ts_adapt_rows gives them.

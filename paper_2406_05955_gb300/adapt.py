@@ -144,6 +144,16 @@ class Adapters:
         return out, grads[0], grads[1]
 
 
+def adapt_error(stream=None) -> int:
+    """``ts_adapt_get_error``: the status of adapters' calls on the current device since it was last asked for."""
+    return int(lib().ts_adapt_get_error(_handle(stream)))
+
+
+def adapt_test_stall(on: bool) -> None:
+    """Failure-detection test hook: a bounded wait of the next calls over many rows runs out."""
+    lib().ts_adapt_set_test_stall(int(bool(on)))
+
+
 class Kept(NamedTuple):
     q_gate: torch.Tensor  # e4m3 [rows][m] gate factors, 0 where either factor is not positive
     q_up: torch.Tensor    # e4m3 [rows][m] up factors

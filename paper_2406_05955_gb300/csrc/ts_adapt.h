@@ -11,6 +11,7 @@ namespace tsffn {
 constexpr int kMaxAdapters = 255;  // and one group of rows that have none: kMaxRouteExperts
 constexpr int kMaxRank = 128;
 constexpr int kFewRows = 64;       // of a call without a list
+constexpr int kWideRank = 64;      // of the kernel of ts_adapt_wide.cu
 
 struct AdaptLaunch {
     const void* x;           // [rows] rows of k bf16, ldx apart
@@ -29,7 +30,13 @@ struct AdaptLaunch {
     void* out;               // the same, ldo apart (nullptr: h alone)
     int64_t ldo;
     float* h;                // [rows][r] or nullptr
+    int test_stall;          // ts_adapt_set_test_stall
 };
+
+// The most tiles of up to mt rows that a list of so many rows, and those of no adapter, can have.
+inline long long most_tiles(int rows, int n_adapters, int mt) {
+    return (long long)rows / mt + (rows < n_adapters + 1 ? rows : n_adapters + 1);
+}
 
 struct AdapterGradsLaunch {
     const float* h;          // [rows][r]
@@ -111,10 +118,12 @@ struct CombineBackwardLaunch {
 
 size_t balance_work(int tokens, int n_experts);  // floats
 
-cudaError_t prepare_adapt();
 cudaError_t launch_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* rows, int32_t* offsets,
                              cudaStream_t stream);
 cudaError_t launch_adapt(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
+cudaError_t launch_adapt_wide(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
+// What kernels on the current device have recorded since the last call (status bits), read and cleared.
+cudaError_t adapt_status(unsigned* bits, cudaStream_t stream);
 cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStream_t stream);
 cudaError_t launch_drelu(const DreluLaunch& a, bool f32, cudaStream_t stream);
 cudaError_t launch_drelu_backward(const DreluBackwardLaunch& a, bool f32, cudaStream_t stream);

@@ -2,9 +2,12 @@
 // and launches. None of these operators keeps anything between calls.
 #include <stdint.h>
 
+#include <atomic>
+
 #include "ts_adapt.h"
 #include "ts_ffn.h"
 #include "ts_grouped.h"
+#include "ts_kernels.cuh"
 
 using namespace tsffn;
 
@@ -12,6 +15,7 @@ namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+std::atomic<int> test_stall{0};  // ts_adapt_set_test_stall
 ts_status launched(cudaError_t e) { return e == cudaSuccess ? TS_OK : TS_ERR_CUDA; }
 int elem_size(ts_dtype dt) { return dt == TS_F32 ? 4 : dt == TS_BF16 ? 2 : 1; }
 
@@ -66,11 +70,18 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
         return TS_ERR_INVALID_ARG;
     if (!out ? y != nullptr || !h : !rows_ok(y, ldy, n, ydtype) || !rows_ok(out, ldo, n, ydtype) || (out == y && ldo != ldy))
         return TS_ERR_INVALID_ARG;
-    if (prepare_adapt() != cudaSuccess) return TS_ERR_CUDA;
     return launched(launch_adapt({x, ldx, rows, k, a, b, scale, ranks, n_adapters, r, n, list ? nullptr : ids, list,
-                                  list ? offsets : nullptr, y, ldy, out, ldo, h},
+                                  list ? offsets : nullptr, y, ldy, out, ldo, h, test_stall.load()},
                                  ydtype == TS_F32, stream));
 }
+
+ts_status ts_adapt_get_error(cudaStream_t stream) {
+    unsigned bits = 0;
+    if (adapt_status(&bits, stream) != cudaSuccess) return TS_ERR_CUDA;
+    return bits & kStatusTimeout ? TS_ERR_TIMEOUT : TS_OK;
+}
+
+void ts_adapt_set_test_stall(int on) { test_stall = on != 0; }
 
 ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
                            int64_t ld_scale, int rows, int k, int n_adapters, const int32_t* list, const int32_t* offsets,
@@ -83,7 +94,6 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
     if (rows > 0 && (!h || !aligned4(h) || !rows_ok(x, ldx, k, xdtype) || !list || !aligned4(list) ||
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
-    if (prepare_adapt() != cudaSuccess) return TS_ERR_CUDA;
     return launched(launch_adapter_grads(
         {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0}, e8, stream));
 }
