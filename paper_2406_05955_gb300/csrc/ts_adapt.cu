@@ -9,8 +9,6 @@
 // come by 16-byte asynchronous copies.
 //
 // Memory bounds it: x, y and out are 2 k + 2 n elements a row, the products 2 r flops for each of them.
-#include <cuda_fp8.h>
-
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
 
@@ -371,283 +369,6 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
     }
 }
 
-// ---------------------------------------------------------------------------
-// gradients
-// ---------------------------------------------------------------------------
-// A CTA has 128 columns of x; the rows of an adapter come in chunks of 64. h is the transposed operand and is split into
-// three bf16 numbers, x is exact in bf16 (e4m3 rows too: the scale that 128 of their columns share is multiplied into h).
-constexpr int kGradCols = 128, kGradRows = 64;
-constexpr int kIdRing = 8;
-
-template <int RP, bool E8>
-struct Grads {
-    static constexpr int kXPitch = kGradCols * (E8 ? 1 : 2);
-    static constexpr int kXBytes = kGradRows * kXPitch, kHBytes = kGradRows * RP * 4, kScaleBytes = E8 ? kGradRows * 4 : 0;
-    static constexpr int kStage = kXBytes + kHBytes + kScaleBytes;
-    static constexpr int kStages = 3;
-    static constexpr int kHPitch = RP * 2 + 16;
-    static constexpr int kPartBytes = kGradRows * kHPitch;
-    static constexpr int kWide = E8 ? kGradRows * kChunk : 0;  // x in bf16
-    static constexpr int kSmem = kStages * kStage + 3 * kPartBytes + kWide;
-    static constexpr int kMGroups = RP == 16 ? 1 : 2;          // ways that the warps share the components
-    static constexpr int kMT = RP / 16 / kMGroups;             // 16-component tiles of a warp
-    static constexpr int kNT = kGradCols / 8 / (kWarps / kMGroups);
-    static_assert(kStages * kStage >= RP * kGradCols * 4 && kStages + 2 <= kIdRing, "");
-};
-
-// Whether an adapter's rows are shared by the CTAs of a cluster: where one CTA would have more than twice the even share.
-__device__ __forceinline__ bool shared_rows(int count, int even) { return count > max(2 * even, kGradRows); }
-
-// First entry of adapter `id` in the list, and their number.
-__device__ __forceinline__ int2 entries(const AdapterGradsLaunch& L, int id) {
-    const int begin = min(max(L.offsets[id], 0), L.rows);
-    return make_int2(begin, min(max(L.offsets[id + 1], begin), L.rows) - begin);
-}
-
-template <int RP, bool E8>
-__global__ void __launch_bounds__(kThreads) k_adapter_grads(const __grid_constant__ AdapterGradsLaunch L, int ctas, int even) {
-    using G = Grads<RP, E8>;
-    extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int ids[kIdRing][kGradRows];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t cta = cluster_rank();
-    unsigned char* const parts = smem + G::kStages * G::kStage;
-    unsigned char* const wide = parts + 3 * G::kPartBytes;
-    const uint32_t smem0 = smem_u32(smem), parts0 = smem_u32(parts), wide0 = smem_u32(wide);
-    const int col0 = (int)(blockIdx.x / ctas) * kGradCols;
-    const bool h_vec = L.r % 4 == 0 && (reinterpret_cast<uintptr_t>(L.h) & 15u) == 0;
-    pdl_wait();
-
-    // The sums over entries begin .. begin + count - 1 of the list, of which `mine` are this CTA's; shared: the cluster's CTAs
-    // join theirs.
-    const auto sums = [&](int id, int begin, int count, bool join) {
-        const int chunks = (count + kGradRows - 1) / kGradRows, parties = join ? ctas : 1, me = join ? (int)cta : 0;
-        const int c0 = (int)((long long)chunks * me / parties), nc = (int)((long long)chunks * (me + 1) / parties) - c0;
-        const int first = begin + c0 * kGradRows, end = begin + count;
-        const auto listed = [&](int i) {
-            const int at = first + i * kGradRows + tid;
-            const int row = tid < kGradRows && i < nc && at < end ? L.list[at] : -1;
-            return (unsigned)row < (unsigned)L.rows ? row : -1;
-        };
-        const auto issue = [&](int i) {
-            if (i < nc) {
-                const uint32_t to = smem0 + (uint32_t)(i % G::kStages) * G::kStage;
-                const int* const rows = ids[i % kIdRing];
-                constexpr int kPieces = G::kXPitch / 16;
-#pragma unroll
-                for (int p = tid; p < kGradRows * kPieces; p += kThreads) {
-                    const int row = p / kPieces, c = p % kPieces, col = col0 + c * (E8 ? 16 : 8);
-                    const bool in = rows[row] >= 0 && col < L.k;
-                    const char* const from = static_cast<const char*>(L.x) + (in ? (rows[row] * L.ldx + col) * (E8 ? 1 : 2) : 0);
-                    copy16(to + (E8 ? p * 16 : place<kChunk>(row, c)), from, in);
-                }
-                const uint32_t h = to + G::kXBytes;
-                if (h_vec) {
-                    for (int p = tid; p < kGradRows * (RP / 4); p += kThreads) {
-                        const int row = p / (RP / 4), j = p % (RP / 4) * 4;
-                        const bool in = rows[row] >= 0 && j < L.r;
-                        copy16(h + p * 16, in ? L.h + (size_t)rows[row] * L.r + j : L.h, in);
-                    }
-                } else {
-                    for (int p = tid; p < kGradRows * RP; p += kThreads) {
-                        const int row = p / RP, j = p % RP;
-                        const bool in = rows[row] >= 0 && j < L.r;
-                        copy4(h + p * 4, in ? L.h + (size_t)rows[row] * L.r + j : L.h, in);
-                    }
-                }
-                if (E8 && tid < kGradRows) {
-                    const bool in = rows[tid] >= 0;
-                    copy4(h + G::kHBytes + tid * 4,
-                          in ? L.x_scale + (int64_t)(col0 / kScaleBlock) * L.ld_scale + rows[tid] : L.x_scale, in);
-                }
-            }
-            copies_commit();
-        };
-        float acc[G::kMT][G::kNT][4] = {}, sum[G::kMT][G::kNT][4] = {};
-        int next = -1;
-        __syncthreads();  // (of what the last sums have in shared memory)
-        for (int i = 0; i < G::kStages; ++i) {
-            next = listed(i);
-            if (tid < kGradRows) ids[i][tid] = next;
-        }
-        next = listed(G::kStages);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < G::kStages - 1; ++i) issue(i);
-        const int mg = warp % G::kMGroups, n0 = warp / G::kMGroups * G::kNT * 8;
-        for (int i = 0; i < nc; ++i) {
-            copies_wait<G::kStages - 2>();
-            __syncthreads();
-            if (tid < kGradRows) ids[(i + G::kStages) % kIdRing][tid] = next;
-            next = listed(i + G::kStages + 1);
-            issue(i + G::kStages - 1);
-            const unsigned char* const stage = smem + (i % G::kStages) * G::kStage;
-            const float* const h = reinterpret_cast<const float*>(stage + G::kXBytes);
-#pragma unroll 4
-            for (int p = tid; p < kGradRows * (RP / 4); p += kThreads) {
-                const int row = p / (RP / 4), j = p % (RP / 4) * 4;
-                float4 v = reinterpret_cast<const float4*>(h)[p];
-                if constexpr (E8) {
-                    const float s = reinterpret_cast<const float*>(stage + G::kXBytes + G::kHBytes)[row];
-                    v.x *= s, v.y *= s, v.z *= s, v.w *= s;
-                }
-                __nv_bfloat16 q[4][3];
-                split<3>(v.x, q[0]);
-                split<3>(v.y, q[1]);
-                split<3>(v.z, q[2]);
-                split<3>(v.w, q[3]);
-#pragma unroll
-                for (int t = 0; t < 3; ++t) {
-                    __nv_bfloat162 two[2] = {__halves2bfloat162(q[0][t], q[1][t]), __halves2bfloat162(q[2][t], q[3][t])};
-                    *reinterpret_cast<uint2*>(parts + t * G::kPartBytes + row * G::kHPitch + j * 2) = *reinterpret_cast<const uint2*>(two);
-                }
-            }
-            if constexpr (E8) {
-#pragma unroll
-                for (int p = tid; p < kGradRows * kGradCols / 16; p += kThreads) {
-                    const int row = p / (kGradCols / 16), c = p % (kGradCols / 16) * 2;
-                    const uint4 v = reinterpret_cast<const uint4*>(stage)[p];
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t b[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const __half2_raw f = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[e / 2] >> 16 * (e & 1)), __NV_E4M3);
-                        const __nv_bfloat162 t = __float22bfloat162_rn(__half22float2(*reinterpret_cast<const __half2*>(&f)));
-                        b[e] = *reinterpret_cast<const uint32_t*>(&t);
-                    }
-                    *reinterpret_cast<uint4*>(wide + place<kChunk>(row, c)) = make_uint4(b[0], b[1], b[2], b[3]);
-                    *reinterpret_cast<uint4*>(wide + place<kChunk>(row, c + 1)) = make_uint4(b[4], b[5], b[6], b[7]);
-                }
-            }
-            __syncthreads();
-            const uint32_t x0 = E8 ? wide0 : smem0 + (uint32_t)(i % G::kStages) * G::kStage;
-#pragma unroll
-            for (int ks = 0; ks < kGradRows / 16; ++ks) {
-                uint32_t w[G::kNT / 2][4];
-#pragma unroll
-                for (int t = 0; t < G::kNT; t += 2)
-                    ldmatrix4_t(w[t / 2], x0 + place<kChunk>(ks * 16 + (lane & 15), n0 / 8 + t + (lane >> 4)));
-#pragma unroll
-                for (int m = 0; m < G::kMT; ++m)
-#pragma unroll
-                    for (int q = 2; q >= 0; --q) {
-                        uint32_t a[4];
-                        ldmatrix4_t(a, parts0 + q * G::kPartBytes + (ks * 16 + (lane & 7) + (lane >> 4) * 8) * G::kHPitch +
-                                           ((mg * G::kMT + m) * 16 + ((lane >> 3) & 1) * 8) * 2);
-#pragma unroll
-                        for (int t = 0; t < G::kNT; t += 2) {
-                            mma(acc[m][t], a, w[t / 2][0], w[t / 2][1]);
-                            mma(acc[m][t + 1], a, w[t / 2][2], w[t / 2][3]);
-                        }
-                    }
-            }
-#pragma unroll
-            for (int m = 0; m < G::kMT; ++m)
-#pragma unroll
-                for (int t = 0; t < G::kNT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {  // (the tensor cores cut bits off a long sum)
-                        sum[m][t][e] += acc[m][t][e];
-                        acc[m][t][e] = 0.0f;
-                    }
-        }
-        float* const grad = L.grad + (size_t)id * L.r * L.k;
-        if (!join) {
-#pragma unroll
-            for (int m = 0; m < G::kMT; ++m)
-#pragma unroll
-                for (int t = 0; t < G::kNT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        const int j = (mg * G::kMT + m) * 16 + lane / 4 + e * 4, col = col0 + n0 + t * 8 + (lane & 3) * 2;
-                        if (j >= L.r || col >= L.k) continue;
-                        float2* const to = reinterpret_cast<float2*>(grad + (size_t)j * L.k + col);
-                        float2 v = make_float2(sum[m][t][e], sum[m][t][e + 1]);
-                        if (L.accumulate) {
-                            const float2 had = *to;
-                            v.x += had.x, v.y += had.y;
-                        }
-                        *to = v;
-                    }
-            return;
-        }
-        copies_wait<0>();
-        __syncthreads();  // the stages hold the sums now
-        float* const mine = reinterpret_cast<float*>(smem);
-#pragma unroll
-        for (int m = 0; m < G::kMT; ++m)
-#pragma unroll
-            for (int t = 0; t < G::kNT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; e += 2)
-                    *reinterpret_cast<float2*>(mine + ((mg * G::kMT + m) * 16 + lane / 4 + e * 4) * kGradCols + n0 + t * 8 + (lane & 3) * 2) =
-                        make_float2(sum[m][t][e], sum[m][t][e + 1]);
-        __syncthreads();
-        cluster_arrive();
-        cluster_wait();
-        constexpr int kQuads = RP * kGradCols / 4;
-        for (int p = (int)cta * kThreads + tid; p < kQuads; p += kThreads * ctas) {
-            const int j = p / (kGradCols / 4), col = col0 + p % (kGradCols / 4) * 4;
-            if (j >= L.r || col >= L.k) continue;
-            float4 v[kMaxCluster];
-#pragma unroll
-            for (int c = 0; c < kMaxCluster; ++c)
-                if (c < ctas) v[c] = cluster_ld4(smem0 + 16 * p, (uint32_t)c);
-            float4* const to = reinterpret_cast<float4*>(grad + (size_t)j * L.k + col);
-            float4 s = v[0];
-#pragma unroll
-            for (int c = 1; c < kMaxCluster; ++c)
-                if (c < ctas) s.x += v[c].x, s.y += v[c].y, s.z += v[c].z, s.w += v[c].w;
-            if (L.accumulate) {
-                const float4 had = *to;
-                s.x += had.x, s.y += had.y, s.z += had.z, s.w += had.w;
-            }
-            *to = s;
-        }
-        __syncthreads();
-        cluster_arrive();
-        cluster_wait();
-    };
-
-    // Adapters whose rows are shared go round by cluster, the others by CTA: thread t looks at adapter t, and the masks say
-    // which ones are this CTA's.
-    __shared__ unsigned bigs[kWarps], smalls[kWarps];
-    const int count_of_mine = tid < L.n_adapters ? entries(L, tid).y : 0;
-    const bool big = ctas > 1 && shared_rows(count_of_mine, even);
-    const bool small = tid < L.n_adapters && !big && !(count_of_mine == 0 && L.accumulate);
-    const unsigned big_here = __ballot_sync(0xffffffffu, big), small_here = __ballot_sync(0xffffffffu, small);
-    if (lane == 0) {
-        bigs[warp] = big_here;
-        smalls[warp] = small_here;
-    }
-    __syncthreads();
-    unsigned nth_big = __popc(big_here & ((1u << lane) - 1u)), nth_small = __popc(small_here & ((1u << lane) - 1u));
-    for (int w = 0; w < warp; ++w) {
-        nth_big += __popc(bigs[w]);
-        nth_small += __popc(smalls[w]);
-    }
-    __syncthreads();
-    const unsigned my_big = __ballot_sync(0xffffffffu, big && nth_big % gridDim.y == blockIdx.y);
-    const unsigned my_small = __ballot_sync(0xffffffffu, small && nth_small % (gridDim.y * ctas) == blockIdx.y * ctas + cta);
-    if (lane == 0) {
-        bigs[warp] = my_big;
-        smalls[warp] = my_small;
-    }
-    __syncthreads();
-    for (int w = 0; w < kWarps; ++w)
-        for (unsigned m = bigs[w]; m != 0u; m &= m - 1u) {
-            const int id = w * kWarp + __ffs(m) - 1;
-            const int2 of = entries(L, id);
-            sums(id, of.x, of.y, true);
-        }
-    for (int w = 0; w < kWarps; ++w)
-        for (unsigned m = smalls[w]; m != 0u; m &= m - 1u) {
-            const int id = w * kWarp + __ffs(m) - 1;
-            const int2 of = entries(L, id);
-            sums(id, of.x, of.y, false);
-        }
-}
-
 template <int MT, int RP, typename TY>
 cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
     // Few tiles: several clusters have one, each with its own h and a part of the columns, of 2 chunks a CTA at least.
@@ -691,47 +412,10 @@ cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
     return small ? launch_rank<16, TY>(a, tiles, ctas, stream) : launch_tiles<64, 128, TY>(a, tiles, ctas, stream);
 }
 
-template <int RP, bool E8>
-cudaError_t launch_grads(const AdapterGradsLaunch& a, cudaStream_t stream) {
-    const auto kernel = k_adapter_grads<RP, E8>;
-    constexpr int kSmem = Grads<RP, E8>::kSmem;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e != cudaSuccess) return e;
-    // about two rounds of CTAs, in clusters of 8: fewer where there are no more adapters or chunks than that
-    const int blocks = (a.k + kGradCols - 1) / kGradCols;
-    int ctas = kMaxCluster;
-    while (ctas > 1 && (long long)ctas * kGradRows / 2 >= a.rows) ctas /= 2;
-    const int wish = (kResidentCtas * 2 + blocks * ctas - 1) / (blocks * ctas);
-    const int ys = wish < a.n_adapters ? wish : a.n_adapters;
-    const int even = (int)((long long)a.rows * blocks / kResidentCtas);
-    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas), (unsigned)ys), kThreads, stream);
-    cfg.dynamicSmemBytes = kSmem;
-    cudaLaunchAttribute at[2]{};
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {(unsigned)ctas, 1, 1};
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, ctas, even);
-}
-
-template <bool E8>
-cudaError_t launch_grads_rank(const AdapterGradsLaunch& a, cudaStream_t stream) {
-    if (a.r <= 16) return launch_grads<16, E8>(a, stream);
-    if (a.r <= 32) return launch_grads<32, E8>(a, stream);
-    if (a.r <= 64) return launch_grads<64, E8>(a, stream);
-    return launch_grads<128, E8>(a, stream);
-}
-
 }  // namespace
 
 cudaError_t launch_adapt(const AdaptLaunch& a, bool y_f32, cudaStream_t stream) {
     return y_f32 ? launch_type<float>(a, stream) : launch_type<__nv_bfloat16>(a, stream);
-}
-
-cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStream_t stream) {
-    return e4m3 ? launch_grads_rank<true>(a, stream) : launch_grads_rank<false>(a, stream);
 }
 
 }  // namespace tsffn

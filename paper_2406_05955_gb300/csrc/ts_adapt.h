@@ -50,6 +50,7 @@ struct AdapterGradsLaunch {
     const int32_t* offsets;
     float* grad;             // [n_adapters][r][k]
     int accumulate;
+    int test_stall;          // ts_adapt_set_test_stall
 };
 
 struct DreluLaunch {
@@ -122,8 +123,9 @@ cudaError_t launch_list_rows(const int32_t* ids, int n_rows, int n_groups, int32
                              cudaStream_t stream);
 cudaError_t launch_adapt(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
 cudaError_t launch_adapt_wide(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
-// What kernels on the current device have recorded since the last call (status bits), read and cleared.
-cudaError_t adapt_status(unsigned* bits, cudaStream_t stream);
+// What the kernels on the current device have recorded since the last call (status bits), read and cleared.
+cudaError_t adapt_wide_status(unsigned* bits, cudaStream_t stream);
+cudaError_t adapter_grads_status(unsigned* bits, cudaStream_t stream);
 cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStream_t stream);
 cudaError_t launch_drelu(const DreluLaunch& a, bool f32, cudaStream_t stream);
 cudaError_t launch_drelu_backward(const DreluBackwardLaunch& a, bool f32, cudaStream_t stream);

@@ -76,9 +76,9 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
 }
 
 ts_status ts_adapt_get_error(cudaStream_t stream) {
-    unsigned bits = 0;
-    if (adapt_status(&bits, stream) != cudaSuccess) return TS_ERR_CUDA;
-    return bits & kStatusTimeout ? TS_ERR_TIMEOUT : TS_OK;
+    unsigned rows = 0, grads = 0;
+    if (adapt_wide_status(&rows, stream) != cudaSuccess || adapter_grads_status(&grads, stream) != cudaSuccess) return TS_ERR_CUDA;
+    return (rows | grads) & kStatusTimeout ? TS_ERR_TIMEOUT : TS_OK;
 }
 
 void ts_adapt_set_test_stall(int on) { test_stall = on != 0; }
@@ -95,7 +95,7 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_adapter_grads(
-        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0}, e8, stream));
+        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, test_stall.load()}, e8, stream));
 }
 
 ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, ts_dtype dtype, const int32_t* n, int rows,

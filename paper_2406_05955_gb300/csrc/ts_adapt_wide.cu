@@ -29,54 +29,6 @@ struct Wide {
     static_assert(kTileRows * RP * 4 <= kParts * kPart, "the sums lie where h will");
 };
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
-__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// 32 lanes x 8 columns, a lane a thread
-__device__ __forceinline__ void tc_ld8(uint32_t at, float* v) {
-    uint32_t r[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(at)
-                 : "memory");
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
-}
-// the values of the loads before: not to be used earlier
-template <int N>
-__device__ __forceinline__ void tc_ld_wait(float (&v)[N]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
-}
-// shared-memory descriptors with the 128-byte swizzle: k along the 128-byte rows (atoms of 8 rows, 1024 bytes apart), or 64
-// columns along them (8 of k an atom, `block` bytes between blocks of 64 columns)
-__device__ __forceinline__ uint64_t desc_k(uint32_t at) {
-    return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-__device__ __forceinline__ uint64_t desc_n(uint32_t at, uint32_t block) {
-    return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)(block >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)2 << 61;
-}
-// D fp32, A and B bf16, 128 rows, n columns; B's columns along its rows
-constexpr uint32_t idesc(int n, bool by_columns) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (by_columns ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (8u << 24);
-}
-
 template <int RP, typename TY>
 __global__ void __launch_bounds__(kThreads, 1) k_adapt_wide(const __grid_constant__ AdaptLaunch L, int ctas) {
     using W = Wide<RP, TY>;
@@ -121,10 +73,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapt_wide(const __grid_constan
         mbar_init(&done[1], 1);
         mbar_fence_init();
     }
-    if (warp == 0 && rank > 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    if (warp == 0 && rank > 0) tc_alloc<512>(&tmem);
     tc_before();
     __syncthreads();
     tc_after();
@@ -195,14 +144,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapt_wide(const __grid_constan
 #pragma unroll
             for (int ks = 0; ks < W::kCols / 16; ++ks)
                 tc_mma(d, desc_k(at + (ks >> 2) * (W::kRowsBytes / 2)) + 2 * (ks & 3), desc_k(mat + (ks >> 2) * (RP * 128)) + 2 * (ks & 3),
-                       idesc(RP, false), (i & 1) != 0 || ks > 0);
+                       idesc(RP, false, false), (i & 1) != 0 || ks > 0);
         } else {
 #pragma unroll
             for (int q = W::kParts - 1; q >= 0; --q)
 #pragma unroll
                 for (int ks = 0; ks < RP / 16; ++ks)
                     tc_mma(t_out + (i & 1) * 128, desc_k(h0 + q * W::kPart) + 2 * ks, desc_n(mat, RP * 128) + 128 * ks,
-                           idesc(W::kOutCols, true), q < W::kParts - 1 || ks > 0);
+                           idesc(W::kOutCols, false, true), q < W::kParts - 1 || ks > 0);
         }
         if (!(L.test_stall && i == total - 1)) tc_commit(&done[i & 1]);
     };
@@ -365,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapt_wide(const __grid_constan
     __syncthreads();
     if (warp == 0 && rank > 0) {
         tc_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        tc_free<512>(tmem);
     }
 }
 
@@ -411,7 +360,7 @@ cudaError_t launch_adapt_wide(const AdaptLaunch& a, bool y_f32, cudaStream_t str
     return y_f32 ? launch_rank<float>(a, stream) : launch_rank<__nv_bfloat16>(a, stream);
 }
 
-cudaError_t adapt_status(unsigned* bits, cudaStream_t stream) {
+cudaError_t adapt_wide_status(unsigned* bits, cudaStream_t stream) {
     static const unsigned zero = 0;
     cudaError_t e = cudaMemcpyFromSymbolAsync(bits, wide_status, sizeof *bits, 0, cudaMemcpyDeviceToHost, stream);
     if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(wide_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, stream);

@@ -360,6 +360,16 @@ def test_a_wait_that_gives_up(ts):
         ts.adapt_test_stall(False)
     assert ts.adapt_error() == 5 and ts.adapt_error() == 0
     assert torch.equal(ad.forward(x, y, ids, out=torch.empty_like(y)), want)
+    rows, h, dy = ad.rows(ids), torch.randn(600, 16, device="cuda"), y.clone()
+    want = ad.backward(dy, None, rows, h, x)
+    ts.adapt_test_stall(True)
+    try:
+        ad.backward(dy, None, rows, h, x)
+        torch.cuda.synchronize()
+    finally:
+        ts.adapt_test_stall(False)
+    assert ts.adapt_error() == 5 and ts.adapt_error() == 0
+    assert all(torch.equal(p, q) for p, q in zip(ad.backward(dy, None, rows, h, x)[1:], want[1:]))
 
 
 def test_refusals(ts):
