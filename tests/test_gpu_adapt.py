@@ -239,6 +239,25 @@ def test_backward(ts, t, k, n, r, adapters, x8):
     assert torch.equal(da2, da + 2.0) and torch.equal(db2, db - 2.0)
 
 
+@pytest.mark.parametrize("t,r,adapters", [(1, 8, 3), (7, 16, 7), (200, 4, 200), (900, 17, 30), (2500, 64, 5), (1100, 128, 9)])
+def test_gradients_of_uneven_adapters(ts, t, r, adapters):
+    """Nearly all rows have one adapter, each its own, few at the ends: whatever part of the list a CTA has."""
+    g = gen(t)
+    k, n = 136, 264
+    x, dy, h = randn(g, t, k).to(BF16), randn(g, t, n).to(BF16), randn(g, t, r)
+    ad = ts.Adapters(torch.zeros(adapters, r, k, dtype=BF16, device="cuda"), torch.zeros(adapters, r, n, dtype=BF16, device="cuda"))
+    some = torch.randint(0, adapters, (t,), generator=g, device="cuda")
+    last = torch.full_like(some, adapters - 1)
+    first = torch.where(torch.arange(t, device="cuda") % 100 == 3, some, 0)
+    for ids in (some, last, first, torch.arange(t, device="cuda") % adapters, torch.arange(t, device="cuda") * adapters // t,
+                torch.where(some == 1, -1, 1), torch.where(torch.arange(t, device="cuda") < t // 2, 0, adapters - 1)):
+        _, _, db = ad.backward(dy, None, ids.to(torch.int32), h, x)
+        one = torch.nn.functional.one_hot(ids.clamp(min=0).long(), adapters).double() * (ids >= 0)[:, None]
+        want = torch.einsum("ta,tr,tn->arn", one, h.double(), dy.double())
+        mag = torch.einsum("ta,tr,tn->arn", one, h.double().abs(), dy.double().abs())
+        assert ((db.double() - want).abs() <= (one.sum(0) + 17)[:, None, None] * U * mag).all()
+
+
 def test_rows_without_an_adapter_do_not_reach_the_gradients(ts):
     x, _, a, b, scale, ids = case(200, 256, 128, 8, 3, seed=9, none=0.3)
     g = gen(10)
