@@ -104,14 +104,15 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     using G = Grads<RP, E8>;
     extern __shared__ unsigned char raw[];
     __shared__ int offs[kMaxAdapters + 1];
-    __shared__ long long x_at[G::kRing][kGradRows], h_at[G::kRing][kGradRows];  // first byte of a chunk's rows, -1: none
+    __shared__ uint2 x_at[G::kRing][kGradRows], h_at[G::kRing][kGradRows];  // first byte of a chunk's rows (none: the highest bit)
     __shared__ int rows[E8 ? G::kRing : 1][kGradRows];
+    __shared__ int ids[G::kRing];  // a chunk's adapter
     __shared__ int chunks, first_id;
     __shared__ uint64_t done;
     __shared__ uint32_t tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t cta = cluster_rank();
-    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* const smem = raw + (-smem_u32(raw) & 1023u);
     unsigned char* const wide = smem + G::kStages * G::kXBytes;
     unsigned char* const parts = wide + G::kWideBytes;
     unsigned char* const hs = parts + G::kPart;
@@ -152,8 +153,9 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     const int x_row = tid / kPieces, x_piece = tid % kPieces, h_row = tid / kQuads, h_quad = tid % kQuads;
     const bool x_in = col0 + x_piece * (E8 ? 16 : 8) < L.k, h_in = h_quad * 4 < L.r;
     const uint32_t x_to = E8 ? tid * 16 : (x_piece >> 3) * G::kBlock + place<128>(x_row, x_piece & 7);
-    const char* const x_from = static_cast<const char*>(L.x) + (int64_t)col0 * (E8 ? 1 : 2) + x_piece * 16;
-    const char* const h_from = reinterpret_cast<const char*>(L.h) + h_quad * 16;
+    const char* const x_from = static_cast<const char*>(L.x) + (x_in ? (int64_t)col0 * (E8 ? 1 : 2) + x_piece * 16 : 0);
+    const char* const h_from = reinterpret_cast<const char*>(L.h) + (h_in ? h_quad * 16 : 0);
+    const float* const scale_from = E8 ? L.x_scale + (int64_t)(col0 / kScaleBlock) * L.ld_scale : nullptr;
     uint32_t part_to[3];
 #pragma unroll
     for (int t = 0; t < 3; ++t) {
@@ -162,59 +164,59 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     }
     static_assert(kXStep % 8 == 0 && kHStep % 8 == 0, "a thread's rows are permuted alike");
 
-    const auto issue = [&](int i) {
+    // Copies 16 bytes (or N) of the row at `at`, zeros where there is none.
+    const auto from = [](const char* base, const uint2& at) { return base + ((uint64_t)(at.y & 0x7fffffffu) << 32 | at.x); };
+    const auto issue = [&](int i, int stage, int ring) {  // chunk i, its places in the rings of rows and of what is known of them
         if (i < nc) {
-            const uint32_t stage = (uint32_t)(i % G::kStages);
             const uint32_t to = smem0 + stage * G::kXBytes + x_to;
-            const long long* const xs = x_at[i % G::kRing];
 #pragma unroll
             for (int p = 0; p < kGradRows / kXStep; ++p) {
-                const long long at = xs[x_row + p * kXStep];
-                const bool in = x_in && at >= 0;
-                copy16(to + p * (E8 ? kThreads * 16 : kXStep * 128), in ? x_from + at : static_cast<const char*>(L.x), in);
+                const uint2 at = x_at[ring][x_row + p * kXStep];
+                copy16(to + p * (E8 ? kThreads * 16 : kXStep * 128), from(x_from, at), x_in && (int)at.y >= 0);
             }
             const uint32_t h = hs0 + stage * G::kHBytes + tid * 16;
-            const long long* const ats = h_at[i % G::kRing];
             if (h_vec) {
 #pragma unroll
                 for (int p = 0; p < kGradRows / kHStep; ++p) {
-                    const long long at = ats[h_row + p * kHStep];
-                    const bool in = h_in && at >= 0;
-                    copy16(h + p * kThreads * 16, in ? h_from + at : reinterpret_cast<const char*>(L.h), in);
+                    const uint2 at = h_at[ring][h_row + p * kHStep];
+                    copy16(h + p * kThreads * 16, from(h_from, at), h_in && (int)at.y >= 0);
                 }
             } else {
 #pragma unroll 1
                 for (int p = 0; p < kGradRows / kHStep; ++p)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const long long at = ats[h_row + p * kHStep];
-                        const bool in = at >= 0 && h_quad * 4 + e < L.r;
-                        copy4(h + p * kThreads * 16 + e * 4, in ? h_from + at + e * 4 : reinterpret_cast<const char*>(L.h), in);
+                        const uint2 at = h_at[ring][h_row + p * kHStep];
+                        const bool in = (int)at.y >= 0 && h_quad * 4 + e < L.r;
+                        copy4(h + p * kThreads * 16 + e * 4, in ? from(h_from, at) + e * 4 : reinterpret_cast<const char*>(L.h), in);
                     }
             }
             if (E8 && tid < kGradRows) {
-                const int row = rows[i % G::kRing][tid];
-                copy4(scales0 + stage * G::kScaleBytes + tid * 4,
-                      L.x_scale + (int64_t)(col0 / kScaleBlock) * L.ld_scale + max(row, 0), row >= 0);
+                const int row = rows[ring][tid];
+                copy4(scales0 + stage * G::kScaleBytes + tid * 4, scale_from + max(row, 0), row >= 0);
             }
         }
         copies_commit();
     };
-    // The rows of chunks are looked up two turns before their copies are issued.
-    Chunks ahead{first_id, begin, end}, here = ahead;
-    const auto look_up = [&]() {
-        int first = 0, of = 0;
+    // The first two warps look up the rows of chunks, two turns before their copies are issued.
+    const bool looks = tid < kGradRows;
+    Chunks ahead{first_id, begin, end};
+    const auto look_up = [&](int& of) {
+        if (!looks) return -1;
+        int first = 0;
         const int n = ahead.next(offs, first, of);
         const int row = tid < n ? L.list[first + tid] : -1;
         return (unsigned)row < (unsigned)L.rows ? row : -1;
     };
-    const auto know = [&](int i, int row) {
-        if (tid < kGradRows) {
-            x_at[i % G::kRing][tid] = row < 0 ? -1 : row * L.ldx * (E8 ? 1 : 2);
-            h_at[i % G::kRing][tid] = row < 0 ? -1 : (long long)row * L.r * 4;
-            if (E8) rows[i % G::kRing][tid] = row;
-        }
+    const auto know = [&](int ring, int row, int of) {
+        if (!looks) return;
+        const uint64_t x = row < 0 ? 1ull << 63 : (uint64_t)(row * L.ldx * (E8 ? 1 : 2)), h = row < 0 ? 1ull << 63 : (uint64_t)row * L.r * 4;
+        x_at[ring][tid] = make_uint2((uint32_t)x, (uint32_t)(x >> 32));
+        h_at[ring][tid] = make_uint2((uint32_t)h, (uint32_t)(h >> 32));
+        if (E8) rows[ring][tid] = row;
+        if (tid == 0) ids[ring] = of;
     };
+    const auto after = [](int at, int n) { return at + 1 == n ? 0 : at + 1; };
     float sum[G::kMine] = {};
     const auto take_over = [&] {  // what the tensor cores have added up
         float v[G::kMine];
@@ -248,28 +250,32 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     };
 
     if (nc > 0) {
-        int ring[G::kStages];
+        int ring[G::kStages], of[G::kStages], next_of = 0;
 #pragma unroll
-        for (int i = 0; i < G::kStages; ++i) ring[i] = look_up();
-        int next = look_up();
+        for (int i = 0; i < G::kStages; ++i) ring[i] = look_up(of[i] = 0);
+        int next = look_up(next_of);
 #pragma unroll
-        for (int i = 0; i < G::kStages; ++i) know(i, ring[i]);
+        for (int i = 0; i < G::kStages; ++i) know(i, ring[i], of[i]);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < G::kStages; ++i) issue(i);
+        for (int i = 0; i < G::kStages; ++i) issue(i, i, i);
+        int stage = G::kStages - 1, last = 0, known = G::kStages, coming = G::kStages - 1, here = G::kRing - 1;
         int id = -1, nth = 0;  // the adapter of the last chunk, and how many of its chunks there were
         for (int i = 0; i < nc; ++i) {
-            const int stage = i % G::kStages;
-            int first, now = 0;
-            here.next(offs, first, now);
+            last = stage;
+            stage = after(stage, G::kStages);
+            here = after(here, G::kRing);
+            const int now = ids[here];
             if (i == 0) copies_wait<G::kStages - 1>();
             else copies_wait<G::kStages - 2>();
             if (E8) __syncthreads();  // (the scales)
-            know(i + G::kStages, next);
-            next = look_up();
+            know(known, next, next_of);
+            known = after(known, G::kRing);
+            next = look_up(next_of);
             if (i > 0) {  // the last chunk's products are done: what they read may be overwritten
                 if (!failed) failed = !mbar_wait(&done, (i - 1) & 1);
-                issue(i - 1 + G::kStages);
+                coming = after(coming, G::kRing);
+                issue(i - 1 + G::kStages, last, coming);
                 if (now != id || (nth & 3) == 0) {  // (every 256 rows too: the tensor cores cut bits off a long sum)
                     tc_after();
                     take_over();
