@@ -577,7 +577,7 @@ ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* ro
  *   scale      device [n_adapters] fp32, NULL: 1
  *   ranks      device [n_adapters] int32, NULL: r. Components from ranks[i] on count as 0 and are not read.
  *   n_adapters 1..255, r 1..128
- *   ids        device [rows] int32; read where there is no list: up to 64 rows
+ *   ids        device [rows] int32; read where there is no list: up to 512 rows
  *   list, offsets   as ts_list_rows writes them from ids for n_adapters groups, or NULL
  *   y, ldy     device, rows of n of ydtype (TS_BF16 or TS_F32), ldy apart
  *   out, ldo   the same; may be y itself. NULL (y as well): h alone
@@ -653,7 +653,7 @@ ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, co
  *   counts     device [n_experts] int32: picks of each expert
  *   share      device [n_experts] fp32
  *   totals     device [2] int32: live tokens, picks
- *   work       device, ts_balance_work(tokens, n_experts) fp32, not shared by calls in flight at once
+ *   work       device, ts_balance_work(tokens, n_experts) fp32 (0: may be NULL), not shared by calls in flight at once
  */
 long long ts_balance_work(int tokens, int n_experts); /* -1: sizes that ts_balance refuses */
 ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32_t* sel, int top_k, float* loss,

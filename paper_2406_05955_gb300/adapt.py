@@ -7,10 +7,11 @@ from typing import NamedTuple, Optional
 import torch
 
 from .binding import TS_BF16, _check, lib
-from .prompt import BLOCK, _CODES, _empty, _handle, _ld, _shaped, _tensor
+from .prompt import BLOCK, _CODES, _current_device, _empty, _handle, _ld, _rows_apart, _shaped, _tensor
 
-FEW_ROWS = 64  # rows of a call without a list
+FEW_ROWS = 512  # rows of a call without a list
 _BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+_ROWS, _ONLY_BF16 = (_BF16, _F32), (_BF16,)  # types of rows that are added to, and of those that are multiplied
 
 
 class AdapterRows(NamedTuple):
@@ -30,10 +31,11 @@ def list_rows(ids: torch.Tensor, groups: int, rows=None, offsets=None, stream=No
     return AdapterRows(rows, offsets)
 
 
-def _matrix(t, what: str, dtypes, shape) -> torch.Tensor:
-    """``t``, checked: rows apart, of this shape."""
-    _tensor(t, what, dtypes, 2, rows_apart=True)
-    if tuple(t.shape) != tuple(shape):
+def _matrix(t, what: str, dtypes, shape, dev: int) -> torch.Tensor:
+    """``t``, checked: on device ``dev`` (the current one), rows apart, of this shape (a tuple)."""
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype not in dtypes or t.get_device() != dev or \
+            not (t.is_contiguous() or _rows_apart(t)):
+        _tensor(t, what, dtypes, 2, rows_apart=True)
         raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
     return t
 
@@ -57,11 +59,19 @@ class Adapters:
             _shaped(ranks, "ranks", _I32, (self.adapters,), a.get_device())
         self.a, self.b, self.scale, self.ranks = a, b, scale, ranks
         self.device = a.get_device()
+        self._a, self._b = a.data_ptr(), b.data_ptr()
+        self._scale, self._ranks = (None if t is None else t.data_ptr() for t in (scale, ranks))
 
     def rows(self, ids: torch.Tensor, rows=None, offsets=None, stream=None) -> AdapterRows:
-        """The list of ``ids [rows]`` (-1: no adapter) that calls of more than 64 rows and gradients go by; layers whose
+        """The list of ``ids [rows]`` (-1: no adapter) that calls of more than 512 rows and gradients go by; layers whose
         rows are the same can share it."""
         return list_rows(ids, self.adapters, rows=rows, offsets=offsets, stream=stream)
+
+    def _here(self) -> int:
+        """The device of the weights, which is the current one."""
+        if _current_device() != self.device:
+            raise ValueError("the adapters are on another device than the current one")
+        return self.device
 
     def _ids(self, ids, t: int, listed: bool, stream):
         """(pointers of ids, list and offsets, what keeps them alive) for ``t`` rows."""
@@ -75,31 +85,34 @@ class Adapters:
             ids = self.rows(ids, stream=stream)
         return None, ids.rows.data_ptr(), ids.offsets.data_ptr(), ids
 
-    def _apply(self, x, a, b, y, ids, out, h, stream):
-        """``ts_adapt_rows`` of ``x`` through ``a`` and ``b``: (out, h)."""
-        t, k, n = x.shape[0], a.shape[2], b.shape[2]
+    def _apply(self, x, t: int, a: int, b: int, k: int, n: int, y, ids, out, h, stream):
+        """``ts_adapt_rows`` of ``x`` through the matrices at ``a`` and ``b``."""
         ids, rows, offsets, _keep = ids
+        yp = op = hp = None
+        ldy = ldo = 0
+        code = TS_BF16
         if y is not None:
-            out = y if out is None else _matrix(out, "out", (y.dtype,), (t, n))
+            code, yp, ldy = _CODES[y.dtype], y.data_ptr(), _ld(y)
+            op, ldo = (yp, ldy) if out is None else (out.data_ptr(), _ld(out))
         if h is not None:
-            _shaped(h, "h", _F32, (t, self.r), self.device)
-        _check(lib().ts_adapt_rows(
-            x.data_ptr(), _ld(x), t, k, a.data_ptr(), b.data_ptr(), None if self.scale is None else self.scale.data_ptr(),
-            None if self.ranks is None else self.ranks.data_ptr(), self.adapters, self.r, n, ids, rows, offsets,
-            None if y is None else y.data_ptr(), 0 if y is None else _ld(y), TS_BF16 if y is None else _CODES[y.dtype],
-            None if y is None else out.data_ptr(), 0 if y is None else _ld(out), None if h is None else h.data_ptr(),
-            _handle(stream)), "ts_adapt_rows")
-        return out
+            hp = h.data_ptr()
+        _check(lib().ts_adapt_rows(x.data_ptr(), _ld(x), t, k, a, b, self._scale, self._ranks, self.adapters, self.r, n, ids,
+                                   rows, offsets, yp, ldy, code, op, ldo, hp, _handle(stream)), "ts_adapt_rows")
 
     def forward(self, x: torch.Tensor, y: torch.Tensor, ids, out=None, h=None, stream=None) -> torch.Tensor:
         """``out[t] = y[t] + scale x[t] A^T B`` of the adapter that ``ids`` (int32 ``[rows]``, or what ``rows`` gives) names
         for row ``t``; without ``out`` in ``y`` itself (bf16 or fp32 ``[rows][n]``). x is bf16 ``[rows][k]``. fp32
         ``h [rows][r]``, if given, gets ``scale x[t] A^T``, for ``backward``."""
-        _tensor(x, "x", (_BF16,), 2, rows_apart=True)
-        t = x.shape[0]
-        _matrix(x, "x", (_BF16,), (t, self.k))
-        _matrix(y, "y", (_BF16, _F32), (t, self.n))
-        return self._apply(x, self.a, self.b, y, self._ids(ids, t, False, stream), out, h, stream)
+        dev = self._here()
+        t = x.shape[0] if isinstance(x, torch.Tensor) and x.dim() == 2 else -1
+        _matrix(x, "x", _ONLY_BF16, (t, self.k), dev)
+        _matrix(y, "y", _ROWS, (t, self.n), dev)
+        if out is not None:
+            _matrix(out, "out", (y.dtype,), (t, self.n), dev)
+        if h is not None:
+            _shaped(h, "h", _F32, (t, self.r), dev)
+        self._apply(x, t, self._a, self._b, self.k, self.n, y, self._ids(ids, t, False, stream), out, h, stream)
+        return y if out is None else out
 
     __call__ = forward
 
@@ -109,16 +122,17 @@ class Adapters:
         no ``dx``: None), and the gradients fp32 ``da [adapters][r][k]``, ``db [adapters][r][n]``, overwritten or added to.
         dy is bf16 ``[rows][n]``, h what ``forward`` gave, x its rows: bf16, or e4m3 with ``x_scale`` as ``quant_rows`` keeps
         them."""
-        _tensor(dy, "dy", (_BF16,), 2, rows_apart=True)
-        t = dy.shape[0]
-        _matrix(dy, "dy", (_BF16,), (t, self.n))
-        _shaped(h, "h", _F32, (t, self.r), self.device)
-        _matrix(x, "x", (_BF16, _E4M3), (t, self.k))
-        if dx is None:
+        dev = self._here()
+        t = dy.shape[0] if isinstance(dy, torch.Tensor) and dy.dim() == 2 else -1
+        _matrix(dy, "dy", _ONLY_BF16, (t, self.n), dev)
+        _shaped(h, "h", _F32, (t, self.r), dev)
+        _matrix(x, "x", (_BF16, _E4M3), (t, self.k), dev)
+        if dx is not None:
+            _matrix(dx, "dx", _ROWS, (t, self.k), dev)
             if out is not None:
-                raise ValueError("out needs a dx")
-        else:
-            _matrix(dx, "dx", (_BF16, _F32), (t, self.k))
+                _matrix(out, "out", (dx.dtype,), (t, self.k), dev)
+        elif out is not None:
+            raise ValueError("out needs a dx")
         sp, ld = None, 0
         if (x_scale is not None) != (x.dtype is _E4M3):
             raise ValueError("e4m3 rows need x_scale, and only they have any")
@@ -135,13 +149,13 @@ class Adapters:
                          _shaped(given, what, _F32, tuple(like.shape), self.device))
         listed = self._ids(ids, t, True, stream)
         dh = _empty(stream, t, self.r, dtype=_F32)
-        out = self._apply(dy, self.b, self.a, dx, listed, out, dh, stream)
+        self._apply(dy, t, self._b, self._a, self.n, self.k, dx, listed, out, dh, stream)
         L, s = lib(), _handle(stream)
         for of, rows, scale, grad in ((dh, x, (sp, ld), grads[0]), (h, dy, (None, 0), grads[1])):
             _check(L.ts_adapter_grads(of.data_ptr(), self.r, rows.data_ptr(), _ld(rows), _CODES[rows.dtype], *scale, t,
                                       rows.shape[1], self.adapters, listed[1], listed[2], grad.data_ptr(),
                                       int(bool(accumulate)), s), "ts_adapter_grads")
-        return out, grads[0], grads[1]
+        return dx if out is None else out, grads[0], grads[1]
 
 
 def adapt_error(stream=None) -> int:
@@ -165,50 +179,55 @@ def _count(n, dev):
     return None if n is None else _shaped(n, "n", _I32, (1,), dev).data_ptr()
 
 
-def _kept(kept, rows: int, m: int, dev) -> Kept:
+def _kept(kept, rows: int, m: int, dev: int):
+    """Pointers of what is kept of ``rows`` rows of ``m``, checked."""
     mb = -(-m // BLOCK)
-    for name, t in zip(Kept._fields, kept):
-        _shaped(t, name, *((_E4M3, (rows, m)) if name[0] == "q" else (_F32, (mb, rows))), dev)
-    return kept
+    q_gate, q_up, s_gate, s_up = kept
+    return (_shaped(q_gate, "q_gate", _E4M3, (rows, m), dev).data_ptr(), _shaped(q_up, "q_up", _E4M3, (rows, m), dev).data_ptr(),
+            _shaped(s_gate, "s_gate", _F32, (mb, rows), dev).data_ptr(), _shaped(s_up, "s_up", _F32, (mb, rows), dev).data_ptr())
 
 
-def _out(t, what: str, rows: int, m: int, stream) -> torch.Tensor:
-    return _empty(stream, rows, m, dtype=_BF16) if t is None else _matrix(t, what, (_BF16,), (rows, m))
+def _out(t, what: str, rows: int, m: int, dev: int, stream) -> torch.Tensor:
+    return _empty(stream, rows, m, dtype=_BF16) if t is None else _matrix(t, what, _ONLY_BF16, (rows, m), dev)
 
 
 def drelu_rows(g: torch.Tensor, u: torch.Tensor, n=None, c=None, keep: bool = False, kept=None, stream=None):
     """``ts_drelu_rows``: bf16 ``c = max(0, g) max(0, u)`` (0 unless both are positive) of the first ``n`` rows (a device
     int32, as ``offsets[-1:]``; all rows without); with ``keep`` (or buffers ``kept`` for it), (c, Kept): what
     ``drelu_rows_backward`` needs, in 8 bits."""
-    _tensor(g, "g", (_BF16, _F32), 2, rows_apart=True)
-    rows, m = g.shape
-    _matrix(u, "u", (g.dtype,), (rows, m))
-    c = _out(c, "c", rows, m, stream)
+    _tensor(g, "g", _ROWS, 2, rows_apart=True)
+    (rows, m), dev = g.shape, g.get_device()
+    _matrix(u, "u", (g.dtype,), (rows, m), dev)
+    c = _out(c, "c", rows, m, dev, stream)
+    p = (None,) * 4
     if kept is not None:
-        _kept(kept, rows, m, g.get_device())
+        p = _kept(kept, rows, m, dev)
     elif keep:
         mb = -(-m // BLOCK)
         kept = Kept(*(_empty(stream, rows, m, dtype=_E4M3) for _ in range(2)),
                     *(_empty(stream, mb, rows, dtype=_F32) for _ in range(2)))
-    p = (None,) * 4 if kept is None else tuple(t.data_ptr() for t in kept)
-    _check(lib().ts_drelu_rows(g.data_ptr(), _ld(g), u.data_ptr(), _ld(u), _CODES[g.dtype], _count(n, g.get_device()), rows,
-                               m, c.data_ptr(), _ld(c), *p, _handle(stream)), "ts_drelu_rows")
+        p = tuple(t.data_ptr() for t in kept)
+    _check(lib().ts_drelu_rows(g.data_ptr(), _ld(g), u.data_ptr(), _ld(u), _CODES[g.dtype], _count(n, dev), rows, m,
+                               c.data_ptr(), _ld(c), *p, _handle(stream)), "ts_drelu_rows")
     return c if kept is None else (c, kept)
 
 
 def drelu_rows_backward(dc: torch.Tensor, kept: Kept, n=None, dg=None, du=None, c=None, again: bool = True, stream=None):
     """``ts_drelu_rows_backward``: bf16 (dg, du, c) of ``dc`` and what ``drelu_rows`` kept; c, that of the factors as they
     were kept, is None if ``again`` is false."""
-    _tensor(dc, "dc", (_BF16, _F32), 2, rows_apart=True)
-    rows, m = dc.shape
-    _kept(kept, rows, m, dc.get_device())
-    dg, du = _out(dg, "dg", rows, m, stream), _out(du, "du", rows, m, stream)
-    c = _out(c, "c", rows, m, stream) if again or c is not None else None
-    _check(lib().ts_drelu_rows_backward(dc.data_ptr(), _ld(dc), _CODES[dc.dtype], *(t.data_ptr() for t in kept),
-                                        _count(n, dc.get_device()), rows, m, dg.data_ptr(), _ld(dg), du.data_ptr(), _ld(du),
-                                        None if c is None else c.data_ptr(), 0 if c is None else _ld(c), _handle(stream)),
-           "ts_drelu_rows_backward")
+    _tensor(dc, "dc", _ROWS, 2, rows_apart=True)
+    (rows, m), dev = dc.shape, dc.get_device()
+    p = _kept(kept, rows, m, dev)
+    dg, du = _out(dg, "dg", rows, m, dev, stream), _out(du, "du", rows, m, dev, stream)
+    c = _out(c, "c", rows, m, dev, stream) if again or c is not None else None
+    _check(lib().ts_drelu_rows_backward(dc.data_ptr(), _ld(dc), _CODES[dc.dtype], *p, _count(n, dev), rows, m, dg.data_ptr(),
+                                        _ld(dg), du.data_ptr(), _ld(du), None if c is None else c.data_ptr(),
+                                        0 if c is None else _ld(c), _handle(stream)), "ts_drelu_rows_backward")
     return dg, du, c
+
+
+def _columns(t) -> int:
+    return t.shape[1] if isinstance(t, torch.Tensor) and t.dim() == 2 else -1
 
 
 class Balance(NamedTuple):
@@ -222,16 +241,18 @@ def balance(logits: torch.Tensor, sel: torch.Tensor, loss=None, counts=None, sha
     """``ts_balance``: the loss on uneven routing of fp32 ``logits [tokens][experts]`` whose picks are ``sel``."""
     _tensor(logits, "logits", (_F32,), 2)
     (t, e), dev = logits.shape, logits.get_device()
-    _tensor(sel, "sel", (_I32,), 2)
-    _shaped(sel, "sel", _I32, (t, sel.shape[1]), dev)
-    outs = []
-    for v, what, dtype, size in ((loss, "loss", _F32, 1), (counts, "counts", _I32, e), (share, "share", _F32, e),
-                                 (totals, "totals", _I32, 2)):
-        outs.append(_empty(stream, size, dtype=dtype) if v is None else _shaped(v, what, dtype, (size,), dev))
-    work = _empty(stream, max(1, lib().ts_balance_work(t, e)), dtype=_F32)
-    _check(lib().ts_balance(logits.data_ptr(), t, e, sel.data_ptr(), sel.shape[1], *(o.data_ptr() for o in outs),
-                            work.data_ptr(), _handle(stream)), "ts_balance")
-    return Balance(*outs)
+    _shaped(sel, "sel", _I32, (t, _columns(sel)), dev)
+    k = sel.shape[1]
+    loss = _empty(stream, 1, dtype=_F32) if loss is None else _shaped(loss, "loss", _F32, (1,), dev)
+    counts = _empty(stream, e, dtype=_I32) if counts is None else _shaped(counts, "counts", _I32, (e,), dev)
+    share = _empty(stream, e, dtype=_F32) if share is None else _shaped(share, "share", _F32, (e,), dev)
+    totals = _empty(stream, 2, dtype=_I32) if totals is None else _shaped(totals, "totals", _I32, (2,), dev)
+    L = lib()
+    size = L.ts_balance_work(t, e)
+    work = _empty(stream, size, dtype=_F32) if size > 0 else None
+    _check(L.ts_balance(logits.data_ptr(), t, e, sel.data_ptr(), k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
+                        totals.data_ptr(), None if work is None else work.data_ptr(), _handle(stream)), "ts_balance")
+    return Balance(loss, counts, share, totals)
 
 
 def route_backward(logits: torch.Tensor, sel: torch.Tensor, w: torch.Tensor, dw=None, balance=None, dloss=None, dlogits=None,
@@ -240,8 +261,7 @@ def route_backward(logits: torch.Tensor, sel: torch.Tensor, w: torch.Tensor, dw=
     balance loss, fp32 ``dloss [1]``, for ``balance`` as it was for these logits and picks."""
     _tensor(logits, "logits", (_F32,), 2)
     (t, e), dev = logits.shape, logits.get_device()
-    _tensor(sel, "sel", (_I32,), 2)
-    k = sel.shape[1]
+    k = _columns(sel)
     _shaped(sel, "sel", _I32, (t, k), dev)
     _shaped(w, "w", _F32, (t, k), dev)
     if (balance is None) != (dloss is None):

@@ -47,32 +47,56 @@ struct Tile {
     static_assert(kStages >= 2, "");
 };
 
-// Without a list, of up to 64 rows: tile number t is there if row t is the first, 17th, 33rd or 49th of its adapter.
+// Without a list, of up to 512 rows: the same tiles, from the rows' ids. Thread t looks at rows 2 t and 2 t + 1.
 template <int MT>
-__device__ __forceinline__ void find_few(const AdaptLaunch& L, int t, TileRows* found, int* rows) {
-    static_assert(kFewRows == 64, "");
-    if (threadIdx.x >= kWarp) return;
-    const int lane = threadIdx.x;
+__device__ __forceinline__ void find_few(const AdaptLaunch& L, int tile, TileRows* found, int* rows) {
+    static_assert(kFewRows == 2 * kThreads, "");
+    __shared__ int counts[kMaxAdapters + 1], sums[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int id[2];
-    unsigned same[2];
-    const int mine = min((unsigned)L.ids[t], (unsigned)L.n_adapters);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int row = lane + i * kWarp;
+        const int row = 2 * tid + i;
         id[i] = row < L.rows ? (int)min((unsigned)L.ids[row], (unsigned)L.n_adapters) : -1;
-        same[i] = __ballot_sync(0xffffffffu, id[i] == mine);
     }
-    const unsigned long long all = (unsigned long long)same[1] << 32 | same[0];
-    const int before = __popcll(all & ((1ull << t) - 1ull));
-    const bool leads = before % MT == 0;
-    if (lane == 0) *found = {leads ? mine : -1, 0, 0, leads ? min(MT, __popcll(all) - before) : 0};
-    for (int i = lane; i < MT; i += kWarp) rows[i] = -1;
-    __syncwarp();
+    counts[tid] = 0;
+    if (tid == 0) *found = {-1, 0, 0, 0};
+    if (tid < MT) rows[tid] = -1;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = lane + i * kWarp, at = __popcll(all & ((1ull << row) - 1ull)) - before;
-        if (id[i] == mine && at >= 0 && at < MT) rows[at] = row;
+    for (int i = 0; i < 2; ++i)
+        if (id[i] >= 0) atomicAdd(&counts[id[i]], 1);
+    __syncthreads();
+    const int tiles = (counts[tid] + MT - 1) / MT;
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
     }
+    if (lane == kWarp - 1) sums[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += sums[w];
+    if (tile < upto && tile >= upto - tiles) {
+        const int first = (tile - (upto - tiles)) * MT;
+        *found = {tid, 0, first, min(MT, counts[tid] - first)};
+    }
+    __syncthreads();
+    // its rows, ascending: those of the warps before, of the lanes before, the thread's own
+    const int mine = found->id, n = (id[0] == mine) + (id[1] == mine);
+    const unsigned one = __ballot_sync(0xffffffffu, n >= 1), two = __ballot_sync(0xffffffffu, n == 2);
+    const unsigned before = (1u << lane) - 1u;
+    int at = __popc(one & before) + __popc(two & before);
+    if (lane == 0) sums[warp] = __popc(one) + __popc(two);
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) at += sums[w];
+    at -= found->first;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (id[i] == mine && mine >= 0) {
+            if (at >= 0 && at < MT) rows[at] = 2 * tid + i;
+            ++at;
+        }
 }
 
 template <int MT, int RP, typename TY>
@@ -402,13 +426,11 @@ cudaError_t launch_rank(const AdaptLaunch& a, long long tiles, int ctas, cudaStr
 
 template <typename TY>
 cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
-    if (a.list == nullptr) return launch_rank<16, TY>(a, a.rows, kMaxCluster, stream);
-    const bool small = a.rows < 512 || a.rows / a.n_adapters <= 24;
+    const bool small = a.list == nullptr || a.rows < 512 || a.rows / a.n_adapters <= 24;
     if (!small && a.r <= kWideRank) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
-    const int mt = small ? 16 : 64;
+    const long long tiles = most_tiles(a.rows, a.n_adapters, small ? 16 : 64);
     int ctas = kMaxCluster;
-    while (ctas > 1 && a.rows / mt * ctas > 2 * kResidentCtas) ctas /= 2;
-    const long long tiles = most_tiles(a.rows, a.n_adapters, mt);
+    while (ctas > 1 && tiles * ctas > kResidentCtas + kResidentCtas / 8) ctas /= 2;
     return small ? launch_rank<16, TY>(a, tiles, ctas, stream) : launch_tiles<64, 128, TY>(a, tiles, ctas, stream);
 }
 

@@ -10,7 +10,7 @@ namespace tsffn {
 
 constexpr int kMaxAdapters = 255;  // and one group of rows that have none: kMaxRouteExperts
 constexpr int kMaxRank = 128;
-constexpr int kFewRows = 64;       // of a call without a list
+constexpr int kFewRows = 512;      // of a call without a list
 constexpr int kWideRank = 64;      // of the kernel of ts_adapt_wide.cu
 
 struct AdaptLaunch {

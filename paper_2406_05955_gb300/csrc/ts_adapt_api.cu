@@ -137,7 +137,7 @@ ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32
     const ts_status s = check_routing(tokens, n_experts, top_k);
     if (s != TS_OK) return s;
     if (!loss || !aligned4(loss) || !counts || !aligned4(counts) || !share || !aligned4(share) || !totals ||
-        !aligned4(totals) || !work || !aligned4(work) || !aligned4(logits) || !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
+        !aligned4(totals) || (!work && balance_work(tokens, n_experts) > 0) || !aligned4(work) || !aligned4(logits) || !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_balance({logits, tokens, n_experts, top_k, sel, loss, counts, share, totals, work}, stream));
 }

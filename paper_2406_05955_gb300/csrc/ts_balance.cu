@@ -6,8 +6,11 @@
 //     dlogits[t][e] = dloss E / (picks tokens) p_e (counts_e - sum_j counts_j p_j)
 //                     + sum over the picks i of e: w_i (dw_i - sum_j w_j dw_j)
 // As many lanes of a token as give each at most 8 experts hold its logits in registers. Sums over tokens are taken in an
-// order that depends on the sizes alone, by thread, CTA and, in a second launch, over the CTAs; counts are whole numbers,
-// whose atomics in shared memory give the same sums in any order.
+// order that depends on the sizes alone, by thread, CTA and over the CTAs, through distributed shared memory where one cluster
+// has the tokens and in a second launch otherwise; counts are whole numbers, whose atomics in shared memory give the same
+// sums in any order.
+//
+// Latency bounds both: 8192 tokens of 64 experts are 2 MB.
 #include "ts_adapt.h"
 #include "ts_grouped.h"
 #include "ts_kernels.cuh"
@@ -16,10 +19,12 @@ namespace tsffn {
 namespace {
 
 constexpr int kPer = 8;  // experts of a lane
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / kWarp;
+constexpr int kCluster = 8;
 constexpr int kMostCtas = 152;
 constexpr int kJoinThreads = 1024;
+constexpr int kBackThreads = 128;
 
 __device__ __forceinline__ float max_over(float v, int lanes) {
     for (int o = lanes / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -63,16 +68,76 @@ __device__ __forceinline__ bool probabilities(const float* logits, int n_experts
     return live;
 }
 
-// Sums of p over a CTA's tokens [n_experts], then its counts and its live tokens, as one record of `work`.
+// What a CTA has of its tokens, in shared memory: sums of p, counts, live tokens.
+struct Sums {
+    float share[kMaxRouteExperts];
+    int counts[kMaxRouteExperts];
+    int live;
+};
+// The same as a record of `work`.
 __host__ __device__ constexpr int record(int n_experts) { return 2 * n_experts + 1; }
 
-template <int G>
+// The outputs, given expert threadIdx.x's sum and count; by the whole CTA, of which the first 256 threads have experts.
+__device__ __forceinline__ void finish(const BalanceLaunch& L, float sum, int count, int tokens) {
+    constexpr int kW = kMaxRouteExperts / kWarp;
+    __shared__ double terms[kW];
+    __shared__ int picks[kW];
+    const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
+    if (warp < kW) {
+        const double mean = e < L.n_experts && tokens > 0 ? (double)sum / tokens : 0.0;
+        double term = 0.0;
+        int n = 0;
+        if (e < L.n_experts) {
+            L.share[e] = (float)mean;
+            L.counts[e] = n = count;
+            term = mean * count;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) term += __shfl_xor_sync(0xffffffffu, term, o);
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) {
+            terms[warp] = term;
+            picks[warp] = n;
+        }
+    }
+    __syncthreads();
+    if (e == 0) {
+        double term = 0.0;
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+            term += terms[w];
+            n += picks[w];
+        }
+        *L.loss = n > 0 ? (float)(L.n_experts * term / (double)n) : 0.0f;
+        L.totals[0] = tokens;
+        L.totals[1] = n;
+    }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_ld(const void* p, uint32_t rank) {
+    uint32_t a, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// JOIN: the grid is one cluster, whose first CTA sums up and finishes; else the sums go to `work`.
+template <int G, bool JOIN>
 __global__ void __launch_bounds__(kThreads) k_balance(const BalanceLaunch L) {
-    __shared__ float sums[kWarps][kMaxRouteExperts];
-    __shared__ int counts[kMaxRouteExperts], live_tokens;
+    __shared__ float sums[kWarps][G * kPer];
+    __shared__ Sums all;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % G;
-    for (int e = tid; e < kMaxRouteExperts; e += kThreads) counts[e] = 0;
-    if (tid == 0) live_tokens = 0;
+    for (int e = tid; e < kMaxRouteExperts; e += kThreads) all.counts[e] = 0;
+    if (tid == 0) all.live = 0;
     __syncthreads();
     pdl_wait();
     constexpr int kTokens = kThreads / G;  // of a CTA at once
@@ -85,12 +150,14 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceLaunch L) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) sum[i] += p[i];
     }
-    const long long picks = (long long)L.tokens * L.top_k;
-    for (long long i = (long long)blockIdx.x * kThreads + tid; i < picks; i += (long long)gridDim.x * kThreads) {
+    const int picks = L.tokens * L.top_k;
+#pragma unroll 4
+    for (int i = blockIdx.x * kThreads + tid; i < picks; i += gridDim.x * kThreads) {
         const int e = L.sel[i];
-        if ((unsigned)e < (unsigned)L.n_experts) atomicAdd(&counts[e], 1);
+        if ((unsigned)e < (unsigned)L.n_experts) atomicAdd(&all.counts[e], 1);
     }
-    if (sub == 0 && live > 0) atomicAdd(&live_tokens, live);
+    live = __reduce_add_sync(0xffffffffu, sub == 0 ? live : 0);
+    if (lane == 0 && live > 0) atomicAdd(&all.live, live);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
 #pragma unroll
@@ -98,24 +165,55 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceLaunch L) {
         if (lane < G) sums[warp][sub * kPer + i] = sum[i];
     }
     __syncthreads();
-    float* to = L.work + (size_t)blockIdx.x * record(L.n_experts);
-    for (int e = tid; e < L.n_experts; e += kThreads) {
+    if (tid < L.n_experts) {
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += sums[w][e];
-        to[e] = s;
-        to[L.n_experts + e] = __int_as_float(counts[e]);
+        for (int w = 0; w < kWarps; ++w) s += sums[w][tid];
+        all.share[tid] = s;
     }
-    if (tid == 0) to[2 * L.n_experts] = __int_as_float(live_tokens);
+    if constexpr (JOIN) {
+        if (gridDim.x > 1) cluster_sync();
+        else __syncthreads();
+        if (cluster_rank() == 0) {
+            float s = 0.0f;
+            int n = 0, tokens = 0;
+            uint32_t part[kCluster][3];
+#pragma unroll
+            for (int c = 0; c < kCluster; ++c)
+                if (c < (int)gridDim.x && tid < kMaxRouteExperts) {
+                    const int e = min(tid, L.n_experts - 1);
+                    part[c][0] = cluster_ld(&all.share[e], (uint32_t)c);
+                    part[c][1] = cluster_ld(&all.counts[e], (uint32_t)c);
+                    part[c][2] = cluster_ld(&all.live, (uint32_t)c);
+                }
+#pragma unroll
+            for (int c = 0; c < kCluster; ++c)
+                if (c < (int)gridDim.x && tid < kMaxRouteExperts) {
+                    s += __uint_as_float(part[c][0]);
+                    n += (int)part[c][1];
+                    tokens += (int)part[c][2];
+                }
+            finish(L, s, n, tokens);
+        }
+        __syncwarp();
+        if (gridDim.x > 1) cluster_sync();  // no CTA leaves while another reads its sums
+    } else {
+        float* const to = L.work + (size_t)blockIdx.x * record(L.n_experts);
+        if (tid < L.n_experts) {
+            to[tid] = all.share[tid];
+            to[L.n_experts + tid] = __int_as_float(all.counts[tid]);
+        }
+        if (tid == 0) to[2 * L.n_experts] = __int_as_float(all.live);
+    }
 }
 
+// E2: experts, rounded up to a power of two; as many threads as there are of those share an expert's records.
+template <int E2>
 __global__ void __launch_bounds__(kJoinThreads) k_balance_join(const BalanceLaunch L, int ctas) {
-    constexpr int kParts = kJoinThreads / kMaxRouteExperts;
-    __shared__ float share[kParts][kMaxRouteExperts];
-    __shared__ int counts[kParts][kMaxRouteExperts], live[kWarp];
-    __shared__ double terms[kMaxRouteExperts];
-    __shared__ long long picks_of[kMaxRouteExperts];
-    const int tid = threadIdx.x, e = tid % kMaxRouteExperts, part = tid / kMaxRouteExperts, E = L.n_experts;
+    constexpr int kParts = kJoinThreads / E2;
+    __shared__ float share[kParts][E2];
+    __shared__ int counts[kParts][E2], live[kWarp];
+    const int tid = threadIdx.x, e = tid % E2, part = tid / E2, E = L.n_experts;
     pdl_wait();
     float sum = 0.0f;
     int count = 0, tokens = 0;
@@ -136,74 +234,65 @@ __global__ void __launch_bounds__(kJoinThreads) k_balance_join(const BalanceLaun
     tokens = 0;
 #pragma unroll
     for (int w = 0; w < kWarp; ++w) tokens += live[w];
-    if (part == 0) {
-#pragma unroll
-        for (int i = 1; i < kParts; ++i) {
-            sum += share[i][e];
-            count += counts[i][e];
+    sum = 0.0f;
+    count = 0;
+    if (tid < E) {
+#pragma unroll 8
+        for (int i = 0; i < kParts; ++i) {
+            sum += share[i][tid];
+            count += counts[i][tid];
         }
-        const double mean = tokens > 0 ? (double)sum / tokens : 0.0;
-        if (e < E) {
-            L.share[e] = (float)mean;
-            L.counts[e] = count;
-        }
-        terms[e] = e < E ? mean * count : 0.0;
-        picks_of[e] = e < E ? count : 0;
     }
-    __syncthreads();
-    for (int half = kMaxRouteExperts / 2; half > 0; half /= 2) {
-        if (tid < half) {
-            terms[tid] += terms[tid + half];
-            picks_of[tid] += picks_of[tid + half];
-        }
-        __syncthreads();
-    }
-    if (tid == 0) {
-        *L.loss = picks_of[0] > 0 ? (float)(E * terms[0] / (double)picks_of[0]) : 0.0f;
-        L.totals[0] = tokens;
-        L.totals[1] = (int)picks_of[0];
-    }
+    finish(L, sum, count, tokens);
 }
 
 template <int G>
-__global__ void __launch_bounds__(kThreads) k_route_backward(const RouteBackwardLaunch L) {
+__global__ void __launch_bounds__(kBackThreads) k_route_backward(const RouteBackwardLaunch L) {
     const int sub = threadIdx.x % G;
     pdl_wait();
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const long long i = (long long)blockIdx.x * kBackThreads + threadIdx.x;
     const bool in = i / G < L.tokens;
     const int t = in ? (int)(i / G) : 0, first = sub * kPer;
-    float d[kPer] = {};
-    if (L.counts != nullptr) {
-        float p[kPer], count[kPer], dot = 0.0f;
-        probabilities<G>(L.logits, L.n_experts, t, in, sub, p);
-        const float tokens = (float)L.totals[0], picks = (float)L.totals[1];
-        const float f = picks > 0.0f && tokens > 0.0f ? *L.dloss * ((float)L.n_experts / picks / tokens) : 0.0f;
+    // everything that is read, at once
+    float w[kMaxRouteK], dw[kMaxRouteK], count[kPer], dloss = 0.0f, tokens = 0.0f, picks = 0.0f;
+    int sel[kMaxRouteK];
+    const bool balance = L.counts != nullptr, weights = L.dw != nullptr && in;
+    const size_t at = (size_t)t * L.top_k;
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            count[j] = first + j < L.n_experts ? (float)L.counts[first + j] : 0.0f;
-            dot = fmaf(count[j], p[j], dot);
-        }
+    for (int j = 0; j < kMaxRouteK; ++j) {
+        const bool there = weights && j < L.top_k;
+        sel[j] = there ? L.sel[at + j] : -1;
+        w[j] = there ? L.w[at + j] : 0.0f;
+        dw[j] = there ? L.dw[at + j] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) count[j] = balance && first + j < L.n_experts ? (float)L.counts[first + j] : 0.0f;
+    if (balance) {
+        dloss = *L.dloss;
+        tokens = (float)L.totals[0];
+        picks = (float)L.totals[1];
+    }
+    float d[kPer] = {};
+    if (balance) {
+        float p[kPer], dot = 0.0f;
+        probabilities<G>(L.logits, L.n_experts, t, in, sub, p);
+        const float f = picks > 0.0f && tokens > 0.0f ? dloss * ((float)L.n_experts / picks / tokens) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) dot = fmaf(count[j], p[j], dot);
         dot = sum_over(dot, G);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) d[j] = f * p[j] * (count[j] - dot);
     }
-    if (L.dw != nullptr && in) {
-        const size_t at = (size_t)t * L.top_k;
-        float mean = 0.0f, w[kMaxRouteK], dw[kMaxRouteK];
-        int sel[kMaxRouteK];
+    float mean = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kMaxRouteK; ++j) {
-            sel[j] = j < L.top_k ? L.sel[at + j] : -1;
-            const bool some = (unsigned)sel[j] < (unsigned)L.n_experts;
-            w[j] = some ? L.w[at + j] : 0.0f;
-            dw[j] = some ? L.dw[at + j] : 0.0f;
-            mean = fmaf(w[j], dw[j], mean);
-        }
+    for (int j = 0; j < kMaxRouteK; ++j)
+        if ((unsigned)sel[j] < (unsigned)L.n_experts) mean = fmaf(w[j], dw[j], mean);
 #pragma unroll
-        for (int j = 0; j < kMaxRouteK; ++j)
+    for (int j = 0; j < kMaxRouteK; ++j) {
+        const float g = w[j] * (dw[j] - mean);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (sel[j] == first + e && sel[j] < L.n_experts) d[e] = fmaf(w[j], dw[j] - mean, d[e]);
+        for (int e = 0; e < kPer; ++e)
+            if (sel[j] == first + e && sel[j] < L.n_experts) d[e] += g;
     }
     if (!in) return;
     float* to = L.dlogits + (size_t)t * L.n_experts + first;
@@ -224,9 +313,12 @@ int lanes_of(int n_experts) {
     while (g * kPer < n_experts) g *= 2;
     return g;
 }
+// One cluster as long as its threads have one token each in turn, or two: a turn takes 1.5 us, the second launch 4.
+bool one_cluster(int tokens, int n_experts) { return (long long)tokens * lanes_of(n_experts) <= 2ll * kCluster * kThreads; }
 unsigned balance_ctas(int tokens, int n_experts) {
     const long long ctas = ((long long)tokens * lanes_of(n_experts) + kThreads - 1) / kThreads;
-    return (unsigned)(ctas < 1 ? 1 : ctas < kMostCtas ? ctas : kMostCtas);
+    const long long most = one_cluster(tokens, n_experts) ? kCluster : kMostCtas;
+    return (unsigned)(ctas < 1 ? 1 : ctas < most ? ctas : most);
 }
 
 template <typename A>
@@ -238,15 +330,33 @@ void (*pick(int lanes, void (*const (&k)[6])(A)))(A) {
 
 }  // namespace
 
-size_t balance_work(int tokens, int n_experts) { return (size_t)balance_ctas(tokens, n_experts) * record(n_experts); }
+size_t balance_work(int tokens, int n_experts) {
+    return one_cluster(tokens, n_experts) ? 0 : (size_t)balance_ctas(tokens, n_experts) * record(n_experts);
+}
 
 cudaError_t launch_balance(const BalanceLaunch& a, cudaStream_t stream) {
-    static constexpr void (*kKernels[])(BalanceLaunch) = {k_balance<1>, k_balance<2>, k_balance<4>,
-                                                          k_balance<8>, k_balance<16>, k_balance<32>};
+    static constexpr void (*kJoined[])(BalanceLaunch) = {k_balance<1, true>, k_balance<2, true>, k_balance<4, true>,
+                                                         k_balance<8, true>, k_balance<16, true>, k_balance<32, true>};
+    static constexpr void (*kApart[])(BalanceLaunch) = {k_balance<1, false>, k_balance<2, false>, k_balance<4, false>,
+                                                        k_balance<8, false>, k_balance<16, false>, k_balance<32, false>};
     const unsigned ctas = balance_ctas(a.tokens, a.n_experts);
-    const cudaError_t e = launch_after(pick(lanes_of(a.n_experts), kKernels), launch_shape(dim3(ctas), kThreads, stream), a);
+    const int lanes = lanes_of(a.n_experts);
+    if (one_cluster(a.tokens, a.n_experts)) {
+        cudaLaunchConfig_t cfg = launch_shape(dim3(ctas), kThreads, stream);
+        cudaLaunchAttribute at[2]{};
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim = {ctas, 1, 1};
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, pick(lanes, kJoined), a);
+    }
+    const cudaError_t e = launch_after(pick(lanes, kApart), launch_shape(dim3(ctas), kThreads, stream), a);
     if (e != cudaSuccess) return e;
-    return launch_after(k_balance_join, launch_shape(dim3(1), kJoinThreads, stream), a, (int)ctas);
+    const auto join = a.n_experts <= 32 ? k_balance_join<32> : a.n_experts <= 64 ? k_balance_join<64>
+                                      : a.n_experts <= 128 ? k_balance_join<128> : k_balance_join<256>;
+    return launch_after(join, launch_shape(dim3(1), kJoinThreads, stream), a, (int)ctas);
 }
 
 cudaError_t launch_route_backward(const RouteBackwardLaunch& a, cudaStream_t stream) {
@@ -254,7 +364,7 @@ cudaError_t launch_route_backward(const RouteBackwardLaunch& a, cudaStream_t str
                                                                 k_route_backward<8>, k_route_backward<16>, k_route_backward<32>};
     const int g = lanes_of(a.n_experts);
     const long long lanes = (long long)a.tokens * g;
-    return launch_after(pick(g, kKernels), launch_shape(dim3((unsigned)((lanes + kThreads - 1) / kThreads)), kThreads, stream), a);
+    return launch_after(pick(g, kKernels), launch_shape(dim3((unsigned)((lanes + kBackThreads - 1) / kBackThreads)), kBackThreads, stream), a);
 }
 
 }  // namespace tsffn

@@ -103,12 +103,10 @@ SIZES = [(1, 64, 64, 1, 1), (1, 4096, 1408, 16, 3), (2, 8, 8, 4, 2), (3, 136, 72
 def test_forward(ts, t, k, n, r, adapters, dtype):
     c = case(t, k, n, r, adapters, seed=t + k, dtype=dtype)
     outs = [check(ts, *c, list_them=lists, in_place=place) for lists in (False, True) for place in (False, True)]
-    for o in outs[1:3]:
-        assert torch.equal(o[1], outs[0][1]) or t <= 64  # (few rows without a list are summed in another order)
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[2][0], outs[3][0])
 
 
-@pytest.mark.parametrize("t", [5, 64, 300, 900])
+@pytest.mark.parametrize("t", [5, 64, 300, 511, 512, 900])
 def test_ids(ts, t):
     """No row has an adapter, all have the same, ids out of range, sorted ids, the last adapter alone."""
     x, y, a, b, scale, _ = case(t, 264, 136, 9, 4, seed=t)
