@@ -4,7 +4,7 @@
 //
 // Both products in one launch. A cluster of CTAs has a tile of up to 16 or 64 rows of one adapter: each CTA sums its part
 // of k for the whole tile, the parts of h meet through distributed shared memory, summed in the same order by all, and each
-// CTA adds h B_i to its part of the columns. One ring of chunks, 256 bytes of each row wide, carries x and A_i and then y and B_i: while h is
+// CTA adds h B_i to its part of the columns. One ring of chunks, 256 or 512 bytes of each row wide, carries x and A_i and then y and B_i: while h is
 // being joined the first chunks of y are already on their way. Rows of a tile are gathered (a list by adapter), so they
 // come by 16-byte asynchronous copies.
 //
@@ -21,6 +21,8 @@ namespace {
 // MT: rows of a tile. RP: r rounded up to 16, 32, 64 or 128.
 template <int MT, int RP, typename TY>
 struct Tile {
+    // bytes of a row in a chunk: the fewer rows, the more of them, as each chunk costs the warps a round of latencies
+    static constexpr int kChunk = MT == 16 && RP <= 32 ? 512 : 256;
     static constexpr int kCols = kChunk / 2;                          // of x and A in a chunk
     static constexpr int kOutCols = kChunk / (int)sizeof(TY);         // of y and out
     static constexpr int kBPitch = kOutCols * 2;                      // bytes of a row of B
@@ -39,7 +41,7 @@ struct Tile {
     static constexpr int kFixed = (MT == 16 ? kSlabs : 1) * kSlabBytes + kParts * kPartBytes;
     // two CTAs on an SM where two stages fit (the loads in flight of two cover the latency, and one works while the other joins)
     static constexpr int kHalf = 113 * 1024 - kFixed, kWhole = 226 * 1024 - kFixed;
-    static constexpr int kWish = MT == 16 ? 8 : 4;
+    static constexpr int kWish = MT == 16 ? 6 : 4;
     static constexpr int kFit = kHalf >= 2 * kStage ? kHalf / kStage : kWhole / kStage;
     static constexpr int kStages = kFit < kWish ? kFit : kWish;
     static constexpr int kSmem = kStages * kStage + kFixed;
@@ -140,9 +142,9 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
 
     // A thread copies the same 16-byte piece of every 16th row of a chunk of x or y, and of the rows of A or B: where it
     // reads moves on by a chunk from one call to the next.
-    constexpr int kPieces = kChunk / 16, kRowStep = kThreads / kPieces, kMine = MT / kRowStep;
+    constexpr int kPieces = T::kChunk / 16, kRowStep = kThreads / kPieces, kMine = MT / kRowStep;
     const int piece = tid % kPieces, row0 = tid / kPieces;
-    const uint32_t to0 = smem0 + place<kChunk>(row0, piece);
+    const uint32_t to0 = smem0 + place<T::kChunk>(row0, piece);
     const char* src[kMine];
     bool there[kMine];
 #pragma unroll
@@ -168,8 +170,8 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
 #pragma unroll
             for (int p = 0; p < kMine; ++p) {
                 const bool take = in && there[p];
-                copy16(to + p * kRowStep * kChunk, take ? src[p] : reinterpret_cast<const char*>(x), take);
-                src[p] += kChunk;
+                copy16(to + p * kRowStep * T::kChunk, take ? src[p] : reinterpret_cast<const char*>(x), take);
+                src[p] += T::kChunk;
             }
             if (i < nk) {
                 const int64_t step = (int64_t)kRowStep * L.k * 2;
@@ -177,15 +179,15 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
 #pragma unroll
                 for (int p = 0; p < RP / kRowStep; ++p) {
                     const bool take = in && row0 + p * kRowStep < rank;
-                    copy16(to + MT * kChunk + p * kRowStep * kChunk, take ? from : reinterpret_cast<const char*>(x), take);
+                    copy16(to + MT * T::kChunk + p * kRowStep * T::kChunk, take ? from : reinterpret_cast<const char*>(x), take);
                     from += step;
                 }
-                mat += kChunk;
+                mat += T::kChunk;
                 col += T::kCols;
             } else {
                 constexpr int kBPieces = T::kBPitch / 16, kBStep = kThreads / kBPieces;
                 const int b_row = tid / kBPieces, b_col = col - piece * (16 / (int)sizeof(TY)) + tid % kBPieces * 8;
-                const uint32_t b_to = smem0 + (uint32_t)(i % T::kStages) * T::kStage + MT * kChunk + place<T::kBPitch>(b_row, tid % kBPieces);
+                const uint32_t b_to = smem0 + (uint32_t)(i % T::kStages) * T::kStage + MT * T::kChunk + place<T::kBPitch>(b_row, tid % kBPieces);
                 const int64_t step = (int64_t)kBStep * L.n * 2;
                 const char* from = mat;
                 if (rank > 0) {
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
         __syncthreads();
         issue(i + T::kStages - 1);
         const int stage = (i % T::kStages) * T::kStage;
-        const uint32_t first = smem0 + stage, second = first + MT * kChunk;
+        const uint32_t first = smem0 + stage, second = first + MT * T::kChunk;
         if (i < nk) {
             if (live) {
                 constexpr int kSteps = T::kCols / 16, kMySteps = kSteps / T::kSlabs;
@@ -305,17 +307,17 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
                 for (int u = 0; u < kMySteps; ++u) {
                     const int ks = T::kSlabs > 1 ? side * kMySteps + u : u;
                     uint32_t xa[4];
-                    ldmatrix4(xa, first + place<kChunk>(m0 + (lane & 15), ks * 2 + (lane >> 4)));
+                    ldmatrix4(xa, first + place<T::kChunk>(m0 + (lane & 15), ks * 2 + (lane >> 4)));
 #pragma unroll
                     for (int t = 0; t < T::kNT; t += 2) {
                         uint32_t w[4];
                         const int j0 = (T::kNSplit == 2 ? side * T::kNT : 0) * 8 + t * 8;
-                        ldmatrix4(w, second + place<kChunk>(j0 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)));
+                        ldmatrix4(w, second + place<T::kChunk>(j0 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)));
                         mma(acc[t], xa, w[0], w[1]);
                         mma(acc[t + 1], xa, w[2], w[3]);
                     }
                 }
-                if (MT > 16 || (i & 7) == 7) take_over();
+                if (MT > 16 || (i + 1) % (8 / kMySteps) == 0) take_over();
             }
             continue;
         }
@@ -327,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
             constexpr int kPer = 16 / (int)sizeof(TY);
             const auto at = [&](int t, int e) -> unsigned char* {  // of o[t][e] and the next one
                 const int row = m0 + lane / 4 + e * 4, c = c0 + t * 8 + (lane & 3) * 2;
-                return tile + place<kChunk>(row, c / kPer) + c % kPer * (int)sizeof(TY);
+                return tile + place<T::kChunk>(row, c / kPer) + c % kPer * (int)sizeof(TY);
             };
             // sums for bf16 begin with y; fp32 ones add it last, as the tensor cores cut bits off a long sum
 #pragma unroll
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
             for (int p = lane; p < 16 * kSeg; p += kWarp) {
                 const int row = m0 + p / kSeg, c = c0 / kPer + p % kSeg, to = col0 + c * kPer;
                 if (rows[row] >= 0 && to < L.n)
-                    *reinterpret_cast<uint4*>(out + rows[row] * L.ldo + to) = *reinterpret_cast<const uint4*>(tile + place<kChunk>(row, c));
+                    *reinterpret_cast<uint4*>(out + rows[row] * L.ldo + to) = *reinterpret_cast<const uint4*>(tile + place<T::kChunk>(row, c));
             }
         }
     }
@@ -395,10 +397,10 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
 
 template <int MT, int RP, typename TY>
 cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
-    // Few tiles: several clusters have one, each with its own h and a part of the columns, of 2 chunks a CTA at least.
+    // Few tiles: several clusters have one, each with its own h and a part of the columns, of a chunk a CTA at least.
     const long long chunks = (a.n + Tile<MT, RP, TY>::kOutCols - 1) / Tile<MT, RP, TY>::kOutCols;
     long long sharing = a.out != nullptr ? kResidentCtas / (tiles * ctas) : 1;
-    if (sharing > chunks / (2 * ctas)) sharing = chunks / (2 * ctas);
+    if (sharing > chunks / ctas) sharing = chunks / ctas;
     if (sharing < 1) sharing = 1;
     const auto kernel = k_adapt<MT, RP, TY>;
     constexpr int kSmem = Tile<MT, RP, TY>::kSmem;
