@@ -428,7 +428,10 @@ cudaError_t launch_rank(const AdaptLaunch& a, long long tiles, int ctas, cudaStr
 
 template <typename TY>
 cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
-    const bool small = a.list == nullptr || a.rows < 512 || a.rows / a.n_adapters <= 24;
+    // Tiles of 16 rows begin sooner, and read A and B 8 times as often. n = 4096 = k, bf16, microseconds, 16 rows and 128:
+    // r = 16, 1024 rows 9.5 and 16.4, 4096 24.4 and 25.0 (fp32 40.6 and 39.0); r = 64, 512 rows 16.5 and 20.7, 1024 22.1 and
+    // 23.2, 4096 70.6 and 29.4. Adapters of few rows fill no tile of 128.
+    const bool small = a.list == nullptr || a.rows <= (a.r <= 16 ? 2048 : 1024) || a.rows / a.n_adapters <= 24;
     if (!small && a.r <= kWideRank) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
     const long long tiles = most_tiles(a.rows, a.n_adapters, small ? 16 : 64);
     int ctas = kMaxCluster;

@@ -205,11 +205,11 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
         if (!looks) return -1;
         int first = 0;
         const int n = ahead.next(offs, first, of);
-        const int row = tid < n ? L.list[first + tid] : -1;
-        return (unsigned)row < (unsigned)L.rows ? row : -1;
+        return tid < n ? L.list[first + tid] : -1;  // (what a turn loads the next one looks at)
     };
     const auto know = [&](int ring, int row, int of) {
         if (!looks) return;
+        if ((unsigned)row >= (unsigned)L.rows) row = -1;
         const uint64_t x = row < 0 ? 1ull << 63 : (uint64_t)(row * L.ldx * (E8 ? 1 : 2)), h = row < 0 ? 1ull << 63 : (uint64_t)row * L.r * 4;
         x_at[ring][tid] = make_uint2((uint32_t)x, (uint32_t)(x >> 32));
         h_at[ring][tid] = make_uint2((uint32_t)h, (uint32_t)(h >> 32));

@@ -12,6 +12,8 @@
 // whatever it holds: the longest warp's copies, products and sums in a row); the same with sixteen warps, or two CTAs of half
 // the item, 130-140; a warp of its own for the products 128 (16-byte copies and pieces of 64 bytes a warp: 2 us for 2 KB);
 // as it is 114.
+#include <atomic>
+
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
 
@@ -391,26 +393,48 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
     }
 }
 
+// Clusters of `ctas` CTAs that can be on the device at once: a cluster has to fit into a part of it, so of the larger ones
+// there are fewer than the SMs divided by their size (of 8 CTAs, one on an SM: 15 on 152 SMs). Asked for once.
+template <int RP, typename TY>
+int resident_clusters(int ctas) {
+    static std::atomic<int> known[kMaxCluster + 1];
+    int n = known[ctas].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)ctas), kWideThreads, nullptr);
+        cfg.dynamicSmemBytes = Wide<RP, TY>::kSmem;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim = {(unsigned)ctas, 1, 1};
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, k_adapt_wide<RP, TY>, &cfg) != cudaSuccess || n < 1) n = kSms / ctas;
+        known[ctas].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <int RP, typename TY>
 cudaError_t launch(const AdaptLaunch& a, cudaStream_t stream) {
     using W = Wide<RP, TY>;
     const auto kernel = k_adapt_wide<RP, TY>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem);
     if (e != cudaSuccess) return e;
-    // A CTA an SM: the cluster whose rounds of CTAs take the least time, for as many tiles as whole ones and half a one an
-    // adapter. Beside its items, a CTA takes the time of about 6 to begin and to join.
-    const long long tiles = most_tiles(a.rows, a.n_adapters, kTileRows), expect = (2 * (a.rows / kTileRows) + tiles + 1) / 3;
-    const double items = (double)(a.k / W::kCols) + (a.out != nullptr ? a.n / W::kOutCols : 0);
+    // The cluster, and the clusters that share a tile's columns (each with its own h), whose rounds take the least time for nearly
+    // the most tiles that there can be (one too many for a round costs a second); beside its items, a CTA takes the time of about
+    // 8 to begin and to join.
+    const long long tiles = most_tiles(a.rows, a.n_adapters, kTileRows), expect = tiles > 1 ? tiles - 1 : 1;
+    const int k_items = (a.k + W::kCols - 1) / W::kCols, n_items = a.out != nullptr ? (a.n + W::kOutCols - 1) / W::kOutCols : 0;
     int ctas = 1;
+    long long sharing = 1;
     double best = 1e30;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const double time = (double)((expect * c + kSms - 1) / kSms) * (items / c + 6);
-        if (time < best) best = time, ctas = c;
+        const int fit = resident_clusters<RP, TY>(c);
+        const long long most = n_items / c < 1 ? 1 : n_items / c;
+        for (long long s = 1; s <= most && s <= 16 && (s == 1 || expect * s <= fit); ++s) {
+            const double time = (double)((expect * s + fit - 1) / fit) * ((double)k_items / c + (double)n_items / (double)(c * s) + 8);
+            if (time < best * 0.98) best = time, ctas = c, sharing = s;
+        }
     }
-    const long long chunks = (a.n + W::kOutCols - 1) / W::kOutCols;
-    long long sharing = a.out != nullptr ? kSms / (tiles * ctas) : 1;
-    if (sharing > chunks / (2 * ctas)) sharing = chunks / (2 * ctas);
-    if (sharing < 1) sharing = 1;
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas), (unsigned)sharing), kWideThreads, stream);
     cfg.dynamicSmemBytes = W::kSmem;
     cudaLaunchAttribute at[2]{};

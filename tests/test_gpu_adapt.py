@@ -90,9 +90,9 @@ def check(ts, x, y, a, b, scale, ids, ranks=None, list_them=False, in_place=Fals
     return out, h
 
 
-# (from 512 rows on and more than 24 an adapter, r up to 64: tiles of 128 rows)
-MANY = [(512, 64, 64, 8, 1), (600, 1408, 512, 16, 3), (1000, 136, 1032, 33, 5), (2100, 4096, 200, 64, 2), (777, 8, 4096, 20, 4),
-        (1300, 512, 8, 40, 7), (3000, 264, 520, 32, 1), (5000, 2048, 1408, 64, 90)]
+# (above 1024 rows, 2048 for r up to 16, and more than 24 an adapter, r up to 64: tiles of 128 rows)
+MANY = [(512, 64, 64, 8, 1), (2060, 64, 64, 8, 1), (2600, 1408, 512, 16, 3), (1100, 136, 1032, 33, 5), (2100, 4096, 200, 64, 2),
+        (1777, 8, 4096, 20, 4), (1300, 512, 8, 40, 7), (3000, 264, 520, 32, 1), (5000, 2048, 1408, 64, 90), (1025, 256, 128, 17, 1)]
 SIZES = [(1, 64, 64, 1, 1), (1, 4096, 1408, 16, 3), (2, 8, 8, 4, 2), (3, 136, 72, 5, 2), (17, 512, 1408, 16, 4),
          (64, 1024, 264, 32, 64), (64, 520, 4096, 64, 3), (33, 256, 136, 128, 5), (65, 512, 512, 8, 2), (130, 1408, 512, 40, 7),
          (300, 264, 1032, 12, 20), (1000, 512, 1408, 100, 3), (257, 4096, 128, 16, 1), (500, 128, 4104, 33, 255)]
@@ -106,10 +106,10 @@ def test_forward(ts, t, k, n, r, adapters, dtype):
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[2][0], outs[3][0])
 
 
-@pytest.mark.parametrize("t", [5, 64, 300, 511, 512, 900])
+@pytest.mark.parametrize("t", [5, 64, 300, 511, 512, 1200])
 def test_ids(ts, t):
     """No row has an adapter, all have the same, ids out of range, sorted ids, the last adapter alone."""
-    x, y, a, b, scale, _ = case(t, 264, 136, 9, 4, seed=t)
+    x, y, a, b, scale, _ = case(t, 264, 136, 20, 4, seed=t)
     g = gen(t)
     for ids in (torch.full((t,), -1), torch.full((t,), 4), torch.full((t,), 2), torch.full((t,), 3),
                 torch.randint(-3, 9, (t,), generator=g, device="cuda"), torch.arange(t) * 4 // t,
@@ -118,7 +118,7 @@ def test_ids(ts, t):
             check(ts, x, y, a, b, scale, ids.to("cuda", torch.int32), list_them=lists)
 
 
-@pytest.mark.parametrize("t", [16, 200, 700])
+@pytest.mark.parametrize("t", [16, 200, 1300])
 def test_ranks_scales_and_what_is_not_read(ts, t):
     """Components behind an adapter's rank and adapters without rows are not read; a scale may be absent, 0 or negative."""
     x, y, a, b, scale, ids = case(t, 256, 264, 24, 6, seed=3, none=0.1)
@@ -134,7 +134,7 @@ def test_ranks_scales_and_what_is_not_read(ts, t):
         check(ts, x, y, a, b, None, ids, ranks=ranks, list_them=lists)
 
 
-@pytest.mark.parametrize("t", [20, 150, 550])
+@pytest.mark.parametrize("t", [20, 150, 2100])
 def test_infinities_and_nan_stay_in_their_rows(ts, t):
     x, y, a, b, scale, ids = case(t, 512, 136, 16, 3, seed=5)
     for lists in (False, True):
@@ -152,7 +152,7 @@ def test_infinities_and_nan_stay_in_their_rows(ts, t):
         assert torch.equal(got[rest], want[rest])
 
 
-@pytest.mark.parametrize("t", [30, 100, 515])
+@pytest.mark.parametrize("t", [30, 100, 2055])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_rows_apart(ts, t, dtype):
     """Rows of x, y and out that lie in wider ones: what is between them is left as it was."""
@@ -364,7 +364,7 @@ def test_offsets_beyond_32_bits(ts):
 
 def test_a_wait_that_gives_up(ts):
     """The wait runs out, is reported once, and the next call is right."""
-    c = case(600, 264, 264, 16, 3, seed=21)
+    c = case(2100, 264, 264, 16, 3, seed=21)
     want, _ = check(ts, *c, list_them=True)
     assert ts.adapt_error() == 0
     x, y, a, b, scale, ids = c
@@ -377,7 +377,7 @@ def test_a_wait_that_gives_up(ts):
         ts.adapt_test_stall(False)
     assert ts.adapt_error() == 5 and ts.adapt_error() == 0
     assert torch.equal(ad.forward(x, y, ids, out=torch.empty_like(y)), want)
-    rows, h, dy = ad.rows(ids), torch.randn(600, 16, device="cuda"), y.clone()
+    rows, h, dy = ad.rows(ids), torch.randn(2100, 16, device="cuda"), y.clone()
     want = ad.backward(dy, None, rows, h, x)
     ts.adapt_test_stall(True)
     try:
