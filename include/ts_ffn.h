@@ -544,6 +544,7 @@ ts_status ts_prompt_check_scratch(ts_prompt* p, cudaStream_t stream);
  *     ts_list_rows              the rows of every adapter
  *     ts_adapt_rows             each row's share of its adapter, added to a product; its backward pass by rows
  *     ts_adapter_grads          gradients of the adapters
+ *     ts_adapters_backward      these two as the backward pass of the first
  *     ts_drelu_rows             the gated activation of products computed apart, kept in 8 bits
  *     ts_drelu_rows_backward    its backward pass from what was kept
  *     ts_balance                loss on uneven routing, with the experts' counts
@@ -612,6 +613,20 @@ void ts_adapt_set_test_stall(int on);
 ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
                            int64_t ld_scale, int rows, int k, int n_adapters, const int32_t* list, const int32_t* offsets,
                            float* grad, int accumulate, cudaStream_t stream);
+
+/*
+ * The backward pass of ts_adapt_rows (x, A, B, y to out, with h): in one call, which lets the two sums of rows overlap,
+ *     ts_adapt_rows of dy, B, A, dx to out, with dh      dh[t] = scale[i] dy[t] B_i^T, out[t] = dx[t] + dh[t] A_i
+ *     ts_adapter_grads of dh and x to da, of h and dy to db
+ * with the arguments of those: dy rows of n bf16, h what the forward gave, x its rows (TS_BF16, or TS_E4M3 with x_scale), dx and
+ * out rows of k of dxdtype (both NULL: not wanted), dh device [rows][r] fp32 (scratch, needed), list and offsets as
+ * ts_list_rows writes them (needed).
+ */
+ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, const void* a, const void* b, const float* scale,
+                               const int32_t* ranks, int n_adapters, int r, int k, const int32_t* list, const int32_t* offsets,
+                               const float* h, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
+                               int64_t ld_scale, const void* dx, int64_t lddx, ts_dtype dxdtype, void* out, int64_t ldo, float* dh,
+                               float* da, float* db, int accumulate, cudaStream_t stream);
 
 /*
  * The gated activation (Eq. 2) of rows whose two products were computed apart: c = max(0, g) max(0, u), 0 unless both are

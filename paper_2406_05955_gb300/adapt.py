@@ -41,7 +41,7 @@ def _matrix(t, what: str, dtypes, shape, dev: int) -> torch.Tensor:
 
 
 class Adapters:
-    """Low-rank adapters of many requests beside one shared product (``ts_adapt_rows``, ``ts_adapter_grads``): bf16
+    """Low-rank adapters of many requests beside one shared product (``ts_adapt_rows``, ``ts_adapters_backward``): bf16
     ``a [adapters][r][k]`` and ``b [adapters][r][n]`` (rows of ``b`` are what a component adds, as in ``w_down``), fp32
     ``scale [adapters]``, int32 ``ranks [adapters]`` where some have fewer than ``r``. Weights are borrowed; those of one
     adapter may be exchanged between calls. Calls keep nothing: any number may be in flight."""
@@ -85,20 +85,6 @@ class Adapters:
             ids = self.rows(ids, stream=stream)
         return None, ids.rows.data_ptr(), ids.offsets.data_ptr(), ids
 
-    def _apply(self, x, t: int, a: int, b: int, k: int, n: int, y, ids, out, h, stream):
-        """``ts_adapt_rows`` of ``x`` through the matrices at ``a`` and ``b``."""
-        ids, rows, offsets, _keep = ids
-        yp = op = hp = None
-        ldy = ldo = 0
-        code = TS_BF16
-        if y is not None:
-            code, yp, ldy = _CODES[y.dtype], y.data_ptr(), _ld(y)
-            op, ldo = (yp, ldy) if out is None else (out.data_ptr(), _ld(out))
-        if h is not None:
-            hp = h.data_ptr()
-        _check(lib().ts_adapt_rows(x.data_ptr(), _ld(x), t, k, a, b, self._scale, self._ranks, self.adapters, self.r, n, ids,
-                                   rows, offsets, yp, ldy, code, op, ldo, hp, _handle(stream)), "ts_adapt_rows")
-
     def forward(self, x: torch.Tensor, y: torch.Tensor, ids, out=None, h=None, stream=None) -> torch.Tensor:
         """``out[t] = y[t] + scale x[t] A^T B`` of the adapter that ``ids`` (int32 ``[rows]``, or what ``rows`` gives) names
         for row ``t``; without ``out`` in ``y`` itself (bf16 or fp32 ``[rows][n]``). x is bf16 ``[rows][k]``. fp32
@@ -111,8 +97,13 @@ class Adapters:
             _matrix(out, "out", (y.dtype,), (t, self.n), dev)
         if h is not None:
             _shaped(h, "h", _F32, (t, self.r), dev)
-        self._apply(x, t, self._a, self._b, self.k, self.n, y, self._ids(ids, t, False, stream), out, h, stream)
-        return y if out is None else out
+        if out is None:
+            out = y
+        ids, rows, offsets, _keep = self._ids(ids, t, False, stream)
+        _check(lib().ts_adapt_rows(x.data_ptr(), _ld(x), t, self.k, self._a, self._b, self._scale, self._ranks, self.adapters,
+                                   self.r, self.n, ids, rows, offsets, y.data_ptr(), _ld(y), _CODES[y.dtype], out.data_ptr(),
+                                   _ld(out), None if h is None else h.data_ptr(), _handle(stream)), "ts_adapt_rows")
+        return out
 
     __call__ = forward
 
@@ -141,21 +132,23 @@ class Adapters:
             if x_scale.shape[0] != -(-self.k // BLOCK) or x_scale.shape[1] < t:
                 raise ValueError(f"x_scale must be [{-(-self.k // BLOCK)}][rows]")
             sp, ld = x_scale.data_ptr(), _ld(x_scale)
-        grads = []
-        for given, what, like in ((da, "da", self.a), (db, "db", self.b)):
-            if given is None and accumulate:
-                raise ValueError(f"{what} is needed to add to")
-            grads.append(_empty(stream, *like.shape, dtype=_F32) if given is None else
-                         _shaped(given, what, _F32, tuple(like.shape), self.device))
-        listed = self._ids(ids, t, True, stream)
+        if accumulate and (da is None or db is None):
+            raise ValueError("da and db are needed to add to")
+        da = _empty(stream, *self.a.shape, dtype=_F32) if da is None else _shaped(da, "da", _F32, self.a.shape, dev)
+        db = _empty(stream, *self.b.shape, dtype=_F32) if db is None else _shaped(db, "db", _F32, self.b.shape, dev)
+        _, rows, offsets, _keep = self._ids(ids, t, True, stream)
         dh = _empty(stream, t, self.r, dtype=_F32)
-        self._apply(dy, t, self._b, self._a, self.n, self.k, dx, listed, out, dh, stream)
-        L, s = lib(), _handle(stream)
-        for of, rows, scale, grad in ((dh, x, (sp, ld), grads[0]), (h, dy, (None, 0), grads[1])):
-            _check(L.ts_adapter_grads(of.data_ptr(), self.r, rows.data_ptr(), _ld(rows), _CODES[rows.dtype], *scale, t,
-                                      rows.shape[1], self.adapters, listed[1], listed[2], grad.data_ptr(),
-                                      int(bool(accumulate)), s), "ts_adapter_grads")
-        return dx if out is None else out, grads[0], grads[1]
+        dp = op = None
+        ldd = ldo = 0
+        code = TS_BF16
+        if dx is not None:
+            code, dp, ldd = _CODES[dx.dtype], dx.data_ptr(), _ld(dx)
+            op, ldo = (dp, ldd) if out is None else (out.data_ptr(), _ld(out))
+        _check(lib().ts_adapters_backward(
+            dy.data_ptr(), _ld(dy), t, self.n, self._a, self._b, self._scale, self._ranks, self.adapters, self.r, self.k, rows,
+            offsets, h.data_ptr(), x.data_ptr(), _ld(x), _CODES[x.dtype], sp, ld, dp, ldd, code, op, ldo, dh.data_ptr(),
+            da.data_ptr(), db.data_ptr(), int(bool(accumulate)), _handle(stream)), "ts_adapters_backward")
+        return dx if out is None else out, da, db
 
 
 def adapt_error(stream=None) -> int:

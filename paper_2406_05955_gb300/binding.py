@@ -94,6 +94,7 @@ SIGNATURES = {
     "ts_adapt_get_error": (I, [P]),
     "ts_adapt_set_test_stall": (None, [I]),
     "ts_adapter_grads": (I, [P, I, P, L64, I, P, L64, I, I, I, P, P, P, I, P]),
+    "ts_adapters_backward": (I, [P, L64, I, I, P, P, P, P, I, I, I, P, P, P, P, L64, I, P, L64, P, L64, I, P, L64, P, P, P, I, P]),
     "ts_drelu_rows": (I, [P, L64, P, L64, I, P, I, I, P, L64, P, P, P, P, P]),
     "ts_drelu_rows_backward": (I, [P, L64, I, P, P, P, P, P, I, I, P, L64, P, L64, P, L64, P]),
     "ts_balance_work": (ctypes.c_longlong, [I, I]),

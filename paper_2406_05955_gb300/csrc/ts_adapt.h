@@ -50,6 +50,7 @@ struct AdapterGradsLaunch {
     const int32_t* offsets;
     float* grad;             // [n_adapters][r][k]
     int accumulate;
+    int follows;             // what it reads was there before the kernel before it, which is one of these too, began
     int test_stall;          // ts_adapt_set_test_stall
 };
 

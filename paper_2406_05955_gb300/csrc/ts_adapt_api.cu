@@ -95,7 +95,34 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_adapter_grads(
-        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, test_stall.load()}, e8, stream));
+        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, 0, test_stall.load()}, e8, stream));
+}
+
+ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, const void* a, const void* b, const float* scale,
+                               const int32_t* ranks, int n_adapters, int r, int k, const int32_t* list, const int32_t* offsets,
+                               const float* h, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
+                               int64_t ld_scale, const void* dx, int64_t lddx, ts_dtype dxdtype, void* out, int64_t ldo, float* dh,
+                               float* da, float* db, int accumulate, cudaStream_t stream) {
+    if (!offsets || !aligned4(offsets) || (rows > 0 && (!list || !dh))) return TS_ERR_INVALID_ARG;
+    // all of it is checked before any of it is launched
+    const bool e8 = xdtype == TS_E4M3;
+    ts_status s = check_adapters(rows, k, n_adapters, r);
+    if (s == TS_OK) s = check_adapters(rows, n, n_adapters, r);
+    if (s != TS_OK) return s;
+    if ((!e8 && xdtype != TS_BF16) || k % (e8 ? 16 : 8) != 0 || n % 8 != 0 || !da || !aligned16(da) || !db || !aligned16(db))
+        return TS_ERR_INVALID_ARG;
+    if (rows > 0 && (!h || !aligned4(h) || !rows_ok(x, ldx, k, xdtype) ||
+                     (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
+        return TS_ERR_INVALID_ARG;
+    s = ts_adapt_rows(dy, ldy, rows, n, b, a, scale, ranks, n_adapters, r, k, nullptr, list, offsets, dx, lddx, dxdtype, out, ldo,
+                      dh, stream);
+    if (s != TS_OK) return s;
+    const int add = accumulate != 0, stall = test_stall.load();
+    const cudaError_t e = launch_adapter_grads(
+        {dh, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, da, add, 0, stall}, e8, stream);
+    if (e != cudaSuccess) return TS_ERR_CUDA;
+    return launched(launch_adapter_grads(
+        {h, r, dy, ldy, nullptr, 0, rows, n, n_adapters, list, offsets, db, add, 1, stall}, false, stream));
 }
 
 ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, ts_dtype dtype, const int32_t* n, int rows,

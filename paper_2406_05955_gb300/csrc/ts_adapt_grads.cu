@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
         mbar_fence_init();
         chunks = first_id = 0;
     }
-    pdl_wait();
+    if (!L.follows) pdl_wait();
+    pdl_launch_dependents();  // one that follows fills the SMs that this one leaves
     if (warp == 0) tc_alloc<G::kColumns>(&tmem);
     if (tid <= L.n_adapters) offs[tid] = min(max(L.offsets[tid], 0), L.rows);
     tc_before();
@@ -343,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
                 for (int i = tid; i < L.r * kGradCols; i += kThreads)
                     if (col0 + i % kGradCols < L.k) L.grad[((size_t)id * L.r + i / kGradCols) * L.k + col0 + i % kGradCols] = 0.0f;
 
+    if (L.follows) pdl_wait();  // (what comes after this kernel comes after the one before it too)
     // Adapters of several parts: each of their CTAs sums some of the elements. A CTA can have two such adapters.
     if (ctas == 1) return;
     __syncthreads();

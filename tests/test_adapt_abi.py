@@ -64,6 +64,23 @@ def test_adapter_grads(lib):
     assert call(lib.ts_adapter_grads, good, k=(1 << 24) + 8, ldx=(1 << 24) + 8) == UNSUPPORTED
 
 
+def test_adapters_backward(lib):
+    from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
+                                                TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_INT4)
+
+    good = {"dy": G, "ldy": 32, "rows": 4, "n": 32, "a": G, "b": G, "scale": None, "ranks": None, "adapters": 3, "r": 8, "k": 64,
+            "list": G, "offsets": G, "h": G, "x": G, "ldx": 64, "dt": TS_BF16, "x_scale": None, "ld_scale": 0, "dx": G,
+            "lddx": 64, "ddt": TS_F32, "out": G, "ldo": 64, "dh": G, "da": G, "db": G, "accumulate": 0, "stream": None}
+    e8 = {"dt": TS_E4M3, "x_scale": G, "ld_scale": 4}
+    for kw in ({"dy": None}, {"dy": G + 8}, {"ldy": 24}, {"rows": -1}, {"n": 36}, {"a": None}, {"b": G + 2}, {"scale": G + 2},
+               {"ranks": G + 1}, {"adapters": 256}, {"r": 129}, {"k": 60}, {"list": None}, {"offsets": None}, {"offsets": G + 2},
+               {"h": None}, {"x": None}, {"x": G + 8}, {"ldx": 60}, {"dt": TS_F32}, {"x_scale": G}, {**e8, "x_scale": None},
+               {**e8, "ld_scale": 3}, {"dx": None}, {"lddx": 62}, {"ddt": TS_INT4}, {"out": None}, {"ldo": 8}, {"dh": None},
+               {"dh": G + 2}, {"da": None}, {"da": G + 4}, {"db": None}, {"db": G + 8}):
+        assert call(lib.ts_adapters_backward, good, **kw) == BAD, kw
+    assert call(lib.ts_adapters_backward, good, rows=(1 << 30) + 1) == UNSUPPORTED
+
+
 def test_drelu_rows(lib):
     from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
                                                 TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_OK)
