@@ -153,10 +153,9 @@ struct TileRows {
     int id, rank, first, count;
 };
 
-// By the list: tile number `tile`, of up to `high` rows, of all groups' in a row, the rows without an adapter last. `rows`
-// gets MT rows' numbers.
+// By the list: tile number `tile` of all groups' in a row, the rows without an adapter last.
 template <int MT>
-__device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, TileRows* found, int* rows, int high = MT) {
+__device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, TileRows* found, int* rows) {
     __shared__ int sums[kWarp];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int begin = 0, end = 0;
@@ -164,7 +163,7 @@ __device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, Tile
         begin = min(max(L.offsets[tid], 0), L.rows);
         end = min(max(L.offsets[tid + 1], begin), L.rows);
     }
-    const int tiles = (end - begin + high - 1) / high;
+    const int tiles = (end - begin + MT - 1) / MT;
     int upto = tiles;
 #pragma unroll
     for (int o = 1; o < kWarp; o <<= 1) {
@@ -176,8 +175,8 @@ __device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, Tile
     __syncthreads();
     for (int w = 0; w < warp; ++w) upto += sums[w];
     if (tile < upto && tile >= upto - tiles) {
-        const int first = begin + (tile - (upto - tiles)) * high;
-        *found = {tid, 0, first, min(high, end - first)};
+        const int first = begin + (tile - (upto - tiles)) * MT;
+        *found = {tid, 0, first, min(MT, end - first)};
     }
     __syncthreads();
     if (tid < MT) {

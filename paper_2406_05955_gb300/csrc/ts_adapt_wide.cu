@@ -3,15 +3,18 @@
 // The tile's cluster shares k and the columns as in ts_adapt.cu. A CTA's items are chunks 256 bytes of each row wide: of x and
 // A_i, whose products are summed in tensor memory, and then of y and B_i. h is the M operand of the second product, as 2 (bf16
 // rows) or 3 (fp32) bf16 numbers in shared memory, and a row of its products is a lane of tensor memory: so a thread has a row of
-// an item to itself. It fetches it by one bulk copy into a row of shared memory, adds to it in place and sends it off by
-// another; no two threads touch the same bytes, and nothing is written twice.
+// an item to itself. It fetches it by one bulk copy into a row of shared memory and adds to it in place; its warp writes the
+// 32 rows, two at a time.
 //
-// Warps 0-3 and 4-7 take items of y in turn (and copy x, 16 bytes at a time, in the order the tensor cores want), warps 8-11
-// copy A and B, warp 12 issues the products. They wait for one another by barriers in shared memory only. What was measured on the
-// way, 8192 rows, k = 4096, n = 14336, r = 64, bf16: eight warps that do everything, a CTA barrier an item, 130 us (0.9 us an item
-// whatever it holds: the longest warp's copies, products and sums in a row); the same with sixteen warps, or two CTAs of half
-// the item, 130-140; a warp of its own for the products 128 (16-byte copies and pieces of 64 bytes a warp: 2 us for 2 KB);
-// as it is 114.
+// Sixteen warps, four an item, take items of y in turn (and copy x, 16 bytes at a time, in the order the tensor cores want), four
+// copy A and B, one issues the products. They wait for one another by barriers in shared memory only.
+//
+// Memory bounds it where the tiles fill the device, latencies otherwise: a row of an item is fetched, added to and written
+// in a chain that takes a warp 4700 cycles for 8 KB, so that many warps have to be at it. Measured on the way, 8192 rows,
+// k = 4096, n = 14336, r = 64, bf16: eight warps that do everything, a CTA barrier an item, 130 us; sixteen so, or two CTAs
+// of half the item, 130-140; a warp of its own for the products 122; a row a thread, bulk copies of 256 bytes both ways, two
+// groups of warps with two items each 112 (a warp's 32 copies take 2000-2600 cycles to issue); of 512 bytes and one item 117;
+// written by 16-byte stores 110; four groups with an item each 96 (4.9 TB/s; 5.6 while y is added to).
 #include <atomic>
 
 #include "ts_adapt.cuh"
@@ -23,15 +26,13 @@ namespace {
 __device__ unsigned wide_status;
 
 constexpr int kTileRows = 128;
-constexpr int kGroup = kTileRows, kWorkers = 2 * kGroup;  // threads that take items of y in turn
+constexpr int kGroup = kTileRows, kGroups = 4, kWorkers = kGroups * kGroup;  // threads that take items of y in turn
 constexpr int kCarriers = 128;                            // that copy A and B
 constexpr int kWideThreads = kWorkers + kCarriers + kWarp;
-constexpr int kXSlots = 4;                                // items of x in the ring
-constexpr int kRowBytes = 2 * kChunk;                     // a group's thread has two items of its row at a time
-constexpr int kPitch = kRowBytes + 16;                    // bytes from a row to the next: 8 rows' same piece lie in 8 banks
-constexpr int kGroupBytes = kTileRows * kPitch;
-constexpr int kRing = 2 * kGroupBytes;                    // rows of y and out of both groups; before, the items of x
-static_assert(kRing % 1024 == 0 && kRing >= kXSlots * kTileRows * kChunk, "");
+constexpr int kSlots = 4;                                 // items of rows: one of each group
+constexpr int kPitch = kChunk + 16;                       // bytes from a row of y to the next: 8 rows' same piece lie in 8 banks
+constexpr int kSlotBytes = kTileRows * kPitch;
+static_assert(kSlots == kGroups && kSlotBytes % 1024 == 0 && kSlotBytes >= kTileRows * kChunk, "x starts on 1024 bytes");
 
 template <int RP, typename TY>
 struct Wide {
@@ -41,37 +42,31 @@ struct Wide {
     static constexpr int kMat = RP * kChunk;                   // of A or B in an item
     static constexpr int kMats = RP == 64 && kParts == 3 ? 2 : 3;
     static constexpr int kPart = kTileRows * 128;              // of h: 128 bytes a row, of which r take 2 r
-    static constexpr int kSmem = 1024 + kRing + kMats * kMat + kParts * kPart;
-    static constexpr int kMine = RP / 2;                       // components of a thread's row
+    static constexpr int kSmem = 1024 + kSlots * kSlotBytes + kMats * kMat + kParts * kPart;
+    static constexpr int kMine = RP / kGroups;                 // components of a thread's row
     static_assert(kTileRows * RP * 4 <= kParts * kPart, "the sums lie where h will");
 };
 
-__device__ __forceinline__ void bulk_store(void* to, uint32_t from, unsigned bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 template <int RP, typename TY>
-__global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_constant__ AdaptLaunch L, int ctas, int high) {
+__global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_constant__ AdaptLaunch L, int ctas) {
     using W = Wide<RP, TY>;
     extern __shared__ unsigned char raw[];
     __shared__ TileRows found;
     __shared__ int rows[kTileRows];
-    __shared__ uint2 x_at[kTileRows];  // first byte of each row of x (none: the highest bit)
-    __shared__ uint64_t come_x[kXSlots], come_y[2][kGroup / kWarp], come_mat[W::kMats];  // copies of x, of a warp's rows of y, of A or B
-    __shared__ uint64_t done_x[kXSlots], done_out[2], done_mat[W::kMats];  // products: of an item of x, of a group's item, with a matrix
-    __shared__ uint64_t have_h, have_read[2];   // h as bf16 numbers; the products of a group's item are in registers
+    __shared__ uint2 x_at[kTileRows];     // first byte of each row of x (none: the highest bit)
+    __shared__ char* out_at[kTileRows];   // and of out (nullptr)
+    __shared__ uint64_t come_x[kSlots], come_y[kSlots][kGroup / kWarp], come_mat[W::kMats];  // an item's copies
+    __shared__ uint64_t done[kSlots];           // its products
+    __shared__ uint64_t have_h, have_read[2];   // h as bf16 numbers; an item's products are in registers (two take turns)
     __shared__ uint32_t tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t cta = cluster_rank();
     unsigned char* const smem = raw + (-smem_u32(raw) & 1023u);
-    unsigned char* const mats = smem + kRing;
+    unsigned char* const mats = smem + kSlots * kSlotBytes;
     unsigned char* const h_parts = mats + W::kMats * W::kMat;
     const uint32_t smem0 = smem_u32(smem), mats0 = smem_u32(mats), h0 = smem_u32(h_parts);
     pdl_wait();
-    find_listed<kTileRows>(L, (int)(blockIdx.x / ctas), &found, rows, high);
+    find_listed<kTileRows>(L, (int)(blockIdx.x / ctas), &found, rows);
     __syncthreads();
     const int id = found.id, count = found.count;
     if (id < 0) return;
@@ -93,20 +88,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
         const int row = rows[tid];
         const uint64_t at = row < 0 ? 1ull << 63 : (uint64_t)(row * L.ldx * 2);
         x_at[tid] = make_uint2((uint32_t)at, (uint32_t)(at >> 32));
+        out_at[tid] = row < 0 ? nullptr : reinterpret_cast<char*>(out + row * L.ldo);
     }
     if (tid == 0) {
-        for (int i = 0; i < kXSlots; ++i) {
+        for (int i = 0; i < kSlots; ++i) {
             mbar_init(&come_x[i], kWorkers);
-            mbar_init(&done_x[i], 1);
+            for (int q = 0; q < kGroup / kWarp; ++q) mbar_init(&come_y[i][q], 1);
+            mbar_init(&done[i], 1);
         }
-        for (int i = 0; i < W::kMats; ++i) {
-            mbar_init(&come_mat[i], kCarriers);
-            mbar_init(&done_mat[i], 1);
-        }
-        for (int g = 0; g < 2; ++g) {
-            for (int q = 0; q < kGroup / kWarp; ++q) mbar_init(&come_y[g][q], 1);
-            mbar_init(&done_out[g], 1);
-        }
+        for (int i = 0; i < W::kMats; ++i) mbar_init(&come_mat[i], kCarriers);
         mbar_init(&have_h, kWorkers);
         for (int i = 0; i < 2; ++i) mbar_init(&have_read[i], kGroup / kWarp);
         mbar_fence_init();
@@ -124,21 +114,17 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
     const int k0 = (int)((long long)k_chunks * cta / ctas), nk = (int)((long long)k_chunks * (cta + 1) / ctas) - k0;
     const int all = ctas * (int)gridDim.y, me = (int)(blockIdx.y * ctas + cta);
     const int n0 = (int)((long long)n_chunks * me / all), nn = (int)((long long)n_chunks * (me + 1) / all) - n0;
-    // The items: nk of x, and then, in the order of their products, those of y, four at a time: the first of two that group 0
-    // has, the first of group 1, the second of group 0, the second of group 1. `part` says which item of this CTA's columns that
-    // is; the last ones may be missing.
-    const int total = nk + (nn + 3) / 4 * 4;
-    const auto part = [&](int i) { return (i - nk) / 4 * 4 + (i - nk) % 2 * 2 + (i - nk) / 2 % 2; };
-    const auto missing = [&](int i) { return i >= nk && part(i) >= nn; };
+    const int total = nk + nn;
 
     bool failed = false;
     const auto wait = [&](uint64_t* bar, unsigned parity) {
         if (!failed) failed = !mbar_wait(bar, parity);  // (after the first that gives up, none waits)
     };
+    const auto products = [&](int i) { wait(&done[i & 3], i >> 2 & 1); };  // of item i
 
     if (warp >= (kWorkers + kCarriers) / kWarp) {
         // ---- the products -------------------------------------------------------------------------------------------
-        int mat = 0, round = 0, taken[2] = {0, 0};
+        int mat = 0, round = 0;
         for (int i = 0; i <= total && rank > 0; ++i) {
             if (i == nk) {
                 if (ctas > 1) {  // the join's barriers are all threads'
@@ -150,21 +136,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
                 wait(&have_h, 0);
             }
             if (i == total) break;
-            if (missing(i)) continue;
-            const int group = (i - nk) & 1;
-            if (i < nk) {
-                wait(&come_x[i & 3], i >> 2 & 1);
-            } else {
-                const int n = group ? taken[1]++ : taken[0]++;  // items of this group before
-                if (n > 0) wait(&have_read[group], (n - 1) & 1);
-            }
+            if (i < nk) wait(&come_x[i & 3], i >> 2 & 1);
+            else if (i >= nk + 2) wait(&have_read[i & 1], ((i - nk) / 2 - 1) & 1);
             wait(&come_mat[mat], round & 1);
             failed = __any_sync(0xffffffffu, failed);
             if (!failed) {
                 fence_proxy_async_smem();
                 tc_after();
                 if (elect_one()) {
-                    const uint32_t m = mats0 + mat * W::kMat, at = smem0 + (i & 3) * (kTileRows * kChunk);
+                    const uint32_t m = mats0 + mat * W::kMat, at = smem0 + (i & 3) * kSlotBytes;
                     if (i < nk) {
                         const uint32_t d = t_h + (i >> 1 & 3) * 64;
 #pragma unroll
@@ -176,11 +156,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
                         for (int q = W::kParts - 1; q >= 0; --q)
 #pragma unroll
                             for (int ks = 0; ks < RP / 16; ++ks)
-                                tc_mma(t_out + group * 128, desc_k(h0 + q * W::kPart) + 2 * ks, desc_n(m, RP * 128) + 128 * ks,
+                                tc_mma(t_out + (i & 1) * 128, desc_k(h0 + q * W::kPart) + 2 * ks, desc_n(m, RP * 128) + 128 * ks,
                                        idesc(W::kOutCols, false, true), q < W::kParts - 1 || ks > 0);
                     }
-                    tc_commit(&done_mat[mat]);
-                    if (!(L.test_stall && i + 4 >= total)) tc_commit(i < nk ? &done_x[i & 3] : &done_out[group]);
+                    if (!(L.test_stall && i == total - 1)) tc_commit(&done[i & 3]);
                 }
                 __syncwarp();
             }
@@ -203,12 +182,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
             cluster_wait();
             met = true;
         };
-        int mat = 0, round = 0;
+        int mat = 0;
         for (int i = 0; i < total && rank > 0; ++i) {
             if (i == nk && !met) cluster_arrive();
             if (i == nk + W::kMats) meet();
-            if (missing(i)) continue;
-            if (round > 0) wait(&done_mat[mat], (round - 1) & 1);
+            if (i >= W::kMats) products(i - W::kMats);
             const uint32_t to = mats0 + mat * W::kMat;
             if (i < nk) {
                 const int col = (k0 + i) * W::kCols + a_piece * 8;
@@ -222,7 +200,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
                     from += a_step;
                 }
             } else {
-                const int col = (n0 + part(i)) * W::kOutCols + b_piece * 8;
+                const int col = (n0 + i - nk) * W::kOutCols + b_piece * 8;
                 const bool in = col < L.n;
                 const char* from = reinterpret_cast<const char*>(b + (size_t)b_row * L.n + (in ? col : 0));
 #pragma unroll
@@ -234,7 +212,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
                 }
             }
             copies_arrive(&come_mat[mat]);
-            if (++mat == W::kMats) mat = 0, ++round;
+            if (++mat == W::kMats) mat = 0;
         }
         if (total == nk && !met) cluster_arrive();
         meet();
@@ -243,65 +221,57 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
         const int group = warp >> 2, quarter = (warp & 3) * 32, mine = quarter + lane;  // this thread's row of the group's items
         const int row = rows[mine];
         const char* const y_row = reinterpret_cast<const char*>(y + (row < 0 ? 0 : row * L.ldy));
-        char* const out_row = reinterpret_cast<char*>(out + (row < 0 ? 0 : row * L.ldo));
         const int there = __popc(__ballot_sync(0xffffffffu, row >= 0));
-        // the two items of y of number `pair` of this group: where they begin in a row, and their bytes
-        const auto at_pair = [&](int pair) { return (int64_t)(n0 + 4 * pair + 2 * group) * kChunk; };
-        const auto bytes = [&](int pair) {
-            const int mine = min(2, nn - 4 * pair - 2 * group);  // items
-            return (int)min((int64_t)mine * kChunk, (int64_t)L.n * (int)sizeof(TY) - at_pair(pair));
-        };
-        const int pairs = (nn - 2 * group + 3) / 4;
-        unsigned char* const mine_at = smem + group * kGroupBytes + mine * kPitch;
-        const auto fetch_y = [&](int pair) {
-            if (pair >= pairs) return;
-            uint64_t* const bar = &come_y[group][warp & 3];
-            const int n = bytes(pair);
-            if (lane == 0) mbar_arrive_expect_tx(bar, (unsigned)(there * n));
-            __syncwarp();
-            if (row >= 0) tma_load_1d(mine_at, y_row + at_pair(pair), (unsigned)n, bar);
-        };
-        // x: a warp copies the half `group` of 32 rows, 8 lanes a row
-        const int piece = group * 8 + (lane & 7), x_row = quarter + (lane >> 3);
-        const uint32_t x_to = group * (kTileRows * 128) + place<128>(x_row, piece & 7);
-        const auto fetch_x = [&](int i) {
-            if (i >= nk) return;
-            const int col = (k0 + i) * W::kCols + piece * 8;
-            const bool in = col < L.k;
-            const char* const base = reinterpret_cast<const char*>(x + (in ? col : 0));
-            const uint32_t to = smem0 + (i & 3) * (kTileRows * kChunk);
+        const auto bytes = [&](int i) { return min(kChunk, (L.n - (n0 + i - nk) * W::kOutCols) * (int)sizeof(TY)); };  // of a row
+        const auto at_col = [&](int i) { return (int64_t)(n0 + i - nk) * kChunk; };
+        // x: a warp copies a fourth of 32 rows, 4 lanes a row
+        const int piece = group * 4 + (lane & 3), x_row = quarter + (lane >> 2);
+        const uint32_t x_to = (piece >> 3) * (kTileRows * 128) + place<128>(x_row, piece & 7);
+        const auto fetch = [&](int i) {  // item i
+            if (i >= total) return;
+            if (i < nk) {
+                const int col = (k0 + i) * W::kCols + piece * 8;
+                const bool in = col < L.k;
+                const char* const base = reinterpret_cast<const char*>(x + (in ? col : 0));
+                const uint32_t to = smem0 + (i & 3) * kSlotBytes;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint2 at = x_at[x_row + j * 4];
-                copy16(to + (x_to ^ (j & 1) << 6) + j * 4 * 128, base + ((uint64_t)(at.y & 0x7fffffffu) << 32 | at.x), in && (int)at.y >= 0);
+                for (int j = 0; j < 4; ++j) {
+                    const uint2 at = x_at[x_row + j * 8];
+                    copy16(to + x_to + j * 8 * 128, base + ((uint64_t)(at.y & 0x7fffffffu) << 32 | at.x), in && (int)at.y >= 0);
+                }
+                copies_arrive(&come_x[i & 3]);
+            } else if ((i & 3) == group) {
+                uint64_t* const bar = &come_y[i & 3][warp & 3];
+                const int n = bytes(i);
+                if (i < nk + kSlots) fence_proxy_async_smem();  // (x was there)
+                if (lane == 0) mbar_arrive_expect_tx(bar, (unsigned)(there * n));
+                __syncwarp();
+                if (row >= 0) tma_load_1d(smem + (i & 3) * kSlotBytes + mine * kPitch, y_row + at_col(i), (unsigned)n, bar);
             }
-            copies_arrive(&come_x[i & 3]);
         };
 #pragma unroll 1
-        for (int i = 0; i < kXSlots; ++i) fetch_x(i);
+        for (int i = 0; i < kSlots; ++i) fetch(i);
         if (rank > 0) {
             float sum[W::kMine] = {};
             for (int i = 1; i <= nk; ++i) {
-                wait(&done_x[(i - 1) & 3], (i - 1) >> 2 & 1);
-                fetch_x(i - 1 + kXSlots);
-                if (i == nk) {  // y comes where x was
-                    fence_proxy_async_smem();
-                    fetch_y(0);
-                }
+                products(i - 1);
                 if (i == nk || (i & 1) == 0) {
                     // The tensor cores cut bits off a long sum: every 256 of k it is added up here.
                     tc_after();
                     float v[W::kMine];
 #pragma unroll
-                    for (int j = 0; j < W::kMine; j += 8)
-                        tc_ld8(t_h + ((i - 1) >> 1 & 3) * 64 + ((uint32_t)quarter << 16) + group * W::kMine + j, v + j);
+                    for (int j = 0; j < W::kMine; j += W::kMine < 8 ? 4 : 8) {
+                        const uint32_t at = t_h + ((i - 1) >> 1 & 3) * 64 + ((uint32_t)quarter << 16) + group * W::kMine + j;
+                        if constexpr (W::kMine < 8) tc_ld4(at, v + j);
+                        else tc_ld8(at, v + j);
+                    }
                     tc_ld_wait(v);
 #pragma unroll
                     for (int j = 0; j < W::kMine; ++j) sum[j] += v[j];
                     tc_before();
                 }
+                fetch(i - 1 + kSlots);
             }
-            if (nk == 0) fetch_y(0);
             // h of the whole tile, summed over the cluster, as bf16 numbers. The sums lie where those will.
             constexpr int kQuads = RP / 4, kAll = kTileRows * kQuads / kWorkers;
             float4* const sums = reinterpret_cast<float4*>(h_parts);
@@ -356,33 +326,29 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
             fence_proxy_async_smem();
             mbar_arrive(&have_h);
         }
-        if (rank == 0) fetch_y(0);
-        // out: this thread's row of the group's items, two at a time
-        constexpr int kPer = 16 / (int)sizeof(TY);
-        int taken = 0;
-        for (int pair = 0; pair < pairs; ++pair) {
-            wait(&come_y[group][warp & 3], pair & 1);
-#pragma unroll 1
-            for (int half = 0; half < 2 && rank > 0 && 4 * pair + 2 * group + half < nn; ++half) {
-                wait(&done_out[group], taken++ & 1);
-                tc_after();
-                unsigned char* const at = mine_at + half * kChunk;
+        // out: this thread's row of every fourth item
+        for (int i = nk + ((group - nk) & 3); i < total; i += kGroups) {
+            wait(&come_y[i & 3][warp & 3], (i - nk) >> 2 & 1);
+            if (rank > 0) products(i);
+            tc_after();
+            unsigned char* const mine_at = smem + (i & 3) * kSlotBytes + mine * kPitch;
+            constexpr int kPer = 16 / (int)sizeof(TY);
+            if (rank > 0) {
+                for (int j0 = 0; j0 < W::kOutCols; j0 += 16) {
+                    float v[16];
+                    tc_ld8(t_out + (i & 1) * 128 + ((uint32_t)quarter << 16) + j0, v);
+                    tc_ld8(t_out + (i & 1) * 128 + ((uint32_t)quarter << 16) + j0 + 8, v + 8);
+                    uint4 had[16 / kPer];
 #pragma unroll
-                for (int j0 = 0; j0 < W::kOutCols; j0 += 32) {
-                    float v[32];
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) tc_ld8(t_out + group * 128 + ((uint32_t)quarter << 16) + j0 + j, v + j);
-                    uint4 had[32 / kPer];
-#pragma unroll
-                    for (int c = 0; c < 32 / kPer; ++c) had[c] = lds128(at + (j0 / kPer + c) * 16);
+                    for (int c = 0; c < 16 / kPer; ++c) had[c] = lds128(mine_at + (j0 / kPer + c) * 16);
                     tc_ld_wait(v);
-                    if (j0 + 32 == W::kOutCols) {
+                    if (j0 + 16 == W::kOutCols) {
                         tc_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&have_read[group]);
+                        if (lane == 0) mbar_arrive(&have_read[i & 1]);
                     }
 #pragma unroll
-                    for (int c = 0; c < 32 / kPer; ++c) {
+                    for (int c = 0; c < 16 / kPer; ++c) {
                         float s[kPer];
                         Vec<TY>::unpack(had[c], s);
 #pragma unroll
@@ -399,19 +365,26 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
                         } else {
                             w = make_uint4(__float_as_uint(s[0]), __float_as_uint(s[1]), __float_as_uint(s[2]), __float_as_uint(s[3]));
                         }
-                        *reinterpret_cast<uint4*>(at + (j0 / kPer + c) * 16) = w;
+                        *reinterpret_cast<uint4*>(mine_at + (j0 / kPer + c) * 16) = w;
                     }
                 }
             }
-            fence_proxy_async_smem();
-            if (row >= 0) bulk_store(out_row + at_pair(pair), smem_u32(mine_at), (unsigned)bytes(pair));
-            if (pair + 1 < pairs) {
-                bulk_wait_read();  // (a thread's row has left before the next one comes there)
-                __syncwarp();
-                fetch_y(pair + 1);
+            __syncwarp();
+            // the warp's 32 rows, two at a time
+            const int piece_out = lane & 15, n_out = bytes(i);
+            const unsigned char* const from = smem + (i & 3) * kSlotBytes + (quarter + (lane >> 4)) * kPitch + piece_out * 16;
+            if (piece_out * 16 < n_out) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    char* const to = out_at[quarter + (lane >> 4) + 2 * j];
+                    const uint4 w = *reinterpret_cast<const uint4*>(from + 2 * j * kPitch);
+                    if (to != nullptr) *reinterpret_cast<uint4*>(to + at_col(i) + piece_out * 16) = w;
+                }
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+            fetch(i + kGroups);
         }
-        bulk_wait();
     }
     copies_wait_all();
     if (failed) {  // copies may be in flight: give them time to land
@@ -453,26 +426,25 @@ cudaError_t launch(const AdaptLaunch& a, cudaStream_t stream) {
     const auto kernel = k_adapt_wide<RP, TY>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem);
     if (e != cudaSuccess) return e;
-    // The rows of a tile, the cluster, and the clusters that share a tile's columns (each with its own h), whose rounds take the
-    // least time for nearly the most tiles that there can be (one too many for a round costs a second). Time in items of 128
-    // rows: an item of fewer takes less, down to what its latencies take, and to begin and to join take about 8.
+    // The cluster, and the clusters that share a tile's columns (each with its own h), whose rounds take the least time for nearly
+    // the most tiles that there can be (one too many for a round costs a second). Measured, in microseconds: an item of x takes
+    // 0.6, one of y 1.2, or what the memory takes for those of all CTAs, and to begin and to join take 8.
+    const long long tiles = most_tiles(a.rows, a.n_adapters, kTileRows), expect = tiles > 1 ? tiles - 1 : 1;
     const int k_items = (a.k + W::kCols - 1) / W::kCols, n_items = a.out != nullptr ? (a.n + W::kOutCols - 1) / W::kOutCols : 0;
-    int ctas = 1, high = kTileRows;
+    int ctas = 1;
     long long sharing = 1;
     double best = 1e30;
     for (int c = 1; c <= kMaxCluster; ++c) {
         const int fit = resident_clusters<RP, TY>(c);
         const long long most = n_items / c < 1 ? 1 : n_items / c;
-        for (int rows = kTileRows; rows >= kTileRows / 2; rows -= 4) {
-            const long long expect = most_tiles(a.rows, a.n_adapters, rows) - 1;
-            const double item = rows > 80 ? rows / (double)kTileRows : 80.0 / kTileRows;
-            for (long long s = 1; s <= most && s <= 16 && (s == 1 || expect * s <= fit); ++s) {
-                const double time = (double)((expect * s + fit - 1) / fit) * (((double)k_items / c + (double)n_items / (double)(c * s)) * item + 8);
-                if (time < best * 0.99) best = time, ctas = c, sharing = s, high = rows;
-            }
+        for (long long s = 1; s <= most && s <= 16 && (s == 1 || expect * s <= fit); ++s) {
+            const long long rounds = (expect * s + fit - 1) / fit;
+            const double at_once = (double)(expect * s * c) / (double)rounds;
+            const double x = at_once * 0.0056 > 0.6 ? at_once * 0.0056 : 0.6, y = at_once * 0.0113 > 1.2 ? at_once * 0.0113 : 1.2;
+            const double time = (double)rounds * ((double)k_items / c * x + (double)n_items / (double)(c * s) * y + 8);
+            if (time < best * 0.99) best = time, ctas = c, sharing = s;
         }
     }
-    const long long tiles = most_tiles(a.rows, a.n_adapters, high);
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas), (unsigned)sharing), kWideThreads, stream);
     cfg.dynamicSmemBytes = W::kSmem;
     cudaLaunchAttribute at[2]{};
@@ -482,7 +454,7 @@ cudaError_t launch(const AdaptLaunch& a, cudaStream_t stream) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, ctas, high);
+    return cudaLaunchKernelEx(&cfg, kernel, a, ctas);
 }
 
 template <typename TY>
