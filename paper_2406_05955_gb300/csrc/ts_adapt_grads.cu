@@ -151,7 +151,11 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
 
     // The 16-byte pieces that a thread copies: the same one of every few rows of x, and of h those that it then splits.
     constexpr int kPieces = kGradCols * (E8 ? 1 : 2) / 16, kXStep = kThreads / kPieces, kQuads = RP / 4, kHStep = kThreads / kQuads;
-    const int x_row = tid / kPieces, x_piece = tid % kPieces, h_row = tid / kQuads, h_quad = tid % kQuads;
+    // Which rows a warp has is so that what 8 lanes (16 bytes of x in bf16) or 16 (8 bytes of h's parts) write is in all banks.
+    const int x_row = E8 ? tid >> 4 << 1 | (tid >> 2 & 1) : tid / kPieces;
+    const int x_piece = E8 ? (tid >> 3 & 1) << 2 | (tid & 3) : tid % kPieces;
+    constexpr int kTurn = RP == 16 ? 1 : RP == 32 ? 2 : 0;  // the three lowest bits of a row, turned to the left
+    const int h_nth = tid / kQuads, h_row = (h_nth & ~7) | (h_nth << kTurn & 7) | (h_nth & 7) >> (3 - kTurn), h_quad = tid % kQuads;
     const bool x_in = col0 + x_piece * (E8 ? 16 : 8) < L.k, h_in = h_quad * 4 < L.r;
     const uint32_t x_to = E8 ? tid * 16 : (x_piece >> 3) * G::kBlock + place<128>(x_row, x_piece & 7);
     const char* const x_from = static_cast<const char*>(L.x) + (x_in ? (int64_t)col0 * (E8 ? 1 : 2) + x_piece * 16 : 0);
