@@ -4,13 +4,13 @@
 //
 // Both products in one launch. A cluster of CTAs has a tile of up to 16 or 64 rows of one adapter: each CTA sums its part
 // of k for the whole tile, the parts of h meet through distributed shared memory, summed in the same order by all, and each
-// CTA adds h B_i to its part of the columns. One ring of chunks, 256 or 512 bytes of each row wide, carries x and A_i and
+// CTA adds h B_i to its part of the columns. One ring of chunks, 256 to 1024 bytes of each row wide, carries x and A_i and
 // then y and B_i: while h is being joined the first chunks of y are already on their way. Rows of a tile are gathered (by
 // a list, or by the rows' ids here), so they come by 16-byte asynchronous copies.
 //
 // Few rows are bound by the chain launch / ids / first chunk / sums of h / join / last chunk, not by bytes. Calls in a row,
-// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.6 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 11.2
-// (12.5 MB, 1.1 TB/s; in chunks of 256 bytes 14.0); 300 rows of 20, k = 1408, n = 512, r = 40, fp32: 9.9. The matrix
+// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.5 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 9.6
+// (12.5 MB, 1.3 TB/s; in chunks of 256 bytes 14.0); 300 rows of 20, k = 1408, n = 512, r = 40, fp32: 8.1. The matrix
 // instructions of a warp do for it: they take 3% of the time.
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
@@ -21,11 +21,10 @@ namespace {
 // ---------------------------------------------------------------------------
 // h and out
 // ---------------------------------------------------------------------------
-// MT: rows of a tile. RP: r rounded up to 16, 32, 64 or 128.
-template <int MT, int RP, typename TY>
+// MT: rows of a tile. RP: r rounded up to 16, 32, 64 or 128. CHUNK: bytes of a row in a chunk.
+template <int MT, int RP, int CHUNK, typename TY>
 struct Tile {
-    // bytes of a row in a chunk: the fewer rows, the more of them, as each chunk costs the warps a round of latencies
-    static constexpr int kChunk = MT == 16 && RP <= 32 ? 512 : 256;
+    static constexpr int kChunk = CHUNK;
     static constexpr int kCols = kChunk / 2;                          // of x and A in a chunk
     static constexpr int kOutCols = kChunk / (int)sizeof(TY);         // of y and out
     static constexpr int kBPitch = kOutCols * 2;                      // bytes of a row of B
@@ -104,9 +103,9 @@ __device__ __forceinline__ void find_few(const AdaptLaunch& L, int tile, TileRow
         }
 }
 
-template <int MT, int RP, typename TY>
-__global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(const __grid_constant__ AdaptLaunch L, int ctas) {
-    using T = Tile<MT, RP, TY>;
+template <int MT, int RP, int CHUNK, typename TY>
+__global__ void __launch_bounds__(kThreads, Tile<MT, RP, CHUNK, TY>::kCtas) k_adapt(const __grid_constant__ AdaptLaunch L, int ctas) {
+    using T = Tile<MT, RP, CHUNK, TY>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ TileRows found;
     __shared__ int rows[MT];
@@ -158,6 +157,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
     }
     const char* mat = reinterpret_cast<const char*>(a + (size_t)row0 * L.k + k0 * T::kCols + piece * 8);
     int col = k0 * T::kCols + piece * 8;
+    const auto flip = [](int step) { return (uint32_t)(step & 4) << 4; };  // (a row 4 further on has its pieces permuted another way)
     const auto issue = [&](int i) {
         if (i < nk + nn) {
             const uint32_t to = to0 + (uint32_t)(i % T::kStages) * T::kStage;
@@ -172,8 +172,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
             const bool in = col < (i < nk ? L.k : L.n);
 #pragma unroll
             for (int p = 0; p < kMine; ++p) {
-                const bool take = in && there[p];
-                copy16(to + p * kRowStep * T::kChunk, take ? src[p] : reinterpret_cast<const char*>(x), take);
+                if (there[p]) copy16((to ^ flip(p * kRowStep)) + p * kRowStep * T::kChunk, in ? src[p] : reinterpret_cast<const char*>(x), in);
                 src[p] += T::kChunk;
             }
             if (i < nk) {
@@ -182,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
 #pragma unroll
                 for (int p = 0; p < RP / kRowStep; ++p) {
                     const bool take = in && row0 + p * kRowStep < rank;
-                    copy16(to + MT * T::kChunk + p * kRowStep * T::kChunk, take ? from : reinterpret_cast<const char*>(x), take);
+                    copy16((to ^ flip(p * kRowStep)) + (MT + p * kRowStep) * T::kChunk, take ? from : reinterpret_cast<const char*>(x), take);
                     from += step;
                 }
                 mat += T::kChunk;
@@ -198,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
                     for (int p = 0; p < (RP + kBStep - 1) / kBStep; ++p) {
                         const bool take = b_col < L.n && b_row + p * kBStep < rank;
                         if (RP >= kBStep || b_row < RP)
-                            copy16(b_to + p * kBStep * T::kBPitch, take ? from : reinterpret_cast<const char*>(x), take);
+                            copy16((b_to ^ flip(p * kBStep)) + p * kBStep * T::kBPitch, take ? from : reinterpret_cast<const char*>(x), take);
                         from += step;
                     }
                 }
@@ -398,19 +397,25 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, TY>::kCtas) k_adapt(con
     }
 }
 
-template <int MT, int RP, typename TY>
-cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
+template <int MT, int RP, int CHUNK, typename TY>
+cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, cudaStream_t stream) {
+    using T = Tile<MT, RP, CHUNK, TY>;
+    // A large cluster has less of a row's bytes in each CTA, but takes longer to find its place beside others. 300 rows of 20
+    // adapters, k = 1408, n = 512, clusters of 8 and of 4: r = 64, fp32 9.7 and 8.1 us, r = 16, bf16 6.3 and 5.9; k = n = 4096, 32 rows
+    // of 32, r = 16, bf16 5.8 and 7.1; and alone on their SMs, 100 rows of 10, k = 2048, n = 1408, r = 32, bf16 6.2 and 6.8.
+    const long long row_bytes = 2ll * a.k + (a.out != nullptr ? (long long)a.n * (int)sizeof(TY) : 0);
+    int ctas = kMaxCluster;
+    while (ctas > 1 && (tiles * ctas > kResidentCtas + kResidentCtas / 8 || (tiles * ctas > kSms && row_bytes < 900 * ctas))) ctas /= 2;
     // Few tiles: several clusters have one, each with its own h and a part of the columns, of a chunk a CTA at least.
-    const long long chunks = (a.n + Tile<MT, RP, TY>::kOutCols - 1) / Tile<MT, RP, TY>::kOutCols;
-    long long sharing = a.out != nullptr ? kResidentCtas / (tiles * ctas) : 1;
-    if (sharing > chunks / ctas) sharing = chunks / ctas;
+    const long long n_chunks = a.out != nullptr ? (a.n + T::kOutCols - 1) / T::kOutCols : 0;
+    long long sharing = kResidentCtas / (tiles * ctas);
+    if (sharing > n_chunks / ctas) sharing = n_chunks / ctas;
     if (sharing < 1) sharing = 1;
-    const auto kernel = k_adapt<MT, RP, TY>;
-    constexpr int kSmem = Tile<MT, RP, TY>::kSmem;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const auto kernel = k_adapt<MT, RP, CHUNK, TY>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(tiles * ctas), (unsigned)sharing), kThreads, stream);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.dynamicSmemBytes = T::kSmem;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim = {(unsigned)ctas, 1, 1};
@@ -421,12 +426,19 @@ cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, int ctas, cudaSt
     return cudaLaunchKernelEx(&cfg, kernel, a, ctas);
 }
 
-template <int MT, typename TY>
-cudaError_t launch_rank(const AdaptLaunch& a, long long tiles, int ctas, cudaStream_t stream) {
-    if (a.r <= 16) return launch_tiles<MT, 16, TY>(a, tiles, ctas, stream);
-    if (a.r <= 32) return launch_tiles<MT, 32, TY>(a, tiles, ctas, stream);
-    if (a.r <= 64) return launch_tiles<MT, 64, TY>(a, tiles, ctas, stream);
-    return launch_tiles<MT, 128, TY>(a, tiles, ctas, stream);
+template <typename TY>
+cudaError_t launch_few(const AdaptLaunch& a, cudaStream_t stream) {
+    // As wide chunks as two or three stages of them fit, since each costs the warps a round of latencies, but for rows of too
+    // few bytes for it. r = 16, k = n = 4096, chunks of 512 bytes and of 1024: 64 rows of 64 adapters, fp32 11.0 and 9.5 us, 8
+    // of 8 6.8 and 5.8, 4 of 4, bf16 5.6 and 5.8; 1 row, n = 14336, 5.6 and 6.4; k = 1408, n = 512, 300 of 20, fp32 6.6 and 6.8.
+    const long long tiles = most_tiles(a.rows, a.n_adapters, 16);
+    if (a.r <= 16) {
+        const bool wide = tiles >= 8 && 2ll * a.k + (long long)a.n * (int)sizeof(TY) >= 8192;
+        return wide ? launch_tiles<16, 16, 1024, TY>(a, tiles, stream) : launch_tiles<16, 16, 512, TY>(a, tiles, stream);
+    }
+    if (a.r <= 32) return launch_tiles<16, 32, 512, TY>(a, tiles, stream);
+    if (a.r <= 64) return launch_tiles<16, 64, 256, TY>(a, tiles, stream);
+    return launch_tiles<16, 128, 256, TY>(a, tiles, stream);
 }
 
 template <typename TY>
@@ -434,12 +446,9 @@ cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
     // Tiles of 16 rows begin sooner, and read A and B 8 times as often. n = 4096 = k, bf16, microseconds, 16 rows and 128:
     // r = 16, 1024 rows 9.5 and 16.4, 4096 24.4 and 25.0 (fp32 40.6 and 39.0); r = 64, 512 rows 16.5 and 20.7, 1024 22.1 and
     // 23.2, 4096 70.6 and 29.4. Adapters of few rows fill no tile of 128.
-    const bool small = a.list == nullptr || a.rows <= (a.r <= 16 ? 2048 : 1024) || a.rows / a.n_adapters <= 24;
-    if (!small && a.r <= kWideRank) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
-    const long long tiles = most_tiles(a.rows, a.n_adapters, small ? 16 : 64);
-    int ctas = kMaxCluster;
-    while (ctas > 1 && tiles * ctas > kResidentCtas + kResidentCtas / 8) ctas /= 2;
-    return small ? launch_rank<16, TY>(a, tiles, ctas, stream) : launch_tiles<64, 128, TY>(a, tiles, ctas, stream);
+    if (a.list == nullptr || a.rows <= (a.r <= 16 ? 2048 : 1024) || a.rows / a.n_adapters <= 24) return launch_few<TY>(a, stream);
+    if (a.r <= kWideRank) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
+    return launch_tiles<64, 128, 256, TY>(a, most_tiles(a.rows, a.n_adapters, 64), stream);
 }
 
 }  // namespace

@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceLaunch L) {
     if (tid == 0) all.live = 0;
     __syncthreads();
     pdl_wait();
+    pdl_launch_dependents();
     constexpr int kTokens = kThreads / G;  // of a CTA at once
     float sum[kPer] = {};
     int live = 0;
@@ -216,6 +217,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_balance_join(const BalanceLaun
     __shared__ int counts[kParts][E2], live[kWarp];
     const int tid = threadIdx.x, e = tid % E2, part = tid / E2, E = L.n_experts;
     pdl_wait();
+    pdl_launch_dependents();
     float sum = 0.0f;
     int count = 0, tokens = 0;
     if (e < E) {
@@ -251,6 +253,7 @@ template <int G>
 __global__ void __launch_bounds__(kBackThreads) k_route_backward(const RouteBackwardLaunch L) {
     const int sub = threadIdx.x % G;
     pdl_wait();
+    pdl_launch_dependents();
     const long long i = (long long)blockIdx.x * kBackThreads + threadIdx.x;
     const bool in = i / G < L.tokens;
     const int t = in ? (int)(i / G) : 0, first = sub * kPer;

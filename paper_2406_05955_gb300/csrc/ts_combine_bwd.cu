@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const CombineBack
     __shared__ float part[kWarps][K];
     const int t = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_wait();
+    pdl_launch_dependents();
     int slot[K];
     float w[K], dot[K] = {};
     bool mine[K];  // this token writes the row here

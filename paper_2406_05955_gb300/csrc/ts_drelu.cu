@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(kThreads) k_drelu(const DreluLaunch L) {
     __shared__ float scales[2][kBlocks][kRows];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
+    pdl_launch_dependents();
     const int rows = L.n != nullptr ? min(L.rows, *L.n) : L.rows, r = blockIdx.x * kRows + warp;
     if (r < rows) {
         const int at = blockIdx.y * (kBlocks * kScaleBlock) + N * lane;
@@ -148,6 +149,7 @@ __global__ void __launch_bounds__(kThreads) k_drelu_backward(const DreluBackward
     constexpr int N = Vec<T>::N;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
+    pdl_launch_dependents();
     const int rows = L.n != nullptr ? min(L.rows, *L.n) : L.rows, r = blockIdx.x * kRows + warp;
     if (r >= rows) return;
     const int at = blockIdx.y * (N * kWarp * kLoads) + N * lane;

@@ -165,6 +165,7 @@ __global__ void __launch_bounds__(kPlaceThreads) k_route_place(const RouteLaunch
     for (int e = lane; e < E; e += kWarp) count[warp][e] = 0;
     __syncwarp();
     if constexpr (G == 0) pdl_wait();  // for the picks
+    if constexpr (LIST) pdl_launch_dependents();
     for (int i0 = begin; i0 < end; i0 += kAhead * kWarp) {
         int es[kAhead];
         load_picks<LIST>(L, i0 + lane, end, es);

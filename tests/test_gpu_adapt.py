@@ -95,7 +95,8 @@ MANY = [(512, 64, 64, 8, 1), (2060, 64, 64, 8, 1), (2600, 1408, 512, 16, 3), (11
         (1777, 8, 4096, 20, 4), (1300, 512, 8, 40, 7), (3000, 264, 520, 32, 1), (5000, 2048, 1408, 64, 90), (1025, 256, 128, 17, 1)]
 SIZES = [(1, 64, 64, 1, 1), (1, 4096, 1408, 16, 3), (2, 8, 8, 4, 2), (3, 136, 72, 5, 2), (17, 512, 1408, 16, 4),
          (64, 1024, 264, 32, 64), (64, 520, 4096, 64, 3), (33, 256, 136, 128, 5), (65, 512, 512, 8, 2), (130, 1408, 512, 40, 7),
-         (300, 264, 1032, 12, 20), (1000, 512, 1408, 100, 3), (257, 4096, 128, 16, 1), (500, 128, 4104, 33, 255)]
+         (300, 264, 1032, 12, 20), (1000, 512, 1408, 100, 3), (257, 4096, 128, 16, 1), (500, 128, 4104, 33, 255),
+         (9, 4104, 1416, 13, 9), (40, 1048, 2952, 16, 30), (700, 4096, 520, 7, 64)]  # (chunks of 1024 bytes)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
