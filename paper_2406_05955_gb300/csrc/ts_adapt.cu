@@ -403,12 +403,13 @@ cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, cudaStream_t str
     // A large cluster has less of a row's bytes in each CTA, but takes longer to find its place beside others. 300 rows of 20
     // adapters, k = 1408, n = 512, clusters of 8 and of 4: r = 64, fp32 9.7 and 8.1 us, r = 16, bf16 6.3 and 5.9; k = n = 4096, 32 rows
     // of 32, r = 16, bf16 5.8 and 7.1; and alone on their SMs, 100 rows of 10, k = 2048, n = 1408, r = 32, bf16 6.2 and 6.8.
+    constexpr int kResident = kSms * T::kCtas;
     const long long row_bytes = 2ll * a.k + (a.out != nullptr ? (long long)a.n * (int)sizeof(TY) : 0);
     int ctas = kMaxCluster;
-    while (ctas > 1 && (tiles * ctas > kResidentCtas + kResidentCtas / 8 || (tiles * ctas > kSms && row_bytes < 900 * ctas))) ctas /= 2;
+    while (ctas > 1 && (tiles * ctas > kResident + kResident / 8 || (tiles * ctas > kSms && row_bytes < 900 * ctas))) ctas /= 2;
     // Few tiles: several clusters have one, each with its own h and a part of the columns, of a chunk a CTA at least.
     const long long n_chunks = a.out != nullptr ? (a.n + T::kOutCols - 1) / T::kOutCols : 0;
-    long long sharing = kResidentCtas / (tiles * ctas);
+    long long sharing = kResident / (tiles * ctas);
     if (sharing > n_chunks / ctas) sharing = n_chunks / ctas;
     if (sharing < 1) sharing = 1;
     const auto kernel = k_adapt<MT, RP, CHUNK, TY>;
@@ -428,26 +429,32 @@ cudaError_t launch_tiles(const AdaptLaunch& a, long long tiles, cudaStream_t str
 
 template <typename TY>
 cudaError_t launch_few(const AdaptLaunch& a, cudaStream_t stream) {
-    // As wide chunks as two or three stages of them fit, since each costs the warps a round of latencies, but for rows of too
-    // few bytes for it. r = 16, k = n = 4096, chunks of 512 bytes and of 1024: 64 rows of 64 adapters, fp32 11.0 and 9.5 us, 8
-    // of 8 6.8 and 5.8, 4 of 4, bf16 5.6 and 5.8; 1 row, n = 14336, 5.6 and 6.4; k = 1408, n = 512, 300 of 20, fp32 6.6 and 6.8.
+    // The wider chunks the better, as each costs the warps a round of latencies, down to two stages of them and up to what leaves
+    // each CTA one at least. Microseconds, k = n = 4096: r = 16, chunks of 512 bytes and of 1024, 64 rows of 64 adapters, fp32, 11.0
+    // and 9.6, 4 of 4, bf16 5.6 and 5.8 (1 row, n = 14336, 5.6 and 6.4); r = 64, of 256 (two CTAs on an SM), 512 (one) and 1024,
+    // 32 of 32, bf16 14.5, 10.7 and 9.9, 1 row 8.7, 7.7 and 8.1; r = 128, of 256 and 512, 256 rows of 8, fp32 24.6 and 18.5. r = 32 has
+    // its best with two CTAs: 8 of 8, bf16 6.4, and 6.6 with one and chunks of 1024.
     const long long tiles = most_tiles(a.rows, a.n_adapters, 16);
-    if (a.r <= 16) {
-        const bool wide = tiles >= 8 && 2ll * a.k + (long long)a.n * (int)sizeof(TY) >= 8192;
-        return wide ? launch_tiles<16, 16, 1024, TY>(a, tiles, stream) : launch_tiles<16, 16, 512, TY>(a, tiles, stream);
-    }
+    const bool wide = tiles >= 8 && 2ll * a.k + (long long)a.n * (int)sizeof(TY) >= 8192;
+    if (a.r <= 16) return wide ? launch_tiles<16, 16, 1024, TY>(a, tiles, stream) : launch_tiles<16, 16, 512, TY>(a, tiles, stream);
     if (a.r <= 32) return launch_tiles<16, 32, 512, TY>(a, tiles, stream);
-    if (a.r <= 64) return launch_tiles<16, 64, 256, TY>(a, tiles, stream);
-    return launch_tiles<16, 128, 256, TY>(a, tiles, stream);
+    if (a.r <= 64) return wide ? launch_tiles<16, 64, 1024, TY>(a, tiles, stream) : launch_tiles<16, 64, 512, TY>(a, tiles, stream);
+    return launch_tiles<16, 128, 512, TY>(a, tiles, stream);
 }
 
 template <typename TY>
 cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
-    // Tiles of 16 rows begin sooner, and read A and B 8 times as often. n = 4096 = k, bf16, microseconds, 16 rows and 128:
-    // r = 16, 1024 rows 9.5 and 16.4, 4096 24.4 and 25.0 (fp32 40.6 and 39.0); r = 64, 512 rows 16.5 and 20.7, 1024 22.1 and
-    // 23.2, 4096 70.6 and 29.4. Adapters of few rows fill no tile of 128.
-    if (a.list == nullptr || a.rows <= (a.r <= 16 ? 2048 : 1024) || a.rows / a.n_adapters <= 24) return launch_few<TY>(a, stream);
-    if (a.r <= kWideRank) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
+    // Tiles of 16 rows begin sooner, and read A and B 8 times as often. By the time of a tile, in 2 ns: 30 + r of 16 rows, 210 of 128 after
+    // 6000 (r above 64: 340 of 64 after 4000). n = k = 4096, bf16, microseconds with the list's 6, 16 rows and 128, of 4, 30 and 100
+    // adapters: r = 8, 4096 rows 27, 28, 30 and 32, 39, 63; 8192 50, 51, 52 and 47, 65, 74. r = 32, 2048 rows 23, 23, 37 and
+    // 24, 31, 62; 4096 36, 37, 41 and 33, 41, 65; 8192 65, 66, 70 and 48, 67, 76. r = 64, 1024 rows 18, 26, 36 and 26, 33, 63;
+    // 4096 53, 57, 61 and 37, 46, 71; 8192 102, 103, 106 and 52, 73, 85. r = 128 (and 64 rows), 1024 rows 26, 45, 55 and 50, 57, 101;
+    // 4096 84, 88, 96 and 59, 102, 104; 8192 160, 165, 170 and 103, 103, 190. n = 2048, k = 1408, fp32 has the same order.
+    const long long few = most_tiles(a.rows, a.n_adapters, 16) * (30 + a.r);
+    const bool wide = a.r <= kWideRank;
+    const long long many = wide ? 6000 + 210 * most_tiles(a.rows, a.n_adapters, 128) : 4000 + 340 * most_tiles(a.rows, a.n_adapters, 64);
+    if (a.list == nullptr || few <= many) return launch_few<TY>(a, stream);
+    if (wide) return launch_adapt_wide(a, sizeof(TY) == 4, stream);
     return launch_tiles<64, 128, 256, TY>(a, most_tiles(a.rows, a.n_adapters, 64), stream);
 }
 

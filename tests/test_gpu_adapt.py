@@ -90,9 +90,11 @@ def check(ts, x, y, a, b, scale, ids, ranks=None, list_them=False, in_place=Fals
     return out, h
 
 
-# (above 1024 rows, 2048 for r up to 16, and more than 24 an adapter, r up to 64: tiles of 128 rows)
 MANY = [(512, 64, 64, 8, 1), (2060, 64, 64, 8, 1), (2600, 1408, 512, 16, 3), (1100, 136, 1032, 33, 5), (2100, 4096, 200, 64, 2),
-        (1777, 8, 4096, 20, 4), (1300, 512, 8, 40, 7), (3000, 264, 520, 32, 1), (5000, 2048, 1408, 64, 90), (1025, 256, 128, 17, 1)]
+        (1777, 8, 4096, 20, 4), (1300, 512, 8, 40, 7), (3000, 264, 520, 32, 1), (5000, 2048, 1408, 64, 90), (1025, 256, 128, 17, 1),
+        # (so many rows that tiles are of 128, or, r above 64, of 64)
+        (10000, 64, 64, 8, 1), (6000, 1408, 512, 16, 3), (3300, 136, 1032, 33, 5), (5000, 8, 4096, 20, 4), (3500, 512, 8, 40, 7),
+        (5000, 256, 128, 17, 1), (2500, 520, 264, 100, 3)]
 SIZES = [(1, 64, 64, 1, 1), (1, 4096, 1408, 16, 3), (2, 8, 8, 4, 2), (3, 136, 72, 5, 2), (17, 512, 1408, 16, 4),
          (64, 1024, 264, 32, 64), (64, 520, 4096, 64, 3), (33, 256, 136, 128, 5), (65, 512, 512, 8, 2), (130, 1408, 512, 40, 7),
          (300, 264, 1032, 12, 20), (1000, 512, 1408, 100, 3), (257, 4096, 128, 16, 1), (500, 128, 4104, 33, 255),
@@ -107,7 +109,7 @@ def test_forward(ts, t, k, n, r, adapters, dtype):
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[2][0], outs[3][0])
 
 
-@pytest.mark.parametrize("t", [5, 64, 300, 511, 512, 1200])
+@pytest.mark.parametrize("t", [5, 64, 300, 511, 512, 1200, 5000])
 def test_ids(ts, t):
     """No row has an adapter, all have the same, ids out of range, sorted ids, the last adapter alone."""
     x, y, a, b, scale, _ = case(t, 264, 136, 20, 4, seed=t)
@@ -119,7 +121,7 @@ def test_ids(ts, t):
             check(ts, x, y, a, b, scale, ids.to("cuda", torch.int32), list_them=lists)
 
 
-@pytest.mark.parametrize("t", [16, 200, 1300])
+@pytest.mark.parametrize("t", [16, 200, 1300, 4500])
 def test_ranks_scales_and_what_is_not_read(ts, t):
     """Components behind an adapter's rank and adapters without rows are not read; a scale may be absent, 0 or negative."""
     x, y, a, b, scale, ids = case(t, 256, 264, 24, 6, seed=3, none=0.1)
@@ -135,7 +137,7 @@ def test_ranks_scales_and_what_is_not_read(ts, t):
         check(ts, x, y, a, b, None, ids, ranks=ranks, list_them=lists)
 
 
-@pytest.mark.parametrize("t", [20, 150, 2100])
+@pytest.mark.parametrize("t", [20, 150, 2100, 6000])
 def test_infinities_and_nan_stay_in_their_rows(ts, t):
     x, y, a, b, scale, ids = case(t, 512, 136, 16, 3, seed=5)
     for lists in (False, True):
@@ -153,7 +155,7 @@ def test_infinities_and_nan_stay_in_their_rows(ts, t):
         assert torch.equal(got[rest], want[rest])
 
 
-@pytest.mark.parametrize("t", [30, 100, 2055])
+@pytest.mark.parametrize("t", [30, 100, 2055, 13000])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_rows_apart(ts, t, dtype):
     """Rows of x, y and out that lie in wider ones: what is between them is left as it was."""
@@ -344,11 +346,11 @@ def _like(t, stream):
         return torch.empty_like(t)
 
 
-def test_offsets_beyond_32_bits(ts):
+@pytest.mark.parametrize("t,r,ld", [(600, 8, 1 << 22), (1800, 64, 1 << 21)])
+def test_offsets_beyond_32_bits(ts, t, r, ld):
     """Rows whose elements are more than 2^31 apart."""
-    t, k, n = 600, 64, 64
-    ld = 1 << 22
-    x, y, a, b, scale, ids = case(t, k, n, 8, 3, seed=18)
+    k, n = 64, 64
+    x, y, a, b, scale, ids = case(t, k, n, r, 3, seed=18)
     want, h = check(ts, x, y, a, b, scale, ids)
     far = torch.empty(t * ld, dtype=BF16, device="cuda")
     fx, fy = far.view(t, ld)[:, :k], far.view(t, ld)[:, 1024:1024 + n]
@@ -365,7 +367,7 @@ def test_offsets_beyond_32_bits(ts):
 
 def test_a_wait_that_gives_up(ts):
     """The wait runs out, is reported once, and the next call is right."""
-    c = case(2100, 264, 264, 16, 3, seed=21)
+    c = case(6000, 264, 264, 16, 3, seed=21)
     want, _ = check(ts, *c, list_them=True)
     assert ts.adapt_error() == 0
     x, y, a, b, scale, ids = c
@@ -378,7 +380,7 @@ def test_a_wait_that_gives_up(ts):
         ts.adapt_test_stall(False)
     assert ts.adapt_error() == 5 and ts.adapt_error() == 0
     assert torch.equal(ad.forward(x, y, ids, out=torch.empty_like(y)), want)
-    rows, h, dy = ad.rows(ids), torch.randn(2100, 16, device="cuda"), y.clone()
+    rows, h, dy = ad.rows(ids), torch.randn(6000, 16, device="cuda"), y.clone()
     want = ad.backward(dy, None, rows, h, x)
     ts.adapt_test_stall(True)
     try:
