@@ -1,9 +1,9 @@
 // ts_adapt_grads.cu -- gradients of low-rank adapters: grad[i] = sum over the rows t of adapter i of h[t]^T x[t]
 // (ts_adapter_grads).
 //
-// A cluster of CTAs has 128 columns of x. Its CTAs divide the list of rows evenly, whichever adapters' they are: each goes
-// through its part in chunks of up to 64 rows of one adapter and stores the sums of adapters that lie in its part; those that
-// reach into other parts are summed over distributed shared memory at the end, in the order of the CTAs.
+// A cluster of CTAs has 128 columns of x. The rows are taken in chunks of up to 64 of one adapter, and its CTAs divide the
+// chunks evenly, whichever adapters' they are: each stores the sums of adapters that lie in its part; those that reach into
+// other parts are summed over distributed shared memory at the end, in the order of the CTAs.
 //
 // The rows are the products' k, gathered by the list. x is exact in bf16 (e4m3 rows too: the scale that 128 of their columns share
 // is multiplied into h), h is split into three bf16 numbers of 8 bits each, so products and sums are as in fp32. The columns of
@@ -90,11 +90,11 @@ struct Grads {
 // Where chunks of up to 64 entries, each of one adapter, lie in entries `at` .. end - 1 of the list, `id` being the adapter of
 // `at`; `first` adapter's entries begin at offs[id].
 struct Chunks {
-    int id, at, end;
+    int id, at, end, n_adapters;
     // The next chunk's entries; none: 0.
     __device__ __forceinline__ int next(const int* offs, int& first, int& of) {
         if (at >= end) return 0;
-        while (offs[id + 1] <= at) ++id;
+        while (id + 1 < n_adapters && offs[id + 1] <= at) ++id;
         first = at;
         of = id;
         const int n = min(min(kGradRows, offs[id + 1] - at), end - at);
@@ -111,7 +111,8 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     __shared__ uint2 x_at[G::kRing][kGradRows], h_at[G::kRing][kGradRows];  // first byte of a chunk's rows (none: the highest bit)
     __shared__ int rows[E8 ? G::kRing : 1][kGradRows];
     __shared__ int ids[G::kRing];  // a chunk's adapter
-    __shared__ int chunks, first_id;
+    __shared__ int part_at[kMaxCluster + 1], part_id[kMaxCluster + 1];  // a CTA's first entry and its adapter
+    __shared__ int sums[kWarps], split;  // split: an adapter is in several parts
     __shared__ uint64_t done;
     __shared__ uint32_t tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     if (tid == 0) {
         mbar_init(&done, 1);
         mbar_fence_init();
-        chunks = first_id = 0;
+        split = 0;
     }
     if (!L.follows) pdl_wait();
     pdl_launch_dependents();  // one that follows fills the SMs that this one leaves
@@ -140,17 +141,38 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     __syncthreads();
     tc_after();
     const uint32_t d = tmem;
-    const long long live = offs[L.n_adapters];
-    const auto begins = [&](int c) { return (int)(live * c / ctas); };  // part of CTA c
-    const int begin = begins((int)cta), end = begins((int)cta + 1);
+    int nc = 0;
     {
-        const int from = tid < L.n_adapters ? max(offs[tid], begin) : 0, to = tid < L.n_adapters ? min(offs[tid + 1], end) : 0;
-        const int n = __reduce_add_sync(0xffffffffu, to > from ? (to - from + kGradRows - 1) / kGradRows : 0);
-        if (lane == 0) atomicAdd(&chunks, n);
-        if (from < to && offs[tid] <= begin) first_id = tid;
+        const int n = tid < L.n_adapters ? (max(offs[tid + 1] - offs[tid], 0) + kGradRows - 1) / kGradRows : 0;  // chunks
+        int upto = n, total = 0;
+#pragma unroll
+        for (int o = 1; o < kWarp; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == kWarp - 1) sums[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            upto += w < warp ? sums[w] : 0;
+            total += sums[w];
+        }
+        for (int c = 0; c <= ctas; ++c) {
+            const int at = (int)((long long)total * c / ctas), nth = at - (upto - n);
+            if (nth >= 0 && nth < n) {
+                part_at[c] = offs[tid] + nth * kGradRows;
+                part_id[c] = tid;
+                if (nth > 0) split = 1;
+            }
+            if (at == total && tid == 0) {
+                part_at[c] = offs[L.n_adapters];
+                part_id[c] = L.n_adapters - 1;
+            }
+            nc = c == (int)cta ? -at : c == (int)cta + 1 ? nc + at : nc;
+        }
     }
     __syncthreads();
-    const int nc = chunks;
+    const int begin = part_at[cta], end = part_at[cta + 1], first_id = part_id[cta];
     bool failed = false;
 
     // The 16-byte pieces that a thread copies: the same one of every few rows of x, and of h those that it then splits.
@@ -209,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     };
     // The first two warps look up the rows of chunks, two turns before their copies are issued.
     const bool looks = tid < kGradRows;
-    Chunks ahead{first_id, begin, end};
+    Chunks ahead{first_id, begin, end, L.n_adapters};
     const auto look_up = [&](int& of) {
         if (!looks) return -1;
         int first = 0;
@@ -354,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
 
     if (L.follows) pdl_wait();  // (what comes after this kernel comes after the one before it too)
     // Adapters of several parts: each of their CTAs sums some of the elements. A CTA can have two such adapters.
-    if (ctas == 1) return;
+    if (ctas == 1 || !split) return;
     __syncthreads();
     cluster_arrive();
     cluster_wait();
@@ -362,14 +384,14 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     for (int side = 0; side < 2 && begin < end; ++side) {
         const int at = side == 0 ? begin : end - 1;  // an entry of the adapter
         int id = first_id;
-        while (offs[id + 1] <= at) ++id;
+        while (id + 1 < L.n_adapters && offs[id + 1] <= at) ++id;
         const int from = offs[id], to = offs[id + 1];
         if (id == did || (from >= begin && to <= end)) continue;
         did = id;
         int parties = 0, nth = 0;
         unsigned in = 0;
         for (int c = 0; c < ctas; ++c)
-            if (begins(c) < begins(c + 1) && begins(c) < to && begins(c + 1) > from) {
+            if (part_at[c] < part_at[c + 1] && part_at[c] < to && part_at[c + 1] > from) {
                 nth = c == (int)cta ? parties : nth;
                 ++parties;
                 in |= 1u << c;
@@ -381,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
             float4 v[kMaxCluster];
 #pragma unroll
             for (int c = 0; c < kMaxCluster; ++c)
-                v[c] = (in >> c & 1) ? cluster_ld4(smem_u32(from <= begins(c) ? begun : goes_on) + 16 * p, (uint32_t)c)
+                v[c] = (in >> c & 1) ? cluster_ld4(smem_u32(from <= part_at[c] ? begun : goes_on) + 16 * p, (uint32_t)c)
                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             float4 s = v[0];
 #pragma unroll
@@ -405,13 +427,13 @@ cudaError_t launch(const AdapterGradsLaunch& a, cudaStream_t stream) {
     const auto kernel = k_adapter_grads<RP, E8>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem);
     if (e != cudaSuccess) return e;
-    // The cluster whose rounds of CTAs take the least time, a CTA's being that of its rows and, to begin and join, of 256 more.
-    const long long blocks = (a.k + kGradCols - 1) / kGradCols;
+    // The cluster whose rounds of CTAs take the least time: measured, in 0.1 us, 8 a chunk, 28 to begin and 17 + 2 c to join.
+    const long long blocks = (a.k + kGradCols - 1) / kGradCols, chunks = a.rows / kGradRows + (a.rows < a.n_adapters ? a.rows : a.n_adapters);
     int ctas = 1;
     long long best = INT64_MAX;
     for (int c = 1; c <= kMaxCluster; c *= 2) {
         const long long rounds = (blocks * c + G::kCtas * kSms - 1) / (G::kCtas * kSms);
-        const long long time = rounds * (a.rows / c + 256);
+        const long long time = rounds * ((chunks + c - 1) / c * 8 + 28 + (c > 1 ? 17 + 2 * c : 0));
         if (time < best) best = time, ctas = c;
     }
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas)), kThreads, stream);
