@@ -71,6 +71,8 @@ template <int RP, bool E8>
 struct Grads {
     static constexpr int kXBytes = kGradRows * kGradCols * (E8 ? 1 : 2), kHBytes = kGradRows * RP * 4;
     static constexpr int kCtas = RP <= 32 ? 2 : 1;    // on an SM
+    static constexpr int kThreads = 512 / kCtas;
+    static constexpr int kSides = kThreads / kGradCols;  // threads that share a column's components
     static constexpr int kStages = RP <= 64 ? 3 : 2;
     static constexpr int kRing = kStages + 2;         // chunks whose rows are known
     // x starts on 1024 bytes in a stage; h, and for e4m3 rows their scales, lie in rings of their own
@@ -83,7 +85,8 @@ struct Grads {
     static constexpr int kSmem = 1024 + kRows + kSums;
     static constexpr int kColumns = RP == 16 ? 64 : RP == 32 ? 128 : RP == 64 ? 256 : 512;  // of tensor memory
     static constexpr int kN = RP <= 64 ? 3 * RP : 3 * RP / 2;              // of an instruction
-    static constexpr int kMine = RP / 2;                                   // components of a thread's column
+    static constexpr int kMine = RP / kSides;                              // components of a thread's column
+    static_assert(kMine * kSides == RP && kMine % 8 == 0 && kThreads > kMaxAdapters, "");
     static_assert(kRows >= kSums && 3 * RP <= kColumns, "those of one that goes on in another part lie where rows were");
 };
 
@@ -104,8 +107,9 @@ struct Chunks {
 };
 
 template <int RP, bool E8>
-__global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grads(const __grid_constant__ AdapterGradsLaunch L, int ctas) {
+__global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas) k_adapter_grads(const __grid_constant__ AdapterGradsLaunch L, int ctas) {
     using G = Grads<RP, E8>;
+    constexpr int kThreads = G::kThreads, kWarps = kThreads / kWarp;
     extern __shared__ unsigned char raw[];
     __shared__ int offs[kMaxAdapters + 1];
     __shared__ uint2 x_at[G::kRing][kGradRows], h_at[G::kRing][kGradRows];  // first byte of a chunk's rows (none: the highest bit)
@@ -127,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     const uint32_t smem0 = smem_u32(smem), hs0 = smem_u32(hs), scales0 = smem_u32(scales);
     const int col0 = (int)(blockIdx.x / ctas) * kGradCols;
     const bool h_vec = L.r % 4 == 0 && (reinterpret_cast<uintptr_t>(L.h) & 15u) == 0;
-    const int quarter = (warp & 3) * 32, half = warp >> 2;
+    const int quarter = (warp & 3) * 32, side = warp >> 2;
     if (tid == 0) {
         mbar_init(&done, 1);
         mbar_fence_init();
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
 #pragma unroll
         for (int q = 2; q >= 0; --q) {
 #pragma unroll
-            for (int j = 0; j < G::kMine; j += 8) tc_ld8(d + ((uint32_t)quarter << 16) + q * RP + half * G::kMine + j, v + j);
+            for (int j = 0; j < G::kMine; j += 8) tc_ld8(d + ((uint32_t)quarter << 16) + q * RP + side * G::kMine + j, v + j);
             tc_ld_wait(v);
 #pragma unroll
             for (int j = 0; j < G::kMine; ++j) sum[j] += v[j];
@@ -263,15 +267,15 @@ __global__ void __launch_bounds__(kThreads, Grads<RP, E8>::kCtas) k_adapter_grad
     const int col = quarter + lane;
     const auto keep = [&](float* to) {
 #pragma unroll
-        for (int j = 0; j < G::kMine; ++j) to[(half * G::kMine + j) * kGradCols + col] = sum[j];
+        for (int j = 0; j < G::kMine; ++j) to[(side * G::kMine + j) * kGradCols + col] = sum[j];
     };
     const auto finish = [&](int id) {
         if (offs[id] >= begin && offs[id + 1] <= end) {
             if (col0 + col < L.k) {
-                float* const to = L.grad + ((size_t)id * L.r + half * G::kMine) * L.k + col0 + col;
+                float* const to = L.grad + ((size_t)id * L.r + side * G::kMine) * L.k + col0 + col;
 #pragma unroll
                 for (int j = 0; j < G::kMine; ++j)
-                    if (half * G::kMine + j < L.r) to[(size_t)j * L.k] = L.accumulate ? to[(size_t)j * L.k] + sum[j] : sum[j];
+                    if (side * G::kMine + j < L.r) to[(size_t)j * L.k] = L.accumulate ? to[(size_t)j * L.k] + sum[j] : sum[j];
             }
         } else {
             keep(offs[id] <= begin ? begun : goes_on);  // (the last one goes on: no rows come any more)
@@ -436,7 +440,7 @@ cudaError_t launch(const AdapterGradsLaunch& a, cudaStream_t stream) {
         const long long time = rounds * ((chunks + c - 1) / c * 8 + 28 + (c > 1 ? 17 + 2 * c : 0));
         if (time < best) best = time, ctas = c;
     }
-    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas)), kThreads, stream);
+    cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas)), G::kThreads, stream);
     cfg.dynamicSmemBytes = G::kSmem;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeClusterDimension;
