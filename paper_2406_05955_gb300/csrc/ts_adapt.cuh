@@ -1,7 +1,10 @@
-// ts_adapt.cuh -- device helpers of the low-rank adapters' kernels (ts_adapt.cu, ts_adapt_wide.cu).
+// ts_adapt.cuh -- helpers of the low-rank adapters' kernels (ts_adapt.cu, ts_adapt_wide.cu, ts_adapt_grads.cu).
 #pragma once
 
+#include <atomic>
+
 #include "ts_adapt.h"
+#include "ts_grouped.h"
 #include "ts_kernels.cuh"
 
 namespace tsffn {
@@ -183,6 +186,25 @@ __device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, Tile
         const int row = tid < found->count ? L.list[found->first + tid] : -1;
         rows[tid] = (unsigned)row < (unsigned)L.rows ? row : -1;
     }
+}
+
+// Clusters of `ctas` CTAs of a kernel that can be on the device at once: a cluster has to fit into a part of it, so of the
+// larger ones there are fewer than the SMs divided by their size (of 8 CTAs, one on an SM: 15 on 152 SMs). Asked for once.
+template <typename K>
+int resident_clusters(K kernel, int ctas, int threads, int smem, std::atomic<int> (&known)[kMaxCluster + 1]) {
+    int n = known[ctas].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)ctas), threads, nullptr);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim = {(unsigned)ctas, 1, 1};
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) n = kSms / ctas;
+        known[ctas].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }
 
 }  // namespace

@@ -18,6 +18,8 @@
 // slower (64 registers each).
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
 
@@ -429,15 +431,18 @@ template <int RP, bool E8>
 cudaError_t launch(const AdapterGradsLaunch& a, cudaStream_t stream) {
     using G = Grads<RP, E8>;
     const auto kernel = k_adapter_grads<RP, E8>;
+    static std::atomic<int> known[kMaxCluster + 1];
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem);
     if (e != cudaSuccess) return e;
-    // The cluster whose rounds of CTAs take the least time: measured, in 0.1 us, 8 a chunk, 28 to begin and 17 + 2 c to join.
+    // The cluster whose rounds take the least time: measured, in 0.1 us, 8 a chunk (10 beside another CTA on the SM), 28 to begin
+    // and 17 + 3 c to join. Where two have an SM, seven eighths of the places are counted on.
     const long long blocks = (a.k + kGradCols - 1) / kGradCols, chunks = a.rows / kGradRows + (a.rows < a.n_adapters ? a.rows : a.n_adapters);
     int ctas = 1;
     long long best = INT64_MAX;
-    for (int c = 1; c <= kMaxCluster; c *= 2) {
-        const long long rounds = (blocks * c + G::kCtas * kSms - 1) / (G::kCtas * kSms);
-        const long long time = rounds * ((chunks + c - 1) / c * 8 + 28 + (c > 1 ? 17 + 2 * c : 0));
+    for (int c = 1; c <= kMaxCluster; ++c) {
+        const int fit = G::kCtas == 1 ? resident_clusters(kernel, c, G::kThreads, G::kSmem, known) : G::kCtas * kSms * 7 / 8 / c;
+        const long long rounds = (blocks + fit - 1) / fit, chunk = blocks * c > kSms && G::kCtas > 1 ? 10 : 8;
+        const long long time = rounds * ((chunks + c - 1) / c * chunk + 28 + (c > 1 ? 17 + 3 * c : 0));
         if (time < best) best = time, ctas = c;
     }
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas)), G::kThreads, stream);

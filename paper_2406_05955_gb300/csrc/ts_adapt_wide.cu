@@ -15,8 +15,6 @@
 // of half the item, 130-140; a warp of its own for the products 122; a row a thread, bulk copies of 256 bytes both ways, two
 // groups of warps with two items each 112 (a warp's 32 copies take 2000-2600 cycles to issue); of 512 bytes and one item 117;
 // written by 16-byte stores 110; four groups with an item each 96 (4.9 TB/s; 5.6 while y is added to).
-#include <atomic>
-
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
 
@@ -400,30 +398,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
     }
 }
 
-// Clusters of `ctas` CTAs that can be on the device at once: a cluster has to fit into a part of it, so of the larger ones
-// there are fewer than the SMs divided by their size (of 8 CTAs, one on an SM: 15 on 152 SMs). Asked for once.
-template <int RP, typename TY>
-int resident_clusters(int ctas) {
-    static std::atomic<int> known[kMaxCluster + 1];
-    int n = known[ctas].load(std::memory_order_relaxed);
-    if (n == 0) {
-        cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)ctas), kWideThreads, nullptr);
-        cfg.dynamicSmemBytes = Wide<RP, TY>::kSmem;
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim = {(unsigned)ctas, 1, 1};
-        cfg.attrs = &at;
-        cfg.numAttrs = 1;
-        if (cudaOccupancyMaxActiveClusters(&n, k_adapt_wide<RP, TY>, &cfg) != cudaSuccess || n < 1) n = kSms / ctas;
-        known[ctas].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 template <int RP, typename TY>
 cudaError_t launch(const AdaptLaunch& a, cudaStream_t stream) {
     using W = Wide<RP, TY>;
     const auto kernel = k_adapt_wide<RP, TY>;
+    static std::atomic<int> known[kMaxCluster + 1];
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem);
     if (e != cudaSuccess) return e;
     // The cluster, and the clusters that share a tile's columns (each with its own h), whose rounds take the least time for nearly
@@ -435,7 +414,7 @@ cudaError_t launch(const AdaptLaunch& a, cudaStream_t stream) {
     long long sharing = 1;
     double best = 1e30;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const int fit = resident_clusters<RP, TY>(c);
+        const int fit = resident_clusters(kernel, c, kWideThreads, W::kSmem, known);
         const long long most = n_items / c < 1 ? 1 : n_items / c;
         for (long long s = 1; s <= most && s <= 16 && (s == 1 || expect * s <= fit); ++s) {
             const long long rounds = (expect * s + fit - 1) / fit;
