@@ -9,8 +9,8 @@
 // a list, or by the rows' ids here), so they come by 16-byte asynchronous copies.
 //
 // Few rows are bound by the chain launch / ids / first chunk / sums of h / join / last chunk, not by bytes. Calls in a row,
-// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.5 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 9.6
-// (12.5 MB, 1.3 TB/s; in chunks of 256 bytes 14.0); 300 rows of 20, k = 1408, n = 512, r = 40, fp32: 8.1. The matrix
+// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.5 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 9.5
+// (12.5 MB, 1.3 TB/s; in chunks of 256 bytes 14.0); 300 rows of 20, k = 1408, n = 512, r = 40, fp32: 7.4. The matrix
 // instructions of a warp do for it: they take 3% of the time.
 #include "ts_adapt.cuh"
 #include "ts_grouped.h"
