@@ -240,7 +240,8 @@ def test_backward(ts, t, k, n, r, adapters, x8):
     assert torch.equal(da2, da + 2.0) and torch.equal(db2, db - 2.0)
 
 
-@pytest.mark.parametrize("t,r,adapters", [(1, 8, 3), (7, 16, 7), (200, 4, 200), (900, 17, 30), (2500, 64, 5), (1100, 128, 9)])
+@pytest.mark.parametrize("t,r,adapters", [(1, 8, 3), (7, 16, 7), (200, 4, 200), (900, 17, 30), (2500, 64, 5), (1100, 128, 9),
+                                          (832, 8, 2), (1000, 12, 3), (1280, 16, 2), (1500, 64, 2), (7000, 30, 40)])  # (clusters of 5, 6, 7)
 def test_gradients_of_uneven_adapters(ts, t, r, adapters):
     """Nearly all rows have one adapter, each its own, few at the ends: whatever part of the list a CTA has."""
     g = gen(t)
