@@ -31,13 +31,16 @@ def list_rows(ids: torch.Tensor, groups: int, rows=None, offsets=None, stream=No
     return AdapterRows(rows, offsets)
 
 
-def _matrix(t, what: str, dtypes, shape, dev: int) -> torch.Tensor:
-    """``t``, checked: on device ``dev`` (the current one), rows apart, of this shape (a tuple)."""
-    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype not in dtypes or t.get_device() != dev or \
-            not (t.is_contiguous() or _rows_apart(t)):
-        _tensor(t, what, dtypes, 2, rows_apart=True)
-        raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
-    return t
+def _matrix(t, what: str, dtypes, shape, dev: int) -> int:
+    """Elements from a row of ``t`` to the next one; ``t`` checked: on device ``dev`` (the current one), rows apart, of this
+    shape (a tuple)."""
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype in dtypes and t.get_device() == dev:
+        if t.is_contiguous():
+            return shape[1]
+        if _rows_apart(t):
+            return _ld(t)
+    _tensor(t, what, dtypes, 2, rows_apart=True)
+    raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
 
 
 class Adapters:
@@ -91,18 +94,18 @@ class Adapters:
         ``h [rows][r]``, if given, gets ``scale x[t] A^T``, for ``backward``."""
         dev = self._here()
         t = x.shape[0] if isinstance(x, torch.Tensor) and x.dim() == 2 else -1
-        _matrix(x, "x", _ONLY_BF16, (t, self.k), dev)
-        _matrix(y, "y", _ROWS, (t, self.n), dev)
-        if out is not None:
-            _matrix(out, "out", (y.dtype,), (t, self.n), dev)
-        if h is not None:
-            _shaped(h, "h", _F32, (t, self.r), dev)
+        ldx = _matrix(x, "x", _ONLY_BF16, (t, self.k), dev)
+        ldo = ldy = _matrix(y, "y", _ROWS, (t, self.n), dev)
         if out is None:
             out = y
+        else:
+            ldo = _matrix(out, "out", (y.dtype,), (t, self.n), dev)
+        if h is not None:
+            _shaped(h, "h", _F32, (t, self.r), dev)
         ids, rows, offsets, _keep = self._ids(ids, t, False, stream)
-        _check(lib().ts_adapt_rows(x.data_ptr(), _ld(x), t, self.k, self._a, self._b, self._scale, self._ranks, self.adapters,
-                                   self.r, self.n, ids, rows, offsets, y.data_ptr(), _ld(y), _CODES[y.dtype], out.data_ptr(),
-                                   _ld(out), None if h is None else h.data_ptr(), _handle(stream)), "ts_adapt_rows")
+        _check(lib().ts_adapt_rows(x.data_ptr(), ldx, t, self.k, self._a, self._b, self._scale, self._ranks, self.adapters,
+                                   self.r, self.n, ids, rows, offsets, y.data_ptr(), ldy, _CODES[y.dtype], out.data_ptr(),
+                                   ldo, None if h is None else h.data_ptr(), _handle(stream)), "ts_adapt_rows")
         return out
 
     __call__ = forward
@@ -115,13 +118,18 @@ class Adapters:
         them."""
         dev = self._here()
         t = dy.shape[0] if isinstance(dy, torch.Tensor) and dy.dim() == 2 else -1
-        _matrix(dy, "dy", _ONLY_BF16, (t, self.n), dev)
+        ldy = _matrix(dy, "dy", _ONLY_BF16, (t, self.n), dev)
         _shaped(h, "h", _F32, (t, self.r), dev)
-        _matrix(x, "x", (_BF16, _E4M3), (t, self.k), dev)
+        ldx = _matrix(x, "x", (_BF16, _E4M3), (t, self.k), dev)
+        dp = op = None
+        ldd = ldo = 0
+        code = TS_BF16
         if dx is not None:
-            _matrix(dx, "dx", _ROWS, (t, self.k), dev)
+            ldo = ldd = _matrix(dx, "dx", _ROWS, (t, self.k), dev)
+            op = dp = dx.data_ptr()
+            code = _CODES[dx.dtype]
             if out is not None:
-                _matrix(out, "out", (dx.dtype,), (t, self.k), dev)
+                ldo, op = _matrix(out, "out", (dx.dtype,), (t, self.k), dev), out.data_ptr()
         elif out is not None:
             raise ValueError("out needs a dx")
         sp, ld = None, 0
@@ -138,15 +146,9 @@ class Adapters:
         db = _empty(stream, *self.b.shape, dtype=_F32) if db is None else _shaped(db, "db", _F32, self.b.shape, dev)
         _, rows, offsets, _keep = self._ids(ids, t, True, stream)
         dh = _empty(stream, t, self.r, dtype=_F32)
-        dp = op = None
-        ldd = ldo = 0
-        code = TS_BF16
-        if dx is not None:
-            code, dp, ldd = _CODES[dx.dtype], dx.data_ptr(), _ld(dx)
-            op, ldo = (dp, ldd) if out is None else (out.data_ptr(), _ld(out))
         _check(lib().ts_adapters_backward(
-            dy.data_ptr(), _ld(dy), t, self.n, self._a, self._b, self._scale, self._ranks, self.adapters, self.r, self.k, rows,
-            offsets, h.data_ptr(), x.data_ptr(), _ld(x), _CODES[x.dtype], sp, ld, dp, ldd, code, op, ldo, dh.data_ptr(),
+            dy.data_ptr(), ldy, t, self.n, self._a, self._b, self._scale, self._ranks, self.adapters, self.r, self.k, rows,
+            offsets, h.data_ptr(), x.data_ptr(), ldx, _CODES[x.dtype], sp, ld, dp, ldd, code, op, ldo, dh.data_ptr(),
             da.data_ptr(), db.data_ptr(), int(bool(accumulate)), _handle(stream)), "ts_adapters_backward")
         return dx if out is None else out, da, db
 
@@ -180,8 +182,9 @@ def _kept(kept, rows: int, m: int, dev: int):
             _shaped(s_gate, "s_gate", _F32, (mb, rows), dev).data_ptr(), _shaped(s_up, "s_up", _F32, (mb, rows), dev).data_ptr())
 
 
-def _out(t, what: str, rows: int, m: int, dev: int, stream) -> torch.Tensor:
-    return _empty(stream, rows, m, dtype=_BF16) if t is None else _matrix(t, what, _ONLY_BF16, (rows, m), dev)
+def _out(t, what: str, rows: int, m: int, dev: int, stream):
+    """(``t``, or a new tensor in its place, and the elements from a row to the next one)."""
+    return (_empty(stream, rows, m, dtype=_BF16), m) if t is None else (t, _matrix(t, what, _ONLY_BF16, (rows, m), dev))
 
 
 def drelu_rows(g: torch.Tensor, u: torch.Tensor, n=None, c=None, keep: bool = False, kept=None, stream=None):
@@ -190,8 +193,8 @@ def drelu_rows(g: torch.Tensor, u: torch.Tensor, n=None, c=None, keep: bool = Fa
     ``drelu_rows_backward`` needs, in 8 bits."""
     _tensor(g, "g", _ROWS, 2, rows_apart=True)
     (rows, m), dev = g.shape, g.get_device()
-    _matrix(u, "u", (g.dtype,), (rows, m), dev)
-    c = _out(c, "c", rows, m, dev, stream)
+    ldu = _matrix(u, "u", (g.dtype,), (rows, m), dev)
+    c, ldc = _out(c, "c", rows, m, dev, stream)
     p = (None,) * 4
     if kept is not None:
         p = _kept(kept, rows, m, dev)
@@ -200,8 +203,8 @@ def drelu_rows(g: torch.Tensor, u: torch.Tensor, n=None, c=None, keep: bool = Fa
         kept = Kept(*(_empty(stream, rows, m, dtype=_E4M3) for _ in range(2)),
                     *(_empty(stream, mb, rows, dtype=_F32) for _ in range(2)))
         p = tuple(t.data_ptr() for t in kept)
-    _check(lib().ts_drelu_rows(g.data_ptr(), _ld(g), u.data_ptr(), _ld(u), _CODES[g.dtype], _count(n, dev), rows, m,
-                               c.data_ptr(), _ld(c), *p, _handle(stream)), "ts_drelu_rows")
+    _check(lib().ts_drelu_rows(g.data_ptr(), _ld(g), u.data_ptr(), ldu, _CODES[g.dtype], _count(n, dev), rows, m,
+                               c.data_ptr(), ldc, *p, _handle(stream)), "ts_drelu_rows")
     return c if kept is None else (c, kept)
 
 
@@ -211,11 +214,11 @@ def drelu_rows_backward(dc: torch.Tensor, kept: Kept, n=None, dg=None, du=None, 
     _tensor(dc, "dc", _ROWS, 2, rows_apart=True)
     (rows, m), dev = dc.shape, dc.get_device()
     p = _kept(kept, rows, m, dev)
-    dg, du = _out(dg, "dg", rows, m, dev, stream), _out(du, "du", rows, m, dev, stream)
-    c = _out(c, "c", rows, m, dev, stream) if again or c is not None else None
+    (dg, ldg), (du, ldu) = _out(dg, "dg", rows, m, dev, stream), _out(du, "du", rows, m, dev, stream)
+    c, ldc = _out(c, "c", rows, m, dev, stream) if again or c is not None else (None, 0)
     _check(lib().ts_drelu_rows_backward(dc.data_ptr(), _ld(dc), _CODES[dc.dtype], *p, _count(n, dev), rows, m, dg.data_ptr(),
-                                        _ld(dg), du.data_ptr(), _ld(du), None if c is None else c.data_ptr(),
-                                        0 if c is None else _ld(c), _handle(stream)), "ts_drelu_rows_backward")
+                                        ldg, du.data_ptr(), ldu, None if c is None else c.data_ptr(), ldc,
+                                        _handle(stream)), "ts_drelu_rows_backward")
     return dg, du, c
 
 
