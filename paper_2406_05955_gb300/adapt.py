@@ -14,6 +14,11 @@ _BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.flo
 _ROWS, _ONLY_BF16 = (_BF16, _F32), (_BF16,)  # types of rows that are added to, and of those that are multiplied
 
 
+def _like(stream, t: torch.Tensor) -> torch.Tensor:
+    """An output like ``t``, which is contiguous, allocated on the stream of the call."""
+    return torch.empty_like(t) if stream is None else _empty(stream, *t.shape, dtype=t.dtype)
+
+
 class AdapterRows(NamedTuple):
     rows: torch.Tensor     # int32 [rows] rows by adapter, those of none behind
     offsets: torch.Tensor  # int32 [adapters + 2] first entry of each adapter
@@ -23,7 +28,7 @@ def list_rows(ids: torch.Tensor, groups: int, rows=None, offsets=None, stream=No
     """``ts_list_rows``: the rows of each of ``groups`` groups by int32 ``ids [rows]``; an id outside them is of none."""
     _tensor(ids, "ids", (_I32,), 1)
     t, dev, groups = ids.shape[0], ids.get_device(), int(groups)
-    rows = _empty(stream, t, dtype=_I32) if rows is None else _shaped(rows, "rows", _I32, (t,), dev)
+    rows = _like(stream, ids) if rows is None else _shaped(rows, "rows", _I32, (t,), dev)
     offsets = _empty(stream, groups + 2, dtype=_I32) if offsets is None else \
         _shaped(offsets, "offsets", _I32, (groups + 2,), dev)
     _check(lib().ts_list_rows(ids.data_ptr(), t, groups, rows.data_ptr(), offsets.data_ptr(), _handle(stream)),
@@ -145,7 +150,7 @@ class Adapters:
         da = _empty(stream, *self.a.shape, dtype=_F32) if da is None else _shaped(da, "da", _F32, self.a.shape, dev)
         db = _empty(stream, *self.b.shape, dtype=_F32) if db is None else _shaped(db, "db", _F32, self.b.shape, dev)
         _, rows, offsets, _keep = self._ids(ids, t, True, stream)
-        dh = _empty(stream, t, self.r, dtype=_F32)
+        dh = _like(stream, h)
         _check(lib().ts_adapters_backward(
             dy.data_ptr(), ldy, t, self.n, self._a, self._b, self._scale, self._ranks, self.adapters, self.r, self.k, rows,
             offsets, h.data_ptr(), x.data_ptr(), ldx, _CODES[x.dtype], sp, ld, dp, ldd, code, op, ldo, dh.data_ptr(),
@@ -270,7 +275,7 @@ def route_backward(logits: torch.Tensor, sel: torch.Tensor, w: torch.Tensor, dw=
         raise ValueError("dw, or balance and dloss, are needed")
     if dw is not None:
         _shaped(dw, "dw", _F32, (t, k), dev)
-    dlogits = _empty(stream, t, e, dtype=_F32) if dlogits is None else _shaped(dlogits, "dlogits", _F32, (t, e), dev)
+    dlogits = _like(stream, logits) if dlogits is None else _shaped(dlogits, "dlogits", _F32, (t, e), dev)
     _check(lib().ts_route_backward(logits.data_ptr(), t, e, sel.data_ptr(), w.data_ptr(), k,
                                    None if dw is None else dw.data_ptr(), *bp, dlogits.data_ptr(), _handle(stream)),
            "ts_route_backward")
@@ -281,15 +286,15 @@ def combine_rows_backward(dy: torch.Tensor, src: torch.Tensor, slots: torch.Tens
                           dsrc=None, dw=None, stream=None):
     """``ts_combine_rows_backward``: (dsrc, dw) of ``dy [tokens][n]`` for ``combine_rows(src, slots, w)`` with ``slots`` and
     ``rows`` as ``route`` gives them; rows of ``dsrc`` that no token has are left as they were."""
-    _tensor(dy, "dy", (_BF16, _F32), 2)
-    _tensor(src, "src", (_BF16, _F32), 2)
+    _tensor(src, "src", _ROWS, 2)
     _tensor(slots, "slots", (_I32,), 2)
     (t, k), dev, (m, n) = slots.shape, src.get_device(), src.shape
-    _shaped(dy, "dy", dy.dtype, (t, n), dev)
+    if _matrix(dy, "dy", _ROWS, (t, n), dev) != n:
+        _tensor(dy, "dy", _ROWS, 2)
     _shaped(w, "w", _F32, (t, k), dev)
     _shaped(rows, "rows", _I32, (m,), dev)
-    dsrc = _empty(stream, m, n, dtype=src.dtype) if dsrc is None else _shaped(dsrc, "dsrc", src.dtype, (m, n), dev)
-    dw = _empty(stream, t, k, dtype=_F32) if dw is None else _shaped(dw, "dw", _F32, (t, k), dev)
+    dsrc = _like(stream, src) if dsrc is None else _shaped(dsrc, "dsrc", src.dtype, (m, n), dev)
+    dw = _like(stream, w) if dw is None else _shaped(dw, "dw", _F32, (t, k), dev)
     _check(lib().ts_combine_rows_backward(dy.data_ptr(), _CODES[dy.dtype], src.data_ptr(), _CODES[src.dtype], m, n,
                                           slots.data_ptr(), w.data_ptr(), rows.data_ptr(), t, k, dsrc.data_ptr(),
                                           dw.data_ptr(), _handle(stream)), "ts_combine_rows_backward")

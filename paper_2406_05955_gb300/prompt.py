@@ -17,6 +17,7 @@ from .binding import TS_BF16, TS_E4M3, TS_F32, TS_KN, TS_NK, Ffn, Moe, P, _check
 _CODES = {torch.float32: TS_F32, torch.bfloat16: TS_BF16, torch.float8_e4m3fn: TS_E4M3}
 _LAYOUTS = {"nk": TS_NK, "kn": TS_KN}
 BLOCK = 128  # elements of one scale
+_CUDA = torch.device("cuda")
 
 
 _current_device = torch._C._cuda_getDevice
@@ -75,9 +76,9 @@ def _handle(stream) -> int:
 def _empty(stream, *shape, dtype) -> torch.Tensor:
     """An output, allocated on the stream of the call."""
     if stream is None:
-        return torch.empty(*shape, dtype=dtype, device="cuda")
+        return torch.empty(shape, dtype=dtype, device=_CUDA)
     with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
-        return torch.empty(*shape, dtype=dtype, device="cuda")
+        return torch.empty(shape, dtype=dtype, device=_CUDA)
 
 
 class Routing(NamedTuple):
