@@ -3,7 +3,8 @@
 //
 // A cluster of CTAs has 128 columns of x. The rows are taken in chunks of up to 64 of one adapter, and its CTAs divide the
 // chunks evenly, whichever adapters' they are: each stores the sums of adapters that lie in its part; those that reach into
-// other parts are summed over distributed shared memory at the end, in the order of the CTAs.
+// other parts are summed over distributed shared memory at the end, in the order of the CTAs. Adapters of up to 8 rows are
+// no chunk's: warps sum them as they are.
 //
 // The rows are the products' k, gathered by the list. x is exact in bf16 (e4m3 rows too: the scale that 128 of their columns share
 // is multiplied into h), h is split into three bf16 numbers of 8 bits each, so products and sums are as in fp32. The columns of
@@ -30,6 +31,7 @@ namespace {
 __device__ unsigned grads_status;
 
 constexpr int kGradCols = 128, kGradRows = 64;
+constexpr int kFewest = 8, kShare = 8;  // rows of an adapter that warps sum by themselves, and components of a warp
 
 // Four numbers as three bf16 numbers each, cut off (8, 8 and the last 8 bits: nothing is lost). An infinity or NaN is the
 // first alone.
@@ -93,14 +95,19 @@ struct Grads {
     static_assert(kRows >= kSums && 3 * RP <= kColumns, "those of one that goes on in another part lie where rows were");
 };
 
-// Where chunks of up to 64 entries, each of one adapter, lie in entries `at` .. end - 1 of the list, `id` being the adapter of
-// `at`; `first` adapter's entries begin at offs[id].
+// Where chunks of up to 64 entries, each of one adapter of more than kFewest, lie in entries `at` .. end - 1 of the list, `id`
+// being the adapter of `at`; `first` adapter's entries begin at offs[id].
 struct Chunks {
     int id, at, end, n_adapters;
     // The next chunk's entries; none: 0.
     __device__ __forceinline__ int next(const int* offs, int& first, int& of) {
         if (at >= end) return 0;
-        while (id + 1 < n_adapters && offs[id + 1] <= at) ++id;
+        if (id + 1 < n_adapters && offs[id + 1] <= at) {
+            do ++id;
+            while (id + 1 < n_adapters && offs[id + 1] - offs[id] <= kFewest);
+            at = max(at, offs[id]);
+            if (at >= end) return 0;
+        }
         first = at;
         of = id;
         const int n = min(min(kGradRows, offs[id + 1] - at), end - at);
@@ -119,7 +126,7 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
     __shared__ int rows[E8 ? G::kRing : 1][kGradRows];
     __shared__ int ids[G::kRing];  // a chunk's adapter
     __shared__ int part_at[kMaxCluster + 1], part_id[kMaxCluster + 1];  // a CTA's first entry and its adapter
-    __shared__ int sums[kWarps], split;  // split: an adapter is in several parts
+    __shared__ int sums[kWarps], split, few;  // an adapter is in several parts; there are adapters of few rows, or none
     __shared__ uint64_t done;
     __shared__ uint32_t tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -138,7 +145,7 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
     if (tid == 0) {
         mbar_init(&done, 1);
         mbar_fence_init();
-        split = 0;
+        split = few = 0;
     }
     if (!L.follows) pdl_wait();
     pdl_launch_dependents();  // one that follows fills the SMs that this one leaves
@@ -150,7 +157,8 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
     const uint32_t d = tmem;
     int nc = 0;
     {
-        const int n = tid < L.n_adapters ? (max(offs[tid + 1] - offs[tid], 0) + kGradRows - 1) / kGradRows : 0;  // chunks
+        const int count = tid < L.n_adapters ? offs[tid + 1] - offs[tid] : 0, n = count > kFewest ? (count + kGradRows - 1) / kGradRows : 0;
+        if (tid < L.n_adapters && count <= kFewest && (count > 0 || !L.accumulate)) few = 1;
         int upto = n, total = 0;
 #pragma unroll
         for (int o = 1; o < kWarp; o <<= 1) {
@@ -375,11 +383,63 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
         tc_free<G::kColumns>(d);
     }
 
-    if (!L.accumulate)  // adapters without rows
-        for (int id = (int)cta; id < L.n_adapters; id += ctas)
-            if (offs[id] >= offs[id + 1])
-                for (int i = tid; i < L.r * kGradCols; i += kThreads)
-                    if (col0 + i % kGradCols < L.k) L.grad[((size_t)id * L.r + i / kGradCols) * L.k + col0 + i % kGradCols] = 0.0f;
+    // adapters of few rows, or none: a warp takes some components of one
+    const int shares = (L.r + kShare - 1) / kShare;
+    for (int u = few ? (int)cta * kWarps + warp : L.n_adapters * shares; u < L.n_adapters * shares; u += ctas * kWarps) {
+        const int id = u / shares, j0 = (u - id * shares) * kShare, n = offs[id + 1] - offs[id], at = col0 + lane * 4;
+        if (n > kFewest || (n <= 0 && L.accumulate)) continue;
+        const bool in = at < L.k;
+        int row = lane < n ? L.list[offs[id] + lane] : -1;
+        if ((unsigned)row >= (unsigned)L.rows) row = -1;
+        int of[kFewest];
+        float v[kFewest][4];
+#pragma unroll
+        for (int t = 0; t < kFewest; ++t) {
+            of[t] = __shfl_sync(0xffffffffu, row, t);
+            uint2 w = make_uint2(0u, 0u);
+            float scale = 1.0f;
+            if (in && of[t] >= 0) {
+                const char* const from = static_cast<const char*>(L.x) + (of[t] * L.ldx + at) * (E8 ? 1 : 2);
+                if constexpr (E8) {
+                    w.x = *reinterpret_cast<const uint32_t*>(from);
+                    scale = scale_from[of[t]];
+                } else {
+                    w = *reinterpret_cast<const uint2*>(from);
+                }
+            }
+            if constexpr (E8) {
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    const __half2_raw f = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w.x >> 8 * e), __NV_E4M3);
+                    const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&f));
+                    v[t][e] = two.x * scale;
+                    v[t][e + 1] = two.y * scale;
+                }
+            } else {
+                v[t][0] = bf16lo(w.x), v[t][1] = bf16hi(w.x), v[t][2] = bf16lo(w.y), v[t][3] = bf16hi(w.y);
+            }
+        }
+        float h[kFewest];
+#pragma unroll
+        for (int t = 0; t < kFewest; ++t) h[t] = of[t] >= 0 && lane < kShare && j0 + lane < L.r ? L.h[(size_t)of[t] * L.r + j0 + lane] : 0.0f;
+        float* to = L.grad + ((size_t)id * L.r + j0) * L.k + at;
+#pragma unroll 4
+        for (int j = 0; j < min(kShare, L.r - j0); ++j, to += L.k) {
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int t = 0; t < kFewest; ++t) {
+                if (t >= n) break;
+                const float a = __shfl_sync(0xffffffffu, h[t], j);
+                s.x = fmaf(a, v[t][0], s.x), s.y = fmaf(a, v[t][1], s.y), s.z = fmaf(a, v[t][2], s.z), s.w = fmaf(a, v[t][3], s.w);
+            }
+            if (!in) continue;
+            if (L.accumulate) {
+                const float4 had = *reinterpret_cast<const float4*>(to);
+                s.x += had.x, s.y += had.y, s.z += had.z, s.w += had.w;
+            }
+            *reinterpret_cast<float4*>(to) = s;
+        }
+    }
 
     if (L.follows) pdl_wait();  // (what comes after this kernel comes after the one before it too)
     // Adapters of several parts: each of their CTAs sums some of the elements. A CTA can have two such adapters.
@@ -437,13 +497,15 @@ cudaError_t launch(const AdapterGradsLaunch& a, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     // The cluster whose rounds take the least time: measured, in 0.1 us, 8 a chunk (10 beside another CTA on the SM), 28 to begin
     // and 17 + 3 c to join. Where two have an SM, seven eighths of the places are counted on.
-    const long long blocks = (a.k + kGradCols - 1) / kGradCols, chunks = a.rows / kGradRows + (a.rows < a.n_adapters ? a.rows : a.n_adapters);
+    const int some = a.rows / (kFewest + 1);  // adapters that may have chunks
+    const long long blocks = (a.k + kGradCols - 1) / kGradCols, chunks = a.rows / kGradRows + (some < a.n_adapters ? some : a.n_adapters);
+    const int warps = G::kThreads / kWarp, shares = (a.r + kShare - 1) / kShare;
     int ctas = 1;
     long long best = INT64_MAX;
     for (int c = 1; c <= kMaxCluster; ++c) {
         const int fit = G::kCtas == 1 ? resident_clusters(kernel, c, G::kThreads, G::kSmem, known) : G::kCtas * kSms * 7 / 8 / c;
         const long long rounds = (blocks + fit - 1) / fit, chunk = blocks * c > kSms && G::kCtas > 1 ? 10 : 8;
-        const long long time = rounds * ((chunks + c - 1) / c * chunk + 28 + (c > 1 ? 17 + 3 * c : 0));
+        const long long time = rounds * ((chunks + c - 1) / c * chunk + 28 + (c > 1 ? 17 + 3 * c : 0) + (a.n_adapters * shares + warps * c - 1) / (warps * c) * 5);
         if (time < best) best = time, ctas = c;
     }
     cudaLaunchConfig_t cfg = launch_shape(dim3((unsigned)(blocks * ctas)), G::kThreads, stream);

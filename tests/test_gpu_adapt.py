@@ -241,6 +241,7 @@ def test_backward(ts, t, k, n, r, adapters, x8):
 
 
 @pytest.mark.parametrize("t,r,adapters", [(1, 8, 3), (7, 16, 7), (200, 4, 200), (900, 17, 30), (2500, 64, 5), (1100, 128, 9),
+                                          (72, 33, 9), (81, 20, 9),  # (8 and 9 rows of each)
                                           (832, 8, 2), (1000, 12, 3), (1280, 16, 2), (1500, 64, 2), (7000, 30, 40)])  # (clusters of 5, 6, 7)
 def test_gradients_of_uneven_adapters(ts, t, r, adapters):
     """Nearly all rows have one adapter, each its own, few at the ends: whatever part of the list a CTA has."""
