@@ -2,6 +2,7 @@
 backward passes): marshalling only. Tensors, outputs and streams as in ``prompt``."""
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
@@ -238,6 +239,11 @@ class Balance(NamedTuple):
     totals: torch.Tensor  # int32 [2] live tokens, picks
 
 
+@lru_cache(maxsize=1024)
+def _balance_work(tokens: int, experts: int) -> int:
+    return lib().ts_balance_work(tokens, experts)
+
+
 def balance(logits: torch.Tensor, sel: torch.Tensor, loss=None, counts=None, share=None, totals=None, stream=None) -> Balance:
     """``ts_balance``: the loss on uneven routing of fp32 ``logits [tokens][experts]`` whose picks are ``sel``."""
     _tensor(logits, "logits", (_F32,), 2)
@@ -248,11 +254,10 @@ def balance(logits: torch.Tensor, sel: torch.Tensor, loss=None, counts=None, sha
     counts = _empty(stream, e, dtype=_I32) if counts is None else _shaped(counts, "counts", _I32, (e,), dev)
     share = _empty(stream, e, dtype=_F32) if share is None else _shaped(share, "share", _F32, (e,), dev)
     totals = _empty(stream, 2, dtype=_I32) if totals is None else _shaped(totals, "totals", _I32, (2,), dev)
-    L = lib()
-    size = L.ts_balance_work(t, e)
+    size = _balance_work(t, e)
     work = _empty(stream, size, dtype=_F32) if size > 0 else None
-    _check(L.ts_balance(logits.data_ptr(), t, e, sel.data_ptr(), k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
-                        totals.data_ptr(), None if work is None else work.data_ptr(), _handle(stream)), "ts_balance")
+    _check(lib().ts_balance(logits.data_ptr(), t, e, sel.data_ptr(), k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
+                            totals.data_ptr(), None if work is None else work.data_ptr(), _handle(stream)), "ts_balance")
     return Balance(loss, counts, share, totals)
 
 
