@@ -630,8 +630,9 @@ ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, con
 
 /*
  * The gated activation (Eq. 2) of rows whose two products were computed apart: c = max(0, g) max(0, u), 0 unless both are
- * positive (so where either is NaN), for rows r < min(*n, rows); the others are left as they were. What its backward
- * pass needs is kept in TS_E4M3: each factor where both are positive and 0 elsewhere, with a scale for each 128 of a row,
+ * positive (so where either is NaN), for rows r < min(*n, rows); the others, all of them where *n is negative, are left as
+ * they were. What its backward pass needs is kept in TS_E4M3: each factor where both are positive and 0 elsewhere, with a
+ * scale for each 128 of a row,
  *     scale = the smallest power of two, at least 2^-100, with max / scale <= 448 (1 where all are 0)
  *     q     = factor / scale rounded to the nearest, ties to even, but at least 2^-9 where the factor is positive
  * (a factor above 1.875 * 2^127 is kept as that).

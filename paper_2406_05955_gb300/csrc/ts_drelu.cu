@@ -71,6 +71,9 @@ __device__ __forceinline__ void store_e4m3(uint8_t* to, const uint32_t (&q)[N / 
     else __stcs(reinterpret_cast<uint32_t*>(to), q[0]);
 }
 
+// The rows that a call is about: none where the device's count is negative.
+__device__ __forceinline__ int live_rows(const int32_t* n, int rows) { return n != nullptr ? max(0, min(rows, *n)) : rows; }
+
 // A warp takes 8 (bf16) or 4 (fp32) blocks of 128 elements of a row, a CTA the same blocks of 8 rows, so that their scales,
 // which lie together by block, are written 32 bytes at a time.
 template <typename T, bool KEEP>
@@ -80,7 +83,7 @@ __global__ void __launch_bounds__(kThreads) k_drelu(const DreluLaunch L) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();
-    const int rows = L.n != nullptr ? min(L.rows, *L.n) : L.rows, r = blockIdx.x * kRows + warp;
+    const int rows = live_rows(L.n, L.rows), r = blockIdx.x * kRows + warp;
     if (r < rows) {
         const int at = blockIdx.y * (kBlocks * kScaleBlock) + N * lane;
         const T* g = static_cast<const T*>(L.g) + r * L.ldg + at;
@@ -126,9 +129,9 @@ __global__ void __launch_bounds__(kThreads) k_drelu(const DreluLaunch L) {
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * kBlocks * kRows; i += kThreads) {
             const int which = i / (kBlocks * kRows), b = i / kRows % kBlocks, row = i % kRows;
-            const int block = blockIdx.y * kBlocks + b;
-            if (block * kScaleBlock < L.m && blockIdx.x * kRows + row < rows)
-                (which ? L.s_up : L.s_gate)[(size_t)block * L.rows + blockIdx.x * kRows + row] = scales[which][b][row];
+            const int block = blockIdx.y * kBlocks + b, to = blockIdx.x * kRows + row;
+            if (block * kScaleBlock < L.m && to < rows)
+                (which ? L.s_up : L.s_gate)[(size_t)block * L.rows + to] = scales[which][b][row];
         }
     }
 }
@@ -150,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) k_drelu_backward(const DreluBackward
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();
-    const int rows = L.n != nullptr ? min(L.rows, *L.n) : L.rows, r = blockIdx.x * kRows + warp;
+    const int rows = live_rows(L.n, L.rows), r = blockIdx.x * kRows + warp;
     if (r >= rows) return;
     const int at = blockIdx.y * (N * kWarp * kLoads) + N * lane;
     uint4 rd[kLoads];

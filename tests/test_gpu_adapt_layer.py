@@ -104,6 +104,24 @@ def test_drelu(ts, r, m, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+def test_drelu_count_below_zero(ts, dtype):
+    """A negative count is of no rows: nothing is written, neither rows nor scales nor what lies behind these."""
+    for r, m in ((9, 272), (8, 128), (1, 1408)):
+        mb = -(-m // 128)
+        g, u, dc = (1.0 + randn(gen(m + i), r, m).abs().to(dtype) for i in range(3))
+        for count in (-1, -2 ** 31):
+            n = torch.tensor([count], dtype=torch.int32, device="cuda")
+            scales = torch.full((2, mb * r + 16), 5.0, device="cuda")  # 16 elements behind each
+            kept = ts.Kept(*(torch.full((r, m), 2.0, device="cuda").to(E4M3) for _ in range(2)),
+                           *(s[:mb * r].view(mb, r) for s in scales))
+            outs = [torch.full((r, m), 3.0, dtype=BF16, device="cuda") for _ in range(4)]
+            ts.drelu_rows(g, u, n=n, c=outs[0], kept=kept)
+            ts.drelu_rows_backward(dc, kept, n=n, dg=outs[1], du=outs[2], c=outs[3])
+            assert (scales == 5).all() and all((o == 3).all() for o in outs)
+            assert (kept.q_gate.float() == 2).all() and (kept.q_up.float() == 2).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_drelu_values(ts, dtype):
     """Zeros, subnormal and huge numbers, infinities, NaN, values next to a scale's border and to 0 in e4m3, in every pair."""
     v = [0.0, -0.0, 1.0, -1.0, 448.0, 449.0, 450.0, 447.0, 1.75, 1.7578125, 2.0 ** -9, 2.0 ** -10, 2.0 ** -11, 1e-30, 1e-38, 1e-40, 3e38,
