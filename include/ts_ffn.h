@@ -583,6 +583,8 @@ ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* ro
  *   y, ldy     device, rows of n of ydtype (TS_BF16 or TS_F32), ldy apart
  *   out, ldo   the same; may be y itself. NULL (y as well): h alone
  *   h          device [rows][r] fp32, or NULL
+ * out and h share no memory with x, with y (but for an out that is y) and with each other: an adapter around the identity, where y is
+ * x, has an out of its own. They may lie between each other's rows, as columns of one buffer (rows equally far apart).
  * Rows of x, y and out and the matrices start on 16-byte boundaries. Weights are finite. Products are exact, sums are in
  * fp32; h enters the second product in 16 (ydtype TS_BF16) or 24 significant bits; out is rounded once.
  * TS_ERR_UNSUPPORTED: k or n above 2^24, or rows above 2^30.
@@ -607,7 +609,7 @@ void ts_adapt_set_test_stall(int on);
  *              them). NULL for TS_BF16.
  *   list, offsets   as ts_list_rows writes them
  *   grad       device [n_adapters][r][k] fp32, on a 16-byte boundary: overwritten (0 for an adapter without rows), or
- *              added to if accumulate is not 0
+ *              added to if accumulate is not 0; shares no memory with h, x and x_scale
  * Products and sums are in fp32, h in 24 significant bits.
  */
 ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
@@ -620,7 +622,8 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
  *     ts_adapter_grads of dh and x to da, of h and dy to db
  * with the arguments of those: dy rows of n bf16, h what the forward gave, x its rows (TS_BF16, or TS_E4M3 with x_scale), dx and
  * out rows of k of dxdtype (both NULL: not wanted), dh device [rows][r] fp32 (scratch, needed), list and offsets as
- * ts_list_rows writes them (needed).
+ * ts_list_rows writes them (needed). out may be dx itself; out, dh, da and db share no memory with dy, h, x and x_scale
+ * (which are read after out is written: where dx is dy, out is another buffer) and with one another.
  */
 ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, const void* a, const void* b, const float* scale,
                                const int32_t* ranks, int n_adapters, int r, int k, const int32_t* list, const int32_t* offsets,

@@ -97,7 +97,8 @@ class Adapters:
     def forward(self, x: torch.Tensor, y: torch.Tensor, ids, out=None, h=None, stream=None) -> torch.Tensor:
         """``out[t] = y[t] + scale x[t] A^T B`` of the adapter that ``ids`` (int32 ``[rows]``, or what ``rows`` gives) names
         for row ``t``; without ``out`` in ``y`` itself (bf16 or fp32 ``[rows][n]``). x is bf16 ``[rows][k]``. fp32
-        ``h [rows][r]``, if given, gets ``scale x[t] A^T``, for ``backward``."""
+        ``h [rows][r]``, if given, gets ``scale x[t] A^T``, for ``backward``. What is written shares no memory with x: where y
+        is x, ``out`` is needed."""
         dev = self._here()
         t = x.shape[0] if isinstance(x, torch.Tensor) and x.dim() == 2 else -1
         ldx = _matrix(x, "x", _ONLY_BF16, (t, self.k), dev)
@@ -121,7 +122,7 @@ class Adapters:
         """(out, da, db): ``out[t] = dx[t] + dh[t] A`` with ``dh[t] = scale dy[t] B^T`` (without ``out`` in ``dx`` itself;
         no ``dx``: None), and the gradients fp32 ``da [adapters][r][k]``, ``db [adapters][r][n]``, overwritten or added to.
         dy is bf16 ``[rows][n]``, h what ``forward`` gave, x its rows: bf16, or e4m3 with ``x_scale`` as ``quant_rows`` keeps
-        them."""
+        them. What is written shares no memory with dy, h and x: where dx is dy, ``out`` is needed."""
         dev = self._here()
         t = dy.shape[0] if isinstance(dy, torch.Tensor) and dy.dim() == 2 else -1
         ldy = _matrix(dy, "dy", _ONLY_BF16, (t, self.n), dev)

@@ -24,6 +24,31 @@ bool rows_ok(const void* p, int64_t ld, int cols, ts_dtype dt) {
     return p != nullptr && aligned16(p) && ld >= cols && ld * elem_size(dt) % 16 == 0;
 }
 
+// Memory that a call reads or writes: rows of `bytes` bytes, `pitch` apart.
+struct Region {
+    const void* p;
+    int64_t pitch;
+    int rows;
+    int64_t bytes;
+};
+Region rows_of(const void* p, int64_t ld, int rows, int cols, ts_dtype dt) {
+    return {p, ld * elem_size(dt), rows, (int64_t)cols * elem_size(dt)};
+}
+Region whole(const void* p, int64_t bytes) { return {p, bytes, 1, bytes}; }
+
+// Whether they share a byte. Rows that lie between those of the other, as columns of one buffer do, share none; that is looked
+// for where the pitch is the same.
+bool overlap(const Region& a, const Region& b) {
+    if (a.p == nullptr || b.p == nullptr || a.rows <= 0 || b.rows <= 0) return false;
+    const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+    if (d >= (a.rows - 1) * a.pitch + a.bytes || -d >= (b.rows - 1) * b.pitch + b.bytes) return false;
+    if (a.pitch != b.pitch || (a.rows == 1 && b.rows == 1)) return true;
+    // row i + q of b begins d + q pitch behind row i of a: the two q that bring it nearest, from above and from below
+    const int64_t rest = (d % a.pitch + a.pitch) % a.pitch, q = (rest - d) / a.pitch;
+    const auto there = [&](int64_t i) { return i > -a.rows && i < b.rows; };
+    return (rest < a.bytes && there(q)) || (a.pitch - rest < b.bytes && there(q - 1));
+}
+
 // The counts that ts_adapt_rows and ts_adapter_grads share.
 ts_status check_adapters(int rows, int k, int n_adapters, int r) {
     if (rows < 0 || k < 1 || n_adapters < 1 || n_adapters > kMaxAdapters || r < 1 || r > kMaxRank) return TS_ERR_INVALID_ARG;
@@ -70,6 +95,11 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
         return TS_ERR_INVALID_ARG;
     if (!out ? y != nullptr || !h : !rows_ok(y, ldy, n, ydtype) || !rows_ok(out, ldo, n, ydtype) || (out == y && ldo != ldy))
         return TS_ERR_INVALID_ARG;
+    // Other CTAs read x while one writes out, and y in other places than it writes: out is y itself, or apart from both.
+    const Region rx = rows_of(x, ldx, rows, k, TS_BF16), ry = rows_of(y, ldy, rows, n, ydtype), ro = rows_of(out, ldo, rows, n, ydtype),
+                 rh = rows_of(h, r, rows, r, TS_F32);
+    if (overlap(ro, rx) || (out != y && overlap(ro, ry)) || overlap(rh, rx) || overlap(rh, ry) || overlap(rh, ro))
+        return TS_ERR_INVALID_ARG;
     return launched(launch_adapt({x, ldx, rows, k, a, b, scale, ranks, n_adapters, r, n, list ? nullptr : ids, list,
                                   list ? offsets : nullptr, y, ldy, out, ldo, h, test_stall.load()},
                                  ydtype == TS_F32, stream));
@@ -94,6 +124,10 @@ ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts
     if (rows > 0 && (!h || !aligned4(h) || !rows_ok(x, ldx, k, xdtype) || !list || !aligned4(list) ||
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
+    const Region to = whole(grad, 4ll * n_adapters * r * k);
+    if (overlap(to, rows_of(h, r, rows, r, TS_F32)) || overlap(to, rows_of(x, ldx, rows, k, xdtype)) ||
+        overlap(to, rows_of(x_scale, ld_scale, (k + kScaleBlock - 1) / kScaleBlock, rows, TS_F32)))
+        return TS_ERR_INVALID_ARG;
     return launched(launch_adapter_grads(
         {h, r, x, ldx, x_scale, ld_scale, rows, k, n_adapters, list, offsets, grad, accumulate != 0, 0, test_stall.load()}, e8,
         stream));
@@ -115,6 +149,19 @@ ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, con
     if (rows > 0 && (!h || !aligned4(h) || !rows_ok(x, ldx, k, xdtype) ||
                      (e8 ? !x_scale || !aligned4(x_scale) || ld_scale < rows : x_scale != nullptr)))
         return TS_ERR_INVALID_ARG;
+    // dy, x and h are read after out and dh were written, and beside da and db (dx before these)
+    if (rows > 0) {
+        const Region outs[4] = {rows_of(out, ldo, rows, k, dxdtype), rows_of(dh, r, rows, r, TS_F32),
+                                whole(da, 4ll * n_adapters * r * k), whole(db, 4ll * n_adapters * r * n)};
+        const Region ins[4] = {rows_of(dy, ldy, rows, n, TS_BF16), rows_of(h, r, rows, r, TS_F32), rows_of(x, ldx, rows, k, xdtype),
+                               rows_of(x_scale, ld_scale, (k + kScaleBlock - 1) / kScaleBlock, rows, TS_F32)};
+        for (int i = 0; i < 4; ++i) {
+            for (const Region& in : ins)
+                if (overlap(outs[i], in)) return TS_ERR_INVALID_ARG;
+            for (int j = 0; j < i; ++j)
+                if (overlap(outs[i], outs[j])) return TS_ERR_INVALID_ARG;
+        }
+    }
     s = ts_adapt_rows(dy, ldy, rows, n, b, a, scale, ranks, n_adapters, r, k, nullptr, list, offsets, dx, lddx, dxdtype, out, ldo,
                       dh, stream);
     if (s != TS_OK) return s;

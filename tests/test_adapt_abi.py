@@ -81,6 +81,73 @@ def test_adapters_backward(lib):
     assert call(lib.ts_adapters_backward, good, rows=(1 << 30) + 1) == UNSUPPORTED
 
 
+X, Y, O, H, M = (i << 32 for i in range(1, 6))  # far apart
+
+
+def test_adapt_rows_over_its_inputs(lib):
+    """out over x, out beside y, h over any of them; the other refusals again, of arguments that share no memory."""
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32, TS_INT4
+
+    good = {"x": X, "ldx": 64, "rows": 4, "k": 64, "a": M, "b": M, "scale": None, "ranks": None, "adapters": 3, "r": 8, "n": 64,
+            "ids": M, "list": None, "offsets": None, "y": Y, "ldy": 64, "dt": TS_BF16, "out": O, "ldo": 64, "h": H,
+            "stream": None}
+    last = 3 * 128 + 112  # byte of the last 16 of 4 rows of 64 bf16
+    wide = {"ldx": 192, "ldy": 192, "ldo": 192}  # (rows 384 bytes apart, of which 128 are used)
+    for kw in ({"out": X}, {"y": X, "out": X}, {"out": X + last}, {"out": X - last}, {"out": X, "ldo": 128}, {"rows": 1, "out": X + 112},
+               {"out": Y + 128}, {"out": Y - 128}, {"out": Y + 16}, {"out": Y - last}, {"out": Y, "ldo": 128, "ldy": 72},
+               {"h": X}, {"h": X + last + 12}, {"h": X - 124}, {"h": Y}, {"h": O + 4}, {"y": O, "h": O},
+               {"dt": TS_F32, "out": X - 1008}, {"dt": TS_F32, "out": Y + 1008},
+               {**wide, "out": X + 112}, {**wide, "out": X - 112}, {**wide, "out": X + 3 * 384 + 112}, {**wide, "out": X + 384 - 112},
+               {**wide, "out": Y - 384 + 112}, {**wide, "out": Y + 2 * 384}, {**wide, "out": X - 3 * 384 - 112},
+               # not of memory that is shared
+               {"x": None}, {"x": X + 8}, {"ldx": 63}, {"ldx": 68}, {"a": None}, {"a": M + 2}, {"b": None}, {"b": M + 8}, {"scale": M + 2},
+               {"ranks": M + 1}, {"ids": None}, {"ids": M + 2}, {"rows": 513}, {"list": M}, {"list": M + 2, "offsets": M},
+               {"list": M, "offsets": M + 2}, {"y": None}, {"y": Y + 4}, {"ldy": 56}, {"ldy": 68}, {"dt": TS_INT4}, {"dt": TS_E4M3},
+               {"out": O + 8}, {"ldo": 56}, {"y": O, "ldo": 72}, {"out": None}, {"out": None, "y": None, "h": None}, {"h": H + 2},
+               {"r": 129}, {"n": 36}, {"k": 60}, {"dt": TS_F32, "y": Y + 8}):
+        assert call(lib.ts_adapt_rows, good, **kw) == BAD, kw
+
+
+def test_adapter_grads_over_their_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32
+
+    good = {"h": H, "r": 8, "x": X, "ldx": 64, "dt": TS_BF16, "x_scale": None, "ld_scale": 0, "rows": 4, "k": 64,
+            "adapters": 3, "list": M, "offsets": M, "grad": O, "accumulate": 0, "stream": None}
+    e8 = {"dt": TS_E4M3, "x_scale": Y, "ld_scale": 4}
+    size = 3 * 8 * 64 * 4
+    for kw in ({"grad": H}, {"grad": H + 112}, {"grad": H - size + 16}, {"grad": X + 496}, {"grad": X - size + 16},
+               {**e8, "grad": Y}, {**e8, "grad": Y - size + 16}, {**e8, "grad": X + 192},
+               # not of memory that is shared
+               {"h": None}, {"h": H + 1}, {"r": 0}, {"r": 129}, {"x": None}, {"x": X + 8}, {"ldx": 56}, {"ldx": 68}, {"dt": TS_F32},
+               {"x_scale": Y}, {"rows": -1}, {"k": 0}, {"k": 60}, {"adapters": 0}, {"adapters": 256}, {"list": None},
+               {"offsets": None}, {"grad": None}, {"grad": O + 4}, {**e8, "x_scale": None}, {**e8, "ld_scale": 3}, {**e8, "k": 56},
+               {**e8, "ldx": 72}):
+        assert call(lib.ts_adapter_grads, good, **kw) == BAD, kw
+
+
+def test_adapters_backward_over_its_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32, TS_INT4
+
+    D, E, A, B = (i << 32 for i in range(6, 10))
+    good = {"dy": Y, "ldy": 64, "rows": 4, "n": 64, "a": M, "b": M, "scale": None, "ranks": None, "adapters": 3, "r": 8, "k": 64,
+            "list": M, "offsets": M, "h": H, "x": X, "ldx": 64, "dt": TS_BF16, "x_scale": None, "ld_scale": 0, "dx": D,
+            "lddx": 64, "ddt": TS_BF16, "out": O, "ldo": 64, "dh": E, "da": A, "db": B, "accumulate": 0, "stream": None}
+    e8 = {"dt": TS_E4M3, "x_scale": M + (1 << 20), "ld_scale": 4}
+    size = 3 * 8 * 64 * 4
+    for kw in ({"dx": Y, "out": Y}, {"out": Y + 496}, {"out": Y - 496}, {"out": X}, {"dx": X, "out": X}, {"out": H}, {"out": D + 128},
+               {"dh": Y}, {"dh": H}, {"dh": X + 508}, {"dh": D}, {"dh": O + 4}, {"da": Y}, {"da": X - size + 16}, {"da": H + 112},
+               {"da": E}, {"da": O}, {"db": Y + 496}, {"db": X}, {"db": H}, {"db": E}, {"db": O - size + 16}, {"db": A + size - 16},
+               {"da": B}, {"out": A, "dx": A}, {**e8, "da": M + (1 << 20)}, {**e8, "out": M + (1 << 20)}, {**e8, "dh": M + (1 << 20)},
+               {"ddt": TS_F32, "out": X - 1008},
+               # not of memory that is shared
+               {"dy": None}, {"dy": Y + 8}, {"ldy": 56}, {"rows": -1}, {"n": 36}, {"a": None}, {"b": M + 2}, {"scale": M + 2},
+               {"ranks": M + 1}, {"adapters": 256}, {"r": 129}, {"k": 60}, {"list": None}, {"offsets": None}, {"offsets": M + 2},
+               {"h": None}, {"x": None}, {"x": X + 8}, {"ldx": 60}, {"dt": TS_F32}, {"x_scale": M}, {**e8, "x_scale": None},
+               {**e8, "ld_scale": 3}, {"dx": None}, {"lddx": 62}, {"ddt": TS_INT4}, {"out": None}, {"ldo": 8}, {"dh": None},
+               {"dh": E + 2}, {"da": None}, {"da": A + 4}, {"db": None}, {"db": B + 8}):
+        assert call(lib.ts_adapters_backward, good, **kw) == BAD, kw
+
+
 def test_drelu_rows(lib):
     from paper_2406_05955_gb300.binding import (TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD,
                                                 TS_ERR_UNSUPPORTED as UNSUPPORTED, TS_F32, TS_OK)

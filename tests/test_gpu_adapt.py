@@ -394,6 +394,45 @@ def test_a_wait_that_gives_up(ts):
     assert all(torch.equal(p, q) for p, q in zip(ad.backward(dy, None, rows, h, x)[1:], want[1:]))
 
 
+def test_outputs_over_inputs(ts):
+    """An adapter around the identity (y is x, dx is dy): written over what others still read it is refused, and nothing is written;
+    into a buffer of its own it is right. Rows between each other's, as columns of one buffer, are apart."""
+    for t, r in ((1, 16), (4, 16), (300, 8), (2100, 64), (1500, 100)):
+        k = 512
+        x, _, a, b, scale, ids = case(t, k, k, r, 3, seed=t + r, none=0.0)
+        ad, h = ts.Adapters(a, b, scale=scale), torch.empty(t, r, device="cuda")
+        want = ad.forward(x, x.clone(), ids, out=torch.empty_like(x), h=h)
+        before = x.clone()
+        flat, step = torch.zeros((t + 1) * k, dtype=BF16, device="cuda"), k if t > 1 else k // 2
+        near, behind = flat[:t * k].view(t, k), flat[step:step + t * k].view(t, k)  # a row apart (half of one)
+        wide = torch.zeros(t, 3 * k, dtype=BF16, device="cuda")
+        for call in (lambda: ad.forward(x, x, ids), lambda: ad.forward(x, before, ids, out=x), lambda: ad.forward(near, behind, ids),
+                     lambda: ad.forward(x, near, ids, out=behind), lambda: ad.forward(x, behind, ids, out=near),
+                     lambda: ad.forward(wide[:, :k], wide[:, k // 2:k // 2 + k], ids),
+                     lambda: ad.forward(x, before, ids, h=x.view(-1)[:t * r * 2].view(F32).view(t, r))):
+            with pytest.raises(ts.TsError):
+                call()
+        torch.cuda.synchronize()
+        assert torch.equal(x, before) and (flat == 0).all() and (wide == 0).all()
+        assert torch.equal(ad.forward(x, x, ids, out=torch.empty_like(x)), want)
+        wide[:, :k], wide[:, k:2 * k] = x, x
+        got = ad.forward(wide[:, :k], wide[:, k:2 * k], ids, out=wide[:, 2 * k:])
+        assert torch.equal(got, want) and torch.equal(wide[:, :k], x) and torch.equal(wide[:, k:2 * k], x)
+        ad.forward(wide[:, :k], wide[:, k:2 * k], ids)
+        assert torch.equal(wide[:, k:2 * k], want) and torch.equal(wide[:, :k], x)
+        # the backward pass
+        dy = (0.1 * randn(gen(t), t, k)).to(BF16)
+        want = ad.backward(dy, dy.clone(), ids, h, x, out=torch.empty_like(dy))
+        before = dy.clone()
+        for call in (lambda: ad.backward(dy, dy, ids, h, x), lambda: ad.backward(dy, before, ids, h, x, out=x),
+                     lambda: ad.backward(dy, before, ids, h, x, out=dy)):
+            with pytest.raises(ts.TsError):
+                call()
+        torch.cuda.synchronize()
+        assert torch.equal(dy, before)
+        assert all(torch.equal(p, q) for p, q in zip(ad.backward(dy, dy, ids, h, x, out=torch.empty_like(dy)), want))
+
+
 def test_refusals(ts):
     x, y, a, b, scale, ids = case(70, 64, 72, 4, 3)
     ad = ts.Adapters(a, b, scale=scale)
