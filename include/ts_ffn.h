@@ -594,8 +594,10 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
                         const int32_t* offsets, const void* y, int64_t ldy, ts_dtype ydtype, void* out, int64_t ldo, float* h,
                         cudaStream_t stream);
 
-/* What calls of ts_adapt_rows and ts_adapter_grads on the current device have recorded since this was last called (synchronises
-   `stream`): TS_OK, or TS_ERR_TIMEOUT where a bounded wait gave up, after which their outputs are not to be used. */
+/* Whether waits in calls of ts_adapt_rows and ts_adapter_grads on the current device have given up since this was last called
+   (synchronises `stream`): TS_OK, or TS_ERR_TIMEOUT, after which their outputs are not to be used. The answer is about the calls
+   of all streams and threads on the device that are done by then, and is given once: one caller asks for all of them. After
+   TS_ERR_CUDA nothing that was recorded is lost. */
 ts_status ts_adapt_get_error(cudaStream_t stream);
 /* Failure-detection test hook: a bounded wait of the next calls over many rows runs out. */
 void ts_adapt_set_test_stall(int on);

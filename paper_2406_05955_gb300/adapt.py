@@ -161,7 +161,8 @@ class Adapters:
 
 
 def adapt_error(stream=None) -> int:
-    """``ts_adapt_get_error``: the status of adapters' calls on the current device since it was last asked for."""
+    """``ts_adapt_get_error``: the status of adapters' calls on the current device, of all streams and threads, since it was last
+    asked for."""
     return int(lib().ts_adapt_get_error(_handle(stream)))
 
 

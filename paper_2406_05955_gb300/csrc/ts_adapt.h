@@ -124,9 +124,9 @@ cudaError_t launch_list_rows(const int32_t* ids, int n_rows, int n_groups, int32
                              cudaStream_t stream);
 cudaError_t launch_adapt(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
 cudaError_t launch_adapt_wide(const AdaptLaunch& a, bool y_f32, cudaStream_t stream);
-// What the kernels on the current device have recorded since the last call (status bits), read and cleared.
-cudaError_t adapt_wide_status(unsigned* bits, cudaStream_t stream);
-cudaError_t adapter_grads_status(unsigned* bits, cudaStream_t stream);
+// How many waits of the kernels on the current device have given up so far: copied on `stream`.
+cudaError_t adapt_wide_timeouts(unsigned* n, cudaStream_t stream);
+cudaError_t adapter_grads_timeouts(unsigned* n, cudaStream_t stream);
 cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStream_t stream);
 cudaError_t launch_drelu(const DreluLaunch& a, bool f32, cudaStream_t stream);
 cudaError_t launch_drelu_backward(const DreluBackwardLaunch& a, bool f32, cudaStream_t stream);

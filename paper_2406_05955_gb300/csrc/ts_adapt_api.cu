@@ -16,6 +16,17 @@ namespace {
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 std::atomic<int> test_stall{0};  // ts_adapt_set_test_stall
+
+// The device's counts of waits that gave up only grow, and what callers have been told of them is kept here: nothing that one
+// stream's kernel counts while another stream asks can be erased.
+constexpr int kDevices = 64;
+std::atomic<unsigned> told[kDevices][2];
+bool moved_on(std::atomic<unsigned>& to, unsigned now) {
+    unsigned had = to.load();
+    while ((int)(now - had) > 0)  // (another caller may have been told of later ones)
+        if (to.compare_exchange_weak(had, now)) return true;
+    return false;
+}
 ts_status launched(cudaError_t e) { return e == cudaSuccess ? TS_OK : TS_ERR_CUDA; }
 int elem_size(ts_dtype dt) { return dt == TS_F32 ? 4 : dt == TS_BF16 ? 2 : 1; }
 
@@ -106,9 +117,13 @@ ts_status ts_adapt_rows(const void* x, int64_t ldx, int rows, int k, const void*
 }
 
 ts_status ts_adapt_get_error(cudaStream_t stream) {
-    unsigned rows = 0, grads = 0;
-    if (adapt_wide_status(&rows, stream) != cudaSuccess || adapter_grads_status(&grads, stream) != cudaSuccess) return TS_ERR_CUDA;
-    return (rows | grads) & kStatusTimeout ? TS_ERR_TIMEOUT : TS_OK;
+    int dev = 0;
+    unsigned n[2] = {0, 0};
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices || adapt_wide_timeouts(&n[0], stream) != cudaSuccess ||
+        adapter_grads_timeouts(&n[1], stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess)
+        return TS_ERR_CUDA;
+    const bool rows = moved_on(told[dev][0], n[0]), grads = moved_on(told[dev][1], n[1]);
+    return rows || grads ? TS_ERR_TIMEOUT : TS_OK;
 }
 
 void ts_adapt_set_test_stall(int on) { test_stall = on != 0; }

@@ -30,7 +30,7 @@
 namespace tsffn {
 namespace {
 
-__device__ unsigned grads_status;
+__device__ unsigned grads_timeouts;  // waits that gave up, ever
 
 constexpr int kGradCols = 128, kGradRows = 64;
 constexpr int kFewest = 8, kShare = 8;  // rows of an adapter that warps sum by themselves, and components of a warp
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
         finish(id);
         tc_before();
     }
-    if (failed) atomicOr(&grads_status, kStatusTimeout);
+    if (failed) atomicAdd(&grads_timeouts, 1u);
     __syncthreads();
     if (warp == 0) {
         tc_after();
@@ -535,11 +535,8 @@ cudaError_t launch_adapter_grads(const AdapterGradsLaunch& a, bool e4m3, cudaStr
     return e4m3 ? launch_rank<true>(a, stream) : launch_rank<false>(a, stream);
 }
 
-cudaError_t adapter_grads_status(unsigned* bits, cudaStream_t stream) {
-    static const unsigned zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(bits, grads_status, sizeof *bits, 0, cudaMemcpyDeviceToHost, stream);
-    if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(grads_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, stream);
-    return e == cudaSuccess ? cudaStreamSynchronize(stream) : e;
+cudaError_t adapter_grads_timeouts(unsigned* n, cudaStream_t stream) {
+    return cudaMemcpyFromSymbolAsync(n, grads_timeouts, sizeof *n, 0, cudaMemcpyDeviceToHost, stream);
 }
 
 }  // namespace tsffn

@@ -21,7 +21,7 @@
 namespace tsffn {
 namespace {
 
-__device__ unsigned wide_status;
+__device__ unsigned wide_timeouts;  // waits that gave up, ever
 
 constexpr int kTileRows = 128;
 constexpr int kGroup = kTileRows, kGroups = 4, kWorkers = kGroups * kGroup;  // threads that take items of y in turn
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) k_adapt_wide(const __grid_con
     }
     copies_wait_all();
     if (failed) {  // copies may be in flight: give them time to land
-        atomicOr(&wide_status, kStatusTimeout);
+        atomicAdd(&wide_timeouts, 1u);
         const unsigned long long t0 = global_ns();
         while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
@@ -447,11 +447,8 @@ cudaError_t launch_adapt_wide(const AdaptLaunch& a, bool y_f32, cudaStream_t str
     return y_f32 ? launch_rank<float>(a, stream) : launch_rank<__nv_bfloat16>(a, stream);
 }
 
-cudaError_t adapt_wide_status(unsigned* bits, cudaStream_t stream) {
-    static const unsigned zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(bits, wide_status, sizeof *bits, 0, cudaMemcpyDeviceToHost, stream);
-    if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(wide_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, stream);
-    return e == cudaSuccess ? cudaStreamSynchronize(stream) : e;
+cudaError_t adapt_wide_timeouts(unsigned* n, cudaStream_t stream) {
+    return cudaMemcpyFromSymbolAsync(n, wide_timeouts, sizeof *n, 0, cudaMemcpyDeviceToHost, stream);
 }
 
 }  // namespace tsffn

@@ -7,6 +7,7 @@ the r components in up to 3 parts (at most 24 steps), y and the rounding of h to
 the rounding to the type of out (half a step: 2^-8 of it in bf16). A gradient over n rows: n + 16 at most, plus the 2^-23 of h
 in 24 bits."""
 import math
+import threading
 
 import pytest
 import torch
@@ -392,6 +393,39 @@ def test_a_wait_that_gives_up(ts):
         ts.adapt_test_stall(False)
     assert ts.adapt_error() == 5 and ts.adapt_error() == 0
     assert all(torch.equal(p, q) for p, q in zip(ad.backward(dy, None, rows, h, x)[1:], want[1:]))
+
+
+def test_a_wait_that_gives_up_while_others_ask(ts):
+    """Whoever asks, on another stream, while waits give up: someone is told of each call, and then nothing is left."""
+    x, y, a, b, scale, ids = case(6000, 264, 264, 16, 3, seed=22)
+    ad = ts.Adapters(a, b, scale=scale)
+    rows, h, out = ad.rows(ids), randn(gen(23), 6000, 16), torch.empty_like(y)
+    torch.cuda.synchronize()
+    assert ts.adapt_error() == 0
+    told, stop = [], threading.Event()
+
+    def ask(stream):
+        while not stop.is_set():
+            told.append(ts.adapt_error(stream=stream))
+
+    for call in (lambda: ad.forward(x, y, rows, out=out), lambda: ad.backward(y, None, rows, h, x)):
+        told.clear()
+        stop.clear()
+        askers = [threading.Thread(target=ask, args=(torch.cuda.Stream(),)) for _ in range(2)]
+        for t in askers:
+            t.start()
+        ts.adapt_test_stall(True)
+        try:
+            call()
+            torch.cuda.synchronize()
+        finally:
+            ts.adapt_test_stall(False)
+            stop.set()
+            for t in askers:
+                t.join()
+        told.append(ts.adapt_error())
+        assert 5 in told and set(told) <= {0, 5}
+        assert ts.adapt_error() == 0
 
 
 def test_outputs_over_inputs(ts):
