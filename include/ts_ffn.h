@@ -612,7 +612,8 @@ void ts_adapt_set_test_stall(int on);
  *   list, offsets   as ts_list_rows writes them
  *   grad       device [n_adapters][r][k] fp32, on a 16-byte boundary: overwritten (0 for an adapter without rows), or
  *              added to if accumulate is not 0; shares no memory with h, x and x_scale
- * Products and sums are in fp32, h in 24 significant bits.
+ * Products and sums are in fp32, h in 24 significant bits: infinities and NaN of x and h come out as they do in fp32 (but for
+ * an infinity times an h below 2^-133, which is NaN).
  */
 ts_status ts_adapter_grads(const float* h, int r, const void* x, int64_t ldx, ts_dtype xdtype, const float* x_scale,
                            int64_t ld_scale, int rows, int k, int n_adapters, const int32_t* list, const int32_t* offsets,

@@ -266,13 +266,25 @@ __global__ void __launch_bounds__(Grads<RP, E8>::kThreads, Grads<RP, E8>::kCtas)
     };
     const auto after = [](int at, int n) { return at + 1 == n ? 0 : at + 1; };
     float sum[G::kMine] = {};
-    const auto take_over = [&] {  // what the tensor cores have added up
+    // What the tensor cores have added up. An infinity in x makes NaN of a second or third part of h that is 0, where h is not: where
+    // x is not finite (and so the third parts' sum), the first parts' sum counts alone, whose infinities and NaN are the product's.
+    const auto take_over = [&] {
         float v[G::kMine];
+        bool odd = false;
 #pragma unroll
         for (int q = 2; q >= 0; --q) {
 #pragma unroll
             for (int j = 0; j < G::kMine; j += 8) tc_ld8(d + ((uint32_t)quarter << 16) + q * RP + side * G::kMine + j, v + j);
             tc_ld_wait(v);
+            if (q == 2) {
+                float any[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                for (int j = 4; j < G::kMine; ++j) any[j & 3] += v[j];
+                odd = __any_sync(0xffffffffu, !(fabsf((any[0] + any[1]) + (any[2] + any[3])) < INFINITY));
+            }
+            if (q > 0 && odd)
+#pragma unroll
+                for (int j = 0; j < G::kMine; ++j) v[j] = fabsf(v[j]) < INFINITY ? v[j] : 0.0f;
 #pragma unroll
             for (int j = 0; j < G::kMine; ++j) sum[j] += v[j];
         }

@@ -282,6 +282,38 @@ def test_rows_without_an_adapter_do_not_reach_the_gradients(ts):
     assert torch.equal(da3[1][:, keep], da[1][:, keep])
 
 
+@pytest.mark.parametrize("r", [16, 20, 64, 100])
+def test_infinities_in_gradients(ts, r):
+    """An infinity in a row times an h of few bits is that infinity, for adapters of any number of rows; 0 times it is NaN, and so
+    are two of both signs. Everything else is as without it."""
+    g = gen(r)
+    k, n, counts = 136, 264, [8, 9, 64, 65, 700]
+    ids = torch.cat([torch.full((c,), i) for i, c in enumerate(counts)]).to("cuda", torch.int32)
+    t = ids.numel()
+    x, dy = randn(g, t, k).to(BF16), randn(g, t, n).to(BF16)
+    # h of 1, 8, 16 and 24 bits, and 0
+    h = torch.stack([(randn(g, t, r) * 0.25).to(BF16).float() if j == 1 else randn(g, t, r) for j in range(4)])
+    h[0], h[2] = 1.0 + (h[0] > 0), h[2].mul(2.0 ** 12).round().mul(2.0 ** -12)
+    h = h.gather(0, torch.randint(0, 4, (1, t, r), generator=g, device="cuda"))[0]
+    h[5], h[5, 0] = 0.0, -1.0
+    first = 0
+    for c in counts:  # in the first, the last and two other rows of each
+        dy[first, 3], dy[first + c - 1, 7], dy[first + 5, 11] = math.inf, -math.inf, math.inf
+        dy[first + 1, 200], dy[first + 4, 200] = math.inf, -math.inf
+        first += c
+    a, b = torch.zeros(len(counts), r, k, dtype=BF16, device="cuda"), torch.zeros(len(counts), r, n, dtype=BF16, device="cuda")
+    _, _, db = ts.Adapters(a, b).backward(dy, None, ids, h, x)
+    _, _, plain_db = ts.Adapters(a, b).backward(torch.where(dy.isinf(), 0.0, dy), None, ids, h, x)
+    for i, c in enumerate(counts):
+        at = ids == i
+        terms = h[at].double()[:, :, None] * dy[at].double()[:, None, :]
+        want, inf = terms.sum(0), dy[at].isinf().any(0)
+        assert inf.sum() == 4
+        assert torch.equal(db[i][:, inf].double().nan_to_num(nan=7.0), want[:, inf].nan_to_num(nan=7.0)), (i, c)
+        assert torch.equal(db[i][:, ~inf], plain_db[i][:, ~inf])
+        assert ((db[i].double() - want).abs() <= (c + 17) * U * terms.abs().sum(0))[:, ~inf].all()
+
+
 def test_gradients_against_differences(ts):
     """<gradient, direction> against central differences of sum(out * weight) in 64 bits: out is linear in each of x, A
     and B, so the differences are exact but for rounding, and what is left are the kernels' own tolerances."""
