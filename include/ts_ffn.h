@@ -687,7 +687,8 @@ ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32
  * the counts and totals of ts_balance for these logits, or all three NULL):
  *     dlogits[t][e] = sum over the picks j of e of w_j (dw_j - sum_i w_i dw_i)
  *                   + dloss n_experts / (picks * live tokens) p_e (counts[e] - sum_f counts[f] p_f)
- * The counts have no gradient. A token without a pick, and an expert of logit -infinity or NaN, gets 0.
+ * The counts have no gradient. A token that is not live, and an expert of logit -infinity or NaN, gets 0; a live token without
+ * a pick (dropped, where an expert takes a limited number of tokens) has the balance loss's term only.
  *   logits     device [tokens][n_experts] fp32 (with dloss); sel, w device [tokens][top_k] as ts_route gives them, dw
  *              the same (with dw)
  *   dloss      device [1] fp32

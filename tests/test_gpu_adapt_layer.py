@@ -279,6 +279,27 @@ def test_balance_masks_and_special_values(ts):
     assert float(even.loss) == 1.0 and even.counts.tolist() == [2] * 4
 
 
+@pytest.mark.parametrize("t,e,k", [(9, 8, 2), (70, 60, 4)])
+def test_balance_of_dropped_tokens(ts, t, e, k):
+    """Live tokens without a pick have the balance loss's gradient and nothing of the weights'; tokens that are not live have 0."""
+    x = randn(gen(t), t, e)
+    x[1::4], x[2::4, 0], x[3, 1] = -math.inf, -math.inf, math.nan
+    r = ts.route(x, k)
+    sel = r.sel.clone()
+    sel[::2] = -1  # dropped
+    sel[4], sel[6, 0] = e, -7
+    b, dw, dloss = ts.balance(x, sel), randn(gen(e), t, k), torch.tensor([float(t)], device="cuda")
+    both = ts.route_backward(x, sel, r.w, dw=dw, balance=b, dloss=dloss)
+    loss = ts.route_backward(x, sel, r.w, balance=b, dloss=dloss)
+    weights = ts.route_backward(x, sel, r.w, dw=dw)
+    assert torch.equal(both[::2], loss[::2]) and (weights[::2] == 0).all() and (weights[3] != 0).sum() == k
+    assert (both[1::4] == 0).all() and (both[2::4, 0] == 0).all() and both[3, 1] == 0
+    live = torch.nonzero((x > -math.inf).any(1))[:, 0]
+    assert (loss[live] != 0).any(1).all()
+    _, _, _, want, mag = plain_balance(x, sel, r.w, dw, dloss)
+    assert ((both.double().cpu() - want).abs() <= 40 * U * mag).all()
+
+
 def test_balance_gradient_against_differences(ts):
     """Of loss + sum(w * weight), by central differences in 64 bits: the step's own error is of third order."""
     t, e, k = 40, 9, 3
