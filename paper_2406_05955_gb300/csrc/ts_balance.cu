@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kBackThreads) k_route_backward(const RouteBack
         for (int j = 0; j < kPer; ++j) dot = fmaf(count[j], p[j], dot);
         dot = sum_over(dot, G);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) d[j] = f * p[j] * (count[j] - dot);
+        for (int j = 0; j < kPer; ++j) d[j] = p[j] > 0.0f ? f * p[j] * (count[j] - dot) : 0.0f;  // (f may be infinite)
     }
     float mean = 0.0f;
 #pragma unroll

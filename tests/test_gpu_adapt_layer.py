@@ -300,6 +300,17 @@ def test_balance_of_dropped_tokens(ts, t, e, k):
     assert ((both.double().cpu() - want).abs() <= 40 * U * mag).all()
 
 
+@pytest.mark.parametrize("scale", [math.inf, -math.inf, math.nan])
+def test_balance_of_a_loss_that_overflowed(ts, scale):
+    """Tokens that are not live, and experts of logit -infinity or NaN, have 0 whatever the loss's gradient is."""
+    x = randn(gen(5), 40, 12)
+    x[::3], x[1::3, 2:5], x[2::3, 11] = -math.inf, -math.inf, math.nan
+    r = ts.route(x, 3)
+    dloss, off = torch.tensor([scale], device="cuda"), ~(x > -math.inf)
+    got = ts.route_backward(x, r.sel, r.w, balance=ts.balance(x, r.sel), dloss=dloss)
+    assert (got[off] == 0).all() and not torch.isfinite(got[~off]).any()
+
+
 def test_balance_gradient_against_differences(ts):
     """Of loss + sum(w * weight), by central differences in 64 bits: the step's own error is of third order."""
     t, e, k = 40, 9, 3
