@@ -369,17 +369,19 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, CHUNK, TY>::kCtas) k_ad
                     }
                 }
             }
+            if (rank > 0) {  // (without an adapter y goes out as it came)
 #pragma unroll
-            for (int t = 0; t < T::kOT; ++t)
+                for (int t = 0; t < T::kOT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    if constexpr (sizeof(TY) == 2) {
-                        *reinterpret_cast<__nv_bfloat162*>(at(t, e)) = __floats2bfloat162_rn(o[t][e], o[t][e + 1]);
-                    } else {
-                        float2* const p = reinterpret_cast<float2*>(at(t, e));
-                        *p = make_float2(p->x + o[t][e], p->y + o[t][e + 1]);
+                    for (int e = 0; e < 4; e += 2) {
+                        if constexpr (sizeof(TY) == 2) {
+                            *reinterpret_cast<__nv_bfloat162*>(at(t, e)) = __floats2bfloat162_rn(o[t][e], o[t][e + 1]);
+                        } else {
+                            float2* const p = reinterpret_cast<float2*>(at(t, e));
+                            *p = make_float2(p->x + o[t][e], p->y + o[t][e + 1]);
+                        }
                     }
-                }
+            }
             __syncwarp();
             constexpr int kSeg = T::kOT * 8 / kPer;  // 16-byte pieces of a row of this warp
             const int col0 = (n0 + i - nk) * T::kOutCols;

@@ -156,6 +156,23 @@ def test_infinities_and_nan_stay_in_their_rows(ts, t):
         assert torch.equal(got[rest], want[rest])
 
 
+@pytest.mark.parametrize("t", [3, 40, 700, 6000])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_without_an_adapter_keep_their_bits(ts, t, dtype):
+    """Zeros of either sign, subnormal numbers, infinities and NaN of any bits, through another buffer too."""
+    x, y, a, b, scale, ids = case(t, 128, 272, 16, 3, seed=t, dtype=dtype)
+    ids[::3], ids[1::3] = -1, 2
+    ranks = torch.tensor([16, 16, 0], dtype=torch.int32, device="cuda")
+    bits, special = (torch.int16, [0x8000, 1, 0x7f80, 0x7fc5, 0xffaa]) if dtype == BF16 else \
+        (torch.int32, [0x80000000, 1, 0x7f800000, 0x7fc00005, 0xff8000aa])
+    width = 16 if dtype == BF16 else 32
+    y.view(bits)[:, 7:12] = torch.tensor([v - (1 << width) if v >> (width - 1) else v for v in special], device="cuda").to(bits)
+    ad, none = ts.Adapters(a, b, scale=scale, ranks=ranks), (ids < 0) | (ids == 2)
+    for given in (ids, ad.rows(ids)):
+        out = ad.forward(x, y, given, out=torch.empty_like(y))
+        assert torch.equal(out.view(bits)[none], y.view(bits)[none])
+
+
 @pytest.mark.parametrize("t", [30, 100, 2055, 13000])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_rows_apart(ts, t, dtype):
