@@ -564,6 +564,7 @@ ts_status ts_prompt_check_scratch(ts_prompt* p, cudaStream_t stream);
  *   n_groups  1..255
  *   rows      device [n_rows] int32
  *   offsets   device [n_groups + 2] int32; offsets[n_groups + 1] = n_rows
+ * The three share no memory.
  */
 ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* rows, int32_t* offsets, cudaStream_t stream);
 

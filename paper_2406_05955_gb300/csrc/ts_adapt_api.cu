@@ -50,7 +50,7 @@ Region whole(const void* p, int64_t bytes) { return {p, bytes, 1, bytes}; }
 // Whether they share a byte. Rows that lie between those of the other, as columns of one buffer do, share none; that is looked
 // for where the pitch is the same.
 bool overlap(const Region& a, const Region& b) {
-    if (a.p == nullptr || b.p == nullptr || a.rows <= 0 || b.rows <= 0) return false;
+    if (a.p == nullptr || b.p == nullptr || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
     const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
     if (d >= (a.rows - 1) * a.pitch + a.bytes || -d >= (b.rows - 1) * b.pitch + b.bytes) return false;
     if (a.pitch != b.pitch || (a.rows == 1 && b.rows == 1)) return true;
@@ -87,6 +87,9 @@ ts_status ts_list_rows(const int32_t* ids, int n_rows, int n_groups, int32_t* ro
     if (n_rows < 0 || n_rows >= 1 << 30 || n_groups < 1 || n_groups > kMaxAdapters || !aligned4(ids) || !aligned4(rows) ||
         !offsets || !aligned4(offsets) || (n_rows > 0 && (!ids || !rows)))
         return TS_ERR_INVALID_ARG;
+    // ids are read again while rows and offsets are written
+    const Region rid = whole(ids, 4ll * n_rows), rr = whole(rows, 4ll * n_rows), ro = whole(offsets, 4ll * (n_groups + 2));
+    if (overlap(rr, rid) || overlap(ro, rid) || overlap(rr, ro)) return TS_ERR_INVALID_ARG;
     return launched(launch_list_rows(ids, n_rows, n_groups, rows, offsets, stream));
 }
 

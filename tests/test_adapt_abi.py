@@ -84,6 +84,18 @@ def test_adapters_backward(lib):
 X, Y, O, H, M = (i << 32 for i in range(1, 6))  # far apart
 
 
+def test_list_rows_over_its_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD
+
+    good = {"ids": X, "n": 100, "groups": 8, "rows": Y, "offsets": O, "stream": None}
+    for kw in ({"rows": X}, {"rows": X + 396}, {"rows": X - 396}, {"offsets": X + 396}, {"offsets": X - 36}, {"offsets": Y + 4},
+               {"rows": O + 36}, {"n": 1, "rows": X},
+               # not of memory that is shared
+               {"ids": None}, {"ids": X + 2}, {"n": -1}, {"n": 1 << 30}, {"groups": 0}, {"groups": 256}, {"rows": None},
+               {"rows": Y + 1}, {"offsets": None}, {"offsets": O + 2}):
+        assert call(lib.ts_list_rows, good, **kw) == BAD, kw
+
+
 def test_adapt_rows_over_its_inputs(lib):
     """out over x, out beside y, h over any of them; the other refusals again, of arguments that share no memory."""
     from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32, TS_INT4
