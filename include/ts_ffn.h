@@ -705,7 +705,7 @@ ts_status ts_route_backward(const float* logits, int tokens, int n_experts, cons
  *     dw[t][j] = sum over i of dy[t][i] src[slots[t][j]][i]              0 for a slot outside 0..n_rows-1
  * Other rows of dsrc are left as they were.
  *   dy         device [tokens][n] of dydtype (TS_F32 or TS_BF16)
- *   src, dsrc  device [n_rows][n] of dtype (TS_F32 or TS_BF16), two buffers
+ *   src, dsrc  device [n_rows][n] of dtype (TS_F32 or TS_BF16); dsrc shares no memory with src and dy
  *   rows       device [n_rows] int32: token of each row
  *   slots, w, dw   device [tokens][top_k], top_k 1..8; n 1..2^30, at most 2^30 tokens
  */

@@ -262,9 +262,12 @@ ts_status ts_combine_rows_backward(const void* dy, ts_dtype dydtype, const void*
     if (tokens == 0) return TS_OK;
     const unsigned size = (unsigned)elem_size(dtype);
     if (!dy || (uintptr_t)dy % (unsigned)elem_size(dydtype) != 0 || (uintptr_t)src % size != 0 || (uintptr_t)dsrc % size != 0 ||
-        (n_rows > 0 && (!src || !rows || !dsrc || src == dsrc)) || !aligned4(rows) || !slots || !aligned4(slots) || !w ||
+        (n_rows > 0 && (!src || !rows || !dsrc)) || !aligned4(rows) || !slots || !aligned4(slots) || !w ||
         !aligned4(w) || !dw || !aligned4(dw))
         return TS_ERR_INVALID_ARG;
+    // a token's CTA writes rows of dsrc while others read dy and rows of src
+    const Region to = rows_of(dsrc, n, n_rows, n, dtype);
+    if (overlap(to, rows_of(src, n, n_rows, n, dtype)) || overlap(to, rows_of(dy, n, tokens, n, dydtype))) return TS_ERR_INVALID_ARG;
     return launched(launch_combine_backward({dy, src, n_rows, n, slots, w, rows, tokens, top_k, dsrc, dw}, dydtype == TS_F32,
                                             dtype == TS_F32, stream));
 }

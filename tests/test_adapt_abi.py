@@ -217,6 +217,21 @@ def test_combine_rows_backward(lib):
     assert call(lib.ts_combine_rows_backward, good, tokens=0, dy=None, dw=None) == TS_OK
 
 
+def test_combine_rows_backward_over_its_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32
+
+    good = {"dy": Y, "ddt": TS_F32, "src": X, "dt": TS_BF16, "n_rows": 8, "n": 64, "slots": M, "w": M, "rows": M, "tokens": 4,
+            "top_k": 2, "dsrc": O, "dw": H, "stream": None}
+    size = 8 * 64 * 2
+    for kw in ({"dsrc": X}, {"dsrc": X + size - 2}, {"dsrc": X - size + 2}, {"dsrc": X + 128}, {"dsrc": Y}, {"dsrc": Y + 1022},
+               {"dsrc": Y - size + 2}, {"dt": TS_F32, "dsrc": Y}, {"ddt": TS_BF16, "dsrc": Y + 256},
+               # not of memory that is shared
+               {"dy": None}, {"dy": Y + 2}, {"ddt": TS_E4M3}, {"src": None}, {"src": X + 1}, {"dt": TS_E4M3}, {"n_rows": -1}, {"n": 0},
+               {"slots": None}, {"w": None}, {"rows": None}, {"tokens": -1}, {"top_k": 0}, {"top_k": 9}, {"dsrc": None}, {"dw": None},
+               {"dw": H + 2}):
+        assert call(lib.ts_combine_rows_backward, good, **kw) == BAD, kw
+
+
 def test_tensors_that_are_not_on_the_gpu_are_refused():
     import torch
 
