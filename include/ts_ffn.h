@@ -647,7 +647,8 @@ ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, con
  *   n          device int32 (as &offsets[n_experts] of ts_route), NULL: rows
  *   c, ldc     device, rows of m bf16, ldc apart
  *   q_gate, q_up   device [rows][m] e4m3, s_gate, s_up device [ceil(m / 128)][rows] fp32; or NULL, all four
- * All rows start on 16-byte boundaries. TS_ERR_UNSUPPORTED: m above 2^24 or rows above 2^30.
+ * All rows start on 16-byte boundaries. c may be a bf16 g or u itself (its rows as far apart); otherwise what is written shares no
+ * memory with what is read. TS_ERR_UNSUPPORTED: m above 2^24 or rows above 2^30.
  */
 ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, ts_dtype dtype, const int32_t* n, int rows,
                         int m, void* c, int64_t ldc, void* q_gate, void* q_up, float* s_gate, float* s_up,
@@ -661,6 +662,7 @@ ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, 
  *   dc, ldd    device, rows of m of dtype (TS_BF16 or TS_F32), ldd apart
  *   dg, du     device, rows of m bf16, ldg and ldu apart
  *   c, ldc     the same, for the gradient of the down product's weights; or NULL
+ * One of them may be a bf16 dc itself; otherwise they share no memory with what is read and with one another.
  */
 ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, const void* q_gate, const void* q_up,
                                  const float* s_gate, const float* s_up, const int32_t* n, int rows, int m, void* dg,

@@ -60,6 +60,20 @@ bool overlap(const Region& a, const Region& b) {
     return (rest < a.bytes && there(q)) || (a.pitch - rest < b.bytes && there(q - 1));
 }
 
+bool same_rows(const Region& a, const Region& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1) && a.bytes == b.bytes; }
+
+// Whether any of `outs` shares memory with another of them or with any of `ins`.
+template <size_t N, size_t M>
+bool overlap(const Region (&outs)[N], const Region (&ins)[M]) {
+    for (size_t i = 0; i < N; ++i) {
+        for (const Region& in : ins)
+            if (overlap(outs[i], in)) return true;
+        for (size_t j = 0; j < i; ++j)
+            if (overlap(outs[i], outs[j])) return true;
+    }
+    return false;
+}
+
 // The counts that ts_adapt_rows and ts_adapter_grads share.
 ts_status check_adapters(int rows, int k, int n_adapters, int r) {
     if (rows < 0 || k < 1 || n_adapters < 1 || n_adapters > kMaxAdapters || r < 1 || r > kMaxRank) return TS_ERR_INVALID_ARG;
@@ -173,12 +187,7 @@ ts_status ts_adapters_backward(const void* dy, int64_t ldy, int rows, int n, con
                                 whole(da, 4ll * n_adapters * r * k), whole(db, 4ll * n_adapters * r * n)};
         const Region ins[4] = {rows_of(dy, ldy, rows, n, TS_BF16), rows_of(h, r, rows, r, TS_F32), rows_of(x, ldx, rows, k, xdtype),
                                rows_of(x_scale, ld_scale, (k + kScaleBlock - 1) / kScaleBlock, rows, TS_F32)};
-        for (int i = 0; i < 4; ++i) {
-            for (const Region& in : ins)
-                if (overlap(outs[i], in)) return TS_ERR_INVALID_ARG;
-            for (int j = 0; j < i; ++j)
-                if (overlap(outs[i], outs[j])) return TS_ERR_INVALID_ARG;
-        }
+        if (overlap(outs, ins)) return TS_ERR_INVALID_ARG;
     }
     s = ts_adapt_rows(dy, ldy, rows, n, b, a, scale, ranks, n_adapters, r, k, nullptr, list, offsets, dx, lddx, dxdtype, out, ldo,
                       dh, stream);
@@ -202,6 +211,14 @@ ts_status ts_drelu_rows(const void* g, int64_t ldg, const void* u, int64_t ldu, 
     if (kept != (q_up != nullptr) || kept != (s_gate != nullptr) || kept != (s_up != nullptr) || !aligned16(q_gate) ||
         !aligned16(q_up) || !aligned4(s_gate) || !aligned4(s_up))
         return TS_ERR_INVALID_ARG;
+    // c may lie over a bf16 g or u, element for element: a thread reads what it then writes
+    const Region rg = rows_of(g, ldg, rows, m, dtype), ru = rows_of(u, ldu, rows, m, dtype), rc = rows_of(c, ldc, rows, m, TS_BF16);
+    const int blocks = (m + kScaleBlock - 1) / kScaleBlock;
+    const Region kept_to[4] = {whole(q_gate, (int64_t)rows * m), whole(q_up, (int64_t)rows * m), whole(s_gate, 4ll * rows * blocks),
+                               whole(s_up, 4ll * rows * blocks)},
+                 others[3] = {rg, ru, rc};
+    if ((!same_rows(rc, rg) && overlap(rc, rg)) || (!same_rows(rc, ru) && overlap(rc, ru)) || overlap(kept_to, others))
+        return TS_ERR_INVALID_ARG;
     return launched(launch_drelu({g, u, ldg, ldu, n, rows, m, c, ldc, static_cast<uint8_t*>(q_gate),
                                   static_cast<uint8_t*>(q_up), s_gate, s_up},
                                  dtype == TS_F32, stream));
@@ -216,6 +233,15 @@ ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, co
         (c && !rows_ok(c, ldc, m, TS_BF16)) || !q_gate || !aligned16(q_gate) || !q_up || !aligned16(q_up) || !s_gate ||
         !aligned4(s_gate) || !s_up || !aligned4(s_up))
         return TS_ERR_INVALID_ARG;
+    // dg, du or c may lie over a bf16 dc, element for element
+    const int blocks = (m + kScaleBlock - 1) / kScaleBlock;
+    const Region rd = rows_of(dc, ldd, rows, m, dtype);
+    const Region outs[3] = {rows_of(dg, ldg, rows, m, TS_BF16), rows_of(du, ldu, rows, m, TS_BF16), rows_of(c, ldc, rows, m, TS_BF16)},
+                 ins[4] = {whole(q_gate, (int64_t)rows * m), whole(q_up, (int64_t)rows * m), whole(s_gate, 4ll * rows * blocks),
+                           whole(s_up, 4ll * rows * blocks)};
+    if (overlap(outs, ins)) return TS_ERR_INVALID_ARG;
+    for (const Region& out : outs)
+        if (!same_rows(out, rd) && overlap(out, rd)) return TS_ERR_INVALID_ARG;
     return launched(launch_drelu_backward({dc, ldd, static_cast<const uint8_t*>(q_gate), static_cast<const uint8_t*>(q_up),
                                            s_gate, s_up, n, rows, m, dg, du, c, ldg, ldu, ldc},
                                           dtype == TS_F32, stream));

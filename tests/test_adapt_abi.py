@@ -217,6 +217,30 @@ def test_combine_rows_backward(lib):
     assert call(lib.ts_combine_rows_backward, good, tokens=0, dy=None, dw=None) == TS_OK
 
 
+def test_drelu_rows_over_their_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32
+
+    QG, QU, SG, SU = (i << 32 for i in range(10, 14))
+    good = {"g": X, "ldg": 256, "u": Y, "ldu": 256, "dt": TS_BF16, "n": None, "rows": 4, "m": 256, "c": O, "ldc": 256, "qg": QG,
+            "qu": QU, "sg": SG, "su": SU, "stream": None}
+    for kw in ({"c": X + 16}, {"c": X - 16}, {"c": X, "ldc": 512}, {"dt": TS_F32, "c": X}, {"dt": TS_F32, "c": X, "ldc": 512}, {"c": Y + 512},
+               {"c": QG}, {"c": SU - 16}, {"qg": X}, {"qu": Y + 2032}, {"qg": QU + 1008}, {"sg": QG + 1020}, {"su": SG + 28}, {"sg": O},
+               # not of memory that is shared
+               {"g": None}, {"g": X + 8}, {"ldg": 255}, {"ldg": 260}, {"u": None}, {"u": Y + 2}, {"ldu": 240}, {"dt": TS_E4M3},
+               {"n": M + 2}, {"rows": -1}, {"m": 0}, {"m": 72}, {"c": None}, {"c": O + 4}, {"ldc": 252}, {"qg": None}, {"qu": None},
+               {"sg": None}, {"su": None}, {"qg": QG + 8}, {"su": SU + 2}, {"dt": TS_F32, "g": X + 4}):
+        assert call(lib.ts_drelu_rows, good, **kw) == BAD, kw
+
+    good = {"dc": X, "ldd": 256, "dt": TS_BF16, "qg": QG, "qu": QU, "sg": SG, "su": SU, "n": None, "rows": 4, "m": 256, "dg": Y,
+            "ldg": 256, "du": O, "ldu": 256, "c": H, "ldc": 256, "stream": None}
+    for kw in ({"dg": O}, {"du": H + 2032}, {"c": Y - 2032}, {"dg": X, "du": X}, {"dg": X + 16}, {"du": X, "ldu": 264}, {"dt": TS_F32, "c": X},
+               {"dg": QG}, {"du": QU + 1008}, {"c": SG}, {"dg": SU - 2032},
+               # not of memory that is shared
+               {"dc": None}, {"dc": X + 8}, {"ldd": 252}, {"dt": TS_E4M3}, {"qg": None}, {"qu": QU + 8}, {"sg": None}, {"su": SU + 1},
+               {"n": M + 2}, {"rows": -1}, {"m": 8}, {"dg": None}, {"ldg": 252}, {"du": O + 4}, {"ldu": 255}, {"c": H + 8}, {"ldc": 248}):
+        assert call(lib.ts_drelu_rows_backward, good, **kw) == BAD, kw
+
+
 def test_combine_rows_backward_over_its_inputs(lib):
     from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32
 

@@ -159,6 +159,32 @@ def test_drelu_columns_of_wider_rows(ts):
     assert torch.equal(d[:, :m], dg) and torch.equal(d[:, m:2 * m], du) and (d[:, 2 * m:] == 7).all()
 
 
+def test_drelu_in_place(ts):
+    """c over g or u, and one of dg, du and c over dc, of one type: as apart. Half over it is refused, and nothing is written."""
+    g = gen(8)
+    for r, m, wide in ((1, 2064, 0), (37, 1408, 0), (20, 272, 32)):
+        gate, up, dc = (randn(g, r, m + wide).to(BF16)[:, wide // 2:wide // 2 + m] for _ in range(3))
+        c, kept = ts.drelu_rows(gate, up, keep=True)
+        want = ts.drelu_rows_backward(dc, kept)
+        for which in range(2):
+            args = [gate.clone(), up.clone()]
+            got, k = ts.drelu_rows(*args, c=args[which], keep=True)
+            assert got is args[which] and torch.equal(got, c) and torch.equal(args[1 - which], (up, gate)[which])
+            assert all(torch.equal(p.float(), q.float()) for p, q in zip(k, kept))
+        for which in ("dg", "du", "c"):
+            d = torch.empty(r, m + wide, dtype=BF16, device="cuda")[:, wide // 2:wide // 2 + m].copy_(dc)
+            got = ts.drelu_rows_backward(d, kept, **{which: d})
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
+        flat = torch.ones((r + 1) * m, dtype=BF16, device="cuda")
+        near, behind = flat[:r * m].view(r, m), flat[m // 2:m // 2 + r * m].view(r, m)
+        for call in (lambda: ts.drelu_rows(near, up, c=behind), lambda: ts.drelu_rows(gate, near, c=behind),
+                     lambda: ts.drelu_rows_backward(near, kept, du=behind), lambda: ts.drelu_rows_backward(dc, kept, dg=near, du=behind)):
+            with pytest.raises(ts.TsError):
+                call()
+        torch.cuda.synchronize()
+        assert (flat == 1).all()
+
+
 def test_drelu_rows_beyond_32_bits(ts):
     r, m = 150_000, 14336  # 2.15e9 elements
     g = torch.empty(r, m, dtype=BF16, device="cuda")
