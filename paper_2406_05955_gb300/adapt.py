@@ -1,11 +1,17 @@
 """ctypes binding of libtsffn's operators for adapted layers (low-rank adapters, the activation kept in 8 bits, balance loss,
-backward passes): marshalling only. Tensors, outputs and streams as in ``prompt``."""
+backward passes): marshalling only. Tensors, outputs and streams as in ``prompt``.
+
+Autograd records none of these calls: their results have no ``grad_fn``, whatever requires a gradient. A caller who wants them
+in its graph puts a call and its backward pass into a ``torch.autograd.Function``. What is written over an input by default (the
+rows of ``Adapters``) counts as a change in place to autograd, which then refuses a backward pass that needs what was there;
+buffers that the caller gives for outputs do not."""
 from __future__ import annotations
 
 from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .binding import TS_BF16, _check, lib
 from .prompt import BLOCK, _CODES, _current_device, _empty, _handle, _ld, _rows_apart, _shaped, _tensor
@@ -113,6 +119,8 @@ class Adapters:
         _check(lib().ts_adapt_rows(x.data_ptr(), ldx, t, self.k, self._a, self._b, self._scale, self._ranks, self.adapters,
                                    self.r, self.n, ids, rows, offsets, y.data_ptr(), ldy, _CODES[y.dtype], out.data_ptr(),
                                    ldo, None if h is None else h.data_ptr(), _handle(stream)), "ts_adapt_rows")
+        if out is y:
+            increment_version(y)
         return out
 
     __call__ = forward
@@ -157,7 +165,11 @@ class Adapters:
             dy.data_ptr(), ldy, t, self.n, self._a, self._b, self._scale, self._ranks, self.adapters, self.r, self.k, rows,
             offsets, h.data_ptr(), x.data_ptr(), ldx, _CODES[x.dtype], sp, ld, dp, ldd, code, op, ldo, dh.data_ptr(),
             da.data_ptr(), db.data_ptr(), int(bool(accumulate)), _handle(stream)), "ts_adapters_backward")
-        return dx if out is None else out, da, db
+        if out is None:
+            if dx is not None:
+                increment_version(dx)
+            out = dx
+        return out, da, db
 
 
 def adapt_error(stream=None) -> int:

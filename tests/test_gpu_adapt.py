@@ -477,6 +477,55 @@ def test_a_wait_that_gives_up_while_others_ask(ts):
         assert ts.adapt_error() == 0
 
 
+def test_autograd(ts):
+    """Rows changed in place are so for autograd too: a backward pass that needs what was there is refused. In a Function of the
+    caller's, gradients are those of the formula."""
+    x, y, a, b, scale, ids = case(90, 128, 72, 8, 3, seed=24, dtype=F32)
+    ad = ts.Adapters(a, b, scale=scale)
+    dy, dx, h = randn(gen(25), 90, 72).to(BF16), randn(gen(26), 90, 128), torch.zeros(90, 8, device="cuda")
+    for t, call in ((y, lambda: ad.forward(x, y, ids)), (dx, lambda: ad.backward(dy, dx, ids, h, x))):
+        w = torch.ones_like(t, requires_grad=True)
+        z = (t * w).sum()  # keeps t
+        before = t.clone()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.backward()
+        t.copy_(before)
+        z = (t * w).sum()
+        ad.forward(x, y, ids, out=torch.empty_like(y))
+        ad.backward(dy, dx, ids, h, x, out=torch.empty_like(dx))
+        z.backward()
+        assert torch.equal(w.grad, before)
+    with torch.inference_mode():
+        assert torch.equal(ad.forward(x, y.clone(), ids), ad.forward(x, y, ids, out=torch.empty_like(y)))
+
+    class Adapted(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, y, a, b):
+            h, out = torch.empty(x.shape[0], a.shape[1], device="cuda"), torch.empty_like(y)
+            ctx.ad = ts.Adapters(a, b, scale=scale)
+            ctx.ad.forward(x, y, ids, out=out, h=h)
+            ctx.save_for_backward(x, h)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            x, h = ctx.saved_tensors
+            dx, da, db = ctx.ad.backward(dout.to(BF16), torch.zeros(x.shape, device="cuda"), ids, h, x)
+            return dx.to(BF16), dout, da, db
+
+    leaves = [v.clone().requires_grad_() for v in (x, y, a, b)]
+    out = Adapted.apply(*leaves)
+    out.backward(dy.float())
+    exact = [v.double().requires_grad_() for v in (x, y, a, b)]
+    i, some = ids.clamp(min=0).long(), torch.where(ids >= 0, scale[ids.clamp(min=0).long()].double(), 0.0)
+    low = torch.einsum("tk,trk->tr", exact[0], exact[2][i]) * some[:, None]
+    want = exact[1] + torch.einsum("tr,trn->tn", low, exact[3][i])
+    want.backward(dy.double())
+    for got, v in zip(leaves, exact):
+        assert (got.grad.double() - v.grad).norm() <= 2.0 ** -8 * v.grad.norm()  # (x's, a's and b's are rounded to bf16)
+
+
 def test_outputs_over_inputs(ts):
     """An adapter around the identity (y is x, dx is dy): written over what others still read it is refused, and nothing is written;
     into a buffer of its own it is right. Rows between each other's, as columns of one buffer, are apart."""
