@@ -359,6 +359,163 @@ def test_gradients_against_differences(ts):
         assert abs(got - want) <= 200 * U * float(grad.double().norm() * d.norm()) * 64, which
 
 
+@pytest.mark.parametrize("t,r,adapters", [(120, 8, 3), (700, 40, 5)])
+def test_gradients_along_themselves(ts, t, r, adapters):
+    """As above, along the gradient itself, where the difference is its square: within the sum of each element's own roundings times
+    it, which is less than half a percent of the difference, so that a wrong scale or a row left out is found."""
+    k, n = 128, 72
+    x, y, a, b, scale, ids = case(t, k, n, r, adapters, seed=11, dtype=F32)
+    dy = randn(gen(12), t, n).to(BF16)
+    ad = ts.Adapters(a, b, scale=scale)
+    h = torch.empty(t, r, device="cuda")
+    ad.forward(x, y, ids, out=torch.empty_like(y), h=h)
+    grads = ad.backward(dy, torch.zeros(t, k, device="cuda"), ids, h, x)
+    some = torch.where(ids >= 0, scale[ids.clamp(min=0).long()].double(), 0.0)[:, None]
+    i = ids.clamp(min=0).long()
+
+    def terms(x, a, b, dy):
+        """h and dh, and the sums dx, da and db."""
+        h, dh = torch.einsum("tk,trk->tr", x, a[i]) * some, torch.einsum("tn,trn->tr", dy, b[i]) * some
+        one = torch.nn.functional.one_hot(i, adapters).double() * (ids >= 0)[:, None]
+        return (h, dh), (torch.einsum("tr,trk->tk", dh, a[i]), torch.einsum("ta,tr,tk->ark", one, dh, x), torch.einsum("ta,tr,tn->arn", one, h, dy))
+
+    at = (x.double(), a.double(), b.double(), dy.double())
+    _, mags = terms(*(v.abs() for v in at))
+    # out's h and dh: 48 roundings; dx 77 with those; da and db as many as an adapter's rows and 17, and those of dh and h
+    m = int(torch.bincount(i[ids >= 0]).max())
+    for which, (grad, mag, roundings) in enumerate(zip(grads, mags, (77, m + 17 + 48, m + 17 + 48))):
+        d = grad.double()
+        plus, minus = list(at), list(at)
+        plus[which], minus[which] = at[which] + 0.5 * d, at[which] - 0.5 * d
+
+        def value(x, a, b, dy):
+            (h, _), _ = terms(x, a, b, dy)
+            return float((dy * torch.einsum("tr,trn->tn", h, b[i])).sum())
+
+        want, got = value(*plus) - value(*minus), float((d * d).sum())
+        tol = roundings * U * float((mag * d.abs()).sum())
+        assert abs(got - want) <= tol <= 0.005 * abs(want), (which, got, want, tol)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t,k,n,r,adapters", [(1, 14336, 136, 16, 2), (70, 14336, 4096, 8, 9), (300, 14336, 264, 64, 20), (2600, 14336, 520, 32, 2),
+                                              (9000, 14336, 128, 64, 3), (2500, 14336, 264, 128, 2)])
+def test_long_rows(ts, t, k, n, r, adapters, dtype):
+    """k of 14336. h: sums of 8 or 16 steps in the tensor cores, one for each 128 of k at most, 8 CTAs' and the scale: k / 128 + 24
+    roundings at most; out 28 more, as above."""
+    x, y, a, b, scale, ids = case(t, k, n, r, adapters, seed=t + r, dtype=dtype)
+    ad, steps = ts.Adapters(a, b, scale=scale), k / 128 + 24
+    want_h, hm, want, mag = plain(x, a, b, scale, ids, y)
+    for given in (ids, ad.rows(ids)):
+        h = torch.full((t, r), 7.0, device="cuda")
+        out = ad.forward(x, y, given, out=torch.empty_like(y), h=h)
+        assert ((h.double() - want_h).abs() <= steps * U * hm).all()
+        tol = ((steps + 28) * U + (2.0 ** -16 if dtype == BF16 else U)) * mag + (2.0 ** -8 * want.abs() if dtype == BF16 else 0.0)
+        assert ((out.double() - want).abs() <= tol).all()
+    # gradients, of k and of n columns
+    dy = (0.1 * randn(gen(t), t, n)).to(BF16)
+    _, da, db = ad.backward(dy, None, ids, h, x)
+    dh, dhm, _, _ = plain(dy, b, a, scale, ids)
+    for i in range(adapters):
+        at = torch.nonzero(ids == i)[:, 0]
+        m, v, d, hi = at.numel(), x[at].double(), dy[at].double(), h[at].double()
+        assert ((db[i].double() - hi.t() @ d).abs() <= (m + 17) * U * (hi.abs().t() @ d.abs())).all()
+        tol = (m + 17) * U * (dh[at].abs().t() @ v.abs()) + 48 * U * (dhm[at].t() @ v.abs())
+        assert ((da[i].double() - dh[at].t() @ v).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("t,k,n,r", [(40, 512, 264, 16), (2500, 264, 520, 64), (9000, 512, 136, 32), (2300, 136, 264, 100)])
+def test_pools_of_which_few_are_hit(ts, t, k, n, r):
+    """255 adapters, whose weights are NaN but for the three that rows have: as a pool of these three, within roundings, and no
+    gradient of the others."""
+    x, y, a, b, scale, ids = case(t, k, n, r, 3, seed=t, dtype=F32)
+    where = torch.tensor([7, 100, 254], device="cuda")
+    pool_a, pool_b = (torch.full((255, r, v.shape[2]), math.nan, dtype=BF16, device="cuda") for v in (a, b))
+    pool_a[where], pool_b[where], pool_scale = a, b, torch.ones(255, device="cuda")
+    pool_scale[where] = scale
+    pool_ids = torch.where(ids >= 0, where.to(torch.int32)[ids.clamp(min=0).long()], -1)
+    ad, few = ts.Adapters(pool_a, pool_b, scale=pool_scale), ts.Adapters(a, b, scale=scale)
+    want_h, hm, want, mag = plain(x, a, b, scale, ids, y)
+    h, dy = torch.empty(t, r, device="cuda"), randn(gen(t), t, n).to(BF16)
+    for given in (pool_ids, ad.rows(pool_ids)):
+        out = ad.forward(x, y, given, out=torch.empty_like(y), h=h)
+        assert ((h.double() - want_h).abs() <= 48 * U * hm).all()
+        assert ((out.double() - want).abs() <= 77 * U * mag).all()
+    _, da, db = ad.backward(dy, None, pool_ids, h, x)
+    _, few_da, few_db = few.backward(dy, None, ids, h, x)
+    off = torch.ones(255, dtype=torch.bool, device="cuda")
+    off[where] = False
+    assert (da[off] == 0).all() and (db[off] == 0).all()
+    m = int(torch.bincount(ids[ids >= 0].long()).max())
+    for i in range(3):
+        at = ids == i
+        hi, d = h[at].double().abs(), dy[at].double().abs()
+        assert ((db[where[i]].double() - few_db[i].double()).abs() <= 2 * (m + 17) * U * (hi.t() @ d)).all()
+        dh, dhm, _, _ = plain(dy, b, a, scale, ids)
+        tol = 2 * ((m + 17) * U * (dh[at].abs().t() @ x[at].double().abs()) + 48 * U * (dhm[at].t() @ x[at].double().abs()))
+        assert ((da[where[i]].double() - few_da[i].double()).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("t,k,r,adapters,x8", [(5, 48, 4, 3, False), (300, 272, 7, 4, True), (2000, 520, 64, 3, False), (1500, 1408, 100, 2, True)])
+def test_gradients_by_themselves(ts, t, k, r, adapters, x8):
+    """``ts_adapter_grads`` of h and rows alone, overwritten and added to: against 64 bits, and the same bits as in the backward pass."""
+    from paper_2406_05955_gb300 import binding
+
+    x, _, a, b, scale, ids = case(t, k, 64, r, adapters, seed=t)
+    g = gen(t)
+    h, dy = randn(g, t, r), randn(g, t, 64).to(BF16)
+    ad = ts.Adapters(a, b, scale=scale)
+    rows, x_scale, wide = ad.rows(ids), None, x.double()
+    if x8:
+        x, x_scale, wide = kept_rows(ts, x)
+
+    def grads(v, v_scale, to, add):
+        code = binding.TS_E4M3 if v_scale is not None else binding.TS_BF16
+        status = ts.lib().ts_adapter_grads(h.data_ptr(), r, v.data_ptr(), v.stride(0), code, None if v_scale is None else v_scale.data_ptr(),
+                                           0 if v_scale is None else v_scale.stride(0), t, v.shape[1], adapters, rows.rows.data_ptr(),
+                                           rows.offsets.data_ptr(), to.data_ptr(), add, torch.cuda.current_stream().cuda_stream)
+        assert status == binding.TS_OK
+        return to
+
+    got = grads(x, x_scale, torch.full((adapters, r, k), 5.0, device="cuda"), 0)
+    for i in range(adapters):
+        at = ids == i
+        want, mag = h[at].double().t() @ wide[at], h[at].double().abs().t() @ wide[at].abs()
+        assert ((got[i].double() - want).abs() <= (int(at.sum()) + 17) * U * mag).all()
+    assert torch.equal(grads(x, x_scale, torch.full_like(got, 3.0), 1), got + 3.0)
+    _, _, db = ad.backward(dy, None, rows, h, x, x_scale=x_scale)
+    assert torch.equal(grads(dy, None, torch.empty_like(db), 0), db)
+
+
+@pytest.mark.parametrize("r", [16, 30, 64])
+def test_many_rows_at_once(ts, r):
+    """A forward of many listed rows on one stream beside backward passes on another, whose sums all lie in tensor memory: the same
+    bits as one after the other."""
+    x, y, a, b, scale, ids = case(7000, 520, 1032, r, 3, seed=27)
+    ad, g = ts.Adapters(a, b, scale=scale), gen(28)
+    dy, h, rows = randn(g, 7000, 1032).to(BF16), randn(g, 7000, r), ad.rows(ids)
+    few, dx = case(900, 264, 520, 12, 4, seed=29), randn(g, 900, 264)
+    ad2, dy2, h2 = ts.Adapters(few[2], few[3], scale=few[4]), randn(g, 900, 520).to(BF16), randn(g, 900, 12)
+    rows2 = ad2.rows(few[5])
+    want = ad.forward(x, y, rows, out=torch.empty_like(y))
+    want_back = ad.backward(dy, None, rows, h, x)[1:]
+    want2 = ad2.backward(dy2, dx, rows2, h2, few[0], out=torch.empty_like(dx))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = [_like(y, streams[0]) for _ in range(10)]
+    back, back2 = [], []
+    for out in outs:
+        ad.forward(x, y, rows, out=out, stream=streams[0])
+        back.append(ad.backward(dy, None, rows, h, x, stream=streams[1])[1:])
+        back2.append(ad2.backward(dy2, dx, rows2, h2, few[0], out=_like(dx, streams[2]), stream=streams[2]))
+    torch.cuda.synchronize()
+    assert ts.adapt_error() == 0
+    assert all(torch.equal(out, want) for out in outs)
+    assert all(torch.equal(p, q) for got in back for p, q in zip(got, want_back))
+    assert all(torch.equal(p, q) for got in back2 for p, q in zip(got, want2))
+
+
 def test_streams_graphs_and_calls_at_once(ts):
     c = case(300, 512, 264, 16, 5, seed=13)
     few = case(40, 512, 264, 16, 5, seed=14)
