@@ -39,8 +39,8 @@ struct Tile {
     static constexpr int kHPitch = RP * 2 + 16;
     static constexpr int kSlabBytes = MT * RP * 4;
     static constexpr int kPartBytes = MT * kHPitch;
-    // the sums of h of this CTA (a slab for each warp of 16 rows; 64 rows' two warps add to one), and h as bf16 numbers
-    static constexpr int kFixed = (MT == 16 ? kSlabs : 1) * kSlabBytes + kParts * kPartBytes;
+    // the sums of h of this CTA (a slab for each warp that has a part of k), and h as bf16 numbers
+    static constexpr int kFixed = kSlabs * kSlabBytes + kParts * kPartBytes;
     // two CTAs on an SM where two stages fit (the loads in flight of two cover the latency, and one works while the other joins)
     static constexpr int kHalf = 113 * 1024 - kFixed, kWhole = 226 * 1024 - kFixed;
     static constexpr int kWish = MT == 16 ? 6 : 4;
@@ -48,7 +48,7 @@ struct Tile {
     static constexpr int kStages = kFit < kWish ? kFit : kWish;
     static constexpr int kSmem = kStages * kStage + kFixed;
     static constexpr int kCtas = kSmem <= 113 * 1024 && RP <= 64 ? 2 : 1;  // on an SM
-    static_assert(kStages >= 2, "");
+    static_assert(kStages >= 2 && kOT % 2 == 0 && (MT == 16 || kSlabs == 1), "");
 };
 
 // Without a list, of up to 512 rows: the same tiles, from the rows' ids. Thread t looks at rows 2 t and 2 t + 1.
@@ -64,7 +64,7 @@ __device__ __forceinline__ void find_few(const AdaptLaunch& L, int tile, TileRow
         id[i] = row < L.rows ? (int)min((unsigned)L.ids[row], (unsigned)L.n_adapters) : -1;
     }
     counts[tid] = 0;
-    if (tid == 0) *found = {-1, 0, 0, 0};
+    if (tid == 0) *found = {-1, 0, 0};
     if (tid < MT) rows[tid] = -1;
     __syncthreads();
 #pragma unroll
@@ -83,7 +83,7 @@ __device__ __forceinline__ void find_few(const AdaptLaunch& L, int tile, TileRow
     for (int w = 0; w < warp; ++w) upto += sums[w];
     if (tile < upto && tile >= upto - tiles) {
         const int first = (tile - (upto - tiles)) * MT;
-        *found = {tid, 0, first, min(MT, counts[tid] - first)};
+        *found = {tid, first, min(MT, counts[tid] - first)};
     }
     __syncthreads();
     // its rows, ascending: those of the warps before, of the lanes before, the thread's own
@@ -227,19 +227,14 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, CHUNK, TY>::kCtas) k_ad
         take_over();
         const int j0 = T::kNSplit == 2 ? side * T::kNT * 8 : 0;
         float4* const mine = reinterpret_cast<float4*>(slabs);
-        const auto store = [&](float* to, bool add) {
+        float* const to = reinterpret_cast<float*>(slabs + (MT == 16 ? side * T::kSlabBytes : 0));
 #pragma unroll
-            for (int t = 0; t < T::kNT; ++t)
+        for (int t = 0; t < T::kNT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    float2* const p = reinterpret_cast<float2*>(to + (m0 + lane / 4 + e * 4) * RP + j0 + t * 8 + (lane & 3) * 2);
-                    const float2 had = add ? *p : make_float2(0.0f, 0.0f);
-                    *p = make_float2(had.x + sum[t][e], had.y + sum[t][e + 1]);
-                }
-        };
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<float2*>(to + (m0 + lane / 4 + e * 4) * RP + j0 + t * 8 + (lane & 3) * 2) = make_float2(sum[t][e], sum[t][e + 1]);
+        __syncthreads();
         if constexpr (MT == 16) {
-            store(reinterpret_cast<float*>(slabs + side * T::kSlabBytes), false);
-            __syncthreads();
             for (int i = tid; i < MT * RP / 4; i += kThreads) {
                 float4 s = mine[i];
 #pragma unroll
@@ -249,13 +244,8 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, CHUNK, TY>::kCtas) k_ad
                 }
                 mine[i] = s;
             }
-        } else {
-            float* const to = reinterpret_cast<float*>(slabs);
-            if (T::kSlabs == 1 || side == 0) store(to, false);
             __syncthreads();
-            if (T::kSlabs == 2 && side == 1) store(to, true);
         }
-        __syncthreads();
         if (ctas > 1) {
             cluster_arrive();
             cluster_wait();
@@ -350,21 +340,14 @@ __global__ void __launch_bounds__(kThreads, Tile<MT, RP, CHUNK, TY>::kCtas) k_ad
                     for (int q = 0; q < T::kParts; ++q)
                         ldmatrix4(h[q], parts0 + q * T::kPartBytes + (m0 + (lane & 15)) * T::kHPitch + ks * 32 + (lane >> 4) * 16);
                     const int j = ks * 16 + (lane & 15);
-                    if constexpr (T::kOT == 1) {
-                        uint32_t w[2];
-                        ldmatrix2_t(w, second + place<T::kBPitch>(j, c0 / 8));
 #pragma unroll
-                        for (int q = T::kParts - 1; q >= 0; --q) mma(o[0], h[q], w[0], w[1]);
-                    } else {
+                    for (int t = 0; t < T::kOT; t += 2) {
+                        uint32_t w[4];
+                        ldmatrix4_t(w, second + place<T::kBPitch>(j, c0 / 8 + t + (lane >> 4)));
 #pragma unroll
-                        for (int t = 0; t < T::kOT; t += 2) {
-                            uint32_t w[4];
-                            ldmatrix4_t(w, second + place<T::kBPitch>(j, c0 / 8 + t + (lane >> 4)));
-#pragma unroll
-                            for (int q = T::kParts - 1; q >= 0; --q) {
-                                mma(o[t], h[q], w[0], w[1]);
-                                mma(o[t + 1], h[q], w[2], w[3]);
-                            }
+                        for (int q = T::kParts - 1; q >= 0; --q) {
+                            mma(o[t], h[q], w[0], w[1]);
+                            mma(o[t + 1], h[q], w[2], w[3]);
                         }
                     }
                 }

@@ -15,7 +15,6 @@ constexpr int kWarps = kThreads / kWarp;
 constexpr int kChunk = 256;  // bytes of a row of x, A, y or out in a chunk
 constexpr int kMaxCluster = 8;
 constexpr int kSms = 152;
-constexpr int kResidentCtas = 2 * kSms;
 
 // ---- matrix instructions, asynchronous copies, clusters ---------------------------------------
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -30,9 +29,6 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&v)[4], uint32_t at) {
 __device__ __forceinline__ void ldmatrix4_t(uint32_t (&v)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void ldmatrix2_t(uint32_t (&v)[2], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at) : "memory");
 }
 // 16 bytes, or zeros.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in) {
@@ -153,7 +149,7 @@ __device__ __forceinline__ void tc_free(uint32_t at) {
 
 // The tile of a cluster: up to MT rows of one adapter.
 struct TileRows {
-    int id, rank, first, count;
+    int id, first, count;
 };
 
 // By the list: tile number `tile` of all groups' in a row, the rows without an adapter last.
@@ -174,12 +170,12 @@ __device__ __forceinline__ void find_listed(const AdaptLaunch& L, int tile, Tile
         if (lane >= o) upto += v;
     }
     if (lane == kWarp - 1) sums[warp] = upto;
-    if (tid == 0) *found = {-1, 0, 0, 0};
+    if (tid == 0) *found = {-1, 0, 0};
     __syncthreads();
     for (int w = 0; w < warp; ++w) upto += sums[w];
     if (tile < upto && tile >= upto - tiles) {
         const int first = begin + (tile - (upto - tiles)) * MT;
-        *found = {tid, 0, first, min(MT, end - first)};
+        *found = {tid, first, min(MT, end - first)};
     }
     __syncthreads();
     if (tid < MT) {
