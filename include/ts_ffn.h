@@ -680,6 +680,7 @@ ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, co
  *   share      device [n_experts] fp32
  *   totals     device [2] int32: live tokens, picks
  *   work       device, ts_balance_work(tokens, n_experts) fp32 (0: may be NULL), not shared by calls in flight at once
+ * What is written shares no memory with what is read.
  */
 long long ts_balance_work(int tokens, int n_experts); /* -1: sizes that ts_balance refuses */
 ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32_t* sel, int top_k, float* loss,
@@ -695,7 +696,7 @@ ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32
  *   logits     device [tokens][n_experts] fp32 (with dloss); sel, w device [tokens][top_k] as ts_route gives them, dw
  *              the same (with dw)
  *   dloss      device [1] fp32
- *   dlogits    device [tokens][n_experts] fp32
+ *   dlogits    device [tokens][n_experts] fp32; may be logits itself, and shares no memory with what else is read
  */
 ts_status ts_route_backward(const float* logits, int tokens, int n_experts, const int32_t* sel, const float* w, int top_k,
                             const float* dw, const int32_t* counts, const int32_t* totals, const float* dloss, float* dlogits,

@@ -259,6 +259,10 @@ ts_status ts_balance(const float* logits, int tokens, int n_experts, const int32
         !aligned4(totals) || (!work && balance_work(tokens, n_experts) > 0) || !aligned4(work) || !aligned4(logits) ||
         !aligned4(sel) || (tokens > 0 && (!logits || !sel)))
         return TS_ERR_INVALID_ARG;
+    const Region outs[5] = {whole(loss, 4), whole(counts, 4ll * n_experts), whole(share, 4ll * n_experts), whole(totals, 8),
+                            whole(work, 4ll * (int64_t)balance_work(tokens, n_experts))},
+                 ins[2] = {whole(logits, 4ll * tokens * n_experts), whole(sel, 4ll * tokens * top_k)};
+    if (overlap(outs, ins)) return TS_ERR_INVALID_ARG;
     return launched(launch_balance({logits, tokens, n_experts, top_k, sel, loss, counts, share, totals, work}, stream));
 }
 
@@ -275,6 +279,12 @@ ts_status ts_route_backward(const float* logits, int tokens, int n_experts, cons
     if ((!balance && !dw) || (balance && !logits) || !aligned4(logits) || !dlogits || !aligned4(dlogits) || !aligned4(dw) ||
         !aligned4(sel) || !aligned4(w) || (dw && (!sel || !w)))
         return TS_ERR_INVALID_ARG;
+    // dlogits may be logits: a token's lanes read theirs before they write
+    const int64_t all = 4ll * tokens * n_experts, picks = 4ll * tokens * top_k;
+    const Region outs[1] = {whole(dlogits, all)};
+    const Region ins[7] = {whole(dlogits != logits ? logits : nullptr, all), whole(dw ? sel : nullptr, picks), whole(dw ? w : nullptr, picks),
+                           whole(dw, picks), whole(counts, 4ll * n_experts), whole(totals, 8), whole(dloss, 4)};
+    if (overlap(outs, ins)) return TS_ERR_INVALID_ARG;
     return launched(launch_route_backward({logits, tokens, n_experts, top_k, sel, w, dw, counts, totals, dloss, dlogits}, stream));
 }
 

@@ -241,6 +241,31 @@ def test_drelu_rows_over_their_inputs(lib):
         assert call(lib.ts_drelu_rows_backward, good, **kw) == BAD, kw
 
 
+def test_balance_over_its_inputs(lib):
+    from paper_2406_05955_gb300.binding import TS_ERR_INVALID_ARG as BAD
+
+    L, C, S, T = (i << 32 for i in range(10, 14))
+    good = {"logits": X, "tokens": 4, "experts": 8, "sel": Y, "top_k": 2, "loss": L, "counts": C, "share": S, "totals": T,
+            "work": None, "stream": None}
+    for kw in ({"loss": X}, {"counts": X + 124}, {"share": X - 28}, {"totals": Y + 28}, {"loss": Y}, {"loss": C}, {"share": C + 4},
+               {"totals": S + 28}, {"tokens": 100000, "work": X}, {"tokens": 100000, "work": C},
+               # not of memory that is shared
+               {"logits": None}, {"logits": X + 2}, {"tokens": -1}, {"tokens": 1 << 29}, {"experts": 0}, {"experts": 257}, {"sel": None},
+               {"top_k": 0}, {"top_k": 9}, {"experts": 1}, {"loss": None}, {"counts": None}, {"share": None}, {"totals": None},
+               {"tokens": 100000}, {"work": M + 2}):
+        assert call(lib.ts_balance, good, **kw) == BAD, kw
+
+    good = {"logits": X, "tokens": 4, "experts": 8, "sel": Y, "w": O, "top_k": 2, "dw": H, "counts": C, "totals": T,
+            "dloss": L, "dlogits": S, "stream": None}
+    for kw in ({"dlogits": X + 4}, {"dlogits": X - 4}, {"dlogits": Y}, {"dlogits": O + 28}, {"dlogits": H - 124}, {"dlogits": C},
+               {"dlogits": T + 4}, {"dlogits": L - 124},
+               # not of memory that is shared
+               {"logits": None}, {"tokens": -1}, {"experts": 300}, {"sel": None}, {"w": None}, {"top_k": 9}, {"counts": None},
+               {"totals": None}, {"dloss": None}, {"dlogits": None}, {"dlogits": S + 2}, {"dw": H + 1},
+               {"dw": None, "counts": None, "totals": None, "dloss": None}):
+        assert call(lib.ts_route_backward, good, **kw) == BAD, kw
+
+
 def test_combine_rows_backward_over_its_inputs(lib):
     from paper_2406_05955_gb300.binding import TS_BF16, TS_E4M3, TS_ERR_INVALID_ARG as BAD, TS_F32
 

@@ -337,6 +337,23 @@ def test_balance_of_a_loss_that_overflowed(ts, scale):
     assert (got[off] == 0).all() and not torch.isfinite(got[~off]).any()
 
 
+@pytest.mark.parametrize("t,e,k", [(1, 8, 2), (700, 7, 3), (300, 256, 8), (90, 60, 4)])
+def test_route_backward_in_place(ts, t, e, k):
+    """The gradient over the logits themselves is as apart; partly over them it is refused, and nothing is written."""
+    flat = randn(gen(t), (t + 1) * e)
+    x = flat[:t * e].view(t, e)
+    r = ts.route(x, k)
+    b, dw, dloss = ts.balance(x, r.sel), randn(gen(e), t, k), torch.tensor([2.0], device="cuda")
+    want, before = ts.route_backward(x, r.sel, r.w, dw=dw, balance=b, dloss=dloss), flat.clone()
+    with pytest.raises(ts.TsError):
+        ts.route_backward(x, r.sel, r.w, dw=dw, balance=b, dloss=dloss, dlogits=flat[1:1 + t * e].view(t, e))
+    with pytest.raises(ts.TsError):
+        ts.balance(x, r.sel, share=x[0])
+    torch.cuda.synchronize()
+    assert torch.equal(flat, before)
+    assert torch.equal(ts.route_backward(x, r.sel, r.w, dw=dw, balance=b, dloss=dloss, dlogits=x), want) and torch.equal(x, want)
+
+
 def test_balance_gradient_against_differences(ts):
     """Of loss + sum(w * weight), by central differences in 64 bits: the step's own error is of third order."""
     t, e, k = 40, 9, 3
