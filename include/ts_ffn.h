@@ -672,7 +672,7 @@ ts_status ts_drelu_rows_backward(const void* dc, int64_t ldd, ts_dtype dtype, co
  * How evenly tokens are routed. A token is live if any of its logits is above -infinity; p[t] is the softmax over its
  * logits (-infinity and NaN count as none, equal +infinities share), and over the live tokens and the picks
  *     share[e] = mean of p[t][e],   loss = n_experts * sum_e (counts[e] / picks) share[e]
- * which is 1 where both are even, and 0 without picks.
+ * which is 1 where both are even, and 0 without picks. Sums over tokens are in fp32, of a thread's tokens, its CTA's and all CTAs' in turn.
  *   logits     device [tokens][n_experts] fp32; sel device [tokens][top_k], as ts_route takes and gives them (an
  *              entry outside 0..n_experts-1 is no pick)
  *   loss       device [1] fp32

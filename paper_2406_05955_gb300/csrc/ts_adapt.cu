@@ -9,7 +9,7 @@
 // a list, or by the rows' ids here), so they come by 16-byte asynchronous copies.
 //
 // Few rows are bound by the chain launch / ids / first chunk / sums of h / join / last chunk, not by bytes. Calls in a row,
-// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.5 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 9.5
+// bf16 unless stated: 1 row, k = 4096, n = 14336, r = 16: 5.4 us; 64 rows of 64 adapters, k = n = 4096, r = 16, fp32: 9.5
 // (12.5 MB, 1.3 TB/s; in chunks of 256 bytes 14.0); 300 rows of 20, k = 1408, n = 512, r = 40, fp32: 7.4. The matrix
 // instructions of a warp do for it: they take 3% of the time.
 #include "ts_adapt.cuh"
@@ -434,7 +434,9 @@ cudaError_t launch_type(const AdaptLaunch& a, cudaStream_t stream) {
     // adapters: r = 8, 4096 rows 27, 28, 30 and 32, 39, 63; 8192 50, 51, 52 and 47, 65, 74. r = 32, 2048 rows 23, 23, 37 and
     // 24, 31, 62; 4096 36, 37, 41 and 33, 41, 65; 8192 65, 66, 70 and 48, 67, 76. r = 64, 1024 rows 18, 26, 36 and 26, 33, 63;
     // 4096 53, 57, 61 and 37, 46, 71; 8192 102, 103, 106 and 52, 73, 85. r = 128 (and 64 rows), 1024 rows 26, 45, 55 and 50, 57, 101;
-    // 4096 84, 88, 96 and 59, 102, 104; 8192 160, 165, 170 and 103, 103, 190. n = 2048, k = 1408, fp32 has the same order.
+    // 4096 84, 88, 96 and 59, 102, 104; 8192 160, 165, 170 and 103, 103, 190. n = 2048, k = 1408, fp32 has the same order. The host
+    // knows how many adapters there are, not how many have rows: of large pools of which few are hit it takes 16 rows too long (8192
+    // rows of one adapter of 255, r = 64, about twice the time), and of r = 128 it takes 64 rows at 4096 of 30 and 8192 of 100, for 16% and 12%.
     const long long few = most_tiles(a.rows, a.n_adapters, 16) * (30 + a.r);
     const bool wide = a.r <= kWideRank;
     const long long many = wide ? 6000 + 210 * most_tiles(a.rows, a.n_adapters, 128) : 4000 + 340 * most_tiles(a.rows, a.n_adapters, 64);

@@ -13,11 +13,12 @@
 //
 // Memory bounds it in principle: x once, h once for each 128 columns from L2. What it spends is latency: chunks in a row,
 // each split, widened (e4m3) and multiplied between barriers by the 16 warps that an SM has room for; an SM issues 1.5
-// instructions a cycle. 8192 rows, k = 4096, r = 32: 34 us from e4m3 rows (35 MB), 31 from bf16 ones (68 MB); 64 rows of one
+// instructions a cycle. 8192 rows, k = 4096, r = 32: 34 us from e4m3 rows (35 MB), 30 from bf16 ones (68 MB; r = 64 45, r = 128 71); 64 rows of one
 // adapter, k = 512, r = 12: 4. Measured on the way: products by the warps' matrix instructions 98 and 40; rows divided
 // instead of chunks, so that every CTA joins, 34 and 31 (64 rows of 8 adapters, k = 512, 10 us, now 5.7); two sets of parts,
 // so that one is split while the other is multiplied by a warp of its own, no faster; 512 threads where two CTAs share an SM
-// 10% slower (64 registers each), where one has it (r above 32) 10% faster. Adapters of up to 8 rows as chunks: a pass over 4
+// 10% slower (64 registers each), where one has it (r above 32) 10% faster; each of the later parts' sums tested for infinities, and not
+// only the third's once a warp, 3% slower at r = 64 and 7 at 128. Adapters of up to 8 rows as chunks: a pass over 4
 // rows of 28 adapters, k = 1520, n = 3504, r = 29, 43 us, now 25; 84 rows of 40, k = 13920, n = 2064, r = 4, 68 and 42 (48 if
 // warps take up to 4 rows only).
 #include <cuda_fp8.h>
